@@ -187,7 +187,7 @@ def prepare(case, seed):
         tok[::17] = -1 if n > 17 else tok[::17]              # padding of a ragged batch
         f32 = dict(device="cuda", dtype=torch.float32)
         st = dict(case=case, logits=logits, tok=tok, g_logp=normal(n), g_ent=normal(n) * 0.01, logp=torch.empty(n, **f32),
-                  ent=torch.empty(n, **f32), lse=torch.empty(n, **f32),
+                  ent=torch.empty(n, **f32), stats=torch.empty((n, 2), **f32),
                   top_id=torch.empty((n, case["top"]), device="cuda", dtype=torch.int32),
                   top_logp=torch.empty((n, case["top"]), **f32))
         if case["train"]:
@@ -335,7 +335,7 @@ def _plain_score(st):
     lp = torch.where(torch.isfinite(z), z - lse, torch.zeros_like(z))
     p = e / tot
     ent = -(p * lp).sum(-1)
-    out = {"logp": logp, "entropy": ent, "lse": lse[:, 0]}
+    out = {"logp": logp, "entropy": ent, "max": x.amax(-1), "sum": tot[:, 0]}
     if case["top"]:
         # a unique key for each id: the logit's order, the lower id first
         bits = x.view(torch.int32).long()
@@ -368,14 +368,14 @@ def run(state):
         sara.sara_kv8_attention(st["q"], st["k_cache"], st["v_cache"], st["k_exp"], st["v_exp"], st["pages"], st["ctx"],
                                 st["off"], st["out"], max_q=st["max_q"], max_ctx=st["max_ctx"])
         return {"out": st["out"]}
-    out = {"logp": st["logp"], "entropy": st["ent"], "lse": st["lse"]}
+    out = {"logp": st["logp"], "entropy": st["ent"], "max": st["stats"][:, 0], "sum": st["stats"][:, 1]}
     top = {}
     if case["top"]:
         top = {"d_top_id": st["top_id"], "d_top_logp": st["top_logp"]}
         out["top_id"], out["top_logp"] = st["top_id"], st["top_logp"]
-    sara.sara_token_logprobs(st["logits"], st["tok"], st["logp"], st["ent"], st["lse"], temperature=case["temperature"], **top)
+    sara.sara_token_logprobs(st["logits"], st["tok"], st["logp"], st["ent"], st["stats"], temperature=case["temperature"], **top)
     if case["train"]:
-        sara.sara_token_logprobs_grad(st["logits"], st["tok"], st["lse"], st["ent"], st["g_logp"], st["g_ent"], st["grad"],
+        sara.sara_token_logprobs_grad(st["logits"], st["tok"], st["stats"], st["ent"], st["g_logp"], st["g_ent"], st["grad"],
                                       temperature=case["temperature"])
         out["grad"] = st["grad"]
     return out
@@ -470,7 +470,7 @@ def _exact_score(case, st):
         has = tok >= 0
         one = torch.zeros_like(z).scatter_(1, tok.clamp(min=0)[:, None], 1.0) * has[:, None]
         got = {"logp": torch.where(has, lp.gather(1, tok.clamp(min=0)[:, None])[:, 0], 0.0 * ent), "entropy": ent,
-               "lse": torch.logsumexp(z, -1)}
+               "max": st["logits"][r:r + 64].double().amax(-1), "sum": torch.exp(z - z.amax(-1, keepdim=True)).sum(-1)}
         if case["top"]:
             got["top_logp"] = torch.topk(lp, case["top"], -1).values
         if case["train"]:
