@@ -366,7 +366,7 @@ def run(state):
         return {"k": st["read_k"], "v": st["read_v"]}
     if case["kind"] == "attend":
         sara.sara_kv8_attention(st["q"], st["k_cache"], st["v_cache"], st["k_exp"], st["v_exp"], st["pages"], st["ctx"],
-                                st["off"], st["out"], max_q=st["max_q"], max_ctx=st["max_ctx"])
+                                st["off"], st["out"], max_ctx=st["max_ctx"])
         return {"out": st["out"]}
     out = {"logp": st["logp"], "entropy": st["ent"], "max": st["stats"][:, 0], "sum": st["stats"][:, 1]}
     top = {}
