@@ -353,6 +353,121 @@ int sara_sample_logits_noalloc(const float* d_logits, int32_t n_rows, int32_t vo
  * failure. */
 int sara_gumbel_fast_max_error(double* h_out, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * KV cache in 8 bits
+ *
+ * A paged cache of one layer that holds K and V in one byte an element, for
+ * decoders that keep their own layers (scoring rollouts, long contexts): half
+ * the memory and half the attention traffic of bf16 pages.
+ *
+ * A page holds 16 tokens of a sequence.  For each page and KV head one scale,
+ * a power of two, serves its 16 x head_dim elements:
+ *     value = code * 2^(b - 127),   b the exponent byte;  b = 255: NaN
+ * with codes int8 (-127..127) or fp8 e4m3 (the OCP format, up to 448).  Every
+ * value is exact in bf16 and fp32 (rounding up to a code may pass the largest
+ * finite number: inf).  The caller owns all memory: pages are
+ * handed out by page tables d_pages [n_seqs][max_pages] (int32): position p
+ * of sequence i lies in page d_pages[i][p / 16], token p % 16.  Sequences may
+ * share pages that no call writes.  A page id outside [0, n_pages), -1 for
+ * example, is no page: writes to it are dropped, reads give 0, attention does
+ * not see its positions.
+ *
+ * Rows of the ragged calls: sequence i owns rows [d_off[i], d_off[i + 1]) of
+ * the caller's tensors (d_off [n_seqs + 1], not decreasing, inside
+ * [0, n_rows]); d_off == NULL: one row a sequence (n_rows == n_seqs).  dtype is
+ * that of the caller's tensors (SARA_BF16 or SARA_F32): row r, head h begins at
+ * r * row_stride + h * head_stride elements, head_dim elements are contiguous.
+ * Those pointers and strides must be multiples of 16 bytes, as the codes'
+ * pointers.  All calls are enqueued on stream and allocate nothing.  head_dim is
+ * 64 or 128.  Argument errors return SARA_EINVAL and enqueue nothing. */
+enum { SARA_KV8_INT8 = 0, SARA_KV8_E4M3 = 1 };
+typedef struct {
+  void *k, *v;               /* codes [n_pages][n_kv_heads][16][head_dim]        */
+  uint8_t *k_exp, *v_exp;    /* exponent bytes [n_pages][n_kv_heads]             */
+  int32_t n_pages, n_kv_heads, head_dim, format;
+} sara_kv8_cache;
+
+/* Quantise new K and V rows into the cache: row t of sequence i goes to
+ * position d_start[i] + t.  For each page and head that gets a row, with a the
+ * largest magnitude of its new elements:
+ *     b = the smallest byte >= 1 with a <= M * 2^(b - 127), M = 127 or 448,
+ * or, where the page keeps tokens from before d_start[i], the larger of that
+ * and the page's old byte; kept codes are rounded to the new scale if it grew.
+ * Codes are rounded to nearest, ties to even.  A NaN or infinite element makes
+ * the page's byte 255 until a write covers the page's first token again.
+ * Positions past the page table are dropped, and so are the rows of a sequence
+ * with d_start[i] < 0.  No two sequences of a call may write the same page. */
+int sara_kv8_write(const sara_kv8_cache* cache, const void* d_k, int64_t k_row_stride, int64_t k_head_stride,
+                   const void* d_v, int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, int32_t n_rows,
+                   const int32_t* d_pages, int32_t max_pages, const int32_t* d_start, const int32_t* d_off,
+                   int32_t n_seqs, void* stream);
+
+/* Read positions d_start[i] + t of the cache back into rows t of sequence i
+ * (0 where there is no page).  Values are exact in both dtypes. */
+int sara_kv8_read(const sara_kv8_cache* cache, void* d_k, int64_t k_row_stride, int64_t k_head_stride, void* d_v,
+                  int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, int32_t n_rows, const int32_t* d_pages,
+                  int32_t max_pages, const int32_t* d_start, const int32_t* d_off, int32_t n_seqs, void* stream);
+
+/* Causal grouped-query attention over the cache.  Sequence i holds d_ctx[i]
+ * tokens, the queries' own among them (write them first): its n_i query rows
+ * are its last n_i positions, row t sees positions 0 .. d_ctx[i] - n_i + t.
+ * n_heads is a multiple of the cache's KV heads; head h reads KV head
+ * h / (n_heads / n_kv_heads).
+ *     out = sum_j softmax_j(scale * q . k_j) v_j    over the visible positions
+ * accumulated in fp32, rounded once to dtype; a row that sees nothing is 0.
+ * max_ctx <= 16 * max_pages: no d_ctx[i] is larger (the rows of one that is
+ * are NaN); it sizes the launch, so keep it near the longest.
+ * d_ws: workspace of at least the bytes that sara_kv8_attention_workspace
+ * gives for the same sizes (16-byte aligned; NULL if 0), free for reuse once
+ * the stream has passed the call. */
+int sara_kv8_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads, int32_t n_seqs,
+                                 int32_t ragged, int32_t max_ctx, int64_t* bytes);
+int sara_kv8_attention(const sara_kv8_cache* cache, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
+                       void* d_out, int64_t out_row_stride, int64_t out_head_stride, int32_t dtype, int32_t n_rows,
+                       int32_t n_heads, const int32_t* d_pages, int32_t max_pages, const int32_t* d_ctx,
+                       const int32_t* d_off, int32_t n_seqs, int32_t max_ctx, float scale, void* d_ws, int64_t ws_bytes,
+                       void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Token log probabilities
+ *
+ * What the policy-gradient objective needs of a rollout (section 2: the
+ * log probabilities of its tokens under a policy) and its gradient.  For rows
+ * r < n_rows of logits d_logits[r * row_stride + id], id < vocab, in dtype
+ * (SARA_BF16 or SARA_F32; any alignment), with z = logit / temperature,
+ * p = softmax(z) and s = sum exp(z - max z):
+ *   d_logp[r]     = log p(d_tok[r]); 0 where d_tok[r] is outside [0, vocab)
+ *                   (rows without a token, such as padding)
+ *   d_entropy[r]  = -sum p log p
+ *   d_stats[r]    = {largest logit, s}: what the gradient needs of the row;
+ *                   log sum exp z = stats[0] / temperature + log(stats[1])
+ *   d_top_id, d_top_logp [n_rows][n_top]  the n_top (0..32) ids with the
+ *                   largest logits, the lower id first among equals, and their
+ *                   log p; (-1, -inf) past the ids with a logit above -inf
+ * Any of d_logp, d_entropy, d_stats may be NULL, d_top_* if n_top is 0.  -inf
+ * logits are masked ids; a row of nothing else gives log p -inf, entropy 0,
+ * stats {-inf, 0}.  A NaN or +inf logit makes the row's outputs NaN (NaN is
+ * never among the top ids).  Sums are fp32; one pass over the logits.
+ * d_ws: workspace of the bytes that sara_token_logprobs_workspace gives.
+ * Enqueued on stream, allocates nothing. */
+int sara_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, int64_t* bytes);
+int sara_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                        const int32_t* d_tok, float temperature, int32_t n_top, float* d_logp, float* d_entropy,
+                        float* d_stats, int32_t* d_top_id, float* d_top_logp, void* d_ws, int64_t ws_bytes, void* stream);
+
+/* Gradient of sum_r (d_g_logp[r] * logp[r] + d_g_entropy[r] * entropy[r]) with
+ * respect to the logits, in the logits' dtype:
+ *   d_grad[r][j] = (g ([j = tok] - p_j) - h p_j (log p_j + entropy)) / temperature
+ * d_stats and d_entropy are those of sara_token_logprobs on the same logits
+ * and temperature.  d_g_logp or d_g_entropy may be NULL (0); d_entropy may be
+ * NULL if d_g_entropy is.  Rows whose g and h are 0, or that have no id left,
+ * get 0.  d_grad may be d_logits (same stride): each element is read
+ * before it is written, by the same thread.  Enqueued on stream. */
+int sara_token_logprobs_grad(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                             const int32_t* d_tok, float temperature, const float* d_stats, const float* d_entropy,
+                             const float* d_g_logp, const float* d_g_entropy, void* d_grad, int64_t grad_row_stride,
+                             void* stream);
+
 /* Per-kernel timing of eager decode steps.  While enabled, every
  * sara_decode_step call (not the graph replays of sara_run) records a HIP
  * event pair around each kernel it launches on the context's stream, waits

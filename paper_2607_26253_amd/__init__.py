@@ -19,6 +19,7 @@ SARA_OK, SARA_EINVAL, SARA_ENOMEM, SARA_EHIP, SARA_ESTATE, SARA_EDEVICE = 0, -1,
 SARA_F32, SARA_BF16 = 0, 1
 SARA_MODE_SARA, SARA_MODE_FIXED_K, SARA_MODE_SARA_THOMPSON = 0, 1, 2
 _MODES = {"sara": SARA_MODE_SARA, "fixed_k": SARA_MODE_FIXED_K, "sara_thompson": SARA_MODE_SARA_THOMPSON}
+SARA_KV8_INT8, SARA_KV8_E4M3 = 0, 1
 SARA_COMMIT, SARA_ABANDON, SARA_CONTINUE = 1, 2, 3
 
 EXPORTED = ["sara_init", "sara_begin_step", "sara_decode_step", "sara_posterior_decide",
@@ -26,6 +27,8 @@ EXPORTED = ["sara_init", "sara_begin_step", "sara_decode_step", "sara_posterior_
             "sara_read_logs", "sara_read_advantages", "sara_peff_batch", "grpo_group_advantages",
             "sara_sample_logits", "sara_sample_logits_noalloc", "sara_gumbel_fast_max_error", "sara_set_profiling", "sara_reset_profile",
             "sara_read_profile", "sara_set_warm_start", "sara_warm_start_update", "sara_poll",
+            "sara_kv8_write", "sara_kv8_read", "sara_kv8_attention_workspace", "sara_kv8_attention",
+            "sara_token_logprobs_workspace", "sara_token_logprobs", "sara_token_logprobs_grad",
             "sara_destroy",
             "sara_last_error"]
 
@@ -59,6 +62,11 @@ class sara_kernel_profile(ctypes.Structure):
                 ("bytes", ctypes.c_double), ("flops", ctypes.c_double)]
 
 
+class sara_kv8_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "format")]
+
+
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise ImportError(f"libsara.so is not built ({path}); run `python -m paper_2607_26253_amd.build`")
@@ -89,6 +97,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "sara_read_profile": [P, ctypes.POINTER(sara_kernel_profile), I32, ctypes.POINTER(I32)],
         "sara_set_warm_start": [P, P, P, P, I32],
         "sara_warm_start_update": [P, F64],
+        "sara_kv8_write": [P, P, I64, I64, P, I64, I64, I32, I32, P, I32, P, P, I32, P],
+        "sara_kv8_read": [P, P, I64, I64, P, I64, I64, I32, I32, P, I32, P, P, I32, P],
+        "sara_kv8_attention_workspace": [I32, I32, I32, I32, I32, I32, I32, ctypes.POINTER(I64)],
+        "sara_kv8_attention": [P, P, I64, I64, P, I64, I64, I32, I32, I32, P, I32, P, P, I32, I32, F32, P, I64, P],
+        "sara_token_logprobs_workspace": [I32, I32, I32, ctypes.POINTER(I64)],
+        "sara_token_logprobs": [P, I32, I64, I32, I32, P, F32, I32, P, P, P, P, P, P, I64, P],
+        "sara_token_logprobs_grad": [P, I32, I64, I32, I32, P, F32, P, P, P, P, P, I64, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -354,3 +369,168 @@ def sara_sample_logits_noalloc(d_logits, d_rid, d_pos, seed, step_index, tempera
                                            float(top_p), int(eos_id), int(forced_eos_u32), _ptr(d_tok),
                                            _stream_handle(stream)),
            "sara_sample_logits_noalloc")
+
+
+# -- 8-bit KV cache ---------------------------------------------------------------
+def _float_dtype(t, what):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return SARA_BF16
+    if t.dtype == torch.float32:
+        return SARA_F32
+    raise TypeError(f"{what} must be bfloat16 or float32, not {t.dtype}")
+
+
+def _kv8(k_cache, v_cache, k_exp, v_exp):
+    """The C descriptor of a cache: codes [n_pages, n_kv_heads, 16, head_dim]
+    (torch.int8 or torch.float8_e4m3fn) and exponents [n_pages, n_kv_heads]
+    (torch.uint8), contiguous."""
+    import torch
+    if k_cache.dtype == torch.int8:
+        fmt = SARA_KV8_INT8
+    elif k_cache.dtype == torch.float8_e4m3fn:
+        fmt = SARA_KV8_E4M3
+    else:
+        raise TypeError(f"codes must be int8 or float8_e4m3fn, not {k_cache.dtype}")
+    shape = k_cache.shape
+    if len(shape) != 4 or shape[2] != 16 or v_cache.shape != shape or v_cache.dtype != k_cache.dtype:
+        raise ValueError("codes must be [n_pages, n_kv_heads, 16, head_dim], alike for K and V")
+    if k_exp.shape != shape[:2] or v_exp.shape != shape[:2] or k_exp.dtype != torch.uint8 or v_exp.dtype != torch.uint8:
+        raise ValueError("exponents must be uint8 [n_pages, n_kv_heads]")
+    return sara_kv8_cache(_ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), shape[0], shape[1], shape[3], fmt)
+
+
+def _rows3(t, heads, dim, what):
+    """(pointer, row stride, head stride) of a [rows, heads, dim] tensor."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or (t.stride(2) != 1 and t.numel()):
+        raise ValueError(f"{what} must be [rows, {heads}, {dim}] with contiguous last dimension")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _seqs(d_pages, d_seq, d_off, n_rows):
+    """Checks a page table and its per-sequence arrays; the number of sequences."""
+    import torch
+    n = d_pages.shape[0]
+    if d_pages.dim() != 2 or d_pages.dtype != torch.int32 or d_seq.dtype != torch.int32 or d_seq.numel() != n:
+        raise ValueError("page table [n_seqs, max_pages] and per-sequence array [n_seqs] must be int32")
+    if d_off is None:
+        if n_rows != n:
+            raise ValueError(f"{n_rows} rows for {n} sequences: give d_off")
+    elif d_off.dtype != torch.int32 or d_off.numel() != n + 1:
+        raise ValueError("d_off must be int32 [n_seqs + 1]")
+    return n
+
+
+def _kv8_rows(name, k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream):
+    cache = _kv8(k_cache, v_cache, k_exp, v_exp)
+    n_rows = d_k.shape[0]
+    if d_v.shape[0] != n_rows or d_v.dtype != d_k.dtype:
+        raise ValueError("K and V must have the same rows and dtype")
+    k, v = (_rows3(t, cache.n_kv_heads, cache.head_dim, what) for t, what in ((d_k, "K"), (d_v, "V")))
+    n = _seqs(d_pages, d_start, d_off, n_rows)
+    _check(getattr(_lib, name)(ctypes.byref(cache), *k, *v, _float_dtype(d_k, "K and V"), n_rows, _ptr(d_pages),
+                               d_pages.shape[1], _ptr(d_start), _ptr(d_off), n, _stream_handle(stream)), name)
+
+
+def sara_kv8_write(k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off=None, stream=None):
+    """Quantise rows d_k, d_v [rows, n_kv_heads, head_dim] into the cache: row t
+    of sequence i (rows d_off[i]..d_off[i + 1], one each without d_off) goes to
+    position d_start[i] + t of page table d_pages [n_seqs, max_pages]."""
+    _kv8_rows("sara_kv8_write", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
+
+
+def sara_kv8_read(k_cache, v_cache, k_exp, v_exp, d_pages, d_start, d_off, d_k, d_v, stream=None):
+    """Read positions d_start[i] + t back into rows of d_k and d_v."""
+    _kv8_rows("sara_kv8_read", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
+
+
+def _workspace(workspace, need, device, stream):
+    """The caller's workspace, or one from torch's allocator that belongs to the stream."""
+    import torch
+    if workspace is not None:
+        return workspace, workspace.numel() * workspace.element_size()
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device=device), need
+    with torch.cuda.stream(stream):
+        return torch.empty(need, dtype=torch.uint8, device=device), need
+
+
+def sara_kv8_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_off, d_out, scale=None, max_ctx=None,
+                       workspace=None, stream=None):
+    """Causal attention of d_q [rows, n_heads, head_dim] over the cache into
+    d_out: the rows of sequence i (d_off as in sara_kv8_write) are the last of
+    its d_ctx[i] tokens.  scale defaults to head_dim ** -0.5; max_ctx bounds
+    d_ctx (default: what the page table holds)."""
+    cache = _kv8(k_cache, v_cache, k_exp, v_exp)
+    n_rows, heads, hd = d_q.shape
+    q, o = (_rows3(t, heads, cache.head_dim, what) for t, what in ((d_q, "q"), (d_out, "out")))
+    if d_out.shape[0] != n_rows or d_out.dtype != d_q.dtype:
+        raise ValueError("out must have q's rows and dtype")
+    n = _seqs(d_pages, d_ctx, d_off, n_rows)
+    if max_ctx is None:
+        max_ctx = 16 * d_pages.shape[1]
+    need = ctypes.c_int64(0)
+    _check(_lib.sara_kv8_attention_workspace(cache.n_kv_heads, hd, n_rows, heads, n, d_off is not None, max_ctx,
+                                             ctypes.byref(need)), "sara_kv8_attention_workspace")
+    ws, ws_bytes = _workspace(workspace, need.value, d_q.device, stream) if need.value else (None, 0)
+    _check(_lib.sara_kv8_attention(ctypes.byref(cache), *q, *o, _float_dtype(d_q, "q"), n_rows, heads, _ptr(d_pages),
+                                   d_pages.shape[1], _ptr(d_ctx), _ptr(d_off), n, max_ctx,
+                                   hd ** -0.5 if scale is None else float(scale), _ptr(ws), ws_bytes,
+                                   _stream_handle(stream)), "sara_kv8_attention")
+
+
+# -- token log probabilities --------------------------------------------------------
+def _logit_rows(t, what):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.numel()):
+        raise ValueError(f"{what} must be [rows, vocab] with contiguous rows")
+    return t.data_ptr(), _float_dtype(t, what), t.stride(0)
+
+
+def _per_row(t, n, dtype, what):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n:
+        raise ValueError(f"{what} must hold {n} elements of {dtype}")
+    return _ptr(t)
+
+
+def sara_token_logprobs(d_logits, d_tok, d_logp=None, d_entropy=None, d_stats=None, d_top_id=None, d_top_logp=None,
+                        temperature=1.0, workspace=None, stream=None):
+    """Log probability of d_tok[r], entropy, (largest logit, sum of exponentials)
+    and the most likely ids of each row of d_logits [rows, vocab] (bf16 or
+    fp32) at a temperature.  d_stats is [rows, 2]; d_top_id / d_top_logp are
+    [rows, n_top]; outputs that are None are not written."""
+    import torch
+    x, dtype, stride = _logit_rows(d_logits, "logits")
+    n, V = d_logits.shape
+    k = 0 if d_top_id is None else d_top_id.shape[1]
+    f32 = torch.float32
+    if (d_top_id is None) != (d_top_logp is None):
+        raise ValueError("give both of d_top_id and d_top_logp")
+    need = ctypes.c_int64(0)
+    _check(_lib.sara_token_logprobs_workspace(n, V, k, ctypes.byref(need)), "sara_token_logprobs_workspace")
+    ws, ws_bytes = _workspace(workspace, need.value, d_logits.device, stream) if need.value else (None, 0)
+    _check(_lib.sara_token_logprobs(x, dtype, stride, n, V, _per_row(d_tok, n, torch.int32, "tokens"), float(temperature), k,
+                                    _per_row(d_logp, n, f32, "logp"), _per_row(d_entropy, n, f32, "entropy"),
+                                    _per_row(d_stats, 2 * n, f32, "stats"), _per_row(d_top_id, n * k, torch.int32, "top ids"),
+                                    _per_row(d_top_logp, n * k, f32, "top logp"), _ptr(ws), ws_bytes,
+                                    _stream_handle(stream)), "sara_token_logprobs")
+
+
+def sara_token_logprobs_grad(d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad, temperature=1.0,
+                             stream=None):
+    """Gradient with respect to the logits of sum(g_logp * logp + g_entropy *
+    entropy) into d_grad (which may be d_logits); d_stats and d_entropy are what
+    sara_token_logprobs gave.  d_g_logp or d_g_entropy may be None."""
+    import torch
+    x, dtype, stride = _logit_rows(d_logits, "logits")
+    y, ydtype, ystride = _logit_rows(d_grad, "gradient")
+    n, V = d_logits.shape
+    if d_grad.shape != d_logits.shape or ydtype != dtype:
+        raise ValueError("the gradient must have the logits' shape and dtype")
+    f32 = torch.float32
+    _check(_lib.sara_token_logprobs_grad(x, dtype, stride, n, V, _per_row(d_tok, n, torch.int32, "tokens"),
+                                         float(temperature), _per_row(d_stats, 2 * n, f32, "stats"),
+                                         _per_row(d_entropy, n, f32, "entropy"), _per_row(d_g_logp, n, f32, "g_logp"),
+                                         _per_row(d_g_entropy, n, f32, "g_entropy"), y, ystride, _stream_handle(stream)),
+           "sara_token_logprobs_grad")

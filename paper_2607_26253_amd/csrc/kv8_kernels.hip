@@ -1,0 +1,601 @@
+// KV cache in 8 bits (gfx950): quantising writes, reads, and attention over its pages.
+//
+// A page holds 16 tokens of one sequence: codes k, v [page][KV head][16][HD], one byte each (int8, or
+// fp8 e4m3), and for each page and KV head two exponent bytes: value = code 2^(b - 127), b = 255 is NaN.
+// A power of two as scale makes x / scale exact, so a code is the one rounding between a value and its
+// cached form, a value is exact in bf16, and a page whose scale grows (a token larger than its others
+// is appended) re-rounds its codes by a shift: it ends as if written at once, but for codes that the
+// shift leaves halfway.  Against amax / 127 it costs int8 up to one bit and e4m3 nothing.
+#include <math.h>
+
+#include <algorithm>
+
+#include "sara_internal.h"
+
+namespace sara {
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------------------
+// codes
+// ---------------------------------------------------------------------------
+// 127 = 1.984375 2^6 and 448 = 1.75 2^8: amax rounds up to the next power of two above those mantissas
+template <int FMT> __device__ __forceinline__ int exponent_of(uint32_t amax_bits) {
+  if (amax_bits >= 0x7F800000u) return 255;
+  return FMT == SARA_KV8_INT8 ? max(1, (int)((amax_bits + 0x1FFFFu) >> 23) - 6)
+                              : max(1, (int)((amax_bits + 0x1FFFFFu) >> 23) - 8);
+}
+__device__ __forceinline__ float exponent_scale(int b) {
+  return b == 255 ? __uint_as_float(0x7FC00000u) : ldexpf(1.f, b - 127);
+}
+// four codes from values already divided by their scale (|y| <= 127 or 448)
+template <int FMT> __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) {
+  if (FMT == SARA_KV8_INT8) {
+    const uint32_t x = __float2int_rn(a), y = __float2int_rn(b), z = __float2int_rn(c), w = __float2int_rn(d);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w, z, 0x0C0C0400u), __builtin_amdgcn_perm(y, x, 0x0C0C0400u),
+                                 0x05040100u);
+  }
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+template <int FMT> __device__ __forceinline__ void decode4(uint32_t w, float* f) {
+  if (FMT == SARA_KV8_INT8) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f[q] = (float)(int8_t)(w >> (8 * q));
+  } else {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    f[0] = lo[0]; f[1] = lo[1]; f[2] = hi[0]; f[3] = hi[1];
+  }
+}
+// four codes as bf16, exactly
+template <int FMT> __device__ __forceinline__ u32x2 codes_bf16(uint32_t w) {
+  float f[4];
+  decode4<FMT>(w, f);
+  return u32x2{__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
+               __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
+}
+
+// ---------------------------------------------------------------------------
+// ragged work
+// ---------------------------------------------------------------------------
+// Sequences own rows [off[i], off[i + 1]).  A launch numbers its items without a pass over the sequences:
+// sequence i's begin at off[i] mul / 16 + add i, which leaves room for floor(rows mul / 16) + add of them.
+// The sequence of item b (-1: none), by a wave that halves the range 64-fold a step.
+__device__ __forceinline__ int find_seq(const int32_t* off, int n_seqs, int b, int mul, int add, int* first) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_seqs, base = 0;
+  while (true) {
+    const int step = (hi - lo + 63) >> 6;
+    const int i = lo + lane * step;
+    int at = 0x7FFFFFFF;
+    if (i < hi) at = (int)((int64_t)off[i] * mul / 16) + add * i;
+    const int n = __popcll(__ballot(at <= b));
+    if (n == 0) return -1;
+    base = __shfl(at, n - 1, 64);
+    lo += (n - 1) * step;
+    hi = min(hi, lo + step);
+    if (step <= 1) break;
+  }
+  *first = base;
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// rows of sequence i: [r0, r1), held inside the caller's tensor
+__device__ __forceinline__ void seq_rows(const int32_t* off, int i, int n_rows, int& r0, int& r1) {
+  r0 = off ? min(max(off[i], 0), n_rows) : i;
+  r1 = off ? min(max(off[i + 1], r0), n_rows) : i + 1;
+}
+
+// ---------------------------------------------------------------------------
+// write and read
+// ---------------------------------------------------------------------------
+struct KvRows {   // rows of K and V in the caller's tensors, strides in elements
+  void *k, *v;
+  int64_t k_row, k_head, v_row, v_head;
+};
+
+// A wave per (page, KV head, K or V): which page, or false where there is none.
+struct PageUnit {
+  int seq, page, head, r0, len, start;   // page: its index in the sequence; rows r0 + t <-> positions start + t
+  bool is_v;
+};
+__device__ __forceinline__ bool page_unit(int unit, int hkv, const int32_t* start, const int32_t* off, int n_seqs,
+                                          int n_rows, PageUnit& u) {
+  u.is_v = unit & 1;
+  const int rest = unit >> 1, item = rest / hkv;
+  u.head = rest - item * hkv;
+  int first = item;
+  u.seq = off ? find_seq(off, n_seqs, item, 1, 2, &first) : item;
+  if (u.seq < 0 || u.seq >= n_seqs || item < first) return false;
+  int r1;
+  seq_rows(off, u.seq, n_rows, u.r0, r1);
+  u.len = r1 - u.r0;
+  u.start = start[u.seq];
+  if (u.start < 0 || u.len <= 0) return false;
+  u.page = (u.start >> 4) + (item - first);
+  return u.page <= (int)(((int64_t)u.start + u.len - 1) >> 4);
+}
+
+// Lane: 8 consecutive dims of 128 / HD token rows of every 8 (HD 64) or 4 (HD 128) of the page.
+template <int HD> struct PageLanes {
+  static constexpr int TPR = HD / 8;          // lanes a token row
+  static constexpr int RPI = 64 / TPR;        // token rows an instruction
+  static constexpr int NI = kBlockTok / RPI;  // instructions a page
+};
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float* f);
+template <> __device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float* f) {
+  const u32x4 w = *(const u32x4*)p;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) { f[2 * q] = __uint_as_float(w[q] << 16); f[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u); }
+}
+template <> __device__ __forceinline__ void load8<float>(const float* p, float* f) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const f32x4 w = *(const f32x4*)(p + 4 * q);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[4 * q + j] = w[j];
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float* f);
+template <> __device__ __forceinline__ void store8<uint16_t>(uint16_t* p, const float* f) {
+  *(u32x4*)p = u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+}
+template <> __device__ __forceinline__ void store8<float>(float* p, const float* f) {
+  *(f32x4*)p = f32x4{f[0], f[1], f[2], f[3]};
+  *(f32x4*)(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
+}
+
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256) void k_kv8_write(sara_kv8_cache c, KvRows src, const int32_t* __restrict__ pages,
+    int max_pages, const int32_t* __restrict__ start, const int32_t* __restrict__ off, int n_seqs, int n_rows) {
+  typedef PageLanes<HD> PL;
+  PageUnit u;
+  if (!page_unit(blockIdx.x * 4 + (threadIdx.x >> 6), c.n_kv_heads, start, off, n_seqs, n_rows, u)) return;
+  if (u.page >= max_pages) return;
+  const int id = pages[(size_t)u.seq * max_pages + u.page];
+  if (id < 0 || id >= c.n_pages) return;
+  const int lane = threadIdx.x & 63, d0 = 8 * (lane % PL::TPR), row = lane / PL::TPR;
+  const T* x = (const T*)(u.is_v ? src.v : src.k) + (u.is_v ? src.v_head : src.k_head) * u.head + d0;
+  const int64_t stride = u.is_v ? src.v_row : src.k_row;
+  const int t0 = 16 * u.page - u.start;                 // row of the page's slot 0, below 0 where it keeps tokens
+  const size_t block = (size_t)id * c.n_kv_heads + u.head;
+  uint8_t* codes = (uint8_t*)(u.is_v ? c.v : c.k) + (block * kBlockTok + row) * HD + d0;
+  uint8_t* exp = (u.is_v ? c.v_exp : c.k_exp) + block;
+  float f[PL::NI][8];
+  uint32_t amax = 0;
+#pragma unroll
+  for (int j = 0; j < PL::NI; ++j) {
+    const int t = t0 + j * PL::RPI + row;
+    if (t >= 0 && t < u.len) {
+      load8<T>(x + (size_t)(u.r0 + t) * stride, f[j]);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) amax = max(amax, __float_as_uint(f[j][q]) & 0x7FFFFFFFu);   // NaN above inf above all
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, 64));
+  int b = exponent_of<FMT>(amax);
+  if (t0 < 0) {
+    const int old = *exp;
+    b = max(b, old);
+    if (b > old && b < 255) {
+#pragma unroll
+      for (int j = 0; j < PL::NI; ++j)
+        if (t0 + j * PL::RPI + row < 0) {
+          u32x2* p = (u32x2*)(codes + (size_t)j * PL::RPI * HD);
+          const u32x2 w = *p;
+          float g[8];
+          decode4<FMT>(w.x, g);
+          decode4<FMT>(w.y, g + 4);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) g[q] = ldexpf(g[q], old - b);
+          *p = u32x2{encode4<FMT>(g[0], g[1], g[2], g[3]), encode4<FMT>(g[4], g[5], g[6], g[7])};
+        }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < PL::NI; ++j) {
+    const int t = t0 + j * PL::RPI + row;
+    if (t >= 0 && t < u.len) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[j][q] = b == 255 ? 0.f : ldexpf(f[j][q], 127 - b);
+      *(u32x2*)(codes + (size_t)j * PL::RPI * HD) =
+          u32x2{encode4<FMT>(f[j][0], f[j][1], f[j][2], f[j][3]), encode4<FMT>(f[j][4], f[j][5], f[j][6], f[j][7])};
+    }
+  }
+  if (lane == 0) *exp = (uint8_t)b;
+}
+
+// Rows of positions without a page are 0.
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256) void k_kv8_read(sara_kv8_cache c, KvRows dst, const int32_t* __restrict__ pages,
+    int max_pages, const int32_t* __restrict__ start, const int32_t* __restrict__ off, int n_seqs, int n_rows) {
+  typedef PageLanes<HD> PL;
+  PageUnit u;
+  if (!page_unit(blockIdx.x * 4 + (threadIdx.x >> 6), c.n_kv_heads, start, off, n_seqs, n_rows, u)) return;
+  const int id = u.page < max_pages ? pages[(size_t)u.seq * max_pages + u.page] : -1;
+  const bool have = id >= 0 && id < c.n_pages;
+  const int lane = threadIdx.x & 63, d0 = 8 * (lane % PL::TPR), row = lane / PL::TPR;
+  const size_t block = (size_t)(have ? id : 0) * c.n_kv_heads + u.head;
+  const uint8_t* codes = (const uint8_t*)(u.is_v ? c.v : c.k) + (block * kBlockTok + row) * HD + d0;
+  const int b = (u.is_v ? c.v_exp : c.k_exp)[block];
+  const float scale = exponent_scale(b);
+  T* y = (T*)(u.is_v ? dst.v : dst.k) + (u.is_v ? dst.v_head : dst.k_head) * u.head + d0;
+  const int64_t stride = u.is_v ? dst.v_row : dst.k_row;
+  const int t0 = 16 * u.page - u.start;
+#pragma unroll
+  for (int j = 0; j < PL::NI; ++j) {
+    const int t = t0 + j * PL::RPI + row;
+    if (t < 0 || t >= u.len) continue;
+    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (have) {
+      const u32x2 w = *(const u32x2*)(codes + (size_t)j * PL::RPI * HD);
+      decode4<FMT>(w.x, f);
+      decode4<FMT>(w.y, f + 4);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[q] *= scale;
+    }
+    store8<T>(y + (size_t)(u.r0 + t) * stride, f);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------
+struct AttnArgs {
+  const void* q;
+  void* out;
+  int64_t q_row, q_head, o_row, o_head;   // strides in elements
+  const int32_t *pages, *ctx, *off;
+  int max_pages, max_ctx, n_seqs, n_rows, hq, splits, pps;   // pps: pages a split
+  float scale_log2;
+  float* part;                            // [row][head][split][HD + 2]
+};
+
+// fp32 as a sum of P bf16 numbers: 8 bits (bf16 inputs are one exactly), 16, or 24
+template <int P> __device__ __forceinline__ void split_bf16(float a, float b, uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    w[i] = pack_bf16(a, b);
+    a -= __uint_as_float(w[i] << 16);
+    b -= __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+
+// byte i of four words to word i
+__device__ __forceinline__ void transpose4(uint32_t* r) {
+  const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), d = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+  r[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  r[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  r[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+  r[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// Block (16 columns of one sequence and KV head, split): column = query token x head of the group.  The 4
+// waves take the split's pages in pairs, wave w pairs w, w + 4, ...; the next pair's codes are loaded while
+// one is computed.  Per pair:
+//   S^T = K q^T   codes as bf16 (exact), the page's scale on the fp32 scores
+//   online softmax per column in base 2 over the 4 lanes that hold it; the maximum kept is the value
+//                 that was subtracted
+//   O^T += V^T P^T   the score registers are the B operand (4 tokens of each page a lane); V's bytes
+//                 are transposed in registers; P, times the page's V scale, enters as PP bf16 parts
+//                 (2: 2^-17 of a weight; 3 for fp32 queries), so the product adds no rounding of its own
+// Queries of fp32 enter as 3 bf16 parts.  A column without a visible key gives 0.
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) {
+  constexpr int NK = HD / 64, NT = HD / 16, DV = HD / 16;   // 16-byte K loads, dim tiles, V dims a lane
+  constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
+  constexpr int PITCH = HD + 4;
+  __shared__ float m_w[4][16], l_w[4][16];
+  __shared__ __attribute__((aligned(16))) float o_w[4][16][PITCH];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  const int hkv = c.n_kv_heads, G = a.hq / hkv;
+  const int item = blockIdx.x / hkv, g = blockIdx.x - item * hkv;
+  int first = item;
+  const int seq = a.off ? find_seq(a.off, a.n_seqs, item, G, 1, &first) : (int)(item / ((G + 15) / 16));
+  if (!a.off) first = seq * ((G + 15) / 16);
+  if (seq < 0 || seq >= a.n_seqs || item < first) return;
+  int r0, r1;
+  seq_rows(a.off, seq, a.n_rows, r0, r1);
+  const int n_cols = (r1 - r0) * G, c0 = 16 * (item - first);
+  if (c0 >= n_cols) return;
+  const int ctx = max(a.ctx[seq], 0);
+  const bool too_long = ctx > a.max_ctx;                 // more than the launch was sized for: the rows are NaN
+  const int np = too_long ? 0 : (ctx + 15) >> 4;
+  const int p0 = blockIdx.y * a.pps, p1 = min(np, p0 + a.pps);
+  if (p0 >= p1 && blockIdx.y > 0) return;
+  // this lane's column: query row and head, and how many keys it sees
+  const int cc = min(c0 + col, n_cols - 1), qt = cc / G, head = g * G + cc - qt * G;
+  const int before = ctx - (r1 - r0);                    // keys before the first query (below 0: its row sees none)
+  const int seen = before + qt + 1;
+  const int seen_all = before + c0 / G + 1;              // keys that every column sees
+  u32x4 qf[QP][2 * NK];
+  {
+    const T* q = (const T*)a.q + (size_t)(r0 + qt) * a.q_row + (size_t)head * a.q_head;
+#pragma unroll
+    for (int i = 0; i < 2 * NK; ++i) {
+      const T* qp = q + 64 * (i >> 1) + 16 * grp + 8 * (i & 1);
+      if constexpr (QP == 1) {
+        qf[0][i] = *(const u32x4*)qp;
+      } else {
+        float f[8];
+        load8<T>(qp, f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t w[QP];
+          split_bf16<QP>(f[2 * j], f[2 * j + 1], w);
+#pragma unroll
+          for (int p = 0; p < QP; ++p) qf[p][i][j] = w[p];
+        }
+      }
+    }
+  }
+  struct Pair {
+    u32x4 k[2][NK];
+    uint32_t v[2][4][DV / 4];
+    int ke[2], ve[2];
+    bool have[2];
+  };
+  const int32_t* table = a.pages + (size_t)seq * a.max_pages;
+  const int n_it = p1 <= p0 + 2 * wave ? 0 : (p1 - p0 - 2 * wave + 7) / 8;
+  int ids = -1;
+  auto load = [&](Pair& t, int it) {
+    if ((it & 31) == 0) {                                // ids of the next 32 pairs, one a lane
+      const int pg = p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1);
+      ids = pg < p1 ? table[pg] : -1;
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int id = __builtin_amdgcn_readlane(ids, 2 * (it & 31) + p);
+      t.have[p] = id >= 0 && id < c.n_pages;
+      const size_t block = (size_t)(t.have[p] ? id : 0) * hkv + g;
+      const uint8_t* kp = (const uint8_t*)c.k + (block * kBlockTok + col) * HD + 16 * grp;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) t.k[p][i] = *(const u32x4*)(kp + 64 * i);
+      const uint8_t* vp = (const uint8_t*)c.v + (block * kBlockTok + 4 * grp) * HD + DV * col;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int w = 0; w < DV / 4; ++w) t.v[p][j][w] = *(const uint32_t*)(vp + j * HD + 4 * w);
+      t.ke[p] = c.k_exp[block];
+      t.ve[p] = c.v_exp[block];
+    }
+  };
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto compute = [&](Pair& t, int it) {
+    f32x4 s[2];
+    float vs[2];
+    float mx = m;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int k0 = 16 * (p0 + 2 * wave + 8 * it + p);
+      s[p] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 2 * NK; ++i) {
+        const u32x2 x = codes_bf16<FMT>(t.k[p][i >> 1][2 * (i & 1)]), y = codes_bf16<FMT>(t.k[p][i >> 1][2 * (i & 1) + 1]);
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, u32x4{x.x, x.y, y.x, y.y});
+#pragma unroll
+        for (int qp = QP - 1; qp >= 0; --qp)
+          s[p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, qf[qp][i]), s[p], 0, 0, 0);
+      }
+      // a page of NaN scale in K or V makes the scores of its keys NaN, so it reaches only the columns that
+      // see them; its V then counts as 0
+      const bool bad = t.ke[p] == 255 || t.ve[p] == 255;
+      const float ks = bad ? __uint_as_float(0x7FC00000u) : ldexpf(a.scale_log2, t.ke[p] - 127);
+      vs[p] = bad ? 0.f : ldexpf(1.f, t.ve[p] - 127);
+      s[p] *= ks;
+      const bool whole = t.have[p] && k0 + 16 <= seen_all;
+      if (!whole) {
+        const int left = t.have[p] ? seen - k0 - 4 * grp : 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s[p][q] = q < left ? s[p][q] : -INFINITY;
+        // codes past the sequence's last token may be anything
+        const int live = t.have[p] ? ctx - k0 - 4 * grp : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int w = 0; w < DV / 4; ++w) t.v[p][j][w] = j < live ? t.v[p][j][w] : 0u;
+      }
+      mx = fmaxf(mx, fmaxf(fmaxf(s[p][0], s[p][1]), fmaxf(s[p][2], s[p][3])));
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float sub = mx == -INFINITY ? 0.f : mx;         // nothing seen yet: every weight is 0
+    const float al = __builtin_amdgcn_exp2f(m - sub);
+    m = mx;
+    l *= al;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) o[i] *= al;
+    u32x4 pf[PP];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int q = 0; q < 4; q += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(s[p][q] - sub), e1 = __builtin_amdgcn_exp2f(s[p][q + 1] - sub);
+        l += e0 + e1;
+        uint32_t w[PP];
+        split_bf16<PP>(e0 * vs[p], e1 * vs[p], w);
+#pragma unroll
+        for (int i = 0; i < PP; ++i) pf[i][2 * p + (q >> 1)] = w[i];
+      }
+#pragma unroll
+    for (int w = 0; w < DV / 4; ++w) {
+      uint32_t x[4] = {t.v[0][0][w], t.v[0][1][w], t.v[0][2][w], t.v[0][3][w]};
+      uint32_t y[4] = {t.v[1][0][w], t.v[1][1][w], t.v[1][2][w], t.v[1][3][w]};
+      transpose4(x);
+      transpose4(y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {                       // dim DV col + 4 w + i of tile 4 w + i
+        const u32x2 u = codes_bf16<FMT>(x[i]), v = codes_bf16<FMT>(y[i]);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{u.x, u.y, v.x, v.y});
+#pragma unroll
+        for (int p = PP - 1; p >= 0; --p)
+          o[4 * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pf[p]), o[4 * w + i], 0, 0, 0);
+      }
+    }
+  };
+  Pair t0, t1;
+  if (n_it > 0) load(t0, 0);
+  for (int it = 0; it < n_it; it += 2) {
+    if (it + 1 < n_it) load(t1, it + 1);
+    compute(t0, it);
+    if (it + 1 < n_it) {
+      if (it + 2 < n_it) load(t0, it + 2);
+      compute(t1, it + 1);
+    }
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  // join the waves: lane (col, grp) holds dims DV (4 grp + q) + t of its column
+  if (grp == 0) { m_w[wave][col] = m; l_w[wave][col] = l; }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int t = 0; t < NT; t += 4)
+      *(f32x4*)&o_w[wave][col][DV * (4 * grp + q) + t] = f32x4{o[t][q], o[t + 1][q], o[t + 2][q], o[t + 3][q]};
+  __syncthreads();
+  constexpr int TPC = HD / 4, CPP = 256 / TPC;
+  const int cols = min(16, n_cols - c0);
+  for (int x = (int)threadIdx.x / TPC; x < cols; x += CPP) {
+    const int d4 = 4 * ((int)threadIdx.x % TPC);
+    const float mx = fmaxf(fmaxf(m_w[0][x], m_w[1][x]), fmaxf(m_w[2][x], m_w[3][x]));
+    const float sub = mx == -INFINITY ? 0.f : mx;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    float den = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float wt = __builtin_amdgcn_exp2f(m_w[w][x] - sub);
+      num += wt * *(const f32x4*)&o_w[w][x][d4];
+      den += wt * l_w[w][x];
+    }
+    const int t = (c0 + x) / G, h = g * G + (c0 + x) - t * G;
+    if (np <= a.pps) {
+      T* dst = (T*)a.out + (size_t)(r0 + t) * a.o_row + (size_t)h * a.o_head + d4;
+      float f[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) f[q] = too_long ? __uint_as_float(0x7FC00000u) : den == 0.f ? 0.f : num[q] / den;
+      if constexpr (sizeof(T) == 2) *(uint2*)dst = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+      else *(f32x4*)dst = f32x4{f[0], f[1], f[2], f[3]};
+    } else {
+      float* dst = a.part + (((size_t)(r0 + t) * a.hq + h) * a.splits + blockIdx.y) * (HD + 2);
+      *(f32x2*)(dst + d4) = f32x2{num[0], num[1]};
+      *(f32x2*)(dst + d4 + 2) = f32x2{num[2], num[3]};
+      if (d4 == 0) *(f32x2*)(dst + HD) = f32x2{mx, den};
+    }
+  }
+}
+
+// A block per (row, head) joins the splits of rows that have more than one, eight at a time.
+template <int HD, typename T>
+__global__ __launch_bounds__(HD) void k_kv8_attn_join(AttnArgs a) {
+  const int row = blockIdx.x / a.hq, h = blockIdx.x - row * a.hq;
+  int first = 0;
+  const int seq = a.off ? find_seq(a.off, a.n_seqs, row, 16, 0, &first) : row;
+  if (seq < 0) return;
+  int r0, r1;
+  seq_rows(a.off, seq, a.n_rows, r0, r1);
+  if (row < r0 || row >= r1) return;
+  const int ctx = a.ctx[seq];
+  const int ns = (((ctx + 15) >> 4) + a.pps - 1) / a.pps;
+  if (ctx > a.max_ctx || ns <= 1) return;
+  const float* p = a.part + ((size_t)row * a.hq + h) * a.splits * (HD + 2);
+  float mx = -INFINITY, num = 0.f, den = 0.f;
+  for (int s0 = 0; s0 < ns; s0 += 8) {
+    float pm[8], pl[8], po[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float* q = p + (size_t)min(s0 + i, ns - 1) * (HD + 2);
+      pm[i] = s0 + i < ns ? q[HD] : -INFINITY;
+      pl[i] = q[HD + 1];
+      po[i] = q[threadIdx.x];
+    }
+    float m2 = mx;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m2 = fmaxf(m2, pm[i]);
+    const float sub = m2 == -INFINITY ? 0.f : m2;
+    const float al = __builtin_amdgcn_exp2f(mx - sub);
+    num *= al;
+    den *= al;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = __builtin_amdgcn_exp2f(pm[i] - sub);
+      num = fmaf(w, po[i], num);
+      den = fmaf(w, pl[i], den);
+    }
+    mx = m2;
+  }
+  st_f32<T>((T*)a.out + (size_t)row * a.o_row + (size_t)h * a.o_head, threadIdx.x, den == 0.f ? 0.f : num / den);
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+template <typename F> static int kv8_dispatch(const sara_kv8_cache& c, int dtype, F&& go) {
+  auto by_type = [&](auto hd, auto fmt) {
+    if (dtype == SARA_BF16) go(hd, fmt, uint16_t{});
+    else go(hd, fmt, float{});
+  };
+  auto by_fmt = [&](auto hd) {
+    if (c.format == SARA_KV8_INT8) by_type(hd, std::integral_constant<int, SARA_KV8_INT8>{});
+    else by_type(hd, std::integral_constant<int, SARA_KV8_E4M3>{});
+  };
+  if (c.head_dim == 64) by_fmt(std::integral_constant<int, 64>{});
+  else by_fmt(std::integral_constant<int, 128>{});
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SARA_OK : hip_fail(e, "8-bit KV cache launch");
+}
+
+static int64_t page_items(int n_seqs, int n_rows, bool ragged) {
+  return ragged ? (int64_t)n_rows / 16 + 2 * (int64_t)n_seqs : n_seqs;
+}
+
+int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int dtype, int64_t k_row, int64_t k_head,
+                    int64_t v_row, int64_t v_head, int n_rows, const int32_t* pages, int max_pages, const int32_t* start,
+                    const int32_t* off, int n_seqs, hipStream_t st) {
+  const KvRows rows = {k, v, k_row, k_head, v_row, v_head};
+  const int64_t units = page_items(n_seqs, n_rows, off != nullptr) * c.n_kv_heads * 2;
+  const dim3 grid((uint32_t)((units + 3) / 4));
+  return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
+    if (write)
+      hipLaunchKernelGGL((k_kv8_write<hd.value, fmt.value, decltype(t)>), grid, dim3(256), 0, st, c, rows, pages,
+                         max_pages, start, off, n_seqs, n_rows);
+    else
+      hipLaunchKernelGGL((k_kv8_read<hd.value, fmt.value, decltype(t)>), grid, dim3(256), 0, st, c, rows, pages, max_pages,
+                         start, off, n_seqs, n_rows);
+  });
+}
+
+Kv8Split kv8_split(int n_rows, int hq, int hkv, int n_seqs, int max_ctx, bool ragged) {
+  const int G = hq / hkv;
+  const int64_t items = ragged ? (int64_t)n_rows * G / 16 + n_seqs : (int64_t)n_seqs * ((G + 15) / 16);
+  const int np = std::max(1, (max_ctx + 15) / 16);
+  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, items * hkv));
+  Kv8Split s;
+  s.pps = (int)std::max<int64_t>(8, ((np + want - 1) / want + 7) / 8 * 8);
+  s.splits = (np + s.pps - 1) / s.pps;
+  s.items = items;
+  return s;
+}
+
+int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows,
+                         int hq, const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
+                         int max_ctx, float scale, void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st) {
+  const Kv8Split s = kv8_split(n_rows, hq, c.n_kv_heads, n_seqs, max_ctx, off != nullptr);
+  const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
+                      s.splits, s.pps, scale * 1.4426950408889634f, (float*)ws};
+  return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
+    hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.items * c.n_kv_heads), s.splits),
+                       dim3(256), 0, st, c, a);
+    if (s.splits > 1)
+      hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t)>), dim3((uint32_t)((int64_t)n_rows * hq)), dim3(hd.value),
+                         0, st, a);
+  });
+}
+
+}  // namespace sara

@@ -872,6 +872,142 @@ extern "C" int sara_sample_logits_noalloc(const float* d_logits, int32_t n_rows,
                                     eos_id, forced_eos_u32, d_tok, (hipStream_t)stream);
 }
 
+// Arguments that the calls on an 8-bit cache share; "" when they are in order.
+static std::string kv8_bad(const sara_kv8_cache* c, int32_t dtype, int32_t n_rows, const int32_t* d_pages,
+                           int32_t max_pages, const int32_t* d_seq, const int32_t* d_off, int32_t n_seqs) {
+  if (!c || !c->k || !c->v || !c->k_exp || !c->v_exp) return "null cache";
+  if (c->format != SARA_KV8_INT8 && c->format != SARA_KV8_E4M3) return "cache format must be SARA_KV8_INT8 or SARA_KV8_E4M3";
+  if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+  if (c->n_pages < 1 || c->n_kv_heads < 1) return "n_pages and n_kv_heads must be >= 1";
+  if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return "codes must be 16-byte aligned";
+  if (dtype != SARA_BF16 && dtype != SARA_F32) return "dtype must be SARA_BF16 or SARA_F32";
+  if (n_rows < 0 || n_seqs < 0 || max_pages < 1) return "n_rows and n_seqs must be >= 0, max_pages >= 1";
+  if (!d_off && n_rows != n_seqs) return "without d_off there is one row a sequence (n_rows == n_seqs)";
+  if (n_rows > 0 && n_seqs > 0 && (!d_pages || !d_seq)) return "null array";
+  return "";
+}
+// a tensor whose rows and heads are read 16 bytes at a time
+static bool rows_unaligned(const void* p, int64_t row, int64_t head, int32_t dtype) {
+  const int64_t E = dtype == SARA_BF16 ? 2 : 4;
+  return ((uintptr_t)p & 15) || (row * E) % 16 || (head * E) % 16;
+}
+
+static int kv8_rows(bool write, const sara_kv8_cache* c, void* k, int64_t k_row, int64_t k_head, void* v, int64_t v_row,
+                    int64_t v_head, int32_t dtype, int32_t n_rows, const int32_t* d_pages, int32_t max_pages,
+                    const int32_t* d_start, const int32_t* d_off, int32_t n_seqs, void* stream) {
+  const std::string bad = kv8_bad(c, dtype, n_rows, d_pages, max_pages, d_start, d_off, n_seqs);
+  if (!bad.empty()) return einval(bad);
+  if (n_rows == 0 || n_seqs == 0) return SARA_OK;
+  if (!k || !v) return einval("null array");
+  if (rows_unaligned(k, k_row, k_head, dtype) || rows_unaligned(v, v_row, v_head, dtype))
+    return einval("K and V must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
+  if (((int64_t)n_rows / 16 + 2 * (int64_t)n_seqs) * c->n_kv_heads > (int64_t)1 << 30) return einval("too many rows");
+  return launch_kv8_rows(write, *c, k, v, dtype, k_row, k_head, v_row, v_head, n_rows, d_pages, max_pages, d_start, d_off,
+                         n_seqs, (hipStream_t)stream);
+}
+
+extern "C" int sara_kv8_write(const sara_kv8_cache* c, const void* d_k, int64_t k_row, int64_t k_head, const void* d_v,
+                              int64_t v_row, int64_t v_head, int32_t dtype, int32_t n_rows, const int32_t* d_pages,
+                              int32_t max_pages, const int32_t* d_start, const int32_t* d_off, int32_t n_seqs,
+                              void* stream) {
+  return kv8_rows(true, c, const_cast<void*>(d_k), k_row, k_head, const_cast<void*>(d_v), v_row, v_head, dtype, n_rows,
+                  d_pages, max_pages, d_start, d_off, n_seqs, stream);
+}
+
+extern "C" int sara_kv8_read(const sara_kv8_cache* c, void* d_k, int64_t k_row, int64_t k_head, void* d_v, int64_t v_row,
+                             int64_t v_head, int32_t dtype, int32_t n_rows, const int32_t* d_pages, int32_t max_pages,
+                             const int32_t* d_start, const int32_t* d_off, int32_t n_seqs, void* stream) {
+  return kv8_rows(false, c, d_k, k_row, k_head, d_v, v_row, v_head, dtype, n_rows, d_pages, max_pages, d_start, d_off,
+                  n_seqs, stream);
+}
+
+extern "C" int sara_kv8_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads,
+                                            int32_t n_seqs, int32_t ragged, int32_t max_ctx, int64_t* bytes) {
+  if (!bytes) return einval("null argument");
+  if (n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128))
+    return einval("n_heads must be a multiple of n_kv_heads, head_dim 64 or 128");
+  if (n_rows < 0 || n_seqs < 0 || max_ctx < 0) return einval("sizes must be >= 0");
+  const Kv8Split s = kv8_split(n_rows, n_heads, n_kv_heads, n_seqs, max_ctx, ragged != 0);
+  *bytes = s.splits > 1 ? (int64_t)sizeof(float) * n_rows * n_heads * s.splits * (head_dim + 2) : 0;
+  return SARA_OK;
+}
+
+extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int64_t q_row, int64_t q_head, void* d_out,
+                                  int64_t o_row, int64_t o_head, int32_t dtype, int32_t n_rows, int32_t n_heads,
+                                  const int32_t* d_pages, int32_t max_pages, const int32_t* d_ctx, const int32_t* d_off,
+                                  int32_t n_seqs, int32_t max_ctx, float scale, void* d_ws, int64_t ws_bytes,
+                                  void* stream) {
+  const std::string bad = kv8_bad(c, dtype, n_rows, d_pages, max_pages, d_ctx, d_off, n_seqs);
+  if (!bad.empty()) return einval(bad);
+  if (n_heads < 1 || n_heads % c->n_kv_heads) return einval("n_heads must be a multiple of n_kv_heads");
+  if (max_ctx < 0 || max_ctx > (int64_t)max_pages * kBlockTok) return einval("max_ctx must be in [0, 16 * max_pages]");
+  if (!(fabsf(scale) <= 3.4e38f)) return einval("scale must be finite");
+  if (n_rows == 0 || n_seqs == 0) return SARA_OK;
+  if (!d_q || !d_out) return einval("null array");
+  if (rows_unaligned(d_q, q_row, q_head, dtype) || rows_unaligned(d_out, o_row, o_head, dtype))
+    return einval("q and out must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
+  if (((int64_t)n_rows + n_seqs) * n_heads > (int64_t)1 << 30) return einval("too many rows");
+  int64_t need = 0;
+  const int rc = sara_kv8_attention_workspace(c->n_kv_heads, c->head_dim, n_rows, n_heads, n_seqs, d_off != nullptr, max_ctx,
+                                              &need);
+  if (rc) return rc;
+  if (need > 0 && (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need))
+    return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
+  return launch_kv8_attention(*c, d_q, dtype, q_row, q_head, n_rows, n_heads, d_pages, max_pages, d_ctx, d_off, n_seqs,
+                              max_ctx, scale, d_out, o_row, o_head, d_ws, (hipStream_t)stream);
+}
+
+static std::string score_bad(int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab, float temperature) {
+  if (dtype != SARA_BF16 && dtype != SARA_F32) return "dtype must be SARA_BF16 or SARA_F32";
+  if (n_rows < 0 || vocab < 1) return "n_rows must be >= 0 and vocab >= 1";
+  if (row_stride < vocab && n_rows > 1) return "row stride must be at least vocab";
+  if (!(temperature > 0.f) || !(temperature <= 3.4e38f)) return "temperature must be > 0 and finite";
+  return "";
+}
+
+extern "C" int sara_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, int64_t* bytes) {
+  if (!bytes) return einval("null argument");
+  if (n_rows < 0 || vocab < 1 || n_top < 0 || n_top > 32) return einval("n_rows >= 0, vocab >= 1, n_top in [0, 32]");
+  *bytes = n_rows == 0 ? 0 : score_workspace(n_rows, vocab, n_top);
+  return SARA_OK;
+}
+
+extern "C" int sara_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                                   const int32_t* d_tok, float temperature, int32_t n_top, float* d_logp,
+                                   float* d_entropy, float* d_stats, int32_t* d_top_id, float* d_top_logp, void* d_ws,
+                                   int64_t ws_bytes, void* stream) {
+  const std::string bad = score_bad(dtype, row_stride, n_rows, vocab, temperature);
+  if (!bad.empty()) return einval(bad);
+  int64_t need = 0;
+  const int rc = sara_token_logprobs_workspace(n_rows, vocab, n_top, &need);
+  if (rc) return rc;
+  if (n_rows == 0) return SARA_OK;
+  if (!d_logits || !d_tok || (n_top > 0 && (!d_top_id || !d_top_logp))) return einval("null array");
+  if ((uintptr_t)d_logits % (dtype == SARA_BF16 ? 2 : 4)) return einval("logits are not aligned to their element");
+  if ((uintptr_t)d_stats & 7) return einval("d_stats must be 8-byte aligned");
+  if (need > 0 && (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need))
+    return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
+  return launch_token_logprobs(d_logits, dtype, row_stride, n_rows, vocab, d_tok, temperature, n_top, d_logp, d_entropy,
+                               d_stats, d_top_id, d_top_logp, d_ws, (hipStream_t)stream);
+}
+
+extern "C" int sara_token_logprobs_grad(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows,
+                                        int32_t vocab, const int32_t* d_tok, float temperature, const float* d_stats,
+                                        const float* d_entropy, const float* d_g_logp, const float* d_g_entropy,
+                                        void* d_grad, int64_t grad_row_stride, void* stream) {
+  std::string bad = score_bad(dtype, row_stride, n_rows, vocab, temperature);
+  if (bad.empty() && grad_row_stride < vocab && n_rows > 1) bad = "row stride of the gradient must be at least vocab";
+  if (!bad.empty()) return einval(bad);
+  if (n_rows == 0) return SARA_OK;
+  if (!d_logits || !d_tok || !d_stats || !d_grad) return einval("null array");
+  if (d_g_entropy && !d_entropy) return einval("a gradient of the entropy needs d_entropy");
+  const int64_t E = dtype == SARA_BF16 ? 2 : 4;
+  if (((uintptr_t)d_logits | (uintptr_t)d_grad) % E) return einval("logits and gradient must be aligned to their element");
+  if (d_grad == d_logits && row_stride != grad_row_stride) return einval("in place, both row strides must be the same");
+  return launch_token_logprobs_grad(d_logits, dtype, row_stride, n_rows, vocab, d_tok, d_stats, d_entropy, d_g_logp,
+                                    d_g_entropy, temperature, d_grad, grad_row_stride, (hipStream_t)stream);
+}
+
 extern "C" int sara_gumbel_fast_max_error(double* h_out, void* stream) {
   if (!h_out) return einval("h_out is null");
   return launch_gumbel_check(h_out, (hipStream_t)stream);

@@ -311,6 +311,23 @@ int launch_sample_rows(const float* logits, int n_rows, int V, const int32_t* ri
 int launch_sample_rows_noalloc(const float* logits, int n_rows, int V, const int32_t* rid, const int32_t* pos,
                                uint64_t seed, int step, float temp, float top_p, int eos, uint32_t feos,
                                int32_t* tok, hipStream_t st);
+// launchers (8-bit KV cache)
+struct Kv8Split { int splits, pps; int64_t items; };   // context splits, pages of one, column tiles
+Kv8Split kv8_split(int n_rows, int hq, int hkv, int n_seqs, int max_ctx, bool ragged);
+int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int dtype, int64_t k_row, int64_t k_head,
+                    int64_t v_row, int64_t v_head, int n_rows, const int32_t* pages, int max_pages, const int32_t* start,
+                    const int32_t* off, int n_seqs, hipStream_t st);
+int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows,
+                         int hq, const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
+                         int max_ctx, float scale, void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st);
+// launchers (token log probabilities)
+int64_t score_workspace(int n_rows, int V, int k);
+int launch_token_logprobs(const void* logits, int dtype, int64_t row_stride, int n_rows, int V, const int32_t* tok,
+                          float temp, int k, float* logp, float* entropy, float* stats, int32_t* top_id, float* top_logp,
+                          void* ws, hipStream_t st);
+int launch_token_logprobs_grad(const void* logits, int dtype, int64_t row_stride, int n_rows, int V, const int32_t* tok,
+                               const float* stats, const float* entropy, const float* g_logp, const float* g_ent,
+                               float temp, void* grad, int64_t grad_stride, hipStream_t st);
 int launch_convert_norms(sara_ctx* c, const void* const* w);
 int launch_gumbel_check(double* h_out, hipStream_t st);
 int launch_tile_weights(sara_ctx* c, const void* src, void* dst, int rows, int K, int tile_mul, int tile_add,

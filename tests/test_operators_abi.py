@@ -1,0 +1,90 @@
+"""Argument checks of the 8-bit KV cache and of the token log probabilities at
+the C ABI, and the 64-bit reference's own pins (no GPU)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import paper_2607_26253_amd as sara
+from tests import kv8_reference as R
+
+L, BAD = sara._lib, sara.SARA_EINVAL
+P = ctypes.c_void_p(4096)
+
+
+def cache(**over):
+    d = dict(k=4096, v=4096, k_exp=4096, v_exp=4096, n_pages=8, n_kv_heads=2, head_dim=128, format=0)
+    d.update(over)
+    return ctypes.byref(sara.sara_kv8_cache(*d.values()))
+
+
+def write(c=None, k=P, row=256, head=128, dtype=1, n_rows=4, pages=P, max_pages=4, start=P, off=P, n_seqs=2):
+    return L.sara_kv8_write(c or cache(), k, row, head, P, 256, 128, dtype, n_rows, pages, max_pages, start, off, n_seqs, None)
+
+
+def attend(c=None, q=P, row=512, dtype=1, n_rows=4, heads=4, pages=P, max_pages=4, ctx=P, off=P, n_seqs=2, max_ctx=64,
+           scale=1.0, ws=None, ws_bytes=0):
+    return L.sara_kv8_attention(c or cache(), q, row, 128, P, 512, 128, dtype, n_rows, heads, pages, max_pages, ctx, off,
+                                n_seqs, max_ctx, scale, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("over", [dict(k=0), dict(v_exp=0), dict(n_pages=0), dict(n_kv_heads=0), dict(head_dim=96),
+                                  dict(format=2), dict(k=4097), dict(v=4104)])
+def test_caches_are_checked(over):
+    assert write(cache(**over)) == BAD and attend(cache(**over)) == BAD
+    assert len(L.sara_last_error()) > 0
+
+
+@pytest.mark.parametrize("over", [dict(dtype=2), dict(n_rows=-1), dict(n_seqs=-1), dict(max_pages=0), dict(pages=None),
+                                  dict(off=None, n_rows=3), dict(row=257), dict(n_rows=2 ** 31 - 1, n_seqs=2 ** 30)])
+def test_rows_are_checked(over):
+    assert write(**over) == BAD and attend(**over) == BAD
+
+
+def test_more_checks():
+    assert write(k=None) == BAD and write(head=129) == BAD and write(start=None) == BAD
+    assert write(k=ctypes.c_void_p(4098)) == BAD
+    assert attend(q=None) == BAD and attend(heads=3) == BAD and attend(heads=0) == BAD and attend(ctx=None) == BAD
+    assert attend(max_ctx=65) == BAD and attend(max_ctx=-1) == BAD
+    for s in (float("nan"), float("inf")):
+        assert attend(scale=s) == BAD
+    assert write(n_rows=0) == sara.SARA_OK and attend(n_rows=0) == sara.SARA_OK      # nothing to do: nothing is launched
+    assert write(n_rows=0, n_seqs=0) == sara.SARA_OK
+    need = ctypes.c_int64(-1)
+    assert L.sara_kv8_attention_workspace(2, 128, 1, 12, 1, 0, 100000, ctypes.byref(need)) == sara.SARA_OK and need.value > 0
+    assert attend(n_rows=1, n_seqs=1, off=None, heads=12, max_pages=6250, max_ctx=100000, ws=P, ws_bytes=need.value - 1) == BAD
+    assert b"workspace" in L.sara_last_error()
+    assert L.sara_kv8_attention_workspace(2, 128, 1, 12, 1, 0, 100, None) == BAD
+    assert L.sara_kv8_attention_workspace(2, 100, 1, 12, 1, 0, 100, ctypes.byref(need)) == BAD
+    assert ctypes.sizeof(sara.sara_kv8_cache) == 4 * 8 + 4 * 4
+
+
+def test_log_probability_arguments():
+    def fwd(x=P, dtype=1, stride=100, n=2, V=100, tok=P, T=1.0, k=0, ids=None, lps=None, stats=P):
+        return L.sara_token_logprobs(x, dtype, stride, n, V, tok, T, k, P, P, stats, ids, lps, None, 0, None)
+
+    def bwd(x=P, dtype=1, stride=100, n=2, V=100, tok=P, T=1.0, stats=P, ent=P, g=P, h=P, y=ctypes.c_void_p(8192), ystride=100):
+        return L.sara_token_logprobs_grad(x, dtype, stride, n, V, tok, T, stats, ent, g, h, y, ystride, None)
+
+    for f in (fwd, bwd):
+        for over in (dict(x=None), dict(dtype=3), dict(stride=99), dict(n=-1), dict(V=0), dict(tok=None), dict(T=0.0),
+                     dict(T=float("nan")), dict(x=ctypes.c_void_p(4097))):
+            assert f(**over) == BAD, (f, over)
+        assert f(n=0) == sara.SARA_OK
+    assert fwd(k=33, ids=P, lps=P) == BAD and fwd(k=2) == BAD and fwd(k=-1) == BAD and fwd(stats=ctypes.c_void_p(4100)) == BAD
+    assert bwd(stats=None) == BAD and bwd(ent=None) == BAD and bwd(y=None) == BAD and bwd(ystride=5) == BAD
+    assert bwd(y=P, ystride=108) == BAD                                              # in place at another stride
+    assert L.sara_token_logprobs_workspace(1, 10, 40, ctypes.byref(ctypes.c_int64())) == BAD
+    assert L.sara_token_logprobs_workspace(1, 10, 4, None) == BAD
+
+
+def test_reference_codes():
+    """The reference's e4m3 table and rounding: 253 finite values, the largest 448, halfway cases to even."""
+    v = R.e4m3_value(np.arange(256))
+    assert np.isnan(v).sum() == 2 and np.nanmax(v) == 448.0 and v[1] == 2.0 ** -9 and v[8] == 2.0 ** -6
+    codes = v[~np.isnan(v)]
+    np.testing.assert_array_equal(np.abs(R.nearest(codes, "fp8")), np.abs(codes))
+    assert R.nearest(np.array([17.0, 19.0, 2.0 ** -10, 3 * 2.0 ** -10, 432.0]), "fp8").tolist() == [16.0, 20.0, 0.0, 2.0 ** -8, 448.0]
+    assert R.nearest(np.array([0.5, 1.5, -2.5, 126.5]), "int8").tolist() == [0.0, 2.0, -2.0, 126.0]
+    assert [R.exponent(a, "int8") for a in (127.0, 127.5, 0.0, np.inf)] == [127, 128, 1, 255]
+    assert [R.exponent(a, "fp8") for a in (448.0, 449.0, 224.0)] == [127, 128, 126]
