@@ -371,88 +371,122 @@ def sara_sample_logits_noalloc(d_logits, d_rid, d_pos, seed, step_index, tempera
            "sara_sample_logits_noalloc")
 
 
-# -- 8-bit KV cache ---------------------------------------------------------------
+# -- operators on the caller's tensors -----------------------------------------------
+# These calls take microseconds, so their checks are kept short: torch is looked up
+# once, and a stream is named by its raw handle (torch.cuda.current_stream builds an
+# object in 2.8 us).
+class _Torch:
+    """torch's names that the checks below use, from the first call on (importing this package does not import torch)."""
+    float_types = None
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.int32, cls.float32, cls.uint8, cls.empty, cls.on = torch.int32, torch.float32, torch.uint8, torch.empty, torch.cuda.stream
+        cls.codes = {torch.int8: SARA_KV8_INT8, torch.float8_e4m3fn: SARA_KV8_E4M3}
+        cls.raw_stream = staticmethod(torch._C._cuda_getCurrentRawStream)
+        cls.float_types = {torch.bfloat16: SARA_BF16, torch.float32: SARA_F32}
+
+
 def _float_dtype(t, what):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return SARA_BF16
-    if t.dtype == torch.float32:
-        return SARA_F32
-    raise TypeError(f"{what} must be bfloat16 or float32, not {t.dtype}")
+    if _Torch.float_types is None:
+        _Torch.load()
+    code = _Torch.float_types.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be bfloat16 or float32, not {t.dtype}")
+    return code
 
 
+def _stream_for(t, stream):
+    """The stream's handle, or that of the current stream of t's device."""
+    return _Torch.raw_stream(t.get_device()) if stream is None else stream.cuda_stream
+
+
+def _workspace(workspace, need, like, stream):
+    """(pointer, bytes) of the caller's workspace or of one that torch's allocator ties to the stream, and its owner."""
+    if need == 0:
+        return None, 0, None
+    if workspace is None:
+        if stream is None:
+            workspace = _Torch.empty(need, dtype=_Torch.uint8, device=like.device)
+        else:
+            with _Torch.on(stream):
+                workspace = _Torch.empty(need, dtype=_Torch.uint8, device=like.device)
+    return workspace.data_ptr(), workspace.nbytes, workspace
+
+
+# -- 8-bit KV cache ---------------------------------------------------------------
 def _kv8(k_cache, v_cache, k_exp, v_exp):
     """The C descriptor of a cache: codes [n_pages, n_kv_heads, 16, head_dim]
     (torch.int8 or torch.float8_e4m3fn) and exponents [n_pages, n_kv_heads]
     (torch.uint8), contiguous."""
-    import torch
-    if k_cache.dtype == torch.int8:
-        fmt = SARA_KV8_INT8
-    elif k_cache.dtype == torch.float8_e4m3fn:
-        fmt = SARA_KV8_E4M3
-    else:
-        raise TypeError(f"codes must be int8 or float8_e4m3fn, not {k_cache.dtype}")
-    shape = k_cache.shape
-    if len(shape) != 4 or shape[2] != 16 or v_cache.shape != shape or v_cache.dtype != k_cache.dtype:
+    shape, dtype = k_cache.shape, k_cache.dtype
+    fmt = _Torch.codes.get(dtype)
+    if fmt is None:
+        raise TypeError(f"codes must be int8 or float8_e4m3fn, not {dtype}")
+    if len(shape) != 4 or shape[2] != 16 or v_cache.shape != shape or v_cache.dtype != dtype:
         raise ValueError("codes must be [n_pages, n_kv_heads, 16, head_dim], alike for K and V")
-    if k_exp.shape != shape[:2] or v_exp.shape != shape[:2] or k_exp.dtype != torch.uint8 or v_exp.dtype != torch.uint8:
+    u8, pages = _Torch.uint8, shape[:2]
+    if k_exp.dtype != u8 or v_exp.dtype != u8 or k_exp.shape != pages or v_exp.shape != pages:
         raise ValueError("exponents must be uint8 [n_pages, n_kv_heads]")
-    return sara_kv8_cache(_ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), shape[0], shape[1], shape[3], fmt)
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_exp.is_contiguous() and v_exp.is_contiguous()):
+        raise ValueError("codes and exponents must be contiguous")
+    return sara_kv8_cache(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), shape[0], shape[1],
+                          shape[3], fmt)
 
 
-def _rows3(t, heads, dim, what):
+def _rows3(t, rows, heads, dim, what):
     """(pointer, row stride, head stride) of a [rows, heads, dim] tensor."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or (t.stride(2) != 1 and t.numel()):
-        raise ValueError(f"{what} must be [rows, {heads}, {dim}] with contiguous last dimension")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    if t.shape != (rows, heads, dim):
+        raise ValueError(f"{what} must be [{rows}, {heads}, {dim}], not {list(t.shape)}")
+    row, head, last = t.stride()
+    if last != 1 and t.numel():
+        raise ValueError(f"{what} must have a contiguous last dimension")
+    return t.data_ptr(), row, head
 
 
 def _seqs(d_pages, d_seq, d_off, n_rows):
-    """Checks a page table and its per-sequence arrays; the number of sequences."""
-    import torch
-    n = d_pages.shape[0]
-    if d_pages.dim() != 2 or d_pages.dtype != torch.int32 or d_seq.dtype != torch.int32 or d_seq.numel() != n:
+    """Checks a page table and its per-sequence arrays; (sequences, pages a sequence, pointer of d_off)."""
+    n, width = d_pages.shape
+    i32 = _Torch.int32
+    if d_pages.dtype != i32 or d_seq.dtype != i32 or d_seq.numel() != n:
         raise ValueError("page table [n_seqs, max_pages] and per-sequence array [n_seqs] must be int32")
+    if not (d_pages.is_contiguous() and d_seq.is_contiguous()):
+        raise ValueError("page table and per-sequence array must be contiguous")
     if d_off is None:
         if n_rows != n:
             raise ValueError(f"{n_rows} rows for {n} sequences: give d_off")
-    elif d_off.dtype != torch.int32 or d_off.numel() != n + 1:
+        return n, width, None
+    if d_off.dtype != i32 or d_off.numel() != n + 1 or not d_off.is_contiguous():
         raise ValueError("d_off must be int32 [n_seqs + 1]")
-    return n
+    return n, width, d_off.data_ptr()
 
 
-def _kv8_rows(name, k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream):
+def _kv8_rows(call, name, k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream):
+    dtype = _float_dtype(d_k, "K and V")
     cache = _kv8(k_cache, v_cache, k_exp, v_exp)
+    if d_v.dtype != d_k.dtype:
+        raise ValueError("K and V must have the same dtype")
     n_rows = d_k.shape[0]
-    if d_v.shape[0] != n_rows or d_v.dtype != d_k.dtype:
-        raise ValueError("K and V must have the same rows and dtype")
-    k, v = (_rows3(t, cache.n_kv_heads, cache.head_dim, what) for t, what in ((d_k, "K"), (d_v, "V")))
-    n = _seqs(d_pages, d_start, d_off, n_rows)
-    _check(getattr(_lib, name)(ctypes.byref(cache), *k, *v, _float_dtype(d_k, "K and V"), n_rows, _ptr(d_pages),
-                               d_pages.shape[1], _ptr(d_start), _ptr(d_off), n, _stream_handle(stream)), name)
+    k, k_row, k_head = _rows3(d_k, n_rows, cache.n_kv_heads, cache.head_dim, "K")
+    v, v_row, v_head = _rows3(d_v, n_rows, cache.n_kv_heads, cache.head_dim, "V")
+    n, width, off = _seqs(d_pages, d_start, d_off, n_rows)
+    rc = call(ctypes.byref(cache), k, k_row, k_head, v, v_row, v_head, dtype, n_rows, d_pages.data_ptr(), width,
+              d_start.data_ptr(), off, n, _stream_for(k_cache, stream))
+    if rc:
+        _check(rc, name)
 
 
 def sara_kv8_write(k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off=None, stream=None):
     """Quantise rows d_k, d_v [rows, n_kv_heads, head_dim] into the cache: row t
     of sequence i (rows d_off[i]..d_off[i + 1], one each without d_off) goes to
     position d_start[i] + t of page table d_pages [n_seqs, max_pages]."""
-    _kv8_rows("sara_kv8_write", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
+    _kv8_rows(_lib.sara_kv8_write, "sara_kv8_write", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
 
 
 def sara_kv8_read(k_cache, v_cache, k_exp, v_exp, d_pages, d_start, d_off, d_k, d_v, stream=None):
     """Read positions d_start[i] + t back into rows of d_k and d_v."""
-    _kv8_rows("sara_kv8_read", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
-
-
-def _workspace(workspace, need, device, stream):
-    """The caller's workspace, or one from torch's allocator that belongs to the stream."""
-    import torch
-    if workspace is not None:
-        return workspace, workspace.numel() * workspace.element_size()
-    if stream is None:
-        return torch.empty(need, dtype=torch.uint8, device=device), need
-    with torch.cuda.stream(stream):
-        return torch.empty(need, dtype=torch.uint8, device=device), need
+    _kv8_rows(_lib.sara_kv8_read, "sara_kv8_read", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
 
 
 def sara_kv8_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_off, d_out, scale=None, max_ctx=None,
@@ -461,37 +495,42 @@ def sara_kv8_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_of
     d_out: the rows of sequence i (d_off as in sara_kv8_write) are the last of
     its d_ctx[i] tokens.  scale defaults to head_dim ** -0.5; max_ctx bounds
     d_ctx (default: what the page table holds)."""
+    dtype = _float_dtype(d_q, "q")
     cache = _kv8(k_cache, v_cache, k_exp, v_exp)
     n_rows, heads, hd = d_q.shape
-    q, o = (_rows3(t, heads, cache.head_dim, what) for t, what in ((d_q, "q"), (d_out, "out")))
-    if d_out.shape[0] != n_rows or d_out.dtype != d_q.dtype:
-        raise ValueError("out must have q's rows and dtype")
-    n = _seqs(d_pages, d_ctx, d_off, n_rows)
+    q, q_row, q_head = _rows3(d_q, n_rows, heads, cache.head_dim, "q")
+    o, o_row, o_head = _rows3(d_out, n_rows, heads, hd, "out")
+    if d_out.dtype != d_q.dtype:
+        raise ValueError("out must have q's dtype")
+    n, width, off = _seqs(d_pages, d_ctx, d_off, n_rows)
     if max_ctx is None:
-        max_ctx = 16 * d_pages.shape[1]
+        max_ctx = 16 * width
     need = ctypes.c_int64(0)
-    _check(_lib.sara_kv8_attention_workspace(cache.n_kv_heads, hd, n_rows, heads, n, d_off is not None, max_ctx,
-                                             ctypes.byref(need)), "sara_kv8_attention_workspace")
-    ws, ws_bytes = _workspace(workspace, need.value, d_q.device, stream) if need.value else (None, 0)
-    _check(_lib.sara_kv8_attention(ctypes.byref(cache), *q, *o, _float_dtype(d_q, "q"), n_rows, heads, _ptr(d_pages),
-                                   d_pages.shape[1], _ptr(d_ctx), _ptr(d_off), n, max_ctx,
-                                   hd ** -0.5 if scale is None else float(scale), _ptr(ws), ws_bytes,
-                                   _stream_handle(stream)), "sara_kv8_attention")
+    rc = _lib.sara_kv8_attention_workspace(cache.n_kv_heads, hd, n_rows, heads, n, off is not None, max_ctx, ctypes.byref(need))
+    if rc:
+        _check(rc, "sara_kv8_attention_workspace")
+    ws, ws_bytes, _owner = _workspace(workspace, need.value, d_q, stream)
+    rc = _lib.sara_kv8_attention(ctypes.byref(cache), q, q_row, q_head, o, o_row, o_head, dtype, n_rows, heads,
+                                 d_pages.data_ptr(), width, d_ctx.data_ptr(), off, n, max_ctx,
+                                 hd ** -0.5 if scale is None else float(scale), ws, ws_bytes, _stream_for(d_q, stream))
+    if rc:
+        _check(rc, "sara_kv8_attention")
 
 
 # -- token log probabilities --------------------------------------------------------
 def _logit_rows(t, what):
+    dtype = _float_dtype(t, what)
     if t.dim() != 2 or (t.stride(1) != 1 and t.numel()):
         raise ValueError(f"{what} must be [rows, vocab] with contiguous rows")
-    return t.data_ptr(), _float_dtype(t, what), t.stride(0)
+    return t.data_ptr(), dtype, t.stride(0)
 
 
 def _per_row(t, n, dtype, what):
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n:
-        raise ValueError(f"{what} must hold {n} elements of {dtype}")
-    return _ptr(t)
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must hold {n} contiguous elements of {dtype}")
+    return t.data_ptr()
 
 
 def sara_token_logprobs(d_logits, d_tok, d_logp=None, d_entropy=None, d_stats=None, d_top_id=None, d_top_logp=None,
@@ -500,21 +539,23 @@ def sara_token_logprobs(d_logits, d_tok, d_logp=None, d_entropy=None, d_stats=No
     and the most likely ids of each row of d_logits [rows, vocab] (bf16 or
     fp32) at a temperature.  d_stats is [rows, 2]; d_top_id / d_top_logp are
     [rows, n_top]; outputs that are None are not written."""
-    import torch
     x, dtype, stride = _logit_rows(d_logits, "logits")
     n, V = d_logits.shape
-    k = 0 if d_top_id is None else d_top_id.shape[1]
-    f32 = torch.float32
+    i32, f32 = _Torch.int32, _Torch.float32
     if (d_top_id is None) != (d_top_logp is None):
         raise ValueError("give both of d_top_id and d_top_logp")
+    k = 0 if d_top_id is None else d_top_id.shape[1]
     need = ctypes.c_int64(0)
-    _check(_lib.sara_token_logprobs_workspace(n, V, k, ctypes.byref(need)), "sara_token_logprobs_workspace")
-    ws, ws_bytes = _workspace(workspace, need.value, d_logits.device, stream) if need.value else (None, 0)
-    _check(_lib.sara_token_logprobs(x, dtype, stride, n, V, _per_row(d_tok, n, torch.int32, "tokens"), float(temperature), k,
-                                    _per_row(d_logp, n, f32, "logp"), _per_row(d_entropy, n, f32, "entropy"),
-                                    _per_row(d_stats, 2 * n, f32, "stats"), _per_row(d_top_id, n * k, torch.int32, "top ids"),
-                                    _per_row(d_top_logp, n * k, f32, "top logp"), _ptr(ws), ws_bytes,
-                                    _stream_handle(stream)), "sara_token_logprobs")
+    rc = _lib.sara_token_logprobs_workspace(n, V, k, ctypes.byref(need))
+    if rc:
+        _check(rc, "sara_token_logprobs_workspace")
+    ws, ws_bytes, _owner = _workspace(workspace, need.value, d_logits, stream)
+    rc = _lib.sara_token_logprobs(x, dtype, stride, n, V, _per_row(d_tok, n, i32, "tokens"), temperature, k,
+                                  _per_row(d_logp, n, f32, "logp"), _per_row(d_entropy, n, f32, "entropy"),
+                                  _per_row(d_stats, 2 * n, f32, "stats"), _per_row(d_top_id, n * k, i32, "top ids"),
+                                  _per_row(d_top_logp, n * k, f32, "top logp"), ws, ws_bytes, _stream_for(d_logits, stream))
+    if rc:
+        _check(rc, "sara_token_logprobs")
 
 
 def sara_token_logprobs_grad(d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad, temperature=1.0,
@@ -522,15 +563,15 @@ def sara_token_logprobs_grad(d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_
     """Gradient with respect to the logits of sum(g_logp * logp + g_entropy *
     entropy) into d_grad (which may be d_logits); d_stats and d_entropy are what
     sara_token_logprobs gave.  d_g_logp or d_g_entropy may be None."""
-    import torch
     x, dtype, stride = _logit_rows(d_logits, "logits")
     y, ydtype, ystride = _logit_rows(d_grad, "gradient")
     n, V = d_logits.shape
     if d_grad.shape != d_logits.shape or ydtype != dtype:
         raise ValueError("the gradient must have the logits' shape and dtype")
-    f32 = torch.float32
-    _check(_lib.sara_token_logprobs_grad(x, dtype, stride, n, V, _per_row(d_tok, n, torch.int32, "tokens"),
-                                         float(temperature), _per_row(d_stats, 2 * n, f32, "stats"),
-                                         _per_row(d_entropy, n, f32, "entropy"), _per_row(d_g_logp, n, f32, "g_logp"),
-                                         _per_row(d_g_entropy, n, f32, "g_entropy"), y, ystride, _stream_handle(stream)),
-           "sara_token_logprobs_grad")
+    f32 = _Torch.float32
+    rc = _lib.sara_token_logprobs_grad(x, dtype, stride, n, V, _per_row(d_tok, n, _Torch.int32, "tokens"), temperature,
+                                       _per_row(d_stats, 2 * n, f32, "stats"), _per_row(d_entropy, n, f32, "entropy"),
+                                       _per_row(d_g_logp, n, f32, "g_logp"), _per_row(d_g_entropy, n, f32, "g_entropy"), y,
+                                       ystride, _stream_for(d_logits, stream))
+    if rc:
+        _check(rc, "sara_token_logprobs_grad")
