@@ -55,12 +55,25 @@ template <int FMT> __device__ __forceinline__ u32x2 codes_bf16(uint32_t w) {
                __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
 }
 
+// four codes times a power of two as bf16, exactly
+template <int FMT> __device__ __forceinline__ u32x2 values_bf16(uint32_t w, float scale) {
+  if (FMT == SARA_KV8_INT8) {
+    float f[4];
+    decode4<FMT>(w, f);
+    return u32x2{__builtin_amdgcn_perm(__float_as_uint(f[1] * scale), __float_as_uint(f[0] * scale), 0x07060302u),
+                 __builtin_amdgcn_perm(__float_as_uint(f[3] * scale), __float_as_uint(f[2] * scale), 0x07060302u)};
+  }
+  return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
+}
+
 // ---------------------------------------------------------------------------
 // ragged work
 // ---------------------------------------------------------------------------
 // Sequences own rows [off[i], off[i + 1]).  A launch numbers its items without a pass over the sequences:
-// sequence i's begin at off[i] mul / 16 + add i, which leaves room for floor(rows mul / 16) + add of them.
-// The sequence of item b (-1: none), by a wave that halves the range 64-fold a step.
+// sequence i's begin at off[i] mul / DIV + add i, which leaves room for floor(rows mul / DIV) + add of them.
+// The sequence of item b (-1: none), by a wave that cuts the range 64-fold a step.
+template <int DIV>
 __device__ __forceinline__ int find_seq(const int32_t* off, int n_seqs, int b, int mul, int add, int* first) {
   const int lane = threadIdx.x & 63;
   int lo = 0, hi = n_seqs, base = 0;
@@ -68,7 +81,7 @@ __device__ __forceinline__ int find_seq(const int32_t* off, int n_seqs, int b, i
     const int step = (hi - lo + 63) >> 6;
     const int i = lo + lane * step;
     int at = 0x7FFFFFFF;
-    if (i < hi) at = (int)((int64_t)off[i] * mul / 16) + add * i;
+    if (i < hi) at = (int)((int64_t)off[i] * mul / DIV) + add * i;
     const int n = __popcll(__ballot(at <= b));
     if (n == 0) return -1;
     base = __shfl(at, n - 1, 64);
@@ -105,7 +118,7 @@ __device__ __forceinline__ bool page_unit(int unit, int hkv, const int32_t* star
   const int rest = unit >> 1, item = rest / hkv;
   u.head = rest - item * hkv;
   int first = item;
-  u.seq = off ? find_seq(off, n_seqs, item, 1, 2, &first) : item;
+  u.seq = off ? find_seq<16>(off, n_seqs, item, 1, 2, &first) : item;
   if (u.seq < 0 || u.seq >= n_seqs || item < first) return false;
   int r1;
   seq_rows(off, u.seq, n_rows, u.r0, r1);
@@ -248,7 +261,8 @@ struct AttnArgs {
   void* out;
   int64_t q_row, q_head, o_row, o_head;   // strides in elements
   const int32_t *pages, *ctx, *off;
-  int max_pages, max_ctx, n_seqs, n_rows, hq, splits, pps;   // pps: pages a split
+  int max_pages, max_ctx, n_seqs, n_rows, hq;
+  int splits, pps, pps_tile;              // most splits of a row; pages a split, in the two kernels below
   float scale_log2;
   float* part;                            // [row][head][split][HD + 2]
 };
@@ -273,6 +287,10 @@ __device__ __forceinline__ void transpose4(uint32_t* r) {
   r[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
+// Sequences with more columns (query tokens x heads of a KV head) than this go through k_kv8_attn_tile.
+constexpr int kFewColumns = 32;
+constexpr int kTileWaves = 4;
+
 // Block (16 columns of one sequence and KV head, split): column = query token x head of the group.  The 4
 // waves take the split's pages in pairs, wave w pairs w, w + 4, ...; the next pair's codes are loaded while
 // one is computed.  Per pair:
@@ -295,13 +313,13 @@ __global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) 
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
   const int item = blockIdx.x / hkv, g = blockIdx.x - item * hkv;
   int first = item;
-  const int seq = a.off ? find_seq(a.off, a.n_seqs, item, G, 1, &first) : (int)(item / ((G + 15) / 16));
+  const int seq = a.off ? find_seq<16>(a.off, a.n_seqs, item, G, 1, &first) : (int)(item / ((G + 15) / 16));
   if (!a.off) first = seq * ((G + 15) / 16);
   if (seq < 0 || seq >= a.n_seqs || item < first) return;
   int r0, r1;
   seq_rows(a.off, seq, a.n_rows, r0, r1);
   const int n_cols = (r1 - r0) * G, c0 = 16 * (item - first);
-  if (c0 >= n_cols) return;
+  if (c0 >= n_cols || (a.off && n_cols > kFewColumns)) return;
   const int ctx = max(a.ctx[seq], 0);
   const bool too_long = ctx > a.max_ctx;                 // more than the launch was sized for: the rows are NaN
   const int np = too_long ? 0 : (ctx + 15) >> 4;
@@ -491,18 +509,270 @@ __global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) 
   }
 }
 
+// The same attention for sequences of many columns: a block owns 32 NW of them, a wave 32, and all its waves
+// read the same 64-key blocks of K and V from LDS, as bf16 values (code times scale, exact), converted once a block.
+// Per key block and wave:
+//   S^T = K q^T    v_mfma_f32_32x32x16_bf16: lane (col l % 32, h = l / 32) gets keys 8 (i / 4) + 4 h + i % 4, i < 16
+//   online softmax in base 2, a column in two lanes; O is rescaled only when some column's maximum moved
+//   O^T += V^T P^T    scores 0..7 and 8..15 of a lane are the B operands of two 16-key steps (keys 4 h + 0..3 and
+//                  8 + 4 h + 0..3 of a page), P in PP bf16 parts as above
+// LDS holds the operands in fragment order.  K: 16 dims of a key are one 16-byte load and the 16 bytes of two lanes;
+// slots are xor-ed with the dim step so that the 8 threads of a token row write to different banks.  V: 4 dims of 8
+// tokens are transposed in registers; row r of a 32-dim tile is dim 4 (r % 8) + r / 8, which spreads the writes and
+// leaves a lane 16 consecutive dims of the output.  The next block's codes travel in registers meanwhile (one barrier
+// a block).
+template <int HD, int FMT, typename T, int NW>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_tile(sara_kv8_cache c, AttnArgs a) {
+  constexpr int NKS = HD / 16, NDT = HD / 32, NTH = 64 * NW;
+  constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
+  constexpr int KU = (64 * NKS + NTH - 1) / NTH, VU = (2 * HD + NTH - 1) / NTH;   // staging units a thread
+  typedef float f32x16 __attribute__((ext_vector_type(16)));
+  __shared__ u32x4 kf[2][2 * NKS * 64], vf[2][4 * NDT * 64];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int hkv = c.n_kv_heads, G = a.hq / hkv;
+  const int item = (int)gridDim.x / hkv - 1 - (int)blockIdx.x / hkv, g = blockIdx.x % hkv;   // long tiles first
+  int first = 0;
+  const int seq = find_seq<32 * NW>(a.off, a.n_seqs, item, G, 1, &first);
+  if (seq < 0 || item < first) return;
+  int r0, r1;
+  seq_rows(a.off, seq, a.n_rows, r0, r1);
+  const int n_cols = (r1 - r0) * G, c0 = 32 * NW * (item - first);
+  if (c0 >= n_cols || n_cols <= kFewColumns) return;
+  const int ctx = max(a.ctx[seq], 0);
+  const bool too_long = ctx > a.max_ctx;
+  const int np = too_long ? 0 : (ctx + 15) >> 4;
+  const int p0 = blockIdx.y * a.pps_tile;
+  if (p0 >= np && blockIdx.y > 0) return;
+  const int before = ctx - (r1 - r0);
+  const int c_last = min(c0 + 32 * NW, n_cols) - 1;
+  const int keys = min(max(before + c_last / G + 1, 0), ctx);       // keys that some column of the block sees
+  const int p1 = min(min(np, p0 + a.pps_tile), (keys + 15) >> 4);
+  const int nkb = p1 > p0 ? (p1 - p0 + 3) >> 2 : 0;
+  const int wc0 = c0 + 32 * wave;
+  const bool live = wc0 < n_cols;
+  const int cc = min(wc0 + col, n_cols - 1), qt = cc / G, head = g * G + cc - qt * G;
+  const int seen = live ? before + qt + 1 : 0;                      // keys this lane's column sees
+  const int w_seen = live ? before + min(wc0 + 31, n_cols - 1) / G + 1 : 0;   // that some column of the wave sees
+  const int w_all = before + wc0 / G + 1;                           // that every column of the wave sees
+  // a negative scale becomes the sign of q; the floor keeps a masked -inf from meeting a scale of 0
+  const float sl2 = fmaxf(fabsf(a.scale_log2), 1e-37f);
+  u32x4 qf[QP][NKS];
+  {
+    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+    const T* q = (const T*)a.q + (size_t)(r0 + qt) * a.q_row + (size_t)head * a.q_head + 8 * h;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      if constexpr (QP == 1) {
+        qf[0][ks] = *(const u32x4*)(q + 16 * ks) ^ flip;
+      } else {
+        float f[8];
+        load8<T>(q + 16 * ks, f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t w[QP];
+          split_bf16<QP>(f[2 * j], f[2 * j + 1], w);
+#pragma unroll
+          for (int p = 0; p < QP; ++p) qf[p][ks][j] = w[p] ^ flip;
+        }
+      }
+    }
+  }
+  const int32_t* table = a.pages + (size_t)seq * a.max_pages;
+  // lane i: page i of a stretch of 64 (16 key blocks), its exponent bytes (0x10000: no page, 0x20000: NaN)
+  int ids = 0, meta = 0;
+  u32x4 kr[KU];
+  uint32_t vr[VU][8];
+  int km[KU], vm[VU];
+  auto load = [&](int kb) {
+    if ((kb & 15) == 0) {
+      const int pg = p0 + 4 * kb + lane;
+      const int id = pg < p1 ? table[pg] : -1;
+      const bool have = id >= 0 && id < c.n_pages;
+      ids = have ? id : 0;
+      const size_t block = (size_t)ids * hkv + g;
+      const int ke = c.k_exp[block], ve = c.v_exp[block];
+      meta = ke | ve << 8 | (have ? 0 : 0x10000) | (ke == 255 || ve == 255 ? 0x20000 : 0);
+    }
+    const int at = 4 * (kb & 15);
+#pragma unroll
+    for (int x = 0; x < KU; ++x) {
+      const int u = tid + NTH * x, ks = u % NKS, r = u / NKS & 63;
+      km[x] = __shfl(meta, at + (r >> 4), 64);
+      const size_t block = (size_t)__shfl(ids, at + (r >> 4), 64) * hkv + g;
+      kr[x] = *(const u32x4*)((const uint8_t*)c.k + (block * kBlockTok + (r & 15)) * HD + 16 * ks);
+    }
+#pragma unroll
+    for (int x = 0; x < VU; ++x) {
+      const int u = (tid + NTH * x) % (2 * HD), cd = u % (HD / 4), hv = u / (HD / 4) & 1, pg = u / (HD / 2);
+      vm[x] = __shfl(meta, at + pg, 64);
+      const size_t block = (size_t)__shfl(ids, at + pg, 64) * hkv + g;
+      const uint8_t* vp = (const uint8_t*)c.v + (block * kBlockTok + 4 * hv) * HD + 4 * cd;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vr[x][j] = *(const uint32_t*)(vp + (j + 4 * (j >> 2)) * HD);
+    }
+  };
+  auto store = [&](int kb, int buf) {
+#pragma unroll
+    for (int x = 0; x < KU; ++x) {
+      const int u = tid + NTH * x, ks = u % NKS, r = u / NKS;
+      if (64 * NKS % NTH != 0 && r >= 64) break;
+      const float scale = ldexpf(1.f, (km[x] & 255) - 127);
+      u32x4 w[2];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        u32x2 y = values_bf16<FMT>(kr[x][q], scale);
+        if (km[x] & 0x20000) y = u32x2{0x7FC07FC0u, 0x7FC07FC0u};    // a NaN page, seen through its keys' scores
+        w[q >> 1][2 * (q & 1)] = y.x;
+        w[q >> 1][2 * (q & 1) + 1] = y.y;
+      }
+      u32x4* dst = &kf[buf][((r >> 5) * NKS + ks) * 64 + ((r & 31) ^ (ks & 7))];
+      dst[0] = w[0];
+      dst[32] = w[1];
+    }
+    const bool tail = 16 * (p0 + 4 * kb) + 64 > ctx;
+#pragma unroll
+    for (int x = 0; x < VU; ++x) {
+      const int u = tid + NTH * x, cd = u % (HD / 4), hv = u / (HD / 4) & 1, pg = u / (HD / 2);
+      if (2 * HD % NTH != 0 && pg >= 4) break;
+      const int live_tok = (vm[x] & 0x30000) ? 0 : tail ? ctx - 16 * (p0 + 4 * kb + pg) : 16;
+      if (live_tok < 16)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vr[x][j] = j + 4 * (j >> 2) + 4 * hv < live_tok ? vr[x][j] : 0u;
+      transpose4(vr[x]);
+      transpose4(vr[x] + 4);
+      const float scale = (vm[x] & 0x20000) ? 0.f : ldexpf(1.f, (vm[x] >> 8 & 255) - 127);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const u32x2 y = values_bf16<FMT>(vr[x][j], scale), z = values_bf16<FMT>(vr[x][4 + j], scale);
+        vf[buf][(pg * NDT + (cd >> 3)) * 64 + 32 * hv + 8 * j + (cd & 7)] = u32x4{y.x, y.y, z.x, z.y};
+      }
+    }
+  };
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[NDT];
+#pragma unroll
+  for (int t = 0; t < NDT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  auto compute = [&](int kb, int buf, int absent) {
+    const int k0 = 16 * (p0 + 4 * kb);
+    f32x16 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {
+        const bf16x8 kk = __builtin_bit_cast(bf16x8, kf[buf][(b * NKS + ks) * 64 + 32 * h + (col ^ (ks & 7))]);
+#pragma unroll
+        for (int p = QP - 1; p >= 0; --p)
+          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, __builtin_bit_cast(bf16x8, qf[p][ks]), s[b], 0, 0, 0);
+      }
+    }
+    if (k0 + 64 > w_all || absent) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool in = k0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) < seen && !(absent >> (2 * b + (i >> 3)) & 1);
+          s[b][i] = in ? s[b][i] : -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = fmaxf(m, mx * sl2);
+    const float sub = mx == -INFINITY ? 0.f : mx;
+    if (__any(mx > m)) {
+      const float al = __builtin_amdgcn_exp2f(m - sub);
+      l *= al;
+#pragma unroll
+      for (int t = 0; t < NDT; ++t) o[t] *= al;
+      m = mx;
+    }
+#pragma unroll
+    for (int st = 0; st < 4; ++st) {
+      u32x4 pf[PP];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 8 * (st & 1) + 2 * j;
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][i], sl2, -sub));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][i + 1], sl2, -sub));
+        l += e0 + e1;
+        uint32_t w[PP];
+        split_bf16<PP>(e0, e1, w);
+#pragma unroll
+        for (int p = 0; p < PP; ++p) pf[p][j] = w[p];
+      }
+#pragma unroll
+      for (int t = 0; t < NDT; ++t) {
+        const bf16x8 vv = __builtin_bit_cast(bf16x8, vf[buf][(st * NDT + t) * 64 + lane]);
+#pragma unroll
+        for (int p = PP - 1; p >= 0; --p)
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, __builtin_bit_cast(bf16x8, pf[p]), o[t], 0, 0, 0);
+      }
+    }
+  };
+  // bit i: page i of the key block has no page id
+  auto absent_pages = [&](int kb) { return (int)(__ballot(meta & 0x10000) >> (4 * (kb & 15)) & 15); };
+  int absent = 0;
+  if (nkb > 0) {
+    load(0);
+    absent = absent_pages(0);
+    store(0, 0);
+  }
+  __syncthreads();
+  for (int kb = 0; kb < nkb; ++kb) {
+    int next_absent = 0;
+    if (kb + 1 < nkb) {
+      load(kb + 1);
+      next_absent = absent_pages(kb + 1);
+    }
+    if (16 * (p0 + 4 * kb) < w_seen) compute(kb, kb & 1, absent);
+    if (kb + 1 < nkb) store(kb + 1, (kb + 1) & 1);
+    absent = next_absent;
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (!live || wc0 + col >= n_cols) return;
+  const float inv = too_long ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : 1.f / l;
+  const bool whole = np <= a.pps_tile;
+  T* out = (T*)a.out + (size_t)(r0 + qt) * a.o_row + (size_t)head * a.o_head + 16 * h;
+  float* part = a.part + (((size_t)(r0 + qt) * a.hq + head) * a.splits + blockIdx.y) * (HD + 2);
+#pragma unroll
+  for (int t = 0; t < NDT; ++t) {
+    float f[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] = o[t][4 * (e & 3) + (e >> 2)];
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) f[e] *= inv;
+      store8<T>(out + 32 * t, f);
+      store8<T>(out + 32 * t + 8, f + 8);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) *(f32x2*)(part + 32 * t + 16 * h + e) = f32x2{f[e], f[e + 1]};
+    }
+  }
+  if (!whole && h == 0) *(f32x2*)(part + HD) = f32x2{m, l};
+}
+
 // A block per (row, head) joins the splits of rows that have more than one, eight at a time.
 template <int HD, typename T>
-__global__ __launch_bounds__(HD) void k_kv8_attn_join(AttnArgs a) {
+__global__ __launch_bounds__(HD) void k_kv8_attn_join(AttnArgs a, int hkv) {
   const int row = blockIdx.x / a.hq, h = blockIdx.x - row * a.hq;
   int first = 0;
-  const int seq = a.off ? find_seq(a.off, a.n_seqs, row, 16, 0, &first) : row;
+  const int seq = a.off ? find_seq<1>(a.off, a.n_seqs, row, 1, 0, &first) : row;
   if (seq < 0) return;
   int r0, r1;
   seq_rows(a.off, seq, a.n_rows, r0, r1);
   if (row < r0 || row >= r1) return;
   const int ctx = a.ctx[seq];
-  const int ns = (((ctx + 15) >> 4) + a.pps - 1) / a.pps;
+  const int pps = a.off && (r1 - r0) * (a.hq / hkv) > kFewColumns ? a.pps_tile : a.pps;
+  const int ns = (((ctx + 15) >> 4) + pps - 1) / pps;
   if (ctx > a.max_ctx || ns <= 1) return;
   const float* p = a.part + ((size_t)row * a.hq + h) * a.splits * (HD + 2);
   float mx = -INFINITY, num = 0.f, den = 0.f;
@@ -572,14 +842,20 @@ int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int d
 }
 
 Kv8Split kv8_split(int n_rows, int hq, int hkv, int n_seqs, int max_ctx, bool ragged) {
-  const int G = hq / hkv;
-  const int64_t items = ragged ? (int64_t)n_rows * G / 16 + n_seqs : (int64_t)n_seqs * ((G + 15) / 16);
-  const int np = std::max(1, (max_ctx + 15) / 16);
-  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(1, items * hkv));
-  Kv8Split s;
-  s.pps = (int)std::max<int64_t>(8, ((np + want - 1) / want + 7) / 8 * 8);
-  s.splits = (np + s.pps - 1) / s.pps;
-  s.items = items;
+  const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16);
+  // pages a split so that about `blocks` blocks share the work, at least `least`, in steps of `step`
+  auto share = [&](int64_t items, int64_t blocks, int least, int step) {
+    const int64_t want = std::max<int64_t>(1, blocks / std::max<int64_t>(1, items * hkv));
+    return (int)std::max<int64_t>(least, ((np + want - 1) / want + step - 1) / step * step);
+  };
+  Kv8Split s = {};
+  s.items = ragged ? (int64_t)n_rows * G / 16 + n_seqs : (int64_t)n_seqs * ((G + 15) / 16);
+  s.tile_items = ragged && (int64_t)n_rows * G > kFewColumns ? (int64_t)n_rows * G / (32 * kTileWaves) + n_seqs : 0;
+  s.pps = share(s.items, 1024, 8, 8);
+  s.pps_tile = s.tile_items ? share(s.tile_items, 512, 64, 64) : s.pps;
+  s.splits = (np + std::min(s.pps, s.pps_tile) - 1) / std::min(s.pps, s.pps_tile);
+  s.few_splits = (np + s.pps - 1) / s.pps;
+  s.tile_splits = s.tile_items ? (np + s.pps_tile - 1) / s.pps_tile : 0;
   return s;
 }
 
@@ -588,13 +864,16 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
                          int max_ctx, float scale, void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st) {
   const Kv8Split s = kv8_split(n_rows, hq, c.n_kv_heads, n_seqs, max_ctx, off != nullptr);
   const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
-                      s.splits, s.pps, scale * 1.4426950408889634f, (float*)ws};
+                      s.splits, s.pps, s.pps_tile, scale * 1.4426950408889634f, (float*)ws};
   return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
-    hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.items * c.n_kv_heads), s.splits),
+    hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.items * c.n_kv_heads), s.few_splits),
                        dim3(256), 0, st, c, a);
+    if (s.tile_items)
+      hipLaunchKernelGGL((k_kv8_attn_tile<hd.value, fmt.value, decltype(t), kTileWaves>),
+                         dim3((uint32_t)(s.tile_items * c.n_kv_heads), s.tile_splits), dim3(64 * kTileWaves), 0, st, c, a);
     if (s.splits > 1)
       hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t)>), dim3((uint32_t)((int64_t)n_rows * hq)), dim3(hd.value),
-                         0, st, a);
+                         0, st, a, c.n_kv_heads);
   });
 }
 
