@@ -38,10 +38,18 @@ template <int FMT> __device__ __forceinline__ uint32_t encode4(float a, float b,
   }
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
+// byte B of a word, signed, as a float: one instruction (left to itself the compiler shifts first)
+template <int B> __device__ __forceinline__ float byte_f32(uint32_t w) {
+  float f;
+  if (B == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(w));
+  if (B == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(w));
+  if (B == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(w));
+  if (B == 3) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(w));
+  return f;
+}
 template <int FMT> __device__ __forceinline__ void decode4(uint32_t w, float* f) {
   if (FMT == SARA_KV8_INT8) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) f[q] = (float)(int8_t)(w >> (8 * q));
+    f[0] = byte_f32<0>(w); f[1] = byte_f32<1>(w); f[2] = byte_f32<2>(w); f[3] = byte_f32<3>(w);
   } else {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     f[0] = lo[0]; f[1] = lo[1]; f[2] = hi[0]; f[3] = hi[1];
@@ -49,6 +57,9 @@ template <int FMT> __device__ __forceinline__ void decode4(uint32_t w, float* f)
 }
 // four codes as bf16, exactly
 template <int FMT> __device__ __forceinline__ u32x2 codes_bf16(uint32_t w) {
+  if (FMT == SARA_KV8_E4M3)
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true))};
   float f[4];
   decode4<FMT>(w, f);
   return u32x2{__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
@@ -292,8 +303,8 @@ constexpr int kFewColumns = 32;
 constexpr int kTileWaves = 4;
 
 // Block (16 columns of one sequence and KV head, split): column = query token x head of the group.  The 4
-// waves take the split's pages in pairs, wave w pairs w, w + 4, ...; the next pair's codes are loaded while
-// one is computed.  Per pair:
+// waves take the split's pages in pairs, wave w pairs w, w + 4, ...; the next pair's K codes are loaded once
+// the scores are there, its V codes at the end.  Per pair:
 //   S^T = K q^T   codes as bf16 (exact), the page's scale on the fp32 scores
 //   online softmax per column in base 2 over the 4 lanes that hold it; the maximum kept is the value
 //                 that was subtracted
@@ -302,7 +313,7 @@ constexpr int kTileWaves = 4;
 //                 (2: 2^-17 of a weight; 3 for fp32 queries), so the product adds no rounding of its own
 // Queries of fp32 enter as 3 bf16 parts.  A column without a visible key gives 0.
 template <int HD, int FMT, typename T>
-__global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) {
   constexpr int NK = HD / 64, NT = HD / 16, DV = HD / 16;   // 16-byte K loads, dim tiles, V dims a lane
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
   constexpr int PITCH = HD + 4;
@@ -312,18 +323,21 @@ __global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) 
   const int col = lane & 15, grp = lane >> 4;
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
   const int item = blockIdx.x / hkv, g = blockIdx.x - item * hkv;
-  int first = item;
-  const int seq = a.off ? find_seq<16>(a.off, a.n_seqs, item, G, 1, &first) : (int)(item / ((G + 15) / 16));
-  if (!a.off) first = seq * ((G + 15) / 16);
-  if (seq < 0 || seq >= a.n_seqs || item < first) return;
+  const int tiles = a.off ? kFewColumns / 16 : (G + 15) / 16;
+  const int seq = item / tiles, c0 = 16 * (item - seq * tiles);
   int r0, r1;
   seq_rows(a.off, seq, a.n_rows, r0, r1);
-  const int n_cols = (r1 - r0) * G, c0 = 16 * (item - first);
+  const int n_cols = (r1 - r0) * G;
   if (c0 >= n_cols || (a.off && n_cols > kFewColumns)) return;
+  const int p0 = blockIdx.y * a.pps;
+  // ids of 32 of the wave's page pairs, one a lane; the first are loaded beside the context's length
+  const int32_t* table = a.pages + (size_t)seq * a.max_pages;
+  auto load_ids = [&](int it) { return table[min(p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1), a.max_pages - 1)]; };
+  int ids = load_ids(0);
   const int ctx = max(a.ctx[seq], 0);
   const bool too_long = ctx > a.max_ctx;                 // more than the launch was sized for: the rows are NaN
   const int np = too_long ? 0 : (ctx + 15) >> 4;
-  const int p0 = blockIdx.y * a.pps, p1 = min(np, p0 + a.pps);
+  const int p1 = min(np, p0 + a.pps);
   if (p0 >= p1 && blockIdx.y > 0) return;
   // this lane's column: query row and head, and how many keys it sees
   const int cc = min(c0 + col, n_cols - 1), qt = cc / G, head = g * G + cc - qt * G;
@@ -351,52 +365,56 @@ __global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) 
       }
     }
   }
-  struct Pair {
-    u32x4 k[2][NK];
-    uint32_t v[2][4][DV / 4];
-    int ke[2], ve[2];
-    bool have[2];
-  };
-  const int32_t* table = a.pages + (size_t)seq * a.max_pages;
   const int n_it = p1 <= p0 + 2 * wave ? 0 : (p1 - p0 - 2 * wave + 7) / 8;
-  int ids = -1;
-  auto load = [&](Pair& t, int it) {
-    if ((it & 31) == 0) {                                // ids of the next 32 pairs, one a lane
-      const int pg = p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1);
-      ids = pg < p1 ? table[pg] : -1;
-    }
+  u32x4 kr[2][NK];
+  uint32_t vr[2][4][DV / 4];
+  int ke[2], ve[2];
+  size_t v_block[2];
+  bool have[2], v_have[2];
+  // K codes and the exponents of pair `it`; its V codes follow by load_v, once V's registers are free
+  auto load_k = [&](int it) {
+    if (it > 0 && (it & 31) == 0) ids = load_ids(it);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int id = __builtin_amdgcn_readlane(ids, 2 * (it & 31) + p);
-      t.have[p] = id >= 0 && id < c.n_pages;
-      const size_t block = (size_t)(t.have[p] ? id : 0) * hkv + g;
-      const uint8_t* kp = (const uint8_t*)c.k + (block * kBlockTok + col) * HD + 16 * grp;
+      have[p] = p0 + 2 * wave + 8 * it + p < p1 && id >= 0 && id < c.n_pages;
+      v_block[p] = (size_t)(have[p] ? id : 0) * hkv + g;
+      const uint8_t* kp = (const uint8_t*)c.k + (v_block[p] * kBlockTok + col) * HD + 16 * grp;
 #pragma unroll
-      for (int i = 0; i < NK; ++i) t.k[p][i] = *(const u32x4*)(kp + 64 * i);
-      const uint8_t* vp = (const uint8_t*)c.v + (block * kBlockTok + 4 * grp) * HD + DV * col;
+      for (int i = 0; i < NK; ++i) kr[p][i] = *(const u32x4*)(kp + 64 * i);
+      ke[p] = c.k_exp[v_block[p]];
+      ve[p] = c.v_exp[v_block[p]];
+    }
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      v_have[p] = have[p];
+      const uint8_t* vp = (const uint8_t*)c.v + (v_block[p] * kBlockTok + 4 * grp) * HD + DV * col;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int w = 0; w < DV / 4; ++w) t.v[p][j][w] = *(const uint32_t*)(vp + j * HD + 4 * w);
-      t.ke[p] = c.k_exp[block];
-      t.ve[p] = c.v_exp[block];
+        for (int w = 0; w < DV / 4; ++w) vr[p][j][w] = *(const uint32_t*)(vp + j * HD + 4 * w);
     }
   };
   float m = -INFINITY, l = 0.f;
   f32x4 o[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto compute = [&](Pair& t, int it) {
+  if (n_it > 0) {
+    load_k(0);
+    load_v();
+  }
+  for (int it = 0; it < n_it; ++it) {
     f32x4 s[2];
     float vs[2];
     float mx = m;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const int k0 = 16 * (p0 + 2 * wave + 8 * it + p);
       s[p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 2 * NK; ++i) {
-        const u32x2 x = codes_bf16<FMT>(t.k[p][i >> 1][2 * (i & 1)]), y = codes_bf16<FMT>(t.k[p][i >> 1][2 * (i & 1) + 1]);
+        const u32x2 x = codes_bf16<FMT>(kr[p][i >> 1][2 * (i & 1)]), y = codes_bf16<FMT>(kr[p][i >> 1][2 * (i & 1) + 1]);
         const bf16x8 kf = __builtin_bit_cast(bf16x8, u32x4{x.x, x.y, y.x, y.y});
 #pragma unroll
         for (int qp = QP - 1; qp >= 0; --qp)
@@ -404,32 +422,38 @@ __global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) 
       }
       // a page of NaN scale in K or V makes the scores of its keys NaN, so it reaches only the columns that
       // see them; its V then counts as 0
-      const bool bad = t.ke[p] == 255 || t.ve[p] == 255;
-      const float ks = bad ? __uint_as_float(0x7FC00000u) : ldexpf(a.scale_log2, t.ke[p] - 127);
-      vs[p] = bad ? 0.f : ldexpf(1.f, t.ve[p] - 127);
+      const bool bad = ke[p] == 255 || ve[p] == 255;
+      const float ks = bad ? __uint_as_float(0x7FC00000u) : ldexpf(a.scale_log2, ke[p] - 127);
+      vs[p] = bad ? 0.f : ldexpf(1.f, ve[p] - 127);
       s[p] *= ks;
-      const bool whole = t.have[p] && k0 + 16 <= seen_all;
-      if (!whole) {
-        const int left = t.have[p] ? seen - k0 - 4 * grp : 0;
+    }
+    if (it + 1 < n_it) load_k(it + 1);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int k0 = 16 * (p0 + 2 * wave + 8 * it + p);
+      if (!v_have[p] || k0 + 16 > seen_all) {
+        const int left = v_have[p] ? seen - k0 - 4 * grp : 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) s[p][q] = q < left ? s[p][q] : -INFINITY;
         // codes past the sequence's last token may be anything
-        const int live = t.have[p] ? ctx - k0 - 4 * grp : 0;
+        const int live = v_have[p] ? ctx - k0 - 4 * grp : 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int w = 0; w < DV / 4; ++w) t.v[p][j][w] = j < live ? t.v[p][j][w] : 0u;
+          for (int w = 0; w < DV / 4; ++w) vr[p][j][w] = j < live ? vr[p][j][w] : 0u;
       }
       mx = fmaxf(mx, fmaxf(fmaxf(s[p][0], s[p][1]), fmaxf(s[p][2], s[p][3])));
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float sub = mx == -INFINITY ? 0.f : mx;         // nothing seen yet: every weight is 0
-    const float al = __builtin_amdgcn_exp2f(m - sub);
-    m = mx;
-    l *= al;
+    if (__any(mx > m)) {
+      const float al = __builtin_amdgcn_exp2f(m - sub);
+      l *= al;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) o[i] *= al;
+      for (int i = 0; i < NT; ++i) o[i] *= al;
+      m = mx;
+    }
     u32x4 pf[PP];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
@@ -444,8 +468,8 @@ __global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) 
       }
 #pragma unroll
     for (int w = 0; w < DV / 4; ++w) {
-      uint32_t x[4] = {t.v[0][0][w], t.v[0][1][w], t.v[0][2][w], t.v[0][3][w]};
-      uint32_t y[4] = {t.v[1][0][w], t.v[1][1][w], t.v[1][2][w], t.v[1][3][w]};
+      uint32_t x[4] = {vr[0][0][w], vr[0][1][w], vr[0][2][w], vr[0][3][w]};
+      uint32_t y[4] = {vr[1][0][w], vr[1][1][w], vr[1][2][w], vr[1][3][w]};
       transpose4(x);
       transpose4(y);
 #pragma unroll
@@ -457,16 +481,7 @@ __global__ __launch_bounds__(256) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) 
           o[4 * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pf[p]), o[4 * w + i], 0, 0, 0);
       }
     }
-  };
-  Pair t0, t1;
-  if (n_it > 0) load(t0, 0);
-  for (int it = 0; it < n_it; it += 2) {
-    if (it + 1 < n_it) load(t1, it + 1);
-    compute(t0, it);
-    if (it + 1 < n_it) {
-      if (it + 2 < n_it) load(t0, it + 2);
-      compute(t1, it + 1);
-    }
+    if (it + 1 < n_it) load_v();
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -760,45 +775,85 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
   if (!whole && h == 0) *(f32x2*)(part + HD) = f32x2{m, l};
 }
 
-// A block per (row, head) joins the splits of rows that have more than one, eight at a time.
-template <int HD, typename T>
-__global__ __launch_bounds__(HD) void k_kv8_attn_join(AttnArgs a, int hkv) {
-  const int row = blockIdx.x / a.hq, h = blockIdx.x - row * a.hq;
-  int first = 0;
-  const int seq = a.off ? find_seq<1>(a.off, a.n_seqs, row, 1, 0, &first) : row;
-  if (seq < 0) return;
-  int r0, r1;
-  seq_rows(a.off, seq, a.n_rows, r0, r1);
-  if (row < r0 || row >= r1) return;
+// A block per (row, head) joins the splits of rows that have more than one: its 4 waves take every fourth split,
+// kJoin of them in flight, and meet in LDS.  TILE: the rows of k_kv8_attn_tile, found by their number; else those of
+// k_kv8_attn, `cols` columns for each sequence and KV head.
+constexpr int kJoin = 4;
+template <int HD, typename T, bool TILE>
+__global__ __launch_bounds__(256) void k_kv8_attn_join(AttnArgs a, int hkv, int cols) {
+  constexpr int DL = HD / 64;                            // dims a lane
+  __shared__ float m_w[4], l_w[4], o_w[4][HD];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, G = a.hq / hkv;
+  int seq, row, h, r0, r1;
+  if (TILE) {
+    int first = 0;
+    row = blockIdx.x / a.hq;
+    h = blockIdx.x - row * a.hq;
+    seq = find_seq<1>(a.off, a.n_seqs, row, 1, 0, &first);
+    if (seq < 0) return;
+    seq_rows(a.off, seq, a.n_rows, r0, r1);
+    if (row < r0 || row >= r1 || (r1 - r0) * G <= kFewColumns) return;
+  } else {
+    const int gc = blockIdx.x / cols, x = blockIdx.x - gc * cols;
+    seq = gc / hkv;
+    seq_rows(a.off, seq, a.n_rows, r0, r1);
+    const int n_cols = (r1 - r0) * G;
+    if (x >= n_cols || (a.off && n_cols > kFewColumns)) return;
+    row = r0 + x / G;
+    h = (gc - seq * hkv) * G + x % G;
+  }
   const int ctx = a.ctx[seq];
-  const int pps = a.off && (r1 - r0) * (a.hq / hkv) > kFewColumns ? a.pps_tile : a.pps;
+  const int pps = TILE ? a.pps_tile : a.pps;
   const int ns = (((ctx + 15) >> 4) + pps - 1) / pps;
   if (ctx > a.max_ctx || ns <= 1) return;
   const float* p = a.part + ((size_t)row * a.hq + h) * a.splits * (HD + 2);
-  float mx = -INFINITY, num = 0.f, den = 0.f;
-  for (int s0 = 0; s0 < ns; s0 += 8) {
-    float pm[8], pl[8], po[8];
+  float m = -INFINITY, l = 0.f, o[DL] = {};
+  for (int s0 = wave; s0 < ns; s0 += 4 * kJoin) {
+    float pm[kJoin], pl[kJoin], po[kJoin][DL];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float* q = p + (size_t)min(s0 + i, ns - 1) * (HD + 2);
-      pm[i] = s0 + i < ns ? q[HD] : -INFINITY;
-      pl[i] = q[HD + 1];
-      po[i] = q[threadIdx.x];
+    for (int i = 0; i < kJoin; ++i) {
+      const float* q = p + (size_t)min(s0 + 4 * i, ns - 1) * (HD + 2);
+      const f32x2 ml = *(const f32x2*)(q + HD);
+      pm[i] = s0 + 4 * i < ns ? ml[0] : -INFINITY;
+      pl[i] = ml[1];
+      if (DL == 2) {
+        const f32x2 v = *(const f32x2*)(q + 2 * lane);
+        po[i][0] = v[0];
+        po[i][DL - 1] = v[1];
+      } else {
+        po[i][0] = q[lane];
+      }
     }
-    float m2 = mx;
+    float mx = m;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m2 = fmaxf(m2, pm[i]);
-    const float sub = m2 == -INFINITY ? 0.f : m2;
-    const float al = __builtin_amdgcn_exp2f(mx - sub);
-    num *= al;
-    den *= al;
+    for (int i = 0; i < kJoin; ++i) mx = fmaxf(mx, pm[i]);
+    const float sub = mx == -INFINITY ? 0.f : mx;
+    const float al = __builtin_amdgcn_exp2f(m - sub);
+    l *= al;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int d = 0; d < DL; ++d) o[d] *= al;
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i) {
       const float w = __builtin_amdgcn_exp2f(pm[i] - sub);
-      num = fmaf(w, po[i], num);
-      den = fmaf(w, pl[i], den);
+      l = fmaf(w, pl[i], l);
+#pragma unroll
+      for (int d = 0; d < DL; ++d) o[d] = fmaf(w, po[i][d], o[d]);
     }
-    mx = m2;
+    m = mx;
+  }
+  if (lane == 0) { m_w[wave] = m; l_w[wave] = l; }
+#pragma unroll
+  for (int d = 0; d < DL; ++d) o_w[wave][DL * lane + d] = o[d];
+  __syncthreads();
+  if (threadIdx.x >= HD) return;
+  const float mx = fmaxf(fmaxf(m_w[0], m_w[1]), fmaxf(m_w[2], m_w[3]));
+  const float sub = mx == -INFINITY ? 0.f : mx;
+  float num = 0.f, den = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float wt = __builtin_amdgcn_exp2f(m_w[w] - sub);
+    num = fmaf(wt, o_w[w][threadIdx.x], num);
+    den = fmaf(wt, l_w[w], den);
   }
   st_f32<T>((T*)a.out + (size_t)row * a.o_row + (size_t)h * a.o_head, threadIdx.x, den == 0.f ? 0.f : num / den);
 }
@@ -843,15 +898,18 @@ int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int d
 
 Kv8Split kv8_split(int n_rows, int hq, int hkv, int n_seqs, int max_ctx, bool ragged) {
   const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16);
-  // pages a split so that about `blocks` blocks share the work, at least `least`, in steps of `step`
+  // Pages a split so that about `blocks` blocks share the work, at least `least`, in steps of `step`, and at most
+  // 128 splits a row.  A split costs its block about 4 us before the first pages are there and the join launch 4 us
+  // more: one row at context 333 takes 7.4 us in one split, 5.4 + 2.9 and a launch in three; 32 rows at 3,000-4,600
+  // take 16.9 us in splits of 24 pages, 18.6 of 32, 18.8 of 16.
   auto share = [&](int64_t items, int64_t blocks, int least, int step) {
-    const int64_t want = std::max<int64_t>(1, blocks / std::max<int64_t>(1, items * hkv));
+    const int64_t want = std::min<int64_t>(128, std::max<int64_t>(1, blocks / std::max<int64_t>(1, items * hkv)));
     return (int)std::max<int64_t>(least, ((np + want - 1) / want + step - 1) / step * step);
   };
   Kv8Split s = {};
-  s.items = ragged ? (int64_t)n_rows * G / 16 + n_seqs : (int64_t)n_seqs * ((G + 15) / 16);
+  s.items = (int64_t)n_seqs * (ragged ? kFewColumns / 16 : (G + 15) / 16);
   s.tile_items = ragged && (int64_t)n_rows * G > kFewColumns ? (int64_t)n_rows * G / (32 * kTileWaves) + n_seqs : 0;
-  s.pps = share(s.items, 1024, 8, 8);
+  s.pps = share(ragged ? n_seqs : s.items, 1024, 24, 8);
   s.pps_tile = s.tile_items ? share(s.tile_items, 512, 64, 64) : s.pps;
   s.splits = (np + std::min(s.pps, s.pps_tile) - 1) / std::min(s.pps, s.pps_tile);
   s.few_splits = (np + s.pps - 1) / s.pps;
@@ -871,9 +929,14 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
     if (s.tile_items)
       hipLaunchKernelGGL((k_kv8_attn_tile<hd.value, fmt.value, decltype(t), kTileWaves>),
                          dim3((uint32_t)(s.tile_items * c.n_kv_heads), s.tile_splits), dim3(64 * kTileWaves), 0, st, c, a);
-    if (s.splits > 1)
-      hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t)>), dim3((uint32_t)((int64_t)n_rows * hq)), dim3(hd.value),
-                         0, st, a, c.n_kv_heads);
+    if (s.few_splits > 1) {
+      const int cols = off ? kFewColumns : hq / c.n_kv_heads;
+      hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t), false>), dim3((uint32_t)((int64_t)n_seqs * c.n_kv_heads * cols)),
+                         dim3(256), 0, st, a, c.n_kv_heads, cols);
+    }
+    if (s.tile_splits > 1)
+      hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t), true>), dim3((uint32_t)((int64_t)n_rows * hq)), dim3(256), 0,
+                         st, a, c.n_kv_heads, 0);
   });
 }
 
