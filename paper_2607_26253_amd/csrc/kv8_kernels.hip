@@ -84,24 +84,33 @@ template <int FMT> __device__ __forceinline__ u32x2 values_bf16(uint32_t w, floa
 // Sequences own rows [off[i], off[i + 1]).  A launch numbers its items without a pass over the sequences:
 // sequence i's begin at off[i] mul / DIV + add i, which leaves room for floor(rows mul / DIV) + add of them.
 // The sequence of item b (-1: none), by a wave that cuts the range 64-fold a step.
+// What the caller needs of the sequence next comes with the last step: its rows and its entry of `per_seq`.
+struct SeqRows { int seq, first, r0, r1, value; };
 template <int DIV>
-__device__ __forceinline__ int find_seq(const int32_t* off, int n_seqs, int b, int mul, int add, int* first) {
+__device__ __forceinline__ SeqRows find_seq(const int32_t* off, const int32_t* per_seq, int n_seqs, int n_rows, int b, int mul,
+                                            int add) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, hi = n_seqs, base = 0;
+  int lo = 0, hi = n_seqs;
   while (true) {
     const int step = (hi - lo + 63) >> 6;
     const int i = lo + lane * step;
-    int at = 0x7FFFFFFF;
-    if (i < hi) at = (int)((int64_t)off[i] * mul / DIV) + add * i;
+    int at = 0x7FFFFFFF, o0 = 0, o1 = 0, value = 0;
+    if (i < hi) {
+      o0 = off[i];
+      if (step <= 1) { o1 = off[i + 1]; value = per_seq[i]; }
+      at = (int)((int64_t)o0 * mul / DIV) + add * i;
+    }
     const int n = __popcll(__ballot(at <= b));
-    if (n == 0) return -1;
-    base = __shfl(at, n - 1, 64);
+    if (n == 0) return SeqRows{-1, 0, 0, 0, 0};
     lo += (n - 1) * step;
     hi = min(hi, lo + step);
-    if (step <= 1) break;
+    if (step > 1) continue;
+    SeqRows s = {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readlane(at, n - 1), __builtin_amdgcn_readlane(o0, n - 1),
+                 __builtin_amdgcn_readlane(o1, n - 1), __builtin_amdgcn_readlane(value, n - 1)};
+    s.r0 = min(max(s.r0, 0), n_rows);
+    s.r1 = min(max(s.r1, s.r0), n_rows);
+    return s;
   }
-  *first = base;
-  return __builtin_amdgcn_readfirstlane(lo);
 }
 
 // rows of sequence i: [r0, r1), held inside the caller's tensor
@@ -128,15 +137,16 @@ __device__ __forceinline__ bool page_unit(int unit, int hkv, const int32_t* star
   u.is_v = unit & 1;
   const int rest = unit >> 1, item = rest / hkv;
   u.head = rest - item * hkv;
-  int first = item;
-  u.seq = off ? find_seq<16>(off, n_seqs, item, 1, 2, &first) : item;
-  if (u.seq < 0 || u.seq >= n_seqs || item < first) return false;
-  int r1;
-  seq_rows(off, u.seq, n_rows, u.r0, r1);
-  u.len = r1 - u.r0;
-  u.start = start[u.seq];
+  SeqRows s = {item, item, item, item + 1, 0};
+  if (off) s = find_seq<16>(off, start, n_seqs, n_rows, item, 1, 2);
+  else if (item < n_seqs) s.value = start[item];
+  if (s.seq < 0 || s.seq >= n_seqs || item < s.first) return false;
+  u.seq = s.seq;
+  u.r0 = s.r0;
+  u.len = s.r1 - s.r0;
+  u.start = s.value;
   if (u.start < 0 || u.len <= 0) return false;
-  u.page = (u.start >> 4) + (item - first);
+  u.page = (u.start >> 4) + (item - s.first);
   return u.page <= (int)(((int64_t)u.start + u.len - 1) >> 4);
 }
 
@@ -147,20 +157,80 @@ template <int HD> struct PageLanes {
   static constexpr int NI = kBlockTok / RPI;  // instructions a page
 };
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float* f);
-template <> __device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float* f) {
-  const u32x4 w = *(const u32x4*)p;
+// 8 elements as they lie in memory
+template <typename T> struct Raw8 { u32x4 w[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Raw8<T> load_raw8(const T* p) {
+  Raw8<T> r;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) { f[2 * q] = __uint_as_float(w[q] << 16); f[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u); }
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ((const u32x4*)p)[i];
+  return r;
 }
-template <> __device__ __forceinline__ void load8<float>(const float* p, float* f) {
+__device__ __forceinline__ void unpack8(const Raw8<uint16_t>& r, float* f) {
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const f32x4 w = *(const f32x4*)(p + 4 * q);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[4 * q + j] = w[j];
+  for (int q = 0; q < 4; ++q) {
+    f[2 * q] = __uint_as_float(r.w[0][q] << 16);
+    f[2 * q + 1] = __uint_as_float(r.w[0][q] & 0xFFFF0000u);
   }
 }
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, float* f) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(r.w[q >> 2][q & 3]);
+}
+template <typename T> __device__ __forceinline__ void load8(const T* p, float* f) { unpack8(load_raw8<T>(p), f); }
+
+// The larger of `most` and the magnitudes of 8 elements, as bits (NaN above inf above all); bf16 as two halves a word.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t magnitude(uint32_t most, const Raw8<uint16_t>& r) {
+  u16x2 m = __builtin_bit_cast(u16x2, most);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, r.w[0][q] & 0x7FFF7FFFu));
+  return __builtin_bit_cast(uint32_t, m);
+}
+__device__ __forceinline__ uint32_t magnitude(uint32_t most, const Raw8<float>& r) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) most = max(most, r.w[q >> 2][q & 3] & 0x7FFFFFFFu);
+  return most;
+}
+template <typename T> __device__ __forceinline__ uint32_t magnitude_bits(uint32_t most) {
+  return sizeof(T) == 4 ? most : max(most << 16, most & 0xFFFF0000u);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  auto with = [&](auto ctrl) { v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl.value, 0xF, 0xF, false)); };
+  with(std::integral_constant<int, 0x111>{});        // row_shr 1, 2, 4, 8
+  with(std::integral_constant<int, 0x112>{});
+  with(std::integral_constant<int, 0x114>{});
+  with(std::integral_constant<int, 0x118>{});
+  with(std::integral_constant<int, 0x142>{});        // row_bcast 15, 31
+  with(std::integral_constant<int, 0x143>{});
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// Codes of 8 elements at a page's exponent b < 255.  int8: the fma rounds x / scale to an integer in the low bits of
+// 1.5 2^23, ties to even.
+template <int FMT, typename T> __device__ __forceinline__ u32x2 quantise8(const Raw8<T>& r, int b) {
+  if constexpr (FMT == SARA_KV8_INT8) {
+    const float inv = ldexpf(1.f, 127 - b), magic = 12582912.f;
+    float f[8];
+    uint32_t c[8];
+    unpack8(r, f);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) c[q] = __float_as_uint(fmaf(f[q], inv, magic));
+    u32x2 w;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      w[q] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[4 * q + 3], c[4 * q + 2], 0x0C0C0400u),
+                                   __builtin_amdgcn_perm(c[4 * q + 1], c[4 * q], 0x0C0C0400u), 0x05040100u);
+    return w;
+  } else {
+    const float inv = ldexpf(1.f, 127 - b);
+    float f[8];
+    unpack8(r, f);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) f[q] *= inv;
+    return u32x2{encode4<FMT>(f[0], f[1], f[2], f[3]), encode4<FMT>(f[4], f[5], f[6], f[7])};
+  }
+}
+
 template <typename T> __device__ __forceinline__ void store8(T* p, const float* f);
 template <> __device__ __forceinline__ void store8<uint16_t>(uint16_t* p, const float* f) {
   *(u32x4*)p = u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
@@ -186,20 +256,16 @@ __global__ __launch_bounds__(256) void k_kv8_write(sara_kv8_cache c, KvRows src,
   const size_t block = (size_t)id * c.n_kv_heads + u.head;
   uint8_t* codes = (uint8_t*)(u.is_v ? c.v : c.k) + (block * kBlockTok + row) * HD + d0;
   uint8_t* exp = (u.is_v ? c.v_exp : c.k_exp) + block;
-  float f[PL::NI][8];
-  uint32_t amax = 0;
+  Raw8<T> r[PL::NI];
+  uint32_t most = 0;
 #pragma unroll
   for (int j = 0; j < PL::NI; ++j) {
     const int t = t0 + j * PL::RPI + row;
-    if (t >= 0 && t < u.len) {
-      load8<T>(x + (size_t)(u.r0 + t) * stride, f[j]);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) amax = max(amax, __float_as_uint(f[j][q]) & 0x7FFFFFFFu);   // NaN above inf above all
-    }
+    r[j] = load_raw8<T>(x + (size_t)(u.r0 + min(max(t, 0), u.len - 1)) * stride);   // rows outside repeat one of the page's
   }
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, 64));
-  int b = exponent_of<FMT>(amax);
+  for (int j = 0; j < PL::NI; ++j) most = magnitude(most, r[j]);
+  int b = exponent_of<FMT>(wave_max(magnitude_bits<T>(most)));
   if (t0 < 0) {
     const int old = *exp;
     b = max(b, old);
@@ -221,12 +287,7 @@ __global__ __launch_bounds__(256) void k_kv8_write(sara_kv8_cache c, KvRows src,
 #pragma unroll
   for (int j = 0; j < PL::NI; ++j) {
     const int t = t0 + j * PL::RPI + row;
-    if (t >= 0 && t < u.len) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) f[j][q] = b == 255 ? 0.f : ldexpf(f[j][q], 127 - b);
-      *(u32x2*)(codes + (size_t)j * PL::RPI * HD) =
-          u32x2{encode4<FMT>(f[j][0], f[j][1], f[j][2], f[j][3]), encode4<FMT>(f[j][4], f[j][5], f[j][6], f[j][7])};
-    }
+    if (t >= 0 && t < u.len) *(u32x2*)(codes + (size_t)j * PL::RPI * HD) = b == 255 ? u32x2{0u, 0u} : quantise8<FMT, T>(r[j], b);
   }
   if (lane == 0) *exp = (uint8_t)b;
 }
@@ -546,14 +607,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
   const int item = (int)gridDim.x / hkv - 1 - (int)blockIdx.x / hkv, g = blockIdx.x % hkv;   // long tiles first
-  int first = 0;
-  const int seq = find_seq<32 * NW>(a.off, a.n_seqs, item, G, 1, &first);
-  if (seq < 0 || item < first) return;
-  int r0, r1;
-  seq_rows(a.off, seq, a.n_rows, r0, r1);
-  const int n_cols = (r1 - r0) * G, c0 = 32 * NW * (item - first);
+  const SeqRows sr = find_seq<32 * NW>(a.off, a.ctx, a.n_seqs, a.n_rows, item, G, 1);
+  const int seq = sr.seq, r0 = sr.r0, r1 = sr.r1;
+  if (seq < 0 || item < sr.first) return;
+  const int n_cols = (r1 - r0) * G, c0 = 32 * NW * (item - sr.first);
   if (c0 >= n_cols || n_cols <= kFewColumns) return;
-  const int ctx = max(a.ctx[seq], 0);
+  const int ctx = max(sr.value, 0);
   const bool too_long = ctx > a.max_ctx;
   const int np = too_long ? 0 : (ctx + 15) >> 4;
   const int p0 = blockIdx.y * a.pps_tile;
@@ -784,25 +843,23 @@ __global__ __launch_bounds__(256) void k_kv8_attn_join(AttnArgs a, int hkv, int 
   constexpr int DL = HD / 64;                            // dims a lane
   __shared__ float m_w[4], l_w[4], o_w[4][HD];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, G = a.hq / hkv;
-  int seq, row, h, r0, r1;
+  int seq, row, h, r0, r1, ctx;
   if (TILE) {
-    int first = 0;
     row = blockIdx.x / a.hq;
     h = blockIdx.x - row * a.hq;
-    seq = find_seq<1>(a.off, a.n_seqs, row, 1, 0, &first);
-    if (seq < 0) return;
-    seq_rows(a.off, seq, a.n_rows, r0, r1);
-    if (row < r0 || row >= r1 || (r1 - r0) * G <= kFewColumns) return;
+    const SeqRows sr = find_seq<1>(a.off, a.ctx, a.n_seqs, a.n_rows, row, 1, 0);
+    ctx = sr.value;
+    if (sr.seq < 0 || row < sr.r0 || row >= sr.r1 || (sr.r1 - sr.r0) * G <= kFewColumns) return;
   } else {
     const int gc = blockIdx.x / cols, x = blockIdx.x - gc * cols;
     seq = gc / hkv;
+    ctx = a.ctx[seq];
     seq_rows(a.off, seq, a.n_rows, r0, r1);
     const int n_cols = (r1 - r0) * G;
     if (x >= n_cols || (a.off && n_cols > kFewColumns)) return;
     row = r0 + x / G;
     h = (gc - seq * hkv) * G + x % G;
   }
-  const int ctx = a.ctx[seq];
   const int pps = TILE ? a.pps_tile : a.pps;
   const int ns = (((ctx + 15) >> 4) + pps - 1) / pps;
   if (ctx > a.max_ctx || ns <= 1) return;
