@@ -20,7 +20,8 @@ SARA_F32, SARA_BF16 = 0, 1
 SARA_MODE_SARA, SARA_MODE_FIXED_K, SARA_MODE_SARA_THOMPSON = 0, 1, 2
 _MODES = {"sara": SARA_MODE_SARA, "fixed_k": SARA_MODE_FIXED_K, "sara_thompson": SARA_MODE_SARA_THOMPSON}
 SARA_KV8_INT8, SARA_KV8_E4M3 = 0, 1
-SARA_COMMIT, SARA_ABANDON, SARA_CONTINUE = 1, 2, 3
+SARA_COMMIT, SARA_ABANDON, SARA_CONTINUE = 1, 2, 3                     # decisions
+SARA_UNDRAWN, SARA_ACTIVE, SARA_COMMITTED, SARA_ABANDONED = 0, 1, 2, 3   # status of a prompt
 
 EXPORTED = ["sara_init", "sara_begin_step", "sara_decode_step", "sara_posterior_decide",
             "sara_refill", "sara_run", "sara_query", "sara_finish_step", "sara_read_rollouts",
