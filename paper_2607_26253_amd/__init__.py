@@ -400,6 +400,8 @@ def _float_dtype(t, what):
 
 def _stream_for(t, stream):
     """The stream's handle, or that of the current stream of t's device."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
     return _Torch.raw_stream(t.get_device()) if stream is None else stream.cuda_stream
 
 
@@ -413,6 +415,8 @@ def _workspace(workspace, need, like, stream):
         else:
             with _Torch.on(stream):
                 workspace = _Torch.empty(need, dtype=_Torch.uint8, device=like.device)
+    elif not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("the workspace must be contiguous, on the GPU")
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
@@ -430,6 +434,8 @@ def _kv8(k_cache, v_cache, k_exp, v_exp):
     u8, pages = _Torch.uint8, shape[:2]
     if k_exp.dtype != u8 or v_exp.dtype != u8 or k_exp.shape != pages or v_exp.shape != pages:
         raise ValueError("exponents must be uint8 [n_pages, n_kv_heads]")
+    if not (k_cache.is_cuda and v_cache.is_cuda and k_exp.is_cuda and v_exp.is_cuda):
+        raise ValueError("the cache must be on the GPU")
     if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_exp.is_contiguous() and v_exp.is_contiguous()):
         raise ValueError("codes and exponents must be contiguous")
     return sara_kv8_cache(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), shape[0], shape[1],
@@ -441,8 +447,8 @@ def _rows3(t, rows, heads, dim, what):
     if t.shape != (rows, heads, dim):
         raise ValueError(f"{what} must be [{rows}, {heads}, {dim}], not {list(t.shape)}")
     row, head, last = t.stride()
-    if last != 1 and t.numel():
-        raise ValueError(f"{what} must have a contiguous last dimension")
+    if (last != 1 and t.numel()) or not t.is_cuda:
+        raise ValueError(f"{what} must be on the GPU, with a contiguous last dimension")
     return t.data_ptr(), row, head
 
 
@@ -452,14 +458,14 @@ def _seqs(d_pages, d_seq, d_off, n_rows):
     i32 = _Torch.int32
     if d_pages.dtype != i32 or d_seq.dtype != i32 or d_seq.numel() != n:
         raise ValueError("page table [n_seqs, max_pages] and per-sequence array [n_seqs] must be int32")
-    if not (d_pages.is_contiguous() and d_seq.is_contiguous()):
-        raise ValueError("page table and per-sequence array must be contiguous")
+    if not (d_pages.is_contiguous() and d_seq.is_contiguous() and d_pages.is_cuda and d_seq.is_cuda):
+        raise ValueError("page table and per-sequence array must be contiguous, on the GPU")
     if d_off is None:
         if n_rows != n:
             raise ValueError(f"{n_rows} rows for {n} sequences: give d_off")
         return n, width, None
-    if d_off.dtype != i32 or d_off.numel() != n + 1 or not d_off.is_contiguous():
-        raise ValueError("d_off must be int32 [n_seqs + 1]")
+    if d_off.dtype != i32 or d_off.numel() != n + 1 or not d_off.is_contiguous() or not d_off.is_cuda:
+        raise ValueError("d_off must be int32 [n_seqs + 1] on the GPU")
     return n, width, d_off.data_ptr()
 
 
@@ -521,16 +527,16 @@ def sara_kv8_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_of
 # -- token log probabilities --------------------------------------------------------
 def _logit_rows(t, what):
     dtype = _float_dtype(t, what)
-    if t.dim() != 2 or (t.stride(1) != 1 and t.numel()):
-        raise ValueError(f"{what} must be [rows, vocab] with contiguous rows")
+    if t.dim() != 2 or (t.stride(1) != 1 and t.numel()) or not t.is_cuda:
+        raise ValueError(f"{what} must be [rows, vocab] with contiguous rows, on the GPU")
     return t.data_ptr(), dtype, t.stride(0)
 
 
 def _per_row(t, n, dtype, what):
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what} must hold {n} contiguous elements of {dtype}")
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what} must hold {n} contiguous elements of {dtype} on the GPU")
     return t.data_ptr()
 
 

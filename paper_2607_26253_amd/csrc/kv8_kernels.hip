@@ -334,9 +334,11 @@ struct AttnArgs {
   int64_t q_row, q_head, o_row, o_head;   // strides in elements
   const int32_t *pages, *ctx, *off;
   int max_pages, max_ctx, n_seqs, n_rows, hq;
-  int splits, pps, pps_tile;              // most splits of a row; pages a split, in the two kernels below
+  int splits, pps, splits_tile, pps_tile; // most splits of a row and pages a split, in the two kernels below
   float scale_log2;
-  float* part;                            // [row][head][split][HD + 2]
+  // partial results (HD numerators, maximum, sum): k_kv8_attn's [sequence][KV head][column][split], k_kv8_attn_tile's
+  // [row][head][split]
+  float *part, *part_tile;
 };
 
 // fp32 as a sum of P bf16 numbers: 8 bits (bf16 inputs are one exactly), 16, or 24
@@ -577,7 +579,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
       if constexpr (sizeof(T) == 2) *(uint2*)dst = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
       else *(f32x4*)dst = f32x4{f[0], f[1], f[2], f[3]};
     } else {
-      float* dst = a.part + (((size_t)(r0 + t) * a.hq + h) * a.splits + blockIdx.y) * (HD + 2);
+      const int slots = a.off ? kFewColumns : G;
+      float* dst = a.part + ((((size_t)seq * hkv + g) * slots + c0 + x) * a.splits + blockIdx.y) * (HD + 2);
       *(f32x2*)(dst + d4) = f32x2{num[0], num[1]};
       *(f32x2*)(dst + d4 + 2) = f32x2{num[2], num[3]};
       if (d4 == 0) *(f32x2*)(dst + HD) = f32x2{mx, den};
@@ -815,7 +818,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
   const float inv = too_long ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : 1.f / l;
   const bool whole = np <= a.pps_tile;
   T* out = (T*)a.out + (size_t)(r0 + qt) * a.o_row + (size_t)head * a.o_head + 16 * h;
-  float* part = a.part + (((size_t)(r0 + qt) * a.hq + head) * a.splits + blockIdx.y) * (HD + 2);
+  float* part = a.part_tile + (((size_t)(r0 + qt) * a.hq + head) * a.splits_tile + blockIdx.y) * (HD + 2);
 #pragma unroll
   for (int t = 0; t < NDT; ++t) {
     float f[16];
@@ -863,7 +866,8 @@ __global__ __launch_bounds__(256) void k_kv8_attn_join(AttnArgs a, int hkv, int 
   const int pps = TILE ? a.pps_tile : a.pps;
   const int ns = (((ctx + 15) >> 4) + pps - 1) / pps;
   if (ctx > a.max_ctx || ns <= 1) return;
-  const float* p = a.part + ((size_t)row * a.hq + h) * a.splits * (HD + 2);
+  const float* p = TILE ? a.part_tile + ((size_t)row * a.hq + h) * a.splits_tile * (HD + 2)
+                        : a.part + (size_t)blockIdx.x * a.splits * (HD + 2);
   float m = -INFINITY, l = 0.f, o[DL] = {};
   for (int s0 = wave; s0 < ns; s0 += 4 * kJoin) {
     float pm[kJoin], pl[kJoin], po[kJoin][DL];
@@ -953,7 +957,7 @@ int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int d
   });
 }
 
-Kv8Split kv8_split(int n_rows, int hq, int hkv, int n_seqs, int max_ctx, bool ragged) {
+Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx, bool ragged) {
   const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16);
   // Pages a split so that about `blocks` blocks share the work, at least `least`, in steps of `step`, and at most
   // 128 splits a row.  A split costs its block about 4 us before the first pages are there and the join launch 4 us
@@ -970,30 +974,33 @@ Kv8Split kv8_split(int n_rows, int hq, int hkv, int n_seqs, int max_ctx, bool ra
   // tiles of 128 columns: two blocks a CU are resident.  64 queries a sequence over 4,000 tokens: 122 us, against 141 in
   // steps of 64 pages; with 1,024 blocks prompts of 300-2,500 tokens are split too and take 104 us for 75.
   s.pps_tile = s.tile_items ? share(s.tile_items, 512, 32, 16) : s.pps;
-  s.splits = (np + std::min(s.pps, s.pps_tile) - 1) / std::min(s.pps, s.pps_tile);
-  s.few_splits = (np + s.pps - 1) / s.pps;
-  s.tile_splits = s.tile_items ? (np + s.pps_tile - 1) / s.pps_tile : 0;
+  s.splits = (np + s.pps - 1) / s.pps;
+  s.splits_tile = s.tile_items ? (np + s.pps_tile - 1) / s.pps_tile : 0;
+  const int64_t one = (int64_t)sizeof(float) * (hd + 2);
+  if (s.splits > 1) s.part_bytes = (one * n_seqs * hkv * (ragged ? kFewColumns : G) * s.splits + 15) / 16 * 16;
+  if (s.splits_tile > 1) s.part_tile_bytes = one * n_rows * hq * s.splits_tile;
   return s;
 }
 
 int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows,
                          int hq, const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
                          int max_ctx, float scale, void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st) {
-  const Kv8Split s = kv8_split(n_rows, hq, c.n_kv_heads, n_seqs, max_ctx, off != nullptr);
+  const Kv8Split s = kv8_split(n_rows, hq, c.n_kv_heads, c.head_dim, n_seqs, max_ctx, off != nullptr);
   const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
-                      s.splits, s.pps, s.pps_tile, scale * 1.4426950408889634f, (float*)ws};
+                      s.splits, s.pps, s.splits_tile, s.pps_tile, scale * 1.4426950408889634f, (float*)ws,
+                      (float*)((char*)ws + s.part_bytes)};
   return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
-    hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.items * c.n_kv_heads), s.few_splits),
+    hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.items * c.n_kv_heads), s.splits),
                        dim3(256), 0, st, c, a);
     if (s.tile_items)
       hipLaunchKernelGGL((k_kv8_attn_tile<hd.value, fmt.value, decltype(t), kTileWaves>),
-                         dim3((uint32_t)(s.tile_items * c.n_kv_heads), s.tile_splits), dim3(64 * kTileWaves), 0, st, c, a);
-    if (s.few_splits > 1) {
+                         dim3((uint32_t)(s.tile_items * c.n_kv_heads), s.splits_tile), dim3(64 * kTileWaves), 0, st, c, a);
+    if (s.splits > 1) {
       const int cols = off ? kFewColumns : hq / c.n_kv_heads;
       hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t), false>), dim3((uint32_t)((int64_t)n_seqs * c.n_kv_heads * cols)),
                          dim3(256), 0, st, a, c.n_kv_heads, cols);
     }
-    if (s.tile_splits > 1)
+    if (s.splits_tile > 1)
       hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t), true>), dim3((uint32_t)((int64_t)n_rows * hq)), dim3(256), 0,
                          st, a, c.n_kv_heads, 0);
   });

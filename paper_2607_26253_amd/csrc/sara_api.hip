@@ -927,8 +927,8 @@ extern "C" int sara_kv8_attention_workspace(int32_t n_kv_heads, int32_t head_dim
   if (n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128))
     return einval("n_heads must be a multiple of n_kv_heads, head_dim 64 or 128");
   if (n_rows < 0 || n_seqs < 0 || max_ctx < 0) return einval("sizes must be >= 0");
-  const Kv8Split s = kv8_split(n_rows, n_heads, n_kv_heads, n_seqs, max_ctx, ragged != 0);
-  *bytes = s.splits > 1 ? (int64_t)sizeof(float) * n_rows * n_heads * s.splits * (head_dim + 2) : 0;
+  const Kv8Split s = kv8_split(n_rows, n_heads, n_kv_heads, head_dim, n_seqs, max_ctx, ragged != 0);
+  *bytes = s.part_bytes + s.part_tile_bytes;
   return SARA_OK;
 }
 
@@ -946,7 +946,8 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
   if (!d_q || !d_out) return einval("null array");
   if (rows_unaligned(d_q, q_row, q_head, dtype) || rows_unaligned(d_out, o_row, o_head, dtype))
     return einval("q and out must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
-  if (((int64_t)n_rows + n_seqs) * n_heads > (int64_t)1 << 30) return einval("too many rows");
+  if ((int64_t)n_rows * n_heads > (int64_t)1 << 30 || (int64_t)n_seqs * std::max(n_heads, 32 * c->n_kv_heads) > (int64_t)1 << 30)
+    return einval("too many rows or sequences");
   int64_t need = 0;
   const int rc = sara_kv8_attention_workspace(c->n_kv_heads, c->head_dim, n_rows, n_heads, n_seqs, d_off != nullptr, max_ctx,
                                               &need);

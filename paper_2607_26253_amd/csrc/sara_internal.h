@@ -312,9 +312,13 @@ int launch_sample_rows_noalloc(const float* logits, int n_rows, int V, const int
                                uint64_t seed, int step, float temp, float top_p, int eos, uint32_t feos,
                                int32_t* tok, hipStream_t st);
 // launchers (8-bit KV cache)
-// context splits of an attention launch (most of a row, of each kernel), pages of one, column tiles of each kernel
-struct Kv8Split { int splits, few_splits, tile_splits, pps, pps_tile; int64_t items, tile_items; };
-Kv8Split kv8_split(int n_rows, int hq, int hkv, int n_seqs, int max_ctx, bool ragged);
+// How an attention call is cut, for the kernel of few columns and for the one of column tiles: most context splits of a
+// row, pages a split, work items, and the partial results' bytes in the workspace.
+struct Kv8Split {
+  int splits, pps, splits_tile, pps_tile;
+  int64_t items, tile_items, part_bytes, part_tile_bytes;
+};
+Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx, bool ragged);
 int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int dtype, int64_t k_row, int64_t k_head,
                     int64_t v_row, int64_t v_head, int n_rows, const int32_t* pages, int max_pages, const int32_t* start,
                     const int32_t* off, int n_seqs, hipStream_t st);

@@ -442,6 +442,8 @@ def test_refusals(env):
     raw = torch.empty(12 * 128 + 8, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(sara.SaraError):                               # q off its 16 bytes
         sara.sara_kv8_attention(raw[1:1 + 12 * 128].view(1, 12, 128), *dev.args, pages, ctx, None, torch.empty_like(q))
+    for i in (0, 1, 4, 5, 6, 8):                                      # host memory
+        bad(ValueError, i, good[i].cpu())
     with pytest.raises(ValueError):                                   # rows without offsets
         sara.sara_kv8_write(*dev.args, q[:, :2].repeat(2, 1, 1), q[:, :2].repeat(2, 1, 1), pages, ctx)
     with pytest.raises(ValueError):
@@ -452,4 +454,7 @@ def test_refusals(env):
     with pytest.raises(sara.SaraError):                               # workspace too small
         sara.sara_kv8_attention(q, *dev2.args, dev2.i32(tables2), dev2.i32([5000]), None, torch.empty_like(q),
                                 workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        sara.sara_kv8_attention(q, *dev2.args, dev2.i32(tables2), dev2.i32([5000]), None, torch.empty_like(q),
+                                workspace=torch.empty(1 << 20, dtype=torch.uint8))
     torch.cuda.synchronize()
