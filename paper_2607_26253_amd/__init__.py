@@ -8,7 +8,9 @@ built (``python -m paper_2607_26253_amd.build``).
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
+import sys
 
 import numpy as np
 
@@ -68,9 +70,22 @@ class sara_kv8_cache(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "format")]
 
 
+def _share_hip_runtime():
+    """Loads the HIP runtime that torch brings, if torch is there and not imported yet.  The process keeps the first
+    library of that name; had libsara.so brought ROCm's own, torch would add a second runtime, and a launch after torch
+    has taken the device then fails with "no ROCm-capable device is detected"."""
+    if "torch" in sys.modules:
+        return
+    spec = importlib.util.find_spec("torch")
+    path = os.path.join(os.path.dirname(spec.origin), "lib", "libamdhip64.so") if spec and spec.origin else ""
+    if os.path.exists(path):
+        ctypes.CDLL(path)
+
+
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise ImportError(f"libsara.so is not built ({path}); run `python -m paper_2607_26253_amd.build`")
+    _share_hip_runtime()
     lib = ctypes.CDLL(path)
     P, I32, I64, U64, F32, F64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64,
                                   ctypes.c_float, ctypes.c_double)

@@ -1,6 +1,9 @@
 """Argument checks of the 8-bit KV cache and of the token log probabilities at
 the C ABI, and the 64-bit reference's own pins (no GPU)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -8,6 +11,7 @@ import pytest
 import paper_2607_26253_amd as sara
 from tests import kv8_reference as R
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 L, BAD = sara._lib, sara.SARA_EINVAL
 P = ctypes.c_void_p(4096)
 
@@ -88,3 +92,10 @@ def test_reference_codes():
     assert R.nearest(np.array([0.5, 1.5, -2.5, 126.5]), "int8").tolist() == [0.0, 2.0, -2.0, 126.0]
     assert [R.exponent(a, "int8") for a in (127.0, 127.5, 0.0, np.inf)] == [127, 128, 1, 255]
     assert [R.exponent(a, "fp8") for a in (448.0, 449.0, 224.0)] == [127, 128, 126]
+
+
+@pytest.mark.parametrize("order", ["import paper_2607_26253_amd, torch", "import torch, paper_2607_26253_amd"])
+def test_one_hip_runtime_whatever_is_imported_first(order):
+    code = order + "\nfor l in open('/proc/self/maps'):\n    if 'libamdhip64' in l: print(l.split()[-1])"
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, check=True).stdout
+    assert len(set(out.split())) == 1, out
