@@ -1,7 +1,8 @@
 """Python binding of libsara (ctypes, argument marshalling only).
 
 Every step of the rollout-allocation hot path runs in the HIP kernels of
-``libsara.so``; this module only converts arguments.  torch is used for device
+``libsara.so``; this module only converts arguments (those of the operators on
+torch tensors in the compiled ``_operators.so``).  torch is used for device
 memory and the stream.  Importing fails loudly when the library has not been
 built (``python -m paper_2607_26253_amd.build``).
 """
@@ -388,127 +389,52 @@ def sara_sample_logits_noalloc(d_logits, d_rid, d_pos, seed, step_index, tempera
 
 
 # -- operators on the caller's tensors -----------------------------------------------
-# These calls take microseconds, so their checks are kept short: torch is looked up
-# once, and a stream is named by its raw handle (torch.cuda.current_stream builds an
-# object in 2.8 us).
-class _Torch:
-    """torch's names that the checks below use, from the first call on (importing this package does not import torch)."""
-    float_types = None
+# These calls take microseconds, so their arguments are checked and marshalled in a
+# compiled module.  It needs torch loaded, which its callers have and an import of
+# this package does not: it is looked up at the first call.
+class _Operators:
+    """The compiled module's functions, from the first call on."""
 
-    @classmethod
-    def load(cls):
-        import torch
-        cls.int32, cls.float32, cls.uint8, cls.empty, cls.on = torch.int32, torch.float32, torch.uint8, torch.empty, torch.cuda.stream
-        cls.codes = {torch.int8: SARA_KV8_INT8, torch.float8_e4m3fn: SARA_KV8_E4M3}
-        cls.raw_stream = staticmethod(torch._C._cuda_getCurrentRawStream)
-        cls.float_types = {torch.bfloat16: SARA_BF16, torch.float32: SARA_F32}
-
-
-def _float_dtype(t, what):
-    if _Torch.float_types is None:
-        _Torch.load()
-    code = _Torch.float_types.get(t.dtype)
-    if code is None:
-        raise TypeError(f"{what} must be bfloat16 or float32, not {t.dtype}")
-    return code
+    def __getattr__(self, name):
+        import torch  # noqa: F401  (the module links to its libraries)
+        try:
+            from . import _operators
+        except ImportError as e:
+            raise ImportError(f"_operators.so is not built or does not load; run `python -m paper_2607_26253_amd.build` ({e})")
+        for f in ("kv8_write", "kv8_read", "kv8_attention", "token_logprobs", "token_logprobs_grad"):
+            setattr(self, f, getattr(_operators, f))
+        self.on = torch.cuda.stream
+        return object.__getattribute__(self, name)
 
 
-def _stream_for(t, stream):
-    """The stream's handle, or that of the current stream of t's device."""
-    if not t.is_cuda:
-        raise ValueError("tensors must be on the GPU")
-    return _Torch.raw_stream(t.get_device()) if stream is None else stream.cuda_stream
+_ops = _Operators()
 
 
-def _workspace(workspace, need, like, stream):
-    """(pointer, bytes) of the caller's workspace or of one that torch's allocator ties to the stream, and its owner."""
-    if need == 0:
-        return None, 0, None
-    if workspace is None:
-        if stream is None:
-            workspace = _Torch.empty(need, dtype=_Torch.uint8, device=like.device)
-        else:
-            with _Torch.on(stream):
-                workspace = _Torch.empty(need, dtype=_Torch.uint8, device=like.device)
-    elif not (workspace.is_cuda and workspace.is_contiguous()):
-        raise ValueError("the workspace must be contiguous, on the GPU")
-    return workspace.data_ptr(), workspace.nbytes, workspace
-
-
-# -- 8-bit KV cache ---------------------------------------------------------------
-def _kv8(k_cache, v_cache, k_exp, v_exp):
-    """The C descriptor of a cache: codes [n_pages, n_kv_heads, 16, head_dim]
-    (torch.int8 or torch.float8_e4m3fn) and exponents [n_pages, n_kv_heads]
-    (torch.uint8), contiguous."""
-    shape, dtype = k_cache.shape, k_cache.dtype
-    fmt = _Torch.codes.get(dtype)
-    if fmt is None:
-        raise TypeError(f"codes must be int8 or float8_e4m3fn, not {dtype}")
-    if len(shape) != 4 or shape[2] != 16 or v_cache.shape != shape or v_cache.dtype != dtype:
-        raise ValueError("codes must be [n_pages, n_kv_heads, 16, head_dim], alike for K and V")
-    u8, pages = _Torch.uint8, shape[:2]
-    if k_exp.dtype != u8 or v_exp.dtype != u8 or k_exp.shape != pages or v_exp.shape != pages:
-        raise ValueError("exponents must be uint8 [n_pages, n_kv_heads]")
-    if not (k_cache.is_cuda and v_cache.is_cuda and k_exp.is_cuda and v_exp.is_cuda):
-        raise ValueError("the cache must be on the GPU")
-    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_exp.is_contiguous() and v_exp.is_contiguous()):
-        raise ValueError("codes and exponents must be contiguous")
-    return sara_kv8_cache(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), shape[0], shape[1],
-                          shape[3], fmt)
-
-
-def _rows3(t, rows, heads, dim, what):
-    """(pointer, row stride, head stride) of a [rows, heads, dim] tensor."""
-    if t.shape != (rows, heads, dim):
-        raise ValueError(f"{what} must be [{rows}, {heads}, {dim}], not {list(t.shape)}")
-    row, head, last = t.stride()
-    if (last != 1 and t.numel()) or not t.is_cuda:
-        raise ValueError(f"{what} must be on the GPU, with a contiguous last dimension")
-    return t.data_ptr(), row, head
-
-
-def _seqs(d_pages, d_seq, d_off, n_rows):
-    """Checks a page table and its per-sequence arrays; (sequences, pages a sequence, pointer of d_off)."""
-    n, width = d_pages.shape
-    i32 = _Torch.int32
-    if d_pages.dtype != i32 or d_seq.dtype != i32 or d_seq.numel() != n:
-        raise ValueError("page table [n_seqs, max_pages] and per-sequence array [n_seqs] must be int32")
-    if not (d_pages.is_contiguous() and d_seq.is_contiguous() and d_pages.is_cuda and d_seq.is_cuda):
-        raise ValueError("page table and per-sequence array must be contiguous, on the GPU")
-    if d_off is None:
-        if n_rows != n:
-            raise ValueError(f"{n_rows} rows for {n} sequences: give d_off")
-        return n, width, None
-    if d_off.dtype != i32 or d_off.numel() != n + 1 or not d_off.is_contiguous() or not d_off.is_cuda:
-        raise ValueError("d_off must be int32 [n_seqs + 1] on the GPU")
-    return n, width, d_off.data_ptr()
-
-
-def _kv8_rows(call, name, k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream):
-    dtype = _float_dtype(d_k, "K and V")
-    cache = _kv8(k_cache, v_cache, k_exp, v_exp)
-    if d_v.dtype != d_k.dtype:
-        raise ValueError("K and V must have the same dtype")
-    n_rows = d_k.shape[0]
-    k, k_row, k_head = _rows3(d_k, n_rows, cache.n_kv_heads, cache.head_dim, "K")
-    v, v_row, v_head = _rows3(d_v, n_rows, cache.n_kv_heads, cache.head_dim, "V")
-    n, width, off = _seqs(d_pages, d_start, d_off, n_rows)
-    rc = call(ctypes.byref(cache), k, k_row, k_head, v, v_row, v_head, dtype, n_rows, d_pages.data_ptr(), width,
-              d_start.data_ptr(), off, n, _stream_for(k_cache, stream))
+def _operator(name, entry, stream, args):
+    """One call on the current stream of the tensors' device, or on the given one."""
+    if stream is None:
+        rc = entry(*args)
+    else:
+        with _ops.on(stream):
+            rc = entry(*args)
     if rc:
         _check(rc, name)
 
 
+# -- 8-bit KV cache ---------------------------------------------------------------
 def sara_kv8_write(k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off=None, stream=None):
     """Quantise rows d_k, d_v [rows, n_kv_heads, head_dim] into the cache: row t
     of sequence i (rows d_off[i]..d_off[i + 1], one each without d_off) goes to
-    position d_start[i] + t of page table d_pages [n_seqs, max_pages]."""
-    _kv8_rows(_lib.sara_kv8_write, "sara_kv8_write", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
+    position d_start[i] + t of page table d_pages [n_seqs, max_pages].  The cache:
+    codes [n_pages, n_kv_heads, 16, head_dim] (torch.int8 or torch.float8_e4m3fn)
+    and exponents [n_pages, n_kv_heads] (torch.uint8), contiguous."""
+    _operator("sara_kv8_write", _ops.kv8_write, stream,
+              (k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off))
 
 
 def sara_kv8_read(k_cache, v_cache, k_exp, v_exp, d_pages, d_start, d_off, d_k, d_v, stream=None):
     """Read positions d_start[i] + t back into rows of d_k and d_v."""
-    _kv8_rows(_lib.sara_kv8_read, "sara_kv8_read", k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off, stream)
+    _operator("sara_kv8_read", _ops.kv8_read, stream, (k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off))
 
 
 def sara_kv8_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_off, d_out, scale=None, max_ctx=None,
@@ -516,68 +442,21 @@ def sara_kv8_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_of
     """Causal attention of d_q [rows, n_heads, head_dim] over the cache into
     d_out: the rows of sequence i (d_off as in sara_kv8_write) are the last of
     its d_ctx[i] tokens.  scale defaults to head_dim ** -0.5; max_ctx bounds
-    d_ctx (default: what the page table holds)."""
-    dtype = _float_dtype(d_q, "q")
-    cache = _kv8(k_cache, v_cache, k_exp, v_exp)
-    n_rows, heads, hd = d_q.shape
-    q, q_row, q_head = _rows3(d_q, n_rows, heads, cache.head_dim, "q")
-    o, o_row, o_head = _rows3(d_out, n_rows, heads, hd, "out")
-    if d_out.dtype != d_q.dtype:
-        raise ValueError("out must have q's dtype")
-    n, width, off = _seqs(d_pages, d_ctx, d_off, n_rows)
-    if max_ctx is None:
-        max_ctx = 16 * width
-    need = ctypes.c_int64(0)
-    rc = _lib.sara_kv8_attention_workspace(cache.n_kv_heads, hd, n_rows, heads, n, off is not None, max_ctx, ctypes.byref(need))
-    if rc:
-        _check(rc, "sara_kv8_attention_workspace")
-    ws, ws_bytes, _owner = _workspace(workspace, need.value, d_q, stream)
-    rc = _lib.sara_kv8_attention(ctypes.byref(cache), q, q_row, q_head, o, o_row, o_head, dtype, n_rows, heads,
-                                 d_pages.data_ptr(), width, d_ctx.data_ptr(), off, n, max_ctx,
-                                 hd ** -0.5 if scale is None else float(scale), ws, ws_bytes, _stream_for(d_q, stream))
-    if rc:
-        _check(rc, "sara_kv8_attention")
+    d_ctx (default: what the page table holds).  Without a workspace one is
+    taken from torch's allocator."""
+    _operator("sara_kv8_attention", _ops.kv8_attention, stream,
+              (k_cache, v_cache, k_exp, v_exp, d_q, d_out, d_pages, d_ctx, d_off, scale, max_ctx, workspace))
 
 
 # -- token log probabilities --------------------------------------------------------
-def _logit_rows(t, what):
-    dtype = _float_dtype(t, what)
-    if t.dim() != 2 or (t.stride(1) != 1 and t.numel()) or not t.is_cuda:
-        raise ValueError(f"{what} must be [rows, vocab] with contiguous rows, on the GPU")
-    return t.data_ptr(), dtype, t.stride(0)
-
-
-def _per_row(t, n, dtype, what):
-    if t is None:
-        return None
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what} must hold {n} contiguous elements of {dtype} on the GPU")
-    return t.data_ptr()
-
-
 def sara_token_logprobs(d_logits, d_tok, d_logp=None, d_entropy=None, d_stats=None, d_top_id=None, d_top_logp=None,
                         temperature=1.0, workspace=None, stream=None):
     """Log probability of d_tok[r], entropy, (largest logit, sum of exponentials)
     and the most likely ids of each row of d_logits [rows, vocab] (bf16 or
     fp32) at a temperature.  d_stats is [rows, 2]; d_top_id / d_top_logp are
     [rows, n_top]; outputs that are None are not written."""
-    x, dtype, stride = _logit_rows(d_logits, "logits")
-    n, V = d_logits.shape
-    i32, f32 = _Torch.int32, _Torch.float32
-    if (d_top_id is None) != (d_top_logp is None):
-        raise ValueError("give both of d_top_id and d_top_logp")
-    k = 0 if d_top_id is None else d_top_id.shape[1]
-    need = ctypes.c_int64(0)
-    rc = _lib.sara_token_logprobs_workspace(n, V, k, ctypes.byref(need))
-    if rc:
-        _check(rc, "sara_token_logprobs_workspace")
-    ws, ws_bytes, _owner = _workspace(workspace, need.value, d_logits, stream)
-    rc = _lib.sara_token_logprobs(x, dtype, stride, n, V, _per_row(d_tok, n, i32, "tokens"), temperature, k,
-                                  _per_row(d_logp, n, f32, "logp"), _per_row(d_entropy, n, f32, "entropy"),
-                                  _per_row(d_stats, 2 * n, f32, "stats"), _per_row(d_top_id, n * k, i32, "top ids"),
-                                  _per_row(d_top_logp, n * k, f32, "top logp"), ws, ws_bytes, _stream_for(d_logits, stream))
-    if rc:
-        _check(rc, "sara_token_logprobs")
+    _operator("sara_token_logprobs", _ops.token_logprobs, stream,
+              (d_logits, d_tok, d_logp, d_entropy, d_stats, d_top_id, d_top_logp, temperature, workspace))
 
 
 def sara_token_logprobs_grad(d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad, temperature=1.0,
@@ -585,15 +464,5 @@ def sara_token_logprobs_grad(d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_
     """Gradient with respect to the logits of sum(g_logp * logp + g_entropy *
     entropy) into d_grad (which may be d_logits); d_stats and d_entropy are what
     sara_token_logprobs gave.  d_g_logp or d_g_entropy may be None."""
-    x, dtype, stride = _logit_rows(d_logits, "logits")
-    y, ydtype, ystride = _logit_rows(d_grad, "gradient")
-    n, V = d_logits.shape
-    if d_grad.shape != d_logits.shape or ydtype != dtype:
-        raise ValueError("the gradient must have the logits' shape and dtype")
-    f32 = _Torch.float32
-    rc = _lib.sara_token_logprobs_grad(x, dtype, stride, n, V, _per_row(d_tok, n, _Torch.int32, "tokens"), temperature,
-                                       _per_row(d_stats, 2 * n, f32, "stats"), _per_row(d_entropy, n, f32, "entropy"),
-                                       _per_row(d_g_logp, n, f32, "g_logp"), _per_row(d_g_entropy, n, f32, "g_entropy"), y,
-                                       ystride, _stream_for(d_logits, stream))
-    if rc:
-        _check(rc, "sara_token_logprobs_grad")
+    _operator("sara_token_logprobs_grad", _ops.token_logprobs_grad, stream,
+              (d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad, temperature))

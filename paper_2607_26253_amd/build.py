@@ -1,13 +1,16 @@
-"""Compile libsara.so (HIP, gfx950) in-tree with hipcc."""
+"""Compile libsara.so (HIP, gfx950) with hipcc and the operators' Python calls
+(_operators.so, C++ against torch's headers) with g++, in-tree."""
 import os
 import shutil
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsara.so")
+OPERATORS = os.path.join(HERE, "_operators.so")
 SOURCES = ["model_kernels.hip", "prefill_kernels.hip", "controller_kernels.hip", "kv8_kernels.hip",
            "score_kernels.hip", "sara_api.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
@@ -46,7 +49,27 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, OUT)
+    build_operators()
     return OUT
+
+
+def build_operators() -> str:
+    """The compiled Python calls; libsara.so is there."""
+    import torch
+
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = os.path.join(os.path.dirname(torch.__file__), "include")
+    tmp = OPERATORS + ".tmp"
+    cmd = [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(ROOT, "include"),
+           "-I" + include, "-I" + os.path.join(include, "torch", "csrc", "api", "include"),
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "operators_binding.cpp"), "-o", tmp, "-L" + HERE, "-L" + lib,
+           "-l:libsara.so", "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for operators_binding.cpp:\n{r.stderr}")
+    os.replace(tmp, OPERATORS)
+    return OPERATORS
 
 
 if __name__ == "__main__":

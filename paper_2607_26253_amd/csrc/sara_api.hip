@@ -962,7 +962,8 @@ static std::string score_bad(int32_t dtype, int64_t row_stride, int32_t n_rows, 
   if (dtype != SARA_BF16 && dtype != SARA_F32) return "dtype must be SARA_BF16 or SARA_F32";
   if (n_rows < 0 || vocab < 1) return "n_rows must be >= 0 and vocab >= 1";
   if (row_stride < vocab && n_rows > 1) return "row stride must be at least vocab";
-  if (!(temperature > 0.f) || !(temperature <= 3.4e38f)) return "temperature must be > 0 and finite";
+  // 1 / temperature and log2(e) / temperature are fp32 factors of the kernels
+  if (!(temperature >= 1e-37f) || !(temperature <= 1e37f)) return "temperature must be in [1e-37, 1e37]";
   return "";
 }
 
