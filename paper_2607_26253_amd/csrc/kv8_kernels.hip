@@ -346,6 +346,8 @@ template <int P> __device__ __forceinline__ void split_bf16(float a, float b, ui
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     w[i] = pack_bf16(a, b);
+    if (i + 1 == P) break;
+    asm("" : "+v"(w[i]));                                  // else the compiler rounds `a` a second time for its part
     a -= __uint_as_float(w[i] << 16);
     b -= __uint_as_float(w[i] & 0xFFFF0000u);
   }
@@ -364,6 +366,9 @@ __device__ __forceinline__ void transpose4(uint32_t* r) {
 // Sequences with more columns (query tokens x heads of a KV head) than this go through k_kv8_attn_tile.
 constexpr int kFewColumns = 32;
 constexpr int kTileWaves = 4;
+// The running maximum of a column follows its scores only once they pass it by this much (base 2): weights up to 2^8
+// lose nothing in fp32 or in bf16 parts, and most key blocks leave the sums where they are.
+constexpr float kSlack = 8.f;
 
 // Block (16 columns of one sequence and KV head, split): column = query token x head of the group.  The 4
 // waves take the split's pages in pairs, wave w pairs w, w + 4, ...; the next pair's K codes are loaded once
@@ -509,14 +514,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float sub = mx == -INFINITY ? 0.f : mx;         // nothing seen yet: every weight is 0
-    if (__any(mx > m)) {
-      const float al = __builtin_amdgcn_exp2f(m - sub);
+    if (__any(mx > m + kSlack)) {
+      const float al = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
       l *= al;
 #pragma unroll
       for (int i = 0; i < NT; ++i) o[i] *= al;
       m = mx;
     }
+    const float sub = m == -INFINITY ? 0.f : m;           // nothing seen yet: every weight is 0
     u32x4 pf[PP];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
@@ -598,16 +603,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
 // LDS holds the operands in fragment order.  K: 16 dims of a key are one 16-byte load and the 16 bytes of two lanes;
 // slots are xor-ed with the dim step so that the 8 threads of a token row write to different banks.  V: 4 dims of 8
 // tokens are transposed in registers; row r of a 32-dim tile is dim 4 (r % 8) + r / 8, which spreads the writes and
-// leaves a lane 16 consecutive dims of the output.  The next block's codes travel in registers meanwhile (one barrier
-// a block).
+// leaves a lane 16 consecutive dims of the output.
+// What bounds it is VALU issue (about 400 instructions and 32 exponentials a wave and key block beside 48 MFMAs of 32
+// cycles), so both run side by side: the codes of block kb + 1 wait in registers and become bf16 in LDS between the score
+// MFMAs of block kb, their successors load behind them, and the weights of 16 keys are made between the MFMAs of the
+// 16 before.  16 sequences of 256 queries over 4,000 tokens, 16 heads: 224 us (619 TFLOP/s); one prompt of 4,590: 165
+// (522), against 182 with conversion, softmax and MFMAs one after the other.  Blocks of 8 waves convert half as much
+// each and gain nothing (16 x 256: 360 us).
 template <int HD, int FMT, typename T, int NW>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_tile(sara_kv8_cache c, AttnArgs a) {
-  constexpr int NKS = HD / 16, NDT = HD / 32, NTH = 64 * NW;
+  constexpr int NKS = HD / 16, NDT = HD / 32;
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
-  constexpr int KU = (64 * NKS + NTH - 1) / NTH, VU = (2 * HD + NTH - 1) / NTH;   // staging units a thread
+  constexpr int KU = NKS / NW, KR = 64 / NKS;                        // staging: K units a thread, token rows a unit of a wave
   typedef float f32x16 __attribute__((ext_vector_type(16)));
   __shared__ u32x4 kf[2][2 * NKS * 64], vf[2][4 * NDT * 64];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
   const int item = (int)gridDim.x / hkv - 1 - (int)blockIdx.x / hkv, g = blockIdx.x % hkv;   // long tiles first
   const SeqRows sr = find_seq<32 * NW>(a.off, a.ctx, a.n_seqs, a.n_rows, item, G, 1);
@@ -657,9 +667,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
   const int32_t* table = a.pages + (size_t)seq * a.max_pages;
   // lane i: page i of a stretch of 64 (16 key blocks), its exponent bytes (0x10000: no page, 0x20000: NaN)
   int ids = 0, meta = 0;
+  // A wave stages KR token rows of K at a time, all of one page, and the V of one page: pages, exponents and addresses
+  // are scalars.  K: lane (token row lane / NKS, 16 dims).  V: lane (8 tokens v_half, 4 dims 4 v_dim).
+  const int k_row = lane / NKS, k_step = lane % NKS, v_dim = lane % (HD / 4), v_half = lane / (HD / 4) & 1;
   u32x4 kr[KU];
-  uint32_t vr[VU][8];
-  int km[KU], vm[VU];
+  uint32_t vr[8];
+  int km[KU], vm;
+  auto first_row = [&](int x) { return (wave + NW * x) * KR; };      // of the wave's unit x
   auto load = [&](int kb) {
     if ((kb & 15) == 0) {
       const int pg = p0 + 4 * kb + lane;
@@ -671,59 +685,56 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
       meta = ke | ve << 8 | (have ? 0 : 0x10000) | (ke == 255 || ve == 255 ? 0x20000 : 0);
     }
     const int at = 4 * (kb & 15);
+    auto page = [&](const void* codes, int pg, int& info) {
+      info = __builtin_amdgcn_readlane(meta, at + pg);
+      return (const uint8_t*)codes + ((size_t)__builtin_amdgcn_readlane(ids, at + pg) * hkv + g) * (kBlockTok * HD);
+    };
 #pragma unroll
     for (int x = 0; x < KU; ++x) {
-      const int u = tid + NTH * x, ks = u % NKS, r = u / NKS & 63;
-      km[x] = __shfl(meta, at + (r >> 4), 64);
-      const size_t block = (size_t)__shfl(ids, at + (r >> 4), 64) * hkv + g;
-      kr[x] = *(const u32x4*)((const uint8_t*)c.k + (block * kBlockTok + (r & 15)) * HD + 16 * ks);
+      const uint8_t* kp = page(c.k, first_row(x) >> 4, km[x]) + (first_row(x) & 15) * HD;
+      kr[x] = *(const u32x4*)(kp + (k_row * HD + 16 * k_step));
     }
+    const uint8_t* vp = page(c.v, wave, vm);
 #pragma unroll
-    for (int x = 0; x < VU; ++x) {
-      const int u = (tid + NTH * x) % (2 * HD), cd = u % (HD / 4), hv = u / (HD / 4) & 1, pg = u / (HD / 2);
-      vm[x] = __shfl(meta, at + pg, 64);
-      const size_t block = (size_t)__shfl(ids, at + pg, 64) * hkv + g;
-      const uint8_t* vp = (const uint8_t*)c.v + (block * kBlockTok + 4 * hv) * HD + 4 * cd;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) vr[x][j] = *(const uint32_t*)(vp + (j + 4 * (j >> 2)) * HD);
-    }
+    for (int j = 0; j < 8; ++j) vr[j] = *(const uint32_t*)(vp + ((j + 4 * (j >> 2) + 4 * v_half) * HD + 4 * v_dim));
   };
-  auto store = [&](int kb, int buf) {
+  // The loaded codes go to LDS in PIECES pieces of about ten instructions, after `settle`.
+  constexpr int PIECES = 4 * KU + 8;
+  float k_scale[KU], v_scale;
+  u32x4 w_k, w_v;
+  auto settle = [&](int kb) {
 #pragma unroll
     for (int x = 0; x < KU; ++x) {
-      const int u = tid + NTH * x, ks = u % NKS, r = u / NKS;
-      if (64 * NKS % NTH != 0 && r >= 64) break;
-      const float scale = ldexpf(1.f, (km[x] & 255) - 127);
-      u32x4 w[2];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        u32x2 y = values_bf16<FMT>(kr[x][q], scale);
-        if (km[x] & 0x20000) y = u32x2{0x7FC07FC0u, 0x7FC07FC0u};    // a NaN page, seen through its keys' scores
-        w[q >> 1][2 * (q & 1)] = y.x;
-        w[q >> 1][2 * (q & 1) + 1] = y.y;
-      }
-      u32x4* dst = &kf[buf][((r >> 5) * NKS + ks) * 64 + ((r & 31) ^ (ks & 7))];
-      dst[0] = w[0];
-      dst[32] = w[1];
+      // a NaN page (its K or its V) is seen through its keys' scores: a NaN scale, or the code of NaN
+      const bool bad = km[x] & 0x20000;
+      if (FMT == SARA_KV8_E4M3 && bad) kr[x] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+      k_scale[x] = bad ? (FMT == SARA_KV8_E4M3 ? 1.f : __uint_as_float(0x7FC00000u)) : ldexpf(1.f, (km[x] & 255) - 127);
     }
-    const bool tail = 16 * (p0 + 4 * kb) + 64 > ctx;
+    const int live_tok = (vm & 0x30000) ? 0 : min(ctx - 16 * (p0 + 4 * kb + wave), 16);
+    if (live_tok < 16) {
 #pragma unroll
-    for (int x = 0; x < VU; ++x) {
-      const int u = tid + NTH * x, cd = u % (HD / 4), hv = u / (HD / 4) & 1, pg = u / (HD / 2);
-      if (2 * HD % NTH != 0 && pg >= 4) break;
-      const int live_tok = (vm[x] & 0x30000) ? 0 : tail ? ctx - 16 * (p0 + 4 * kb + pg) : 16;
-      if (live_tok < 16)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) vr[x][j] = j + 4 * (j >> 2) + 4 * hv < live_tok ? vr[x][j] : 0u;
-      transpose4(vr[x]);
-      transpose4(vr[x] + 4);
-      const float scale = (vm[x] & 0x20000) ? 0.f : ldexpf(1.f, (vm[x] >> 8 & 255) - 127);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32x2 y = values_bf16<FMT>(vr[x][j], scale), z = values_bf16<FMT>(vr[x][4 + j], scale);
-        vf[buf][(pg * NDT + (cd >> 3)) * 64 + 32 * hv + 8 * j + (cd & 7)] = u32x4{y.x, y.y, z.x, z.y};
-      }
+      for (int j = 0; j < 8; ++j) vr[j] = j + 4 * (j >> 2) + 4 * v_half < live_tok ? vr[j] : 0u;
     }
+    v_scale = (vm & 0x20000) ? 0.f : ldexpf(1.f, (vm >> 8 & 255) - 127);
+  };
+  auto store = [&](int i, int buf) {
+    if (i < 4 * KU) {
+      const int x = i >> 2, q = i & 3, r = first_row(x) + k_row;
+      const u32x2 y = values_bf16<FMT>(kr[x][q], k_scale[x]);
+      w_k[2 * (q & 1)] = y.x;
+      w_k[2 * (q & 1) + 1] = y.y;
+      if (q & 1) kf[buf][((r >> 5) * NKS + k_step) * 64 + 32 * (q >> 1) + ((r & 31) ^ (k_step & 7))] = w_k;
+      return;
+    }
+    const int j = (i - 4 * KU) >> 1, half = i & 1;         // 4 KU is even
+    if (i == 4 * KU) {
+      transpose4(vr);
+      transpose4(vr + 4);
+    }
+    const u32x2 y = values_bf16<FMT>(vr[4 * half + j], v_scale);
+    w_v[2 * half] = y.x;
+    w_v[2 * half + 1] = y.y;
+    if (half && (HD == 128 || lane < HD / 2)) vf[buf][(wave * NDT + (v_dim >> 3)) * 64 + 32 * v_half + 8 * j + (v_dim & 7)] = w_v;
   };
   float m = -INFINITY, l = 0.f;
   f32x16 o[NDT];
@@ -731,21 +742,37 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
   for (int t = 0; t < NDT; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-  auto compute = [&](int kb, int buf, int absent) {
-    const int k0 = 16 * (p0 + 4 * kb);
-    f32x16 s[2];
+  auto v_frag = [&](int buf, int st, int t) { return vf[buf][(st * NDT + t) * 64 + lane]; };
+  // Scores of a key block, each MFMA beside a piece of the next block's way to LDS.  LDS reads run half of the MFMAs ahead.
+  f32x16 s[2];
+  u32x4 vv[2][NDT];
+  auto scores = [&](int buf) {
+    auto k_frag = [&](int b, int ks) { return kf[buf][(b * NKS + ks) * 64 + 32 * h + (col ^ (ks & 7))]; };
+    u32x4 kk[2][NKS];
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) kk[0][ks] = k_frag(0, ks);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
-        const bf16x8 kk = __builtin_bit_cast(bf16x8, kf[buf][(b * NKS + ks) * 64 + 32 * h + (col ^ (ks & 7))]);
+        const int n = b * NKS + ks;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int p = QP - 1; p >= 0; --p)
-          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, __builtin_bit_cast(bf16x8, qf[p][ks]), s[b], 0, 0, 0);
+          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kk[b][ks]), __builtin_bit_cast(bf16x8, qf[p][ks]),
+                                                         s[b], 0, 0, 0);
+        if (b == 0) kk[1][ks] = k_frag(1, ks);
+        else if (ks < NDT) vv[0][ks] = v_frag(buf, 0, ks);
+#pragma unroll
+        for (int i = PIECES * n / (2 * NKS); i < PIECES * (n + 1) / (2 * NKS); ++i) store(i, buf ^ 1);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto compute = [&](int kb, int buf, int absent) {
+    const int k0 = 16 * (p0 + 4 * kb);
     if (k0 + 64 > w_all || absent) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -762,55 +789,80 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     mx = fmaxf(m, mx * sl2);
-    const float sub = mx == -INFINITY ? 0.f : mx;
-    if (__any(mx > m)) {
-      const float al = __builtin_amdgcn_exp2f(m - sub);
+    if (__any(mx > m + kSlack)) {
+      const float al = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
       l *= al;
 #pragma unroll
       for (int t = 0; t < NDT; ++t) o[t] *= al;
       m = mx;
     }
+    const float sub = m == -INFINITY ? 0.f : m;
+    // weights of keys pair j of step st, in PP bf16 parts
+    u32x4 pf[2][PP];
+    auto weights = [&](int st, int j) {
+      const int i = 8 * (st & 1) + 2 * j;
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][i], sl2, -sub));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][i + 1], sl2, -sub));
+      l += e0 + e1;
+      uint32_t w[PP];
+      split_bf16<PP>(e0, e1, w);
+#pragma unroll
+      for (int p = 0; p < PP; ++p) pf[st & 1][p][j] = w[p];
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) weights(0, j);
+    // a step's MFMAs in four groups, each with a quarter of the next step's weights
+    constexpr int M = NDT * PP;
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
-      u32x4 pf[PP];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int i = 8 * (st & 1) + 2 * j;
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][i], sl2, -sub));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[st >> 1][i + 1], sl2, -sub));
-        l += e0 + e1;
-        uint32_t w[PP];
-        split_bf16<PP>(e0, e1, w);
+        __builtin_amdgcn_sched_barrier(0);
+        if (st < 3 && j < NDT) vv[(st + 1) & 1][j] = v_frag(buf, st + 1, j);
 #pragma unroll
-        for (int p = 0; p < PP; ++p) pf[p][j] = w[p];
-      }
-#pragma unroll
-      for (int t = 0; t < NDT; ++t) {
-        const bf16x8 vv = __builtin_bit_cast(bf16x8, vf[buf][(st * NDT + t) * 64 + lane]);
-#pragma unroll
-        for (int p = PP - 1; p >= 0; --p)
-          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, __builtin_bit_cast(bf16x8, pf[p]), o[t], 0, 0, 0);
+        for (int n = M * j / 4; n < M * (j + 1) / 4; ++n) {
+          const int t = n % NDT, p = PP - 1 - n / NDT;
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vv[st & 1][t]),
+                                                         __builtin_bit_cast(bf16x8, pf[st & 1][p]), o[t], 0, 0, 0);
+        }
+        if (st < 3) weights(st + 1, j);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
   // bit i: page i of the key block has no page id
   auto absent_pages = [&](int kb) { return (int)(__ballot(meta & 0x10000) >> (4 * (kb & 15)) & 15); };
-  int absent = 0;
+  // Key block kb is in LDS, kb + 1 in registers; kb + 2 is loaded once those are free.
+  int absent = 0, next_absent = 0;
   if (nkb > 0) {
     load(0);
     absent = absent_pages(0);
-    store(0, 0);
+    settle(0);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) store(i, 0);
+    if (nkb > 1) {
+      load(1);
+      next_absent = absent_pages(1);
+    }
   }
   __syncthreads();
   for (int kb = 0; kb < nkb; ++kb) {
-    int next_absent = 0;
-    if (kb + 1 < nkb) {
-      load(kb + 1);
-      next_absent = absent_pages(kb + 1);
+    const int buf = kb & 1;
+    const bool mine = 16 * (p0 + 4 * kb) < w_seen;         // else no column of the wave sees the block
+    settle(kb + 1);                                        // past the last block: stale codes, to a buffer that is not read
+    if (mine) {
+      scores(buf);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) store(i, buf ^ 1);
     }
-    if (16 * (p0 + 4 * kb) < w_seen) compute(kb, kb & 1, absent);
-    if (kb + 1 < nkb) store(kb + 1, (kb + 1) & 1);
+    const int now_absent = absent;
     absent = next_absent;
+    if (kb + 2 < nkb) {
+      load(kb + 2);
+      next_absent = absent_pages(kb + 2);
+    }
+    if (mine) compute(kb, buf, now_absent);
     __syncthreads();
   }
   l += __shfl_xor(l, 32, 64);
