@@ -85,25 +85,14 @@ struct TopList {
 };
 constexpr TopList kEmptyTop = {-INFINITY, -1, -INFINITY, -1, -INFINITY, -1};
 __device__ __forceinline__ bool beats(float v, int id, float lv, int lid) { return v > lv || (v == lv && id < lid); }
-// the k-th largest of the lanes' n values (-inf if fewer are above that), which are used up
-template <int n> __device__ __forceinline__ float kth_largest(int k, float* v) {
-  float f = -INFINITY;
-#pragma unroll 1
-  for (int i = 0; i < k; ++i) {
-    float mx = v[0];
-#pragma unroll
-    for (int j = 1; j < n; ++j) mx = fmaxf(mx, v[j]);
-    f = wave_max(mx);
-    if (!(f > -INFINITY)) break;
-    bool take = (int)(threadIdx.x & 63) == __ffsll((unsigned long long)__ballot(mx == f)) - 1;
-#pragma unroll
-    for (int j = 0; j < n; ++j) {
-      const bool here = take && v[j] == f;
-      v[j] = here ? -INFINITY : v[j];
-      take = take && !here;
-    }
-  }
-  return f;
+// the k-th largest of the lanes' values: the smallest of those that fewer than k are above, counted in 64 steps of three
+// instructions (taking the largest k times took 0.3 us a time)
+__device__ __forceinline__ float kth_largest(int k, float v) {
+  if (k == 1) return wave_max(v);
+  int above = 0;
+#pragma unroll 16
+  for (int j = 0; j < 64; ++j) above += lane_value(v, j) > v;
+  return -wave_max(above < k ? -v : -INFINITY);
 }
 __device__ __forceinline__ void set_floor(TopList& l, float f) {
   if (f > -INFINITY) {
@@ -135,6 +124,33 @@ __device__ __forceinline__ void top_offer(TopList& l, int k, float v, int id) {
     top_insert(l, k, lane_value(v, src), __builtin_amdgcn_readlane(id, src));
     who = __ballot(beats(v, id, l.last_v, l.last_id)) & (who & (who - 1));
   }
+}
+
+// Candidates of a block's (or wave's) k best, gathered in any order and then ranked all at once.  More than 64 can reach
+// a floor where logits are equal; then n exceeds 64 and the list has to be built by offers.
+struct Pool { int n; float v[64]; int id[64]; };
+__device__ __forceinline__ void pool_add(Pool& p, bool keep, float v, int id) {
+  const unsigned long long who = __ballot(keep);
+  if (!who) return;
+  const int lane = threadIdx.x & 63;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(&p.n, __popcll(who));
+  at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
+  if (keep && at < 64) { p.v[at] = v; p.id[at] = id; }
+}
+// the k best of a pool of n <= 64, rank i in lane i: by a wave
+__device__ __forceinline__ TopList pool_best(const Pool& p, int n, int k) {
+  const int lane = threadIdx.x & 63;
+  TopList l = kEmptyTop;
+  const float v = lane < n ? p.v[lane] : -INFINITY;
+  const int id = lane < n ? p.id[lane] : -1;
+  int rank = lane < n ? 0 : lane;
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) rank += lane < n && beats(lane_value(v, j), __builtin_amdgcn_readlane(id, j), v, id);
+  const float rv = __uint_as_float(__builtin_amdgcn_ds_permute(4 * rank, __float_as_uint(v)));
+  const int ri = __builtin_amdgcn_ds_permute(4 * rank, id);
+  if (lane < min(n, k)) { l.v = rv; l.id = ri; }
+  return l;
 }
 
 // fmaxf makes quiet every operand that may be a signalling NaN, an instruction each
@@ -186,10 +202,11 @@ __device__ __forceinline__ void write_row(const ScoreOut& out, int r, RowSum a, 
 // Block (split, row).  The row's 16-byte aligned vectors are shared out over the splits, the few logits before the
 // first and after the last go to split 0.  A lane sums U vectors (a group) under one look at its maximum.
 // Top ids: while they stream by, a lane keeps only its largest logit and that one's group, and the largest of its other
-// groups.  The k-th largest of the block's lane maxima is a floor that k logits reach, so only the lanes whose maximum
-// reaches it, about k, hold any of the k best: their group is read again (all their groups if a second one reaches
-// the floor) and its logits offered to a sorted list.  Offering logits as they come took 30-60 us more for 2,048 bf16
-// rows x 151,936 ids (k = 8-20), which sum in 105.
+// groups.  Over the waves lane i keeps the largest of their lanes i; the k-th largest of these 64 is a floor that k logits
+// reach, so only the lanes whose maximum reaches it, little more than k, hold any of the k best: their group is read
+// again (all their groups if a second one reaches the floor), what reaches the floor is gathered in LDS and ranked at
+// once.  Logits equal to the floor can be too many for that; then waves offer theirs one by one to sorted lists.
+// Offering logits as they come took 30-60 us more for 2,048 bf16 rows x 151,936 ids (k = 8-20), which sum in 105.
 // STREAM: non-temporal loads (see launch_score).
 template <typename T, int W, bool TOP, bool STREAM>
 __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__ logits, int64_t row_stride, int V,
@@ -198,6 +215,7 @@ __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__
   constexpr int N = Vec16<T>::N, U = 4;
   __shared__ RowSum sum_w[W];
   __shared__ float max_w[TOP ? W : 1][64];
+  __shared__ Pool pool;
   __shared__ float lv_w[W][32];
   __shared__ int li_w[W][32];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -278,12 +296,12 @@ __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__
   TopList l = kEmptyTop;
   if (TOP) {
     max_w[wave][lane] = m1;
+    if (threadIdx.x == 0) pool.n = 0;
     __syncthreads();
-    float all[W];
+    float most = max_w[0][lane];
 #pragma unroll
-    for (int w = 0; w < W; ++w) all[w] = max_w[w][lane];
-    const float floor_v = kth_largest<W>(k, all);
-    set_floor(l, floor_v);
+    for (int w = 1; w < W; ++w) most = fmaxf(most, max_w[w][lane]);
+    const float floor_v = kth_largest(k, most);
     // element i of group g of lane `src`: its id, or -1
     auto element = [&](int src, int g, int i) {
       if (g >= groups) return i == 0 && src < head + tail ? end_id(src) : -1;
@@ -291,27 +309,35 @@ __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__
       const int vec = first + i / N * W * 64;
       return i < (g < whole ? U * N : N) && vec < v1 ? head + vec * N + i % N : -1;
     };
-    auto offer = [&](int id) { top_offer(l, k, id >= 0 ? ld_f32<T>(x, id) : -INFINITY, id); };
-    unsigned long long few = __ballot(m1 > -INFINITY && m1 >= floor_v);
-    unsigned long long more = __ballot(m2 > -INFINITY && m2 >= floor_v) & few;
-    few &= ~more;
-    constexpr int PER = U * N, AT_ONCE = 64 / PER;     // lanes whose groups are read together
-    while (few) {
-      int id = -1;
+    auto each_candidate = [&](auto offer) {
+      auto offer_id = [&](int id) { offer(id >= 0 ? ld_f32<T>(x, id) : -INFINITY, id); };
+      unsigned long long few = __ballot(m1 > -INFINITY && m1 >= floor_v);
+      unsigned long long more = __ballot(m2 > -INFINITY && m2 >= floor_v) & few;
+      few &= ~more;
+      constexpr int PER = U * N, AT_ONCE = 64 / PER;   // lanes whose groups are read together
+      while (few) {
+        int id = -1;
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) {
-        if (!few) break;
-        const int src = __ffsll(few) - 1, g = __builtin_amdgcn_readlane(g1, src);
-        few &= few - 1;
-        if (lane / PER == i) id = element(src, g, lane % PER);
+        for (int i = 0; i < AT_ONCE; ++i) {
+          if (!few) break;
+          const int src = __ffsll(few) - 1, g = __builtin_amdgcn_readlane(g1, src);
+          few &= few - 1;
+          if (lane / PER == i) id = element(src, g, lane % PER);
+        }
+        offer_id(id);
       }
-      offer(id);
-    }
-    while (more) {
-      const int src = __ffsll(more) - 1;
-      more &= more - 1;
-      const int n = (groups + (ends ? 1 : 0)) * PER;
-      for (int e = lane; e - lane < n; e += 64) offer(e < n ? element(src, e / PER, e % PER) : -1);
+      while (more) {
+        const int src = __ffsll(more) - 1;
+        more &= more - 1;
+        const int n = (groups + (ends ? 1 : 0)) * PER;
+        for (int e = lane; e - lane < n; e += 64) offer_id(e < n ? element(src, e / PER, e % PER) : -1);
+      }
+    };
+    each_candidate([&](float v, int id) { pool_add(pool, v > -INFINITY && v >= floor_v, v, id); });
+    __syncthreads();
+    if (pool.n > 64) {
+      set_floor(l, floor_v);
+      each_candidate([&](float v, int id) { top_offer(l, k, v, id); });
     }
   }
   a = wave_merge(a, c);
@@ -319,9 +345,11 @@ __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__
   if (lane < k) { lv_w[wave][lane] = l.v; li_w[wave][lane] = l.id; }
   __syncthreads();
   if (wave) return;
-  for (int w = 1; w < W; ++w) {
-    merge(a, sum_w[w], c);
-    if (TOP) top_offer(l, k, lane < k ? lv_w[w][lane] : -INFINITY, lane < k ? li_w[w][lane] : -1);
+  for (int w = 1; w < W; ++w) merge(a, sum_w[w], c);
+  if (TOP) {
+    if (pool.n <= 64) l = pool_best(pool, pool.n, k);
+    else
+      for (int w = 1; w < W; ++w) top_offer(l, k, lane < k ? lv_w[w][lane] : -INFINITY, lane < k ? li_w[w][lane] : -1);
   }
   if (splits == 1) {
     write_row(out, r, a, has_tok, x_tok, l, k, inv_t);
@@ -347,14 +375,28 @@ __global__ __launch_bounds__(64) void k_token_logprobs_join(const T* __restrict_
   a = wave_merge(a, c);
   TopList l = kEmptyTop;
   if (k > 0) {
-    float best[1] = {lane < splits ? p[(size_t)lane * (4 + 2 * k) + 4] : -INFINITY};
-    set_floor(l, kth_largest<1>(k, best));
-  }
-  for (int e0 = 0; e0 < splits * k; e0 += 64) {
-    const int e = e0 + lane;
-    const float* q = p + (size_t)(e / k) * (4 + 2 * k) + 4 + e % k;
-    const bool in = e < splits * k;
-    top_offer(l, k, in ? q[0] : -INFINITY, in ? __float_as_int(q[k]) : -1);
+    // floor: the k-th largest of 64 entries, as many from the front of each split's list
+    __shared__ Pool pool;
+    if (lane == 0) pool.n = 0;
+    auto value = [&](int split, int rank) { return p[(size_t)split * (4 + 2 * k) + 4 + rank]; };
+    const float floor_v = kth_largest(k, lane / splits < k ? value(lane % splits, lane / splits) : -INFINITY);
+    auto each_entry = [&](auto offer) {
+#pragma unroll 4
+      for (int e0 = 0; e0 < splits * k; e0 += 64) {
+        const int e = min(e0 + lane, splits * k - 1);
+        const float* q = p + (size_t)(e / k) * (4 + 2 * k) + 4 + e % k;
+        const bool in = e0 + lane < splits * k;
+        offer(in ? q[0] : -INFINITY, in ? __float_as_int(q[k]) : -1);
+      }
+    };
+    each_entry([&](float v, int id) { pool_add(pool, v > -INFINITY && v >= floor_v, v, id); });
+    const int n = __builtin_amdgcn_readfirstlane(pool.n);
+    if (n <= 64) {
+      l = pool_best(pool, n, k);
+    } else {
+      set_floor(l, floor_v);
+      each_entry([&](float v, int id) { top_offer(l, k, v, id); });
+    }
   }
   write_row(out, r, a, has_tok, x_tok, l, k, inv_t);
 }
