@@ -365,39 +365,44 @@ __device__ __forceinline__ void transpose4(uint32_t* r) {
 
 // Sequences with more columns (query tokens x heads of a KV head) than this go through k_kv8_attn_tile.
 constexpr int kFewColumns = 32;
-constexpr int kTileWaves = 4;
-// The running maximum of a column follows its scores only once they pass it by this much (base 2): weights up to 2^8
-// lose nothing in fp32 or in bf16 parts, and most key blocks leave the sums where they are.
+constexpr int kTileWaves = 4;          // one for each page of a key block
+
+// The value m subtracted from a column's scores follows them only once they pass it, and is then set this much above them
+// (base 2): weights stay at or below 1, and most key blocks leave the sums where they are (16 sequences of 256 queries
+// over 4,000 tokens: 226 us, against 229 with the maximum itself).
 constexpr float kSlack = 8.f;
+
+template <int HD> struct FewLds {
+  float m_w[4][16], l_w[4][16], o_w[4][16][HD + 4];
+};
 
 // Block (16 columns of one sequence and KV head, split): column = query token x head of the group.  The 4
 // waves take the split's pages in pairs, wave w pairs w, w + 4, ...; the next pair's K codes are loaded once
 // the scores are there, its V codes at the end.  Per pair:
 //   S^T = K q^T   codes as bf16 (exact), the page's scale on the fp32 scores
-//   online softmax per column in base 2 over the 4 lanes that hold it; the maximum kept is the value
-//                 that was subtracted
+//   online softmax per column in base 2 over the 4 lanes that hold it; m, l: the value that was subtracted
+//                 and the sum
 //   O^T += V^T P^T   the score registers are the B operand (4 tokens of each page a lane); V's bytes
 //                 are transposed in registers; P, times the page's V scale, enters as PP bf16 parts
 //                 (2: 2^-17 of a weight; 3 for fp32 queries), so the product adds no rounding of its own
 // Queries of fp32 enter as 3 bf16 parts.  A column without a visible key gives 0.
 template <int HD, int FMT, typename T>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) {
+__device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs& a, FewLds<HD>& lds, int bx, int split) {
   constexpr int NK = HD / 64, NT = HD / 16, DV = HD / 16;   // 16-byte K loads, dim tiles, V dims a lane
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
-  constexpr int PITCH = HD + 4;
-  __shared__ float m_w[4][16], l_w[4][16];
-  __shared__ __attribute__((aligned(16))) float o_w[4][16][PITCH];
+  auto &m_w = lds.m_w, &l_w = lds.l_w;
+  auto& o_w = lds.o_w;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
-  const int item = blockIdx.x / hkv, g = blockIdx.x - item * hkv;
+  const int item = bx / hkv, g = bx - item * hkv;
   const int tiles = a.off ? kFewColumns / 16 : (G + 15) / 16;
   const int seq = item / tiles, c0 = 16 * (item - seq * tiles);
   int r0, r1;
   seq_rows(a.off, seq, a.n_rows, r0, r1);
   const int n_cols = (r1 - r0) * G;
   if (c0 >= n_cols || (a.off && n_cols > kFewColumns)) return;
-  const int p0 = blockIdx.y * a.pps;
+  const int p0 = split * a.pps;
   // ids of 32 of the wave's page pairs, one a lane; the first are loaded beside the context's length
   const int32_t* table = a.pages + (size_t)seq * a.max_pages;
   auto load_ids = [&](int it) { return table[min(p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1), a.max_pages - 1)]; };
@@ -406,7 +411,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
   const bool too_long = ctx > a.max_ctx;                 // more than the launch was sized for: the rows are NaN
   const int np = too_long ? 0 : (ctx + 15) >> 4;
   const int p1 = min(np, p0 + a.pps);
-  if (p0 >= p1 && blockIdx.y > 0) return;
+  if (p0 >= p1 && split > 0) return;
   // this lane's column: query row and head, and how many keys it sees
   const int cc = min(c0 + col, n_cols - 1), qt = cc / G, head = g * G + cc - qt * G;
   const int before = ctx - (r1 - r0);                    // keys before the first query (below 0: its row sees none)
@@ -471,6 +476,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
   for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (n_it > 0) {
     load_k(0);
+    __builtin_amdgcn_sched_barrier(0);                     // K first: a wait for it must not be one for V (9% at 512 rows)
     load_v();
   }
   for (int it = 0; it < n_it; ++it) {
@@ -514,12 +520,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    if (__any(mx > m + kSlack)) {
-      const float al = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
+    if (__any(mx > m)) {
+      const float to = mx > m ? mx + kSlack : m;
+      const float al = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
       l *= al;
 #pragma unroll
       for (int i = 0; i < NT; ++i) o[i] *= al;
-      m = mx;
+      m = to;
     }
     const float sub = m == -INFINITY ? 0.f : m;           // nothing seen yet: every weight is 0
     u32x4 pf[PP];
@@ -585,7 +592,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
       else *(f32x4*)dst = f32x4{f[0], f[1], f[2], f[3]};
     } else {
       const int slots = a.off ? kFewColumns : G;
-      float* dst = a.part + ((((size_t)seq * hkv + g) * slots + c0 + x) * a.splits + blockIdx.y) * (HD + 2);
+      float* dst = a.part + ((((size_t)seq * hkv + g) * slots + c0 + x) * a.splits + split) * (HD + 2);
       *(f32x2*)(dst + d4) = f32x2{num[0], num[1]};
       *(f32x2*)(dst + d4 + 2) = f32x2{num[2], num[3]};
       if (d4 == 0) *(f32x2*)(dst + HD) = f32x2{mx, den};
@@ -593,7 +600,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
   }
 }
 
-// The same attention for sequences of many columns: a block owns 32 NW of them, a wave 32, and all its waves
+template <int HD> struct TileLds {
+  u32x4 kf[2][2 * (HD / 16) * 64], vf[2][4 * (HD / 32) * 64];
+};
+
+// The same attention for sequences of many columns: a block owns 128 of them, a wave 32, and all its waves
 // read the same 64-key blocks of K and V from LDS, as bf16 values (code times scale, exact), converted once a block.
 // Per key block and wave:
 //   S^T = K q^T    v_mfma_f32_32x32x16_bf16: lane (col l % 32, h = l / 32) gets keys 8 (i / 4) + 4 h + i % 4, i < 16
@@ -607,19 +618,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_k
 // What bounds it is VALU issue (about 400 instructions and 32 exponentials a wave and key block beside 48 MFMAs of 32
 // cycles), so both run side by side: the codes of block kb + 1 wait in registers and become bf16 in LDS between the score
 // MFMAs of block kb, their successors load behind them, and the weights of 16 keys are made between the MFMAs of the
-// 16 before.  16 sequences of 256 queries over 4,000 tokens, 16 heads: 224 us (619 TFLOP/s); one prompt of 4,590: 165
-// (522), against 182 with conversion, softmax and MFMAs one after the other.  Blocks of 8 waves convert half as much
+// 16 before.  16 sequences of 256 queries over 4,000 tokens, 16 heads: 226 us (612 TFLOP/s); one prompt of 4,590: 164
+// (525), against 182 with conversion, softmax and MFMAs one after the other.  Blocks of 8 waves convert half as much
 // each and gain nothing (16 x 256: 360 us).
-template <int HD, int FMT, typename T, int NW>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_tile(sara_kv8_cache c, AttnArgs a) {
-  constexpr int NKS = HD / 16, NDT = HD / 32;
+template <int HD, int FMT, typename T>
+__device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArgs& a, TileLds<HD>& lds, int bx, int n_bx, int split) {
+  constexpr int NW = kTileWaves, NKS = HD / 16, NDT = HD / 32;
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
   constexpr int KU = NKS / NW, KR = 64 / NKS;                        // staging: K units a thread, token rows a unit of a wave
   typedef float f32x16 __attribute__((ext_vector_type(16)));
-  __shared__ u32x4 kf[2][2 * NKS * 64], vf[2][4 * NDT * 64];
+  auto &kf = lds.kf;
+  auto &vf = lds.vf;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
-  const int item = (int)gridDim.x / hkv - 1 - (int)blockIdx.x / hkv, g = blockIdx.x % hkv;   // long tiles first
+  const int item = n_bx / hkv - 1 - bx / hkv, g = bx % hkv;          // long tiles first
   const SeqRows sr = find_seq<32 * NW>(a.off, a.ctx, a.n_seqs, a.n_rows, item, G, 1);
   const int seq = sr.seq, r0 = sr.r0, r1 = sr.r1;
   if (seq < 0 || item < sr.first) return;
@@ -628,8 +640,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
   const int ctx = max(sr.value, 0);
   const bool too_long = ctx > a.max_ctx;
   const int np = too_long ? 0 : (ctx + 15) >> 4;
-  const int p0 = blockIdx.y * a.pps_tile;
-  if (p0 >= np && blockIdx.y > 0) return;
+  const int p0 = split * a.pps_tile;
+  if (p0 >= np && split > 0) return;
   const int before = ctx - (r1 - r0);
   const int c_last = min(c0 + 32 * NW, n_cols) - 1;
   const int keys = min(max(before + c_last / G + 1, 0), ctx);       // keys that some column of the block sees
@@ -789,12 +801,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     mx = fmaxf(m, mx * sl2);
-    if (__any(mx > m + kSlack)) {
-      const float al = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
+    if (__any(mx > m)) {
+      const float to = mx > m ? mx + kSlack : m;
+      const float al = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.f : to));
       l *= al;
 #pragma unroll
       for (int t = 0; t < NDT; ++t) o[t] *= al;
-      m = mx;
+      m = to;
     }
     const float sub = m == -INFINITY ? 0.f : m;
     // weights of keys pair j of step st, in PP bf16 parts
@@ -870,7 +883,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
   const float inv = too_long ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : 1.f / l;
   const bool whole = np <= a.pps_tile;
   T* out = (T*)a.out + (size_t)(r0 + qt) * a.o_row + (size_t)head * a.o_head + 16 * h;
-  float* part = a.part_tile + (((size_t)(r0 + qt) * a.hq + head) * a.splits_tile + blockIdx.y) * (HD + 2);
+  float* part = a.part_tile + (((size_t)(r0 + qt) * a.hq + head) * a.splits_tile + split) * (HD + 2);
 #pragma unroll
   for (int t = 0; t < NDT; ++t) {
     float f[16];
@@ -887,6 +900,25 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_ti
     }
   }
   if (!whole && h == 0) *(f32x2*)(part + HD) = f32x2{m, l};
+}
+
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) FewLds<HD> lds;
+  attn_few<HD, FMT, T>(c, a, lds, blockIdx.x, blockIdx.y);
+}
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_tile(sara_kv8_cache c, AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) TileLds<HD> lds;
+  attn_tile<HD, FMT, T>(c, a, lds, blockIdx.x, gridDim.x, blockIdx.y);
+}
+// Both in one launch (see launch_kv8_attention): n_tile x splits_tile blocks of tiles, then n_few x splits of few columns.
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_both(sara_kv8_cache c, AttnArgs a, int n_tile, int n_few) {
+  __shared__ __attribute__((aligned(16))) union { FewLds<HD> few; TileLds<HD> tile; } lds;
+  const int b = blockIdx.x, few = b - n_tile * a.splits_tile;
+  if (few < 0) attn_tile<HD, FMT, T>(c, a, lds.tile, b % n_tile, n_tile, b / n_tile);
+  else attn_few<HD, FMT, T>(c, a, lds.few, few % n_few, few / n_few);
 }
 
 // A block per (row, head) joins the splits of rows that have more than one: its 4 waves take every fourth split,
@@ -1042,11 +1074,18 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
                       s.splits, s.pps, s.splits_tile, s.pps_tile, scale * 1.4426950408889634f, (float*)ws,
                       (float*)((char*)ws + s.part_bytes)};
   return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
-    hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.items * c.n_kv_heads), s.splits),
-                       dim3(256), 0, st, c, a);
-    if (s.tile_items)
-      hipLaunchKernelGGL((k_kv8_attn_tile<hd.value, fmt.value, decltype(t), kTileWaves>),
-                         dim3((uint32_t)(s.tile_items * c.n_kv_heads), s.splits_tile), dim3(64 * kTileWaves), 0, st, c, a);
+    const int n_few = (int)(s.items * c.n_kv_heads), n_tile = (int)(s.tile_items * c.n_kv_heads);
+    // One launch for both where the blocks of few columns fit beside each other at the tiles' two a CU: 64 sequences of
+    // 1-33 fp32 queries over up to 63 tokens 12.4 -> 8.0 us, of 1-33 bf16 ones over up to 500 31.2 -> 22.9.  More of them
+    // lose the third wave a SIMD that streaming pages wants: 512 sequences of 1-2 queries over 1,000 tokens 70 -> 80.
+    if (s.tile_items && (int64_t)n_few * s.splits <= 512) {
+      hipLaunchKernelGGL((k_kv8_attn_both<hd.value, fmt.value, decltype(t)>), dim3(n_tile * s.splits_tile + n_few * s.splits), dim3(256),
+                         0, st, c, a, n_tile, n_few);
+    } else {
+      hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3(n_few, s.splits), dim3(256), 0, st, c, a);
+      if (s.tile_items)
+        hipLaunchKernelGGL((k_kv8_attn_tile<hd.value, fmt.value, decltype(t)>), dim3(n_tile, s.splits_tile), dim3(256), 0, st, c, a);
+    }
     if (s.splits > 1) {
       const int cols = off ? kFewColumns : hq / c.n_kv_heads;
       hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t), false>), dim3((uint32_t)((int64_t)n_seqs * c.n_kv_heads * cols)),
