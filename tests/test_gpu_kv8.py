@@ -253,6 +253,22 @@ def test_ragged_queries(env, hq, hkv, hd, fmt, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,hd", [(12, 2, 128), (4, 4, 64)])
+def test_ragged_queries_of_many_sequences(env, hq, hkv, hd, dtype):
+    """300 sequences of no query to 40, with keys for some queries only: right, and the same bits in a call of ten."""
+    rng = np.random.default_rng([hq, hkv, hd, 2])
+    nq = [int(n) for n in rng.choice([0, 1, 2, 5, 40], 300, p=[0.1, 0.5, 0.2, 0.1, 0.1])]
+    ctx = [max(0, n + int(rng.integers(-2, 60))) for n in nq]
+    dev, tables = filled(env, rng, hkv, hd, "int8", ctx)
+    off = offsets(nq)
+    q = dev.tensor(rng.standard_normal((sum(nq), hq, hd)) * 2, env[0].bfloat16 if dtype == "bf16" else env[0].float32)
+    got = attend(dev, q, tables, ctx, off)
+    check_attention(dev, q, got, tables, ctx, off)
+    few = attend(dev, q[:off[10]], tables[:10], ctx[:10], off[:11])
+    assert env[0].equal(few, got[:off[10]])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_long_contexts_join_their_splits(env, dtype):
     rng = np.random.default_rng(11)
     ctx = [3000, 1, 777, 2049]

@@ -205,6 +205,25 @@ def test_gradient_against_differences(env):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,n", [(5000, 6), (5000, 600), (60000, 6)])
+@pytest.mark.parametrize("k", [1, 2, 20, 32])
+def test_top_ids_among_equal_logits(env, V, n, k, dtype):
+    """k - 1 larger logits and 1 to 300 equal ones at rank k, among them as many as are ranked at once and one more:
+    the lowest ids of the equal ones, whether a row is split or not."""
+    torch, sara = env
+    rng = np.random.default_rng([V, n, k])
+    x = np.clip(rng.standard_normal((n, V)), -4, 4)
+    for r, equal in zip(range(n), [1, 64 - (k - 1), 65 - (k - 1), 63, 300, 65] * (n // 6)):
+        at = rng.permutation(V)[:k - 1 + equal]
+        x[r, at] = 8.0
+        x[r, at[:k - 1]] = 16.0 + np.arange(k - 1) // 2          # pairs of equal ones above too
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    dx = place(torch, x, td, 0, 0)
+    t, out, top = forward(env, dx, np.zeros(n, np.int32), 1.0, k)
+    check_forward(dx.double().cpu().numpy(), np.zeros(n, np.int64), 1.0, k, out, top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_not_a_number_stays_in_its_row(env, dtype):
     torch, sara = env
     rng = np.random.default_rng(22)

@@ -99,3 +99,28 @@ def test_one_hip_runtime_whatever_is_imported_first(order):
     code = order + "\nfor l in open('/proc/self/maps'):\n    if 'libamdhip64' in l: print(l.split()[-1])"
     out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, check=True).stdout
     assert len(set(out.split())) == 1, out
+
+
+def test_temperatures_without_a_reciprocal_are_refused():
+    for T in (1e-39, 1e-38, 2e37, float("inf")):
+        assert L.sara_token_logprobs(P, 1, 100, 2, 100, P, T, 0, P, P, P, None, None, None, 0, None) == BAD
+        assert L.sara_token_logprobs_grad(P, 1, 100, 2, 100, P, T, P, P, P, P, P, 100, None) == BAD
+
+
+def test_calls_refuse_host_tensors_and_other_objects():
+    import torch
+    x, ids = torch.zeros((2, 8)), torch.zeros(2, dtype=torch.int32)
+    for bad, exc in ((x, ValueError), (x.half(), TypeError), (None, TypeError), ([1.0], TypeError)):
+        with pytest.raises(exc):
+            sara.sara_token_logprobs(bad, ids)
+        with pytest.raises(exc):
+            sara.sara_token_logprobs_grad(bad, ids, None, None, None, None, x)
+    codes, exps = torch.zeros((2, 1, 16, 64), dtype=torch.int8), torch.zeros((2, 1), dtype=torch.uint8)
+    kv, pages, seq = torch.zeros((1, 1, 64)), torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    for bad, exc in ((kv, ValueError), (kv.double(), TypeError), (3, TypeError)):
+        with pytest.raises(exc):
+            sara.sara_kv8_write(codes, codes, exps, exps, bad, bad, pages, seq)
+        with pytest.raises(exc):
+            sara.sara_kv8_read(codes, codes, exps, exps, pages, seq, None, bad, bad)
+        with pytest.raises(exc):
+            sara.sara_kv8_attention(bad, codes, codes, exps, exps, pages, seq, None, bad)
