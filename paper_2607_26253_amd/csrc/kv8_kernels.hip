@@ -1055,8 +1055,8 @@ Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx,
   s.items = (int64_t)n_seqs * (ragged ? kFewColumns / 16 : (G + 15) / 16);
   s.tile_items = ragged && (int64_t)n_rows * G > kFewColumns ? (int64_t)n_rows * G / (32 * kTileWaves) + n_seqs : 0;
   s.pps = share(ragged ? n_seqs : s.items, 1024, 24, 8);
-  // tiles of 128 columns: two blocks a CU are resident.  64 queries a sequence over 4,000 tokens: 122 us, against 141 in
-  // steps of 64 pages; with 1,024 blocks prompts of 300-2,500 tokens are split too and take 104 us for 75.
+  // tiles of 128 columns: two blocks a CU are resident.  16 sequences of 64 queries over 4,000 tokens: 115 us, against 130
+  // in steps of 64 pages; 256 queries over 16,000: 86, against 105, and 93 with 1,024 blocks
   s.pps_tile = s.tile_items ? share(s.tile_items, 512, 32, 16) : s.pps;
   s.splits = (np + s.pps - 1) / s.pps;
   s.splits_tile = s.tile_items ? (np + s.pps_tile - 1) / s.pps_tile : 0;

@@ -463,11 +463,12 @@ __global__ __launch_bounds__(256) void k_token_logprobs_grad(const T* logits, in
   }
 }
 
-// Waves of a block and splits of a row.  From 512 rows on a block has a row to itself, of 8 waves while there are fewer
-// than four blocks a CU (512 fp32 rows x 151,936 ids with 8 top ids: 56 us, against 63 as two splits of 4 waves and a
-// join; 2,048 bf16 rows: 145 us, against 139 with 4 waves).  Fewer rows are split until 1,024 blocks share them, but not
-// below 4,096 ids, about what a block's start and the join cost.
-static int score_waves(int n_rows) { return n_rows >= 512 && n_rows < 1024 ? 8 : 4; }
+// Waves of a block and splits of a row.  From 512 rows on a block has a row to itself, of 8 waves where rows are long (600
+// bf16 rows x 151,936 ids with 20 top ids: 50 us, against 54 with 4 waves; 512 fp32 rows with 8: 61 either way, 66 as two
+// splits of 4 waves and a join), of 4 where they are not (700 bf16 rows x 32,016 ids: 17 us, against 20; x 100,000: 34
+// either way).  Fewer rows are split until 1,024 blocks share them, but not below 4,096 ids, about what a block's start
+// and the join cost.
+static int score_waves(int n_rows, int V) { return n_rows >= 512 && V >= 98304 ? 8 : 4; }
 static int score_splits(int n_rows, int V) {
   if (n_rows >= 512) return 1;
   const int by_rows = (1024 + n_rows - 1) / n_rows, by_size = (V + 4095) / 4096;
@@ -505,7 +506,7 @@ static void launch_score(const T* logits, int64_t row_stride, int n_rows, int V,
       else go(k_token_logprobs<T, w.value, top.value, false>, w.value);
     };
     auto by_top = [&](auto w) { k ? by_loads(w, std::true_type{}) : by_loads(w, std::false_type{}); };
-    if (score_waves(n_rows) == 8) by_top(std::integral_constant<int, 8>{});
+    if (score_waves(n_rows, V) == 8) by_top(std::integral_constant<int, 8>{});
     else by_top(std::integral_constant<int, 4>{});
     if (sp > 1)
       hipLaunchKernelGGL(k_token_logprobs_join<T>, dim3(n), dim3(64), 0, st, x, row_stride, V, tok + r0, c, inv_t, k, sp,
