@@ -240,6 +240,9 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float*
   *(f32x4*)(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
 }
 
+// A wave has a page's 16 rows of one head in registers: their largest magnitude gives the scale, the codes follow with no
+// second read, and a page that keeps earlier tokens is re-rounded by the same wave.  Bound by memory on a pool (256
+// prompts of 128-512 tokens, 21 us; with the read back 50 us, 4.98 TB/s) and by its load chain on a token (2.2 us).
 template <int HD, int FMT, typename T>
 __global__ __launch_bounds__(256) void k_kv8_write(sara_kv8_cache c, KvRows src, const int32_t* __restrict__ pages,
     int max_pages, const int32_t* __restrict__ start, const int32_t* __restrict__ off, int n_seqs, int n_rows) {
@@ -292,7 +295,7 @@ __global__ __launch_bounds__(256) void k_kv8_write(sara_kv8_cache c, KvRows src,
   if (lane == 0) *exp = (uint8_t)b;
 }
 
-// Rows of positions without a page are 0.
+// The same units as the write.  Rows of positions without a page are 0.  The pool above: 21 us.
 template <int HD, int FMT, typename T>
 __global__ __launch_bounds__(256) void k_kv8_read(sara_kv8_cache c, KvRows dst, const int32_t* __restrict__ pages,
     int max_pages, const int32_t* __restrict__ start, const int32_t* __restrict__ off, int n_seqs, int n_rows) {
@@ -386,6 +389,9 @@ template <int HD> struct FewLds {
 //                 are transposed in registers; P, times the page's V scale, enters as PP bf16 parts
 //                 (2: 2^-17 of a weight; 3 for fp32 queries), so the product adds no rounding of its own
 // Queries of fp32 enter as 3 bf16 parts.  A column without a visible key gives 0.
+// What bounds it is the pages' memory traffic from some 100 rows on (512 rows at 256-1,700 tokens: 51 us, 5.1 TB/s; 32
+// rows at 3,000-4,600 in splits: 15.5 us, 4.0 TB/s), below that its load round trips (one row at 333: 7.0 us).  Blocks of
+// 8 waves take 6.7 us there, but 22 for the 32 rows' 18.3 with the join.
 template <int HD, int FMT, typename T>
 __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs& a, FewLds<HD>& lds, int bx, int split) {
   constexpr int NK = HD / 64, NT = HD / 16, DV = HD / 16;   // 16-byte K loads, dim tiles, V dims a lane
