@@ -405,8 +405,10 @@ __global__ __launch_bounds__(64) void k_token_logprobs_join(const T* __restrict_
 }
 
 // dx_j = (1/T) [ g ([j = tok] - p_j) - h p_j (log p_j + H) ],  p_j = 2^((x_j - m) c) / s.
-// With d = x_j - m:  dx_j = 2^(d c) (A + B d) + [j = tok] g / T,
-//   A = -(g + h (H - log s)) / (T s),  B = -h / (T^2 s).
+// With u = (x_j - m) c:  dx_j = (2^u (A + B u) + [j = tok] g) / T,
+//   A = -(g + h (H - log s)) / s,  B = -h log(2) / s.
+// No power of T enters A or B and u is held above -150, where 2^u is 0 already: at every accepted temperature a masked
+// id gets 0, and 1 / T overflows only where the gradient does.
 // The rounded d and d c alone would cost the p of an id far below the largest |d c| 2^-23 of itself: nothing
 // beside the rounding of a bf16 gradient, but an fp32 one adds what the difference and the product lost (c in
 // two parts), which its twice as many bytes hide.
@@ -425,8 +427,8 @@ __global__ __launch_bounds__(256) void k_token_logprobs_grad(const T* logits, in
   const float m = stats[2 * (size_t)r], s = stats[2 * (size_t)r + 1];
   const float g = tk >= 0 && tk < V && g_logp ? g_logp[r] : 0.f, h = g_ent ? g_ent[r] : 0.f;
   const bool none = s == 0.f || (g == 0.f && h == 0.f);   // nothing left of the row, or nothing asked of it
-  const float A = -(g + (h == 0.f ? 0.f : h * (entropy[r] - logf(s)))) * inv_t / s, B = -h * inv_t * inv_t / s;
-  const float at_tok = g * inv_t;
+  const float A = -(g + (h == 0.f ? 0.f : h * (entropy[r] - logf(s)))) / s, B = -0.69314718f * h / s;
+  // T times the gradient of a logit, but for the token's own g
   auto one = [&](float f) {
     const float d = f - m, a = d * c;
     float e = __builtin_amdgcn_exp2f(a);
@@ -435,12 +437,11 @@ __global__ __launch_bounds__(256) void k_token_logprobs_grad(const T* logits, in
       const float lost = fmaf(dl, c, fmaf(d, c_lo, fmaf(d, c, -a)));   // not a number where d c overflows, and e is 0
       e = a > -150.f ? fmaf(e, lost * 0.69314718f, e) : e;
     }
-    // where d matters (d c > -150) it is far above this bound, which keeps B d finite for masked ids
-    return e * fmaf(B, fmaxf(d, -1e20f), A);             // a NaN is in e
+    return e * fmaf(B, fmaxf(a, -150.f), A);             // a NaN is in e
   };
   const int stride = gridDim.x * 256, t0 = blockIdx.x * 256 + threadIdx.x;
   if (!VEC) {
-    for (int j = t0; j < V; j += stride) st_f32<T>(y, j, none ? 0.f : one(ld_f32<T>(x, j)) + (j == tk ? at_tok : 0.f));
+    for (int j = t0; j < V; j += stride) st_f32<T>(y, j, none ? 0.f : (one(ld_f32<T>(x, j)) + (j == tk ? g : 0.f)) * inv_t);
     return;
   }
   const int head = min(V, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
@@ -455,7 +456,9 @@ __global__ __launch_bounds__(256) void k_token_logprobs_grad(const T* logits, in
       const int at = tk - (head + b * N);
       if (at >= 0 && at < N)
 #pragma unroll
-        for (int q = 0; q < N; ++q) f[q] += q == at ? at_tok : 0.f;
+        for (int q = 0; q < N; ++q) f[q] += q == at ? g : 0.f;
+#pragma unroll
+      for (int q = 0; q < N; ++q) f[q] *= inv_t;
 #pragma unroll
       for (int q = 0; q < 4; ++q) w[q] = sizeof(T) == 2 ? pack_bf16(f[2 * q], f[2 * q + 1]) : __float_as_uint(f[q]);
     }
@@ -463,7 +466,7 @@ __global__ __launch_bounds__(256) void k_token_logprobs_grad(const T* logits, in
   }
   if (t0 < head + tail) {
     const int j = t0 < head ? t0 : V - tail + (t0 - head);
-    st_f32<T>(y, j, none ? 0.f : one(ld_f32<T>(x, j)) + (j == tk ? at_tok : 0.f));
+    st_f32<T>(y, j, none ? 0.f : (one(ld_f32<T>(x, j)) + (j == tk ? g : 0.f)) * inv_t);
   }
 }
 

@@ -320,3 +320,51 @@ def test_refusals(env):
     with pytest.raises(TypeError):
         sara.sara_token_logprobs_grad(x, t, stats, None, logp, None, torch.empty_like(x, dtype=torch.float16))
     torch.cuda.synchronize()
+
+
+# -- temperatures -------------------------------------------------------------------
+def spread_rows(rng, T, V, dtype, torch):
+    """Rows whose z = x / T are ordinary at any temperature: normal ones, one with ids masked by -inf and by the type's
+    lowest value, a tied one, and one that a single id is left of."""
+    top = np.float64(3.38e38)
+    x = np.clip(rng.standard_normal((5, V)) * 3.0 * T, -top, top)
+    x[1, ::3], x[1, 1::3] = -np.inf, -top
+    x[2] = T
+    x[3] = -np.inf
+    x[3, V // 2] = -T
+    x[4] *= 4.0
+    return torch.from_numpy(np.clip(x, -np.inf, top)).to(torch.bfloat16 if dtype == "bf16" else torch.float32).double().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1.01e-37, 1e-20, 3e-12, 1e-9, 1e-3, 1e4, 1e12, 1e18, 3e25, 1e33])
+def test_gradient_over_the_temperatures(env, T, dtype):
+    """Statistics of 64 bits, so that the gradient alone is looked at.  An element's error: p relative to 2^-19 (fp32) or,
+    of bf16 logits, |u| 2^-23 with |u| < 150: 2^-15, of the sum of the magnitudes of its terms; exponentials below 2^-126
+    may count as 0, at which |log p| is at most 104; its rounding; and subnormal results (2^-126)."""
+    torch, sara = env
+    rng = np.random.default_rng(31)
+    T = float(np.float32(T))
+    for V, shift in ((37, 0), (2051, 1)):
+        x = spread_rows(rng, T, V, dtype, torch)
+        n, bf16 = len(x), dtype == "bf16"
+        dx = place(torch, x, torch.bfloat16 if bf16 else torch.float32, shift, 0)
+        tok = np.array([3, 1, 5, V // 2, -1])
+        _, H, m, s, _, _, lp, p = reference(x, tok, T, 0)
+        f = dict(dtype=torch.float32, device="cuda")
+        stats = torch.tensor(np.stack([m, s], 1), **f)
+        t, ent = torch.tensor(tok, dtype=torch.int32, device="cuda"), torch.tensor(H, **f)
+        g, h = np.array([1.0, -0.5, 2.0, 1.0, 0.5]), np.array([0.5, 1.0, -1.0, 0.3, 1.0])
+        lp, has = np.where(p > 0, lp, 0.0), tok >= 0
+        for gg, hh in ((g, h), (0 * g, h), (g, 0 * h)):
+            want = grad_reference(x, tok, T, gg, hh)
+            dst = torch.full_like(dx, 5.0)
+            backward(env, dx, t, (None, ent, stats), T, gg, hh, dst)
+            got = dst.double().cpu().numpy()
+            size = np.abs(gg)[:, None] + np.abs(hh)[:, None] * (2 + 2 * np.minimum(np.abs(lp), 104.0) + 2 * H[:, None])
+            terms = size * p / T
+            terms[np.arange(n)[has], tok[has]] += np.abs(gg[has]) / T
+            bound = ((2.0 ** -15 if bf16 else 2.0 ** -19) * terms + 2.0 ** -126 * (1 + size / T) +
+                     (2.0 ** -8 if bf16 else 2.0 ** -23) * np.abs(want))
+            err = np.abs(got - want)
+            assert np.all(err <= bound), (V, np.nanmax(err / bound), int(np.isnan(err).sum()))
