@@ -10,20 +10,21 @@
 
 namespace sara {
 
-// With z = x / T, m the row's largest logit and c = log2(e) / T:
-//   s = sum 2^((x - m) c),  t = sum 2^((x - m) c) (x - m)
-//   logp(id) = (x_id - m) / T - log s,   H = log s - t / (T s)
+// With z = x / T, m the row's largest logit, c = log2(e) / T and u = (x - m) c:
+//   s = sum 2^u,  t = sum 2^u u
+//   logp(id) = (x_id - m) / T - log s,   H = log s - log(2) t / s
 // one pass over the row with a running (m, s, t).  Logits enter as x - m, never as x c:
-// the type's lowest value (a mask) would overflow there, and a row of nothing else is uniform.
+// the type's lowest value (a mask) would overflow there, and a row of nothing else is uniform.  t sums u, not
+// x - m: |2^u u| is at most 0.54, where 2^u (x - m) overflows for logits as large as an accepted temperature allows.
 // Running sums start at m = -FLT_MAX, so that x - m is -inf (weight 0), not NaN, for masked ids.
 struct RowSum { float m, s, t; };
 constexpr RowSum kEmptySum = {-FLT_MAX, 0.f, 0.f};
 
-// (m, s, t) under the larger maximum `m`.  The old maximum may be a mask's, so that d is huge
-// and r is 0: r d is formed first, and d is held above -inf.
+// (m, s, t) under the larger maximum `m`.  The old maximum may be a mask's, so that u is huge
+// and r is 0: r u is formed first, and u is held above -inf.
 __device__ __forceinline__ void rescale(RowSum& a, float m, float c) {
-  const float d = a.m - m, r = __builtin_amdgcn_exp2f(d * c);
-  a.t = fmaf(r * fmaxf(d, -FLT_MAX), a.s, r * a.t);
+  const float u = (a.m - m) * c, r = __builtin_amdgcn_exp2f(u);
+  a.t = fmaf(r * fmaxf(u, -FLT_MAX), a.s, r * a.t);
   a.s *= r;
   a.m = m;
 }
@@ -36,9 +37,9 @@ __device__ __forceinline__ void merge(RowSum& a, RowSum b, float c) {
 }
 // weight 0 of a masked id times its -inf must count as 0; a NaN stays in s
 __device__ __forceinline__ void add_logit(RowSum& a, float x, float c) {
-  const float d = x - a.m, e = __builtin_amdgcn_exp2f(d * c);
+  const float u = (x - a.m) * c, e = __builtin_amdgcn_exp2f(u);
   a.s += e;
-  a.t = fmaf(e, fmaxf(d, -FLT_MAX), a.t);
+  a.t = fmaf(e, fmaxf(u, -FLT_MAX), a.t);
 }
 
 // Reductions over a wave along its rows of 16 lanes and then across them; the result of lane 63 is everyone's.
@@ -182,6 +183,12 @@ struct ScoreOut {
   float* top_logp;
 };
 
+// (x - m) / T - log s.  Of two finite logits x - m may be -inf, which T above 5e35 would bring back: then each is divided.
+__device__ __forceinline__ float log_prob(float x, float m, float inv_t, float logs) {
+  const float d = x - m;
+  return d < -FLT_MAX ? fmaf(x, inv_t, -m * inv_t) - logs : fmaf(d, inv_t, -logs);
+}
+
 // a row's outputs from its sums and its sorted list
 __device__ __forceinline__ void write_row(const ScoreOut& out, int r, RowSum a, bool has_tok, float x_tok,
                                           const TopList& l, int k, float inv_t) {
@@ -189,13 +196,13 @@ __device__ __forceinline__ void write_row(const ScoreOut& out, int r, RowSum a, 
   const bool none = a.s == 0.f;                     // no id above -inf
   const float logs = logf(a.s);
   if (lane == 0) {
-    if (out.logp) out.logp[r] = !has_tok ? 0.f : none ? -INFINITY : fmaf(x_tok - a.m, inv_t, -logs);
-    if (out.entropy) out.entropy[r] = none ? 0.f : fmaf(-inv_t, a.t / a.s, logs);
+    if (out.logp) out.logp[r] = !has_tok ? 0.f : none ? -INFINITY : log_prob(x_tok, a.m, inv_t, logs);
+    if (out.entropy) out.entropy[r] = none ? 0.f : fmaf(-0.69314718f, a.t / a.s, logs);
     if (out.stats) *(float2*)(out.stats + 2 * (size_t)r) = make_float2(none ? -INFINITY : a.m, a.s);
   }
   if (lane < k) {
     out.top_id[(size_t)r * k + lane] = l.id;
-    out.top_logp[(size_t)r * k + lane] = l.id < 0 ? -INFINITY : fmaf(l.v - a.m, inv_t, -logs);
+    out.top_logp[(size_t)r * k + lane] = l.id < 0 ? -INFINITY : log_prob(l.v, a.m, inv_t, logs);
   }
 }
 

@@ -368,3 +368,35 @@ def test_gradient_over_the_temperatures(env, T, dtype):
                      (2.0 ** -8 if bf16 else 2.0 ** -23) * np.abs(want))
             err = np.abs(got - want)
             assert np.all(err <= bound), (V, np.nanmax(err / bound), int(np.isnan(err).sum()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1.01e-37, 1e-20, 1e-3, 1e12, 1e33, 9.9e36])
+def test_forward_over_the_temperatures(env, T, dtype):
+    """The bounds of check_forward: they are relative to z = x / T.  An id of probability below 2^-126 may count as 0 in
+    the entropy (2^-126 104 V, beside them)."""
+    torch, sara = env
+    rng = np.random.default_rng(32)
+    T = float(np.float32(T))
+    for V, k, shift in ((37, 5, 0), (2051, 3, 1), (50000, 8, 0)):
+        x = spread_rows(rng, T, V, dtype, torch)
+        dx = place(torch, x, torch.bfloat16 if dtype == "bf16" else torch.float32, shift, 0)
+        tok = np.array([3, 1, 5, V // 2, -1])
+        _, out, top = forward(env, dx, tok, T, k)
+        check_forward(x, tok, T, k, out, top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_further_apart_than_the_largest_number(env, dtype):
+    """x - max overflows although z = x / T is ordinary: the log probability is what the definition gives."""
+    torch, sara = env
+    T = float(np.float32(9.9e36))
+    x = np.full((3, 900), -3.3e38)
+    x[:, 7] = 3.3e38
+    x[1, 9:400] = np.linspace(-2e38, 2e38, 391)
+    x[2] = -x[2]
+    x = torch.from_numpy(x).to(torch.bfloat16 if dtype == "bf16" else torch.float32).double().numpy()
+    dx = place(torch, x, torch.bfloat16 if dtype == "bf16" else torch.float32, 0, 0)
+    tok = np.array([0, 2, 7])
+    _, out, top = forward(env, dx, tok, T, 6)
+    check_forward(x, tok, T, 6, out, top)
