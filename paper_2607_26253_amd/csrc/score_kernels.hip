@@ -154,10 +154,11 @@ __device__ __forceinline__ TopList pool_best(const Pool& p, int n, int k) {
   return l;
 }
 
-// fmaxf makes quiet every operand that may be a signalling NaN, an instruction each
+// The largest of three, NaN if any is.  fmaxf would pass over a NaN, but it makes every operand quiet that may be
+// signalling, an instruction each, and the bare maximum loses its other operands to a signalling one.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float m;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+  asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
   return m;
 }
 
@@ -256,6 +257,15 @@ __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__
         for (int q = 0; q < N; ++q) f[u][q] = -INFINITY;
 #pragma unroll
       for (int q = 0; q < N; q += 2) all = max3(all, f[u][q], f[u][q + 1]);
+    }
+    if (all != all) {                                  // the largest of the numbers
+      all = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u >= n) break;
+#pragma unroll
+        for (int q = 0; q < N; ++q) all = f[u][q] > all ? f[u][q] : all;
+      }
     }
     if (all > a.m) rescale(a, all, c);
 #pragma unroll

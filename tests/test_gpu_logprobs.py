@@ -400,3 +400,27 @@ def test_logits_further_apart_than_the_largest_number(env, dtype):
     tok = np.array([0, 2, 7])
     _, out, top = forward(env, dx, tok, T, 6)
     check_forward(x, tok, T, 6, out, top)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [700, 40000])
+def test_a_signalling_nan_hides_no_other_id(env, V, dtype):
+    """NaN of every kind (quiet and signalling, of both signs) beside the row's best logits: the row is NaN, the top ids
+    are the best of its numbers, and its largest logit is one of them."""
+    torch, sara = env
+    rng = np.random.default_rng(33)
+    x = np.clip(rng.standard_normal((8, V)), -4, 4)
+    best = [rng.permutation(V // 8 - 1)[:6] * 8 for _ in x]
+    for r, at in enumerate(best):
+        x[r, at] = 9.0 + np.arange(6)
+    td, kinds = (torch.bfloat16, [0x7F81, -0x7F, 0x7FC0, -0x40]) if dtype == "bf16" else (torch.float32, [0x7F800001, -0x7FFFFF, 0x7FC00000, -1])
+    dx = torch.tensor(x).to(td).cuda()
+    bits = dx.view(torch.int16 if dtype == "bf16" else torch.int32)
+    for r, at in enumerate(best):
+        bits[r, torch.tensor(at + 1 + r % 7)] = kinds[r % 4]     # close by each of the best
+    assert bool((dx.isnan().sum(1) == 6).all())
+    t, out, top = forward(env, dx, np.zeros(8, np.int32), 1.0, 6)
+    assert bool(out[0].isnan().all()) and bool(out[1].isnan().all())
+    for r, at in enumerate(best):
+        assert top[0][r].tolist() == at[::-1].tolist(), r
+    np.testing.assert_array_equal(out[2][:, 0].cpu().numpy(), 14.0)
