@@ -403,7 +403,8 @@ int sara_kv8_write(const sara_kv8_cache* cache, const void* d_k, int64_t k_row_s
                    int32_t n_seqs, void* stream);
 
 /* Read positions d_start[i] + t of the cache back into rows t of sequence i
- * (0 where there is no page).  Values are exact in both dtypes. */
+ * (0 where there is no page, positions below 0 among them).  Values are exact
+ * in both dtypes. */
 int sara_kv8_read(const sara_kv8_cache* cache, void* d_k, int64_t k_row_stride, int64_t k_head_stride, void* d_v,
                   int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, int32_t n_rows, const int32_t* d_pages,
                   int32_t max_pages, const int32_t* d_start, const int32_t* d_off, int32_t n_seqs, void* stream);

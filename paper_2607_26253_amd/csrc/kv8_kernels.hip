@@ -127,7 +127,7 @@ struct KvRows {   // rows of K and V in the caller's tensors, strides in element
   int64_t k_row, k_head, v_row, v_head;
 };
 
-// A wave per (page, KV head, K or V): which page, or false where there is none.
+// A wave per (page, KV head, K or V): which page, or false where there is none.  A start below 0 begins at a page below 0.
 struct PageUnit {
   int seq, page, head, r0, len, start;   // page: its index in the sequence; rows r0 + t <-> positions start + t
   bool is_v;
@@ -145,7 +145,7 @@ __device__ __forceinline__ bool page_unit(int unit, int hkv, const int32_t* star
   u.r0 = s.r0;
   u.len = s.r1 - s.r0;
   u.start = s.value;
-  if (u.start < 0 || u.len <= 0) return false;
+  if (u.len <= 0) return false;
   u.page = (u.start >> 4) + (item - s.first);
   return u.page <= (int)(((int64_t)u.start + u.len - 1) >> 4);
 }
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(256) void k_kv8_write(sara_kv8_cache c, KvRows src,
   typedef PageLanes<HD> PL;
   PageUnit u;
   if (!page_unit(blockIdx.x * 4 + (threadIdx.x >> 6), c.n_kv_heads, start, off, n_seqs, n_rows, u)) return;
-  if (u.page >= max_pages) return;
+  if (u.start < 0 || u.page >= max_pages) return;
   const int id = pages[(size_t)u.seq * max_pages + u.page];
   if (id < 0 || id >= c.n_pages) return;
   const int lane = threadIdx.x & 63, d0 = 8 * (lane % PL::TPR), row = lane / PL::TPR;
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(256) void k_kv8_read(sara_kv8_cache c, KvRows dst, 
   typedef PageLanes<HD> PL;
   PageUnit u;
   if (!page_unit(blockIdx.x * 4 + (threadIdx.x >> 6), c.n_kv_heads, start, off, n_seqs, n_rows, u)) return;
-  const int id = u.page < max_pages ? pages[(size_t)u.seq * max_pages + u.page] : -1;
+  const int id = u.page >= 0 && u.page < max_pages ? pages[(size_t)u.seq * max_pages + u.page] : -1;
   const bool have = id >= 0 && id < c.n_pages;
   const int lane = threadIdx.x & 63, d0 = 8 * (lane % PL::TPR), row = lane / PL::TPR;
   const size_t block = (size_t)(have ? id : 0) * c.n_kv_heads + u.head;

@@ -474,3 +474,26 @@ def test_refusals(env):
         sara.sara_kv8_attention(q, *dev2.args, dev2.i32(tables2), dev2.i32([5000]), None, torch.empty_like(q),
                                 workspace=torch.empty(1 << 20, dtype=torch.uint8))
     torch.cuda.synchronize()
+
+
+def test_reads_from_below_position_zero(env):
+    """Every row of a read is written: 0 for positions below 0, the cache's values for the rest."""
+    torch, sara = env
+    rng = np.random.default_rng(20)
+    lowest = -2 ** 31
+    for fmt, hkv, hd in (("int8", 2, 128), ("fp8", 3, 64)):
+        dev, tables = filled(env, rng, hkv, hd, fmt, [70, 16, 5, 40, 9])
+        start, n = [-1, -16, -37, -5, lowest], [60, 33, 30, 6, 40]
+        off = offsets(n)
+        got = dev.read(tables, start, off, torch.float32)
+        for c, x in zip(dev.ref, got):
+            for i in range(len(n)):
+                want = np.zeros((n[i], hkv, hd))
+                below = min(n[i], -start[i])
+                want[below:] = c.read(tables[i], 0, n[i] - below)
+                np.testing.assert_array_equal(x[off[i]:off[i + 1]], want)
+        out = [torch.full((5, hkv, hd), 7.0, device="cuda") for _ in range(2)]      # one row a sequence
+        sara.sara_kv8_read(*dev.args, dev.i32(tables), dev.i32([-1, 0, -9, 3, lowest]), None, *out)
+        for c, x in zip(dev.ref, out):
+            want = [np.zeros((hkv, hd)), c.read(tables[1], 0, 1)[0], np.zeros((hkv, hd)), c.read(tables[3], 3, 1)[0], np.zeros((hkv, hd))]
+            np.testing.assert_array_equal(x.double().cpu().numpy(), np.array(want))
