@@ -416,6 +416,8 @@ int sara_kv8_read(const sara_kv8_cache* cache, void* d_k, int64_t k_row_stride, 
  * h / (n_heads / n_kv_heads).
  *     out = sum_j softmax_j(scale * q . k_j) v_j    over the visible positions
  * accumulated in fp32, rounded once to dtype; a row that sees nothing is 0.
+ * A value whose code rounded past the largest finite number may count as the
+ * largest multiple of its page's scale that is finite.
  * max_ctx <= 16 * max_pages: no d_ctx[i] is larger (the rows of one that is
  * are NaN); it sizes the launch, so keep it near the longest.
  * d_ws: workspace of at least the bytes that sara_kv8_attention_workspace

@@ -78,6 +78,20 @@ template <int FMT> __device__ __forceinline__ u32x2 values_bf16(uint32_t w, floa
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
 }
 
+// The first exponent byte whose scale takes some code past the largest finite number, and four codes under such a byte
+// held at the largest multiple of the scale that is finite (b = 255, a page of NaN, leaves none).
+template <int FMT> constexpr int kFirstInf = FMT == SARA_KV8_INT8 ? 249 : 247;
+template <int FMT> __device__ __forceinline__ uint32_t finite_codes(uint32_t w, int b) {
+  const int top = FMT == SARA_KV8_INT8 ? (1 << (255 - b)) - 1 : 8 * (262 - b) - 1;   // below 2^(255 - b), as a code
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 32; i += 8) {
+    const int c = (int)(w << (24 - i)) >> 24;
+    r |= (uint32_t)((FMT == SARA_KV8_INT8 ? min(max(c, -top), top) : (c & 0x80) | min(c & 0x7F, top)) & 255) << i;
+  }
+  return r;
+}
+
 // ---------------------------------------------------------------------------
 // ragged work
 // ---------------------------------------------------------------------------
@@ -683,7 +697,7 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
     }
   }
   const int32_t* table = a.pages + (size_t)seq * a.max_pages;
-  // lane i: page i of a stretch of 64 (16 key blocks), its exponent bytes (0x10000: no page, 0x20000: NaN)
+  // lane i: page i of a stretch of 64 (16 key blocks), its exponent bytes (0x10000: no page, 0x20000: NaN, 0x40000: values may be inf)
   int ids = 0, meta = 0;
   // A wave stages KR token rows of K at a time, all of one page, and the V of one page: pages, exponents and addresses
   // are scalars.  K: lane (token row lane / NKS, 16 dims).  V: lane (8 tokens v_half, 4 dims 4 v_dim).
@@ -700,7 +714,8 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
       ids = have ? id : 0;
       const size_t block = (size_t)ids * hkv + g;
       const int ke = c.k_exp[block], ve = c.v_exp[block];
-      meta = ke | ve << 8 | (have ? 0 : 0x10000) | (ke == 255 || ve == 255 ? 0x20000 : 0);
+      meta = ke | ve << 8 | (have ? 0 : 0x10000) | (ke == 255 || ve == 255 ? 0x20000 : 0) |
+             (max(ke, ve) >= kFirstInf<FMT> ? 0x40000 : 0);
     }
     const int at = 4 * (kb & 15);
     auto page = [&](const void* codes, int pg, int& info) {
@@ -716,22 +731,37 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
 #pragma unroll
     for (int j = 0; j < 8; ++j) vr[j] = *(const uint32_t*)(vp + ((j + 4 * (j >> 2) + 4 * v_half) * HD + 4 * v_dim));
   };
-  // The loaded codes go to LDS in PIECES pieces of about ten instructions, after `settle`.
+  // The loaded codes go to LDS in PIECES pieces of about ten instructions, after `settle`.  A value that rounded past the
+  // largest finite number must not enter LDS as inf: a weight of 0, or a q of 0, would make it NaN for columns that do not
+  // see its key or its dim.
   constexpr int PIECES = 4 * KU + 8;
   float k_scale[KU], v_scale;
   u32x4 w_k, w_v;
   auto settle = [&](int kb) {
+    int large = vm & 0x40000;
+#pragma unroll
+    for (int x = 0; x < KU; ++x) large |= km[x] & 0x40000;
+    const int tokens = (vm & 0x30000) ? 0 : min(ctx - 16 * (p0 + 4 * kb + wave), 16);
+    if ((large ? 0 : tokens) < 16) {                       // one branch for all that is rare (two cost 1.5% of a prompt)
+      if (large) {
+#pragma unroll
+        for (int x = 0; x < KU; ++x)
+          if ((km[x] & 255) >= kFirstInf<FMT>)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) kr[x][q] = finite_codes<FMT>(kr[x][q], km[x] & 255);
+        if ((vm >> 8 & 255) >= kFirstInf<FMT>)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) vr[j] = finite_codes<FMT>(vr[j], vm >> 8 & 255);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vr[j] = j + 4 * (j >> 2) + 4 * v_half < tokens ? vr[j] : 0u;
+    }
 #pragma unroll
     for (int x = 0; x < KU; ++x) {
       // a NaN page (its K or its V) is seen through its keys' scores: a NaN scale, or the code of NaN
       const bool bad = km[x] & 0x20000;
       if (FMT == SARA_KV8_E4M3 && bad) kr[x] = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
       k_scale[x] = bad ? (FMT == SARA_KV8_E4M3 ? 1.f : __uint_as_float(0x7FC00000u)) : ldexpf(1.f, (km[x] & 255) - 127);
-    }
-    const int live_tok = (vm & 0x30000) ? 0 : min(ctx - 16 * (p0 + 4 * kb + wave), 16);
-    if (live_tok < 16) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) vr[j] = j + 4 * (j >> 2) + 4 * v_half < live_tok ? vr[j] : 0u;
     }
     v_scale = (vm & 0x20000) ? 0.f : ldexpf(1.f, (vm >> 8 & 255) - 127);
   };

@@ -497,3 +497,48 @@ def test_reads_from_below_position_zero(env):
         for c, x in zip(dev.ref, out):
             want = [np.zeros((hkv, hd)), c.read(tables[1], 0, 1)[0], np.zeros((hkv, hd)), c.read(tables[3], 3, 1)[0], np.zeros((hkv, hd))]
             np.testing.assert_array_equal(x.double().cpu().numpy(), np.array(want))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_values_past_the_largest_number_reach_only_who_sees_them(env, fmt):
+    """A V element whose code rounds to 2^128 at position 70: queries before it are as ever, those that see it get its
+    share to 1/15 (a code below it in e4m3) of that element; and a K element as large in a dim where every q is 0 changes
+    nothing.  Both kernels."""
+    torch = env[0]
+    rng = np.random.default_rng(24)
+    ctx = [100, 100]
+    dev, tables = filled(env, rng, 1, 128, fmt, ctx)
+    x = [rng.standard_normal((16, 1, 128)) for _ in range(2)]
+    x[1][6, 0, 9] = 3.4e38
+    k, v = (dev.tensor(y, torch.float32) for y in x)
+    assert bool(v.isfinite().all())
+    dev.write(k, v, tables[:1], [64], [0, 16])
+    x[0][6, 0, 9], x[1][6, 0, 9] = -3.4e38, 1.0
+    dev.write(dev.tensor(x[0], torch.float32), dev.tensor(x[1], torch.float32), tables[1:], [64], [0, 16])
+    assert dev.ref[1].read(tables[0], 70, 1)[0, 0, 9] == 2.0 ** 128 == -dev.ref[0].read(tables[1], 70, 1)[0, 0, 9]
+    for nq in ([100, 100], [8, 8]):                                       # tiles of columns; few columns
+        q = dev.tensor(rng.standard_normal((sum(nq), 4, 128)), torch.float32)
+        q[:, :, 9] = 0.0
+        got = attend(dev, q, tables, ctx, offsets(nq))
+        seen = max(0, nq[0] - 30)                                         # the first row that sees position 70
+        check_attention(dev, q[nq[0]:], got[nq[0]:], tables[1:], ctx[1:], offsets(nq[1:]))
+        if seen:
+            early = got[:seen]
+            assert bool(early.isfinite().all())
+            alone = attend(dev, q[:seen].contiguous(), tables[:1], [70], [0, seen])
+            torch.testing.assert_close(early, alone, rtol=1e-5, atol=1e-6)
+        want = R.attention(q[seen:nq[0]].double().cpu().numpy(), *(c.read(tables[0], 0, 100) for c in dev.ref), np.ones(100, bool),
+                           100, 128 ** -0.5)
+        have = got[seen:nq[0]].double().cpu().numpy()
+        assert not np.isnan(have).any()
+        other = np.arange(128) != 9
+        np.testing.assert_allclose(have[..., other], want[..., other], rtol=1e-4, atol=1e-5)
+        np.testing.assert_allclose(have[..., 9], want[..., 9], rtol=1 / 15)
+    for t in (75, 99):                                                    # single tokens
+        q = dev.tensor(rng.standard_normal((2, 4, 128)), torch.float32)
+        q[:, :, 9] = 0.0
+        got = attend(dev, q, tables, [t + 1, t + 1], None)
+        check_attention(dev, q[1:], got[1:], tables[1:], [t + 1], None)
+        want = R.attention(q[:1].double().cpu().numpy(), *(c.read(tables[0], 0, t + 1) for c in dev.ref), np.ones(t + 1, bool), t + 1,
+                           128 ** -0.5)
+        np.testing.assert_allclose(got[:1].double().cpu().numpy(), want, rtol=1e-4, atol=1e-5)
