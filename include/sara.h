@@ -418,8 +418,8 @@ int sara_kv8_read(const sara_kv8_cache* cache, void* d_k, int64_t k_row_stride, 
  * accumulated in fp32, rounded once to dtype; a row that sees nothing is 0.
  * A value whose code rounded past the largest finite number may count as the
  * largest multiple of its page's scale that is finite.
- * max_ctx <= 16 * max_pages: no d_ctx[i] is larger (the rows of one that is
- * are NaN); it sizes the launch, so keep it near the longest.
+ * max_ctx <= 16 * max_pages and 2^30: no d_ctx[i] is larger (the rows of one
+ * that is are NaN); it sizes the launch, so keep it near the longest.
  * d_ws: workspace of at least the bytes that sara_kv8_attention_workspace
  * gives for the same sizes (16-byte aligned; NULL if 0), free for reuse once
  * the stream has passed the call. */

@@ -921,12 +921,15 @@ extern "C" int sara_kv8_read(const sara_kv8_cache* c, void* d_k, int64_t k_row, 
                   n_seqs, stream);
 }
 
+// Longest context of an attention call: the kernels' positions are 32-bit and run a key block past the last.
+static constexpr int32_t kMaxCtx = 1 << 30;
+
 extern "C" int sara_kv8_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads,
                                             int32_t n_seqs, int32_t ragged, int32_t max_ctx, int64_t* bytes) {
   if (!bytes) return einval("null argument");
   if (n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128))
     return einval("n_heads must be a multiple of n_kv_heads, head_dim 64 or 128");
-  if (n_rows < 0 || n_seqs < 0 || max_ctx < 0) return einval("sizes must be >= 0");
+  if (n_rows < 0 || n_seqs < 0 || max_ctx < 0 || max_ctx > kMaxCtx) return einval("sizes must be >= 0, max_ctx <= 2^30");
   const Kv8Split s = kv8_split(n_rows, n_heads, n_kv_heads, head_dim, n_seqs, max_ctx, ragged != 0);
   *bytes = s.part_bytes + s.part_tile_bytes;
   return SARA_OK;
@@ -940,7 +943,8 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
   const std::string bad = kv8_bad(c, dtype, n_rows, d_pages, max_pages, d_ctx, d_off, n_seqs);
   if (!bad.empty()) return einval(bad);
   if (n_heads < 1 || n_heads % c->n_kv_heads) return einval("n_heads must be a multiple of n_kv_heads");
-  if (max_ctx < 0 || max_ctx > (int64_t)max_pages * kBlockTok) return einval("max_ctx must be in [0, 16 * max_pages]");
+  if (max_ctx < 0 || max_ctx > kMaxCtx || max_ctx > (int64_t)max_pages * kBlockTok)
+    return einval("max_ctx must be in [0, 16 * max_pages], at most 2^30");
   if (!(fabsf(scale) <= 3.4e38f)) return einval("scale must be finite");
   if (n_rows == 0 || n_seqs == 0) return SARA_OK;
   if (!d_q || !d_out) return einval("null array");

@@ -124,3 +124,17 @@ def test_calls_refuse_host_tensors_and_other_objects():
             sara.sara_kv8_read(codes, codes, exps, exps, pages, seq, None, bad, bad)
         with pytest.raises(exc):
             sara.sara_kv8_attention(bad, codes, codes, exps, exps, pages, seq, None, bad)
+
+
+def test_contexts_past_the_kernels_positions_are_refused():
+    """Near 2^31 the number of pages overflowed: a call got one split, no workspace and partial results all the same."""
+    need = ctypes.c_int64(-1)
+
+    def workspace(max_ctx):
+        return L.sara_kv8_attention_workspace(2, 128, 1, 12, 1, 0, max_ctx, ctypes.byref(need))
+
+    assert workspace(2 ** 30) == sara.SARA_OK and need.value > 0
+    for c in (2 ** 30 + 1, 2 ** 31 - 16, 2 ** 31 - 15, 2 ** 31 - 1):
+        assert workspace(c) == BAD
+        assert attend(n_rows=1, n_seqs=1, off=None, heads=12, max_pages=2 ** 31 - 1, max_ctx=c, ws=P, ws_bytes=2 ** 40) == BAD
+        assert b"max_ctx" in L.sara_last_error()
