@@ -138,3 +138,14 @@ def test_contexts_past_the_kernels_positions_are_refused():
         assert workspace(c) == BAD
         assert attend(n_rows=1, n_seqs=1, off=None, heads=12, max_pages=2 ** 31 - 1, max_ctx=c, ws=P, ws_bytes=2 ** 40) == BAD
         assert b"max_ctx" in L.sara_last_error()
+
+
+def test_vocabularies_past_the_kernels_ids_are_refused():
+    """The gradient of rows that lie unlike their logits steps by up to 2^27 ids: past 2^31 - 2^27 its id wrapped below 0."""
+    need = ctypes.c_int64(-1)
+    assert L.sara_token_logprobs_workspace(1, 2 ** 30, 0, ctypes.byref(need)) == sara.SARA_OK
+    for V in (2 ** 30 + 1, 2 ** 31 - 2 ** 27 + 1, 2 ** 31 - 1):
+        assert L.sara_token_logprobs_workspace(1, V, 0, ctypes.byref(need)) == BAD
+        assert L.sara_token_logprobs(P, 1, V, 1, V, P, 1.0, 0, P, P, P, None, None, P, 2 ** 40, None) == BAD
+        assert L.sara_token_logprobs_grad(P, 1, V, 1, V, P, 1.0, P, P, P, P, ctypes.c_void_p(8194), V, None) == BAD
+        assert b"vocab" in L.sara_last_error()
