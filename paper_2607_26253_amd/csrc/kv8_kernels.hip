@@ -1057,16 +1057,17 @@ template <typename F> static int kv8_dispatch(const sara_kv8_cache& c, int dtype
   return e == hipSuccess ? SARA_OK : hip_fail(e, "8-bit KV cache launch");
 }
 
-static int64_t page_items(int n_seqs, int n_rows, bool ragged) {
-  return ragged ? (int64_t)n_rows / 16 + 2 * (int64_t)n_seqs : n_seqs;
+// blocks of a write or read: four units of (page, KV head, K or V)
+int64_t kv8_rows_blocks(int n_seqs, int n_rows, bool ragged, int hkv) {
+  const int64_t items = ragged ? (int64_t)n_rows / 16 + 2 * (int64_t)n_seqs : n_seqs;
+  return (items * hkv * 2 + 3) / 4;
 }
 
 int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int dtype, int64_t k_row, int64_t k_head,
                     int64_t v_row, int64_t v_head, int n_rows, const int32_t* pages, int max_pages, const int32_t* start,
                     const int32_t* off, int n_seqs, hipStream_t st) {
   const KvRows rows = {k, v, k_row, k_head, v_row, v_head};
-  const int64_t units = page_items(n_seqs, n_rows, off != nullptr) * c.n_kv_heads * 2;
-  const dim3 grid((uint32_t)((units + 3) / 4));
+  const dim3 grid((uint32_t)kv8_rows_blocks(n_seqs, n_rows, off != nullptr, c.n_kv_heads));
   return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
     if (write)
       hipLaunchKernelGGL((k_kv8_write<hd.value, fmt.value, decltype(t)>), grid, dim3(256), 0, st, c, rows, pages,

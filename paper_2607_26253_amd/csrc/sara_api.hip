@@ -872,6 +872,9 @@ extern "C" int sara_sample_logits_noalloc(const float* d_logits, int32_t n_rows,
                                     eos_id, forced_eos_u32, d_tok, (hipStream_t)stream);
 }
 
+// A launch's grid holds fewer than 2^32 threads along x: blocks of 256 that the calls on an 8-bit cache may have.
+static constexpr int64_t kMaxBlocks = (1 << 24) - 1;
+
 // Arguments that the calls on an 8-bit cache share; "" when they are in order.
 static std::string kv8_bad(const sara_kv8_cache* c, int32_t dtype, int32_t n_rows, const int32_t* d_pages,
                            int32_t max_pages, const int32_t* d_seq, const int32_t* d_off, int32_t n_seqs) {
@@ -901,7 +904,7 @@ static int kv8_rows(bool write, const sara_kv8_cache* c, void* k, int64_t k_row,
   if (!k || !v) return einval("null array");
   if (rows_unaligned(k, k_row, k_head, dtype) || rows_unaligned(v, v_row, v_head, dtype))
     return einval("K and V must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
-  if (((int64_t)n_rows / 16 + 2 * (int64_t)n_seqs) * c->n_kv_heads > (int64_t)1 << 30) return einval("too many rows");
+  if (kv8_rows_blocks(n_seqs, n_rows, d_off != nullptr, c->n_kv_heads) > kMaxBlocks) return einval("too many rows or sequences");
   return launch_kv8_rows(write, *c, k, v, dtype, k_row, k_head, v_row, v_head, n_rows, d_pages, max_pages, d_start, d_off,
                          n_seqs, (hipStream_t)stream);
 }
@@ -952,10 +955,9 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
     return einval("q and out must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
   if ((int64_t)n_rows * n_heads > (int64_t)1 << 30 || (int64_t)n_seqs * std::max(n_heads, 32 * c->n_kv_heads) > (int64_t)1 << 30)
     return einval("too many rows or sequences");
-  int64_t need = 0;
-  const int rc = sara_kv8_attention_workspace(c->n_kv_heads, c->head_dim, n_rows, n_heads, n_seqs, d_off != nullptr, max_ctx,
-                                              &need);
-  if (rc) return rc;
+  const Kv8Split split = kv8_split(n_rows, n_heads, c->n_kv_heads, c->head_dim, n_seqs, max_ctx, d_off != nullptr);
+  if (std::max(split.items, split.tile_items) * c->n_kv_heads > kMaxBlocks) return einval("too many rows or sequences");
+  const int64_t need = split.part_bytes + split.part_tile_bytes;
   if (need > 0 && (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need))
     return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
   return launch_kv8_attention(*c, d_q, dtype, q_row, q_head, n_rows, n_heads, d_pages, max_pages, d_ctx, d_off, n_seqs,

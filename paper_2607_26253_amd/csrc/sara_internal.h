@@ -319,6 +319,7 @@ struct Kv8Split {
   int64_t items, tile_items, part_bytes, part_tile_bytes;
 };
 Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx, bool ragged);
+int64_t kv8_rows_blocks(int n_seqs, int n_rows, bool ragged, int hkv);
 int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int dtype, int64_t k_row, int64_t k_head,
                     int64_t v_row, int64_t v_head, int n_rows, const int32_t* pages, int max_pages, const int32_t* start,
                     const int32_t* off, int n_seqs, hipStream_t st);

@@ -149,3 +149,12 @@ def test_vocabularies_past_the_kernels_ids_are_refused():
         assert L.sara_token_logprobs(P, 1, V, 1, V, P, 1.0, 0, P, P, P, None, None, P, 2 ** 40, None) == BAD
         assert L.sara_token_logprobs_grad(P, 1, V, 1, V, P, 1.0, P, P, P, P, ctypes.c_void_p(8194), V, None) == BAD
         assert b"vocab" in L.sara_last_error()
+
+
+def test_calls_past_a_launch_are_refused():
+    """A grid of 2^24 blocks of 256 threads is refused by the runtime, which is not an argument error any more."""
+    for n_rows, n_seqs, off in ((2 ** 24, 2 ** 24, None), (2 ** 24, 2 ** 24, P), (2 ** 30, 1, P)):
+        assert write(n_rows=n_rows, n_seqs=n_seqs, off=off) == BAD, (n_rows, n_seqs)
+    for n_rows, n_seqs, off in ((2 ** 23, 2 ** 23, None), (2 ** 22, 2 ** 22, P)):
+        assert attend(n_rows=n_rows, n_seqs=n_seqs, off=off) == BAD, (n_rows, n_seqs)
+    assert b"too many" in L.sara_last_error()
