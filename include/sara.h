@@ -436,7 +436,7 @@ int sara_kv8_attention(const sara_kv8_cache* cache, const void* d_q, int64_t q_r
  *
  * What the policy-gradient objective needs of a rollout (section 2: the
  * log probabilities of its tokens under a policy) and its gradient.  For rows
- * r < n_rows of logits d_logits[r * row_stride + id], id < vocab (at most
+ * r < n_rows of logits d_logits[r * row_stride + id], id < vocab (both at most
  * 2^30), in dtype (SARA_BF16 or SARA_F32; any alignment), with
  * z = logit / temperature
  * (1e-37 to 1e37),

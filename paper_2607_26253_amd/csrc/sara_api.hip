@@ -964,12 +964,14 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
                               max_ctx, scale, d_out, o_row, o_head, d_ws, (hipStream_t)stream);
 }
 
-// Largest vocabulary: the kernels' ids are 32-bit and run a grid's stride past the last.
-static constexpr int32_t kMaxVocab = 1 << 30;
+// Largest vocabulary and most rows: the kernels' ids are 32-bit and run a grid's stride past the last, the launches' row
+// numbers a chunk.
+static constexpr int32_t kMaxVocab = 1 << 30, kMaxScoreRows = 1 << 30;
 
 static std::string score_bad(int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab, float temperature) {
   if (dtype != SARA_BF16 && dtype != SARA_F32) return "dtype must be SARA_BF16 or SARA_F32";
-  if (n_rows < 0 || vocab < 1 || vocab > kMaxVocab) return "n_rows must be >= 0 and vocab in [1, 2^30]";
+  if (n_rows < 0 || n_rows > kMaxScoreRows || vocab < 1 || vocab > kMaxVocab)
+    return "n_rows must be in [0, 2^30] and vocab in [1, 2^30]";
   if (row_stride < vocab && n_rows > 1) return "row stride must be at least vocab";
   // 1 / temperature and log2(e) / temperature are fp32 factors of the kernels
   if (!(temperature >= 1e-37f) || !(temperature <= 1e37f)) return "temperature must be in [1e-37, 1e37]";
@@ -978,8 +980,8 @@ static std::string score_bad(int32_t dtype, int64_t row_stride, int32_t n_rows, 
 
 extern "C" int sara_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, int64_t* bytes) {
   if (!bytes) return einval("null argument");
-  if (n_rows < 0 || vocab < 1 || vocab > kMaxVocab || n_top < 0 || n_top > 32)
-    return einval("n_rows >= 0, vocab in [1, 2^30], n_top in [0, 32]");
+  if (n_rows < 0 || n_rows > kMaxScoreRows || vocab < 1 || vocab > kMaxVocab || n_top < 0 || n_top > 32)
+    return einval("n_rows in [0, 2^30], vocab in [1, 2^30], n_top in [0, 32]");
   *bytes = n_rows == 0 ? 0 : score_workspace(n_rows, vocab, n_top);
   return SARA_OK;
 }

@@ -158,3 +158,14 @@ def test_calls_past_a_launch_are_refused():
     for n_rows, n_seqs, off in ((2 ** 23, 2 ** 23, None), (2 ** 22, 2 ** 22, P)):
         assert attend(n_rows=n_rows, n_seqs=n_seqs, off=off) == BAD, (n_rows, n_seqs)
     assert b"too many" in L.sara_last_error()
+
+
+def test_rows_past_the_launches_numbers_are_refused():
+    """The launches go through the rows in chunks of 65,535: the last step of 2^31 - 1 rows wrapped below 0."""
+    need = ctypes.c_int64(-1)
+    assert L.sara_token_logprobs_workspace(2 ** 30, 5, 0, ctypes.byref(need)) == sara.SARA_OK and need.value == 0
+    for n in (2 ** 30 + 1, 2 ** 31 - 1):
+        assert L.sara_token_logprobs_workspace(n, 5, 0, ctypes.byref(need)) == BAD
+        assert L.sara_token_logprobs(P, 1, 5, n, 5, P, 1.0, 0, P, P, P, None, None, None, 0, None) == BAD
+        assert L.sara_token_logprobs_grad(P, 1, 5, n, 5, P, 1.0, P, P, P, P, ctypes.c_void_p(8192), 5, None) == BAD
+        assert b"n_rows" in L.sara_last_error()
