@@ -378,7 +378,8 @@ int sara_gumbel_fast_max_error(double* h_out, void* stream);
  * that of the caller's tensors (SARA_BF16 or SARA_F32): row r, head h begins at
  * r * row_stride + h * head_stride elements, head_dim elements are contiguous.
  * Those pointers and strides must be multiples of 16 bytes, as the codes'
- * pointers.  All calls are enqueued on stream and allocate nothing.  head_dim is
+ * pointers.  Rows and heads that a call writes must not overlap: the larger of
+ * their strides spans the other axis.  All calls are enqueued on stream and allocate nothing.  head_dim is
  * 64 or 128.  Argument errors return SARA_EINVAL and enqueue nothing. */
 enum { SARA_KV8_INT8 = 0, SARA_KV8_E4M3 = 1 };
 typedef struct {

@@ -895,6 +895,13 @@ static bool rows_unaligned(const void* p, int64_t row, int64_t head, int32_t dty
   return ((uintptr_t)p & 15) || (row * E) % 16 || (head * E) % 16;
 }
 
+// rows and heads of an output that share elements: one stride has to span the other axis
+static bool rows_overlap(int64_t row, int64_t head, int32_t n_rows, int32_t n_heads, int32_t dim) {
+  const __int128 r = row < 0 ? -(__int128)row : row, h = head < 0 ? -(__int128)head : head;
+  if (n_rows <= 1 || n_heads <= 1) return (n_rows > 1 && r < dim) || (n_heads > 1 && h < dim);
+  return r < h ? r < dim || h < r * (n_rows - 1) + dim : h < dim || r < h * (n_heads - 1) + dim;
+}
+
 static int kv8_rows(bool write, const sara_kv8_cache* c, void* k, int64_t k_row, int64_t k_head, void* v, int64_t v_row,
                     int64_t v_head, int32_t dtype, int32_t n_rows, const int32_t* d_pages, int32_t max_pages,
                     const int32_t* d_start, const int32_t* d_off, int32_t n_seqs, void* stream) {
@@ -904,6 +911,9 @@ static int kv8_rows(bool write, const sara_kv8_cache* c, void* k, int64_t k_row,
   if (!k || !v) return einval("null array");
   if (rows_unaligned(k, k_row, k_head, dtype) || rows_unaligned(v, v_row, v_head, dtype))
     return einval("K and V must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
+  if (!write && (rows_overlap(k_row, k_head, n_rows, c->n_kv_heads, c->head_dim) ||
+                 rows_overlap(v_row, v_head, n_rows, c->n_kv_heads, c->head_dim)))
+    return einval("rows and heads of K and V to read into must not overlap");
   if (kv8_rows_blocks(n_seqs, n_rows, d_off != nullptr, c->n_kv_heads) > kMaxBlocks) return einval("too many rows or sequences");
   return launch_kv8_rows(write, *c, k, v, dtype, k_row, k_head, v_row, v_head, n_rows, d_pages, max_pages, d_start, d_off,
                          n_seqs, (hipStream_t)stream);
@@ -955,6 +965,7 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
     return einval("q and out must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
   if ((int64_t)n_rows * n_heads > (int64_t)1 << 30 || (int64_t)n_seqs * std::max(n_heads, 32 * c->n_kv_heads) > (int64_t)1 << 30)
     return einval("too many rows or sequences");
+  if (rows_overlap(o_row, o_head, n_rows, n_heads, c->head_dim)) return einval("rows and heads of out must not overlap");
   const Kv8Split split = kv8_split(n_rows, n_heads, c->n_kv_heads, c->head_dim, n_seqs, max_ctx, d_off != nullptr);
   if (std::max(split.items, split.tile_items) * c->n_kv_heads > kMaxBlocks) return einval("too many rows or sequences");
   const int64_t need = split.part_bytes + split.part_tile_bytes;

@@ -542,3 +542,27 @@ def test_values_past_the_largest_number_reach_only_who_sees_them(env, fmt):
         want = R.attention(q[:1].double().cpu().numpy(), *(c.read(tables[0], 0, t + 1) for c in dev.ref), np.ones(t + 1, bool), t + 1,
                            128 ** -0.5)
         np.testing.assert_allclose(got[:1].double().cpu().numpy(), want, rtol=1e-4, atol=1e-5)
+
+
+def test_expanded_outputs_are_refused_and_transposed_ones_are_not(env):
+    torch, sara = env
+    rng = np.random.default_rng(25)
+    dev, tables = filled(env, rng, 2, 128, "int8", [40, 40])
+    pages, ctx, off = dev.i32(tables), dev.i32([40, 40]), dev.i32([0, 40, 80])
+    q = dev.tensor(rng.standard_normal((80, 4, 128)), torch.bfloat16)
+    want = attend(dev, q, tables, [40, 40], [0, 40, 80])
+    one, kv = torch.zeros((1, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((80, 2, 128), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(sara.SaraError):
+        sara.sara_kv8_attention(q, *dev.args, pages, ctx, off, one.expand(80, 4, 128))
+    for bad in (one[:, :2].expand(80, 2, 128), kv[:, :1].expand(80, 2, 128)):
+        for k, v in ((bad, kv), (kv, bad)):
+            with pytest.raises(sara.SaraError):
+                sara.sara_kv8_read(*dev.args, pages, dev.i32([0, 0]), off, k, v)
+    by_head = torch.empty((4, 80, 128), dtype=torch.bfloat16, device="cuda")              # [heads, rows, dim]
+    assert torch.equal(attend(dev, q, tables, [40, 40], [0, 40, 80], out=by_head.transpose(0, 1)), want)
+    k, v = torch.empty((2, 2, 80, 128), dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    sara.sara_kv8_read(*dev.args, pages, dev.i32([0, 0]), off, k, v)
+    np.testing.assert_array_equal(k[40:].double().cpu().numpy(), dev.ref[0].read(tables[1], 0, 40))
+    last = torch.empty((1, 4, 128), dtype=torch.bfloat16, device="cuda")
+    few = attend(dev, q[79:], tables[1:], [40], None, out=last.as_strided((1, 4, 128), (0, 128, 1)))   # one row: any row stride
+    check_attention(dev, q[79:], few, tables[1:], [40], None)

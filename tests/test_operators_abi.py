@@ -169,3 +169,20 @@ def test_rows_past_the_launches_numbers_are_refused():
         assert L.sara_token_logprobs(P, 1, 5, n, 5, P, 1.0, 0, P, P, P, None, None, None, 0, None) == BAD
         assert L.sara_token_logprobs_grad(P, 1, 5, n, 5, P, 1.0, P, P, P, P, ctypes.c_void_p(8192), 5, None) == BAD
         assert b"n_rows" in L.sara_last_error()
+
+
+def test_outputs_that_overlap_are_refused():
+    """Rows and heads that share elements (an expanded tensor's have stride 0) would be written by several blocks at once."""
+    def read(krow=256, khead=128, vrow=256, vhead=128, n_rows=4):
+        return L.sara_kv8_read(cache(), P, krow, khead, P, vrow, vhead, 1, n_rows, P, 4, P, P, 2, None)
+
+    def out(row, head, n_rows=4, heads=4):
+        return L.sara_kv8_attention(cache(), P, 512, 128, P, row, head, 1, n_rows, heads, P, 4, P, P, 2, 64, 1.0, None, 0, None)
+
+    for row, head in ((0, 128), (256, 0), (128, 128), (64, 128), (-128, 128), (136, 128), (256, 64), (128, 256), (248, 128)):
+        assert read(krow=row, khead=head) == BAD and read(vrow=row, vhead=head) == BAD, (row, head)
+        assert b"overlap" in L.sara_last_error()
+    for row, head in ((0, 128), (512, 0), (256, 128), (504, 128), (128, 504), (-256, 128), (128, 128)):
+        assert out(row, head) == BAD, (row, head)
+        assert b"overlap" in L.sara_last_error()
+    assert out(0, 0, n_rows=1, heads=2) == BAD and read(khead=0, n_rows=1) == BAD
