@@ -8,6 +8,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
 
+#include <initializer_list>
 #include <optional>
 #include <sstream>
 #include <string>
@@ -155,6 +156,14 @@ Workspace workspace(PyObject* o, int64_t need, const at::Tensor& like, const Pla
   return w;
 }
 
+// A call that has written to tensors raises their version, so that autograd notices where one was saved for a backward pass.
+int written(int rc, std::initializer_list<PyObject*> outputs) {
+  if (rc == SARA_OK)
+    for (PyObject* o : outputs)
+      if (o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+  return rc;
+}
+
 template <typename F> int without_gil(F&& call) {
   int rc;
   Py_BEGIN_ALLOW_THREADS;
@@ -192,13 +201,14 @@ template <bool WRITE> PyObject* kv8_rows(PyObject*, PyObject* const* a, Py_ssize
     const Seqs s = sequences(a[6], a[7], a[8], rows, at);
     const int32_t n_rows = size32(rows, "rows");
     void* st = at.stream();
-    return without_gil([&] {
+    const int rc = without_gil([&] {
       if (WRITE)
         return sara_kv8_write(&c, rk.p, rk.row, rk.head, rv.p, rv.row, rv.head, type, n_rows, s.pages, s.width, s.seq, s.off,
                               s.n, st);
       return sara_kv8_read(&c, rk.p, rk.row, rk.head, rv.p, rv.row, rv.head, type, n_rows, s.pages, s.width, s.seq, s.off, s.n,
                            st);
     });
+    return WRITE ? written(rc, {a[0], a[1], a[2], a[3]}) : written(rc, {a[4], a[5]});
   });
 }
 
@@ -222,15 +232,15 @@ PyObject* kv8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (max_ctx != (int32_t)max_ctx) value_error("max_ctx must be below 2^31");
     int64_t need = 0;
-    const int rc = sara_kv8_attention_workspace(c.n_kv_heads, c.head_dim, n_rows, heads, s.n, s.off != nullptr, (int32_t)max_ctx,
-                                                &need);
+    int rc = sara_kv8_attention_workspace(c.n_kv_heads, c.head_dim, n_rows, heads, s.n, s.off != nullptr, (int32_t)max_ctx, &need);
     if (rc) return rc;
     const Workspace ws = workspace(a[11], need, q, at);
     void* st = at.stream();
-    return without_gil([&] {
+    rc = without_gil([&] {
       return sara_kv8_attention(&c, rq.p, rq.row, rq.head, ro.p, ro.row, ro.head, type, n_rows, heads, s.pages, s.width, s.seq,
                                 s.off, s.n, (int32_t)max_ctx, scale, ws.p, ws.bytes, st);
     });
+    return written(rc, {a[5]});
   });
 }
 
@@ -257,7 +267,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const float temp = number(a[7]);
     int64_t need = 0;
-    const int rc = sara_token_logprobs_workspace(rows, V, k, &need);
+    int rc = sara_token_logprobs_workspace(rows, V, k, &need);
     if (rc) return rc;
     const int32_t* tok = per_row<int32_t>(a[1], rows, at::kInt, at, "tokens");
     float* logp = per_row<float>(a[2], rows, at::kFloat, at, "logp");
@@ -267,10 +277,11 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float* lp = per_row<float>(a[6], (int64_t)rows * k, at::kFloat, at, "top logp");
     const Workspace ws = workspace(a[8], need, x, at);
     void* st = at.stream();
-    return without_gil([&] {
+    rc = without_gil([&] {
       return sara_token_logprobs(x.data_ptr(), type, x.stride(0), rows, V, tok, temp, k, logp, ent, stats, id, lp, ws.p, ws.bytes,
                                  st);
     });
+    return written(rc, {a[2], a[3], a[4], a[5], a[6]});
   });
 }
 
@@ -292,10 +303,11 @@ PyObject* token_logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float* h = per_row<float>(a[5], rows, at::kFloat, at, "g_entropy");
     const float temp = number(a[7]);
     void* st = at.stream();
-    return without_gil([&] {
+    const int rc = without_gil([&] {
       return sara_token_logprobs_grad(x.data_ptr(), type, x.stride(0), rows, V, tok, temp, stats, ent, g, h, y.data_ptr(),
                                       y.stride(0), st);
     });
+    return written(rc, {a[6]});
   });
 }
 

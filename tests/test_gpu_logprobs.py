@@ -424,3 +424,40 @@ def test_a_signalling_nan_hides_no_other_id(env, V, dtype):
     for r, at in enumerate(best):
         assert top[0][r].tolist() == at[::-1].tolist(), r
     np.testing.assert_array_equal(out[2][:, 0].cpu().numpy(), 14.0)
+
+
+def test_autograd_notices_what_a_call_writes(env):
+    """Every output's version rises, no input's; a backward pass that needs logits which the gradient has replaced raises;
+    tensors of inference mode, which have no version, serve as ever."""
+    torch, sara = env
+    w = torch.randn((3, 500), device="cuda", requires_grad=True)
+    logits = w * 2.0
+    loss = (logits * logits).sum()                          # saves the logits
+    x, tok = logits.detach(), torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda")
+    out = [torch.empty(s, device="cuda") for s in (3, 3, (3, 2))]
+    top = [torch.empty((3, 4), dtype=torch.int32, device="cuda"), torch.empty((3, 4), device="cuda")]
+    g = torch.ones(3, device="cuda")
+
+    def risen(call, written, read):
+        before = [t._version for t in written + read]
+        call()
+        after = [t._version for t in written + read]
+        assert [b > a for a, b in zip(before, after)] == [True] * len(written) + [False] * len(read)
+
+    risen(lambda: sara.sara_token_logprobs(x, tok, *out, *top), out + top, [x, tok])
+    risen(lambda: sara.sara_token_logprobs_grad(x, tok, out[2], out[1], g, g, x), [x], out + [tok, g])
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    hkv, hd = 2, 64
+    codes = [torch.zeros((4, hkv, 16, hd), dtype=torch.int8, device="cuda") for _ in range(2)]
+    exps = [torch.zeros((4, hkv), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    k, v, q, o = (torch.randn((1, h, hd), device="cuda") for h in (hkv, hkv, 4, 4))
+    pages, one, zero = (torch.tensor(a, dtype=torch.int32, device="cuda") for a in ([[0, 1]], [1], [0]))
+    off = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    risen(lambda: sara.sara_kv8_write(*codes, *exps, k, v, pages, zero), codes + exps, [k, v, pages])
+    risen(lambda: sara.sara_kv8_read(*codes, *exps, pages, zero, off, k, v), [k, v], codes + exps)
+    risen(lambda: sara.sara_kv8_attention(q, *codes, *exps, pages, one, None, o), [o], codes + exps + [q])
+    with torch.inference_mode():
+        kept = torch.empty(3, device="cuda")
+    sara.sara_token_logprobs(w.detach(), tok, kept)
+    torch.testing.assert_close(kept, torch.log_softmax(w.detach(), -1)[torch.arange(3), [1, 2, 3]], rtol=0, atol=1e-5)
