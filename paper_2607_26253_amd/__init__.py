@@ -411,10 +411,13 @@ _ops = _Operators()
 
 
 def _operator(name, entry, stream, args):
-    """One call on the current stream of the tensors' device, or on the given one."""
+    """One call on the current stream of the tensors' device, or on the given one of that device."""
     if stream is None:
         rc = entry(*args)
     else:
+        device = getattr(args[0], "device", stream.device)
+        if device != stream.device and device.type == "cuda":
+            raise ValueError(f"{name}: the stream is on {stream.device}, the tensors are on {device}")
         with _ops.on(stream):
             rc = entry(*args)
     if rc:

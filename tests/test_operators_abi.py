@@ -186,3 +186,21 @@ def test_outputs_that_overlap_are_refused():
         assert out(row, head) == BAD, (row, head)
         assert b"overlap" in L.sara_last_error()
     assert out(0, 0, n_rows=1, heads=2) == BAD and read(khead=0, n_rows=1) == BAD
+
+
+def test_a_stream_of_another_device_is_refused():
+    """The call would go to the tensors' device all the same, to its current stream."""
+    import torch
+
+    class On:
+        def __init__(self, index):
+            self.device = torch.device("cuda", index)
+
+    x = On(0)
+    for call in (lambda s: sara.sara_token_logprobs(x, None, stream=s),
+                 lambda s: sara.sara_token_logprobs_grad(x, None, None, None, None, None, None, stream=s),
+                 lambda s: sara.sara_kv8_write(x, *[None] * 7, stream=s),
+                 lambda s: sara.sara_kv8_read(x, *[None] * 8, stream=s),
+                 lambda s: sara.sara_kv8_attention(None, x, *[None] * 7, stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            call(On(1))
