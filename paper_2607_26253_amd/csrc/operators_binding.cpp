@@ -93,6 +93,9 @@ sara_kv8_cache kv8_cache(PyObject* const* a, const Place& at) {
                         type == at::kChar ? SARA_KV8_INT8 : SARA_KV8_E4M3};
 }
 
+// the stride of an axis; of one that holds a single element torch's may be anything
+int64_t stride_of(const at::Tensor& t, int64_t axis, int64_t single) { return t.size(axis) > 1 ? t.stride(axis) : single; }
+
 // a [rows, heads, dim] tensor whose last dimension is contiguous
 struct Rows { void* p; int64_t row, head; };
 Rows rows3(const at::Tensor& t, int64_t rows, int64_t heads, int64_t dim, const Place& at, const char* what) {
@@ -103,7 +106,7 @@ Rows rows3(const at::Tensor& t, int64_t rows, int64_t heads, int64_t dim, const 
   }
   at.check(t, what);
   if (t.stride(2) != 1 && t.numel()) value_error(std::string(what) + " must have a contiguous last dimension");
-  return Rows{t.data_ptr(), t.stride(0), t.stride(1)};
+  return Rows{t.data_ptr(), stride_of(t, 0, 0), stride_of(t, 1, 0)};
 }
 
 // a page table and its per-sequence arrays
@@ -246,7 +249,7 @@ PyObject* kv8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // [rows, vocab] with contiguous rows
 void check_logits(const at::Tensor& t, const Place& at, const char* what) {
-  if (t.dim() != 2 || (t.stride(1) != 1 && t.numel())) value_error(std::string(what) + " must be [rows, vocab] with contiguous rows");
+  if (t.dim() != 2 || (stride_of(t, 1, 1) != 1 && t.numel())) value_error(std::string(what) + " must be [rows, vocab] with contiguous rows");
   at.check(t, what);
 }
 
@@ -278,7 +281,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Workspace ws = workspace(a[8], need, x, at);
     void* st = at.stream();
     rc = without_gil([&] {
-      return sara_token_logprobs(x.data_ptr(), type, x.stride(0), rows, V, tok, temp, k, logp, ent, stats, id, lp, ws.p, ws.bytes,
+      return sara_token_logprobs(x.data_ptr(), type, stride_of(x, 0, V), rows, V, tok, temp, k, logp, ent, stats, id, lp, ws.p, ws.bytes,
                                  st);
     });
     return written(rc, {a[2], a[3], a[4], a[5], a[6]});
@@ -304,8 +307,8 @@ PyObject* token_logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float temp = number(a[7]);
     void* st = at.stream();
     const int rc = without_gil([&] {
-      return sara_token_logprobs_grad(x.data_ptr(), type, x.stride(0), rows, V, tok, temp, stats, ent, g, h, y.data_ptr(),
-                                      y.stride(0), st);
+      return sara_token_logprobs_grad(x.data_ptr(), type, stride_of(x, 0, V), rows, V, tok, temp, stats, ent, g, h, y.data_ptr(),
+                                      stride_of(y, 0, V), st);
     });
     return written(rc, {a[6]});
   });

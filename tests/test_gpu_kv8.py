@@ -566,3 +566,20 @@ def test_expanded_outputs_are_refused_and_transposed_ones_are_not(env):
     last = torch.empty((1, 4, 128), dtype=torch.bfloat16, device="cuda")
     few = attend(dev, q[79:], tables[1:], [40], None, out=last.as_strided((1, 4, 128), (0, 128, 1)))   # one row: any row stride
     check_attention(dev, q[79:], few, tables[1:], [40], None)
+
+
+def test_the_stride_of_a_single_row_or_head_does_not_matter(env):
+    """One row of a buffer whose rows are 8 bytes off 16, and one KV head likewise: the strides are never followed."""
+    torch, sara = env
+    rng = np.random.default_rng(26)
+    dev, tables = filled(env, rng, 1, 128, "int8", [50])
+    buf = dev.tensor(rng.standard_normal((4, 6 * 128 + 4)), torch.bfloat16)
+    q = buf[:, :6 * 128].unflatten(1, (6, 128))[:1]
+    assert q.stride(0) % 8
+    got = attend(dev, q, tables, [50], None, out=torch.empty_like(buf)[:, :6 * 128].unflatten(1, (6, 128))[:1])
+    check_attention(dev, q, got, tables, [50], None)
+    k = buf.as_strided((6, 1, 128), (128, 132, 1))
+    back = torch.empty((2, 6, 128), dtype=torch.bfloat16, device="cuda").as_strided((2, 6, 1, 128), (768, 128, 132, 1))
+    dev.write(k, k, tables, [44], [0, 6])
+    sara.sara_kv8_read(*dev.args, dev.i32(tables), dev.i32([44]), dev.i32([0, 6]), back[0], back[1])
+    np.testing.assert_array_equal(back[1].double().cpu().numpy(), dev.ref[1].read(tables[0], 44, 6))

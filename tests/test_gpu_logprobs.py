@@ -461,3 +461,20 @@ def test_autograd_notices_what_a_call_writes(env):
         kept = torch.empty(3, device="cuda")
     sara.sara_token_logprobs(w.detach(), tok, kept)
     torch.testing.assert_close(kept, torch.log_softmax(w.detach(), -1)[torch.arange(3), [1, 2, 3]], rtol=0, atol=1e-5)
+
+
+def test_strides_of_single_rows_and_ids_do_not_matter(env):
+    torch, sara = env
+    x = torch.randn(700, device="cuda")
+    tok, one = torch.tensor([3], dtype=torch.int32, device="cuda"), torch.ones(1, device="cuda")
+    logp, stats = torch.empty(1, device="cuda"), torch.empty((1, 2), device="cuda")
+    row = x.as_strided((1, 700), (5, 1))
+    sara.sara_token_logprobs(row, tok, logp, None, stats)
+    torch.testing.assert_close(logp[0], torch.log_softmax(x, 0)[3], rtol=0, atol=1e-5)
+    want = torch.empty_like(row)
+    sara.sara_token_logprobs_grad(row, tok, stats, None, one, None, want)
+    sara.sara_token_logprobs_grad(row, tok, stats, None, one, None, x.as_strided((1, 700), (9, 1)))       # in place
+    assert torch.equal(x, want[0])
+    ids, out = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.empty(4, device="cuda")
+    sara.sara_token_logprobs(torch.randn(4, device="cuda").as_strided((4, 1), (1, 7)), ids, out)          # a vocabulary of one
+    assert out.tolist() == [0.0] * 4
