@@ -1,8 +1,11 @@
 """Compile libsara.so (HIP, gfx950) with hipcc and the operators' Python calls
-(_operators.so, C++ against torch's headers) with g++, in-tree."""
+(_operators.so, C++ against torch's headers) with g++, in-tree.  Without torch
+only the library is built."""
+import importlib.util
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
@@ -49,7 +52,11 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, OUT)
-    build_operators()
+    if importlib.util.find_spec("torch"):
+        build_operators()
+    else:
+        print(f"torch is not installed: {os.path.basename(OPERATORS)} (the operators on torch tensors) is not built",
+              file=sys.stderr)
     return OUT
 
 

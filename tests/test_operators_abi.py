@@ -204,3 +204,26 @@ def test_a_stream_of_another_device_is_refused():
                  lambda s: sara.sara_kv8_attention(None, x, *[None] * 7, stream=s)):
         with pytest.raises(ValueError, match="stream"):
             call(On(1))
+
+
+@pytest.mark.parametrize("torch_there", [True, False])
+def test_the_library_builds_without_torch(tmp_path, monkeypatch, capsys, torch_there):
+    """The compiler is replaced by one that writes its output file: which outputs there are is what is looked at."""
+    from paper_2607_26253_amd import build as B
+
+    def compiler(cmd, **kw):
+        with open(cmd[cmd.index("-o") + 1], "w") as f:
+            f.write(cmd[0])
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+
+    monkeypatch.setattr(B, "HERE", str(tmp_path))
+    monkeypatch.setattr(B, "OUT", str(tmp_path / "libsara.so"))
+    monkeypatch.setattr(B, "OPERATORS", str(tmp_path / "_operators.so"))
+    monkeypatch.setattr(B, "hipcc", lambda: "hipcc")
+    monkeypatch.setattr(B.subprocess, "run", compiler)
+    if not torch_there:
+        monkeypatch.setitem(sys.modules, "torch", None)
+    assert B.build() == str(tmp_path / "libsara.so")
+    assert (tmp_path / "libsara.so").exists()
+    assert (tmp_path / "_operators.so").exists() == torch_there
+    assert ("_operators.so" in capsys.readouterr().err) != torch_there
