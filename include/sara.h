@@ -364,8 +364,10 @@ int sara_gumbel_fast_max_error(double* h_out, void* stream);
  * a power of two, serves its 16 x head_dim elements:
  *     value = code * 2^(b - 127),   b the exponent byte;  b = 255: NaN
  * with codes int8 (-127..127) or fp8 e4m3 (the OCP format, up to 448).  Every
- * value is exact in bf16 and fp32 (rounding up to a code may pass the largest
- * finite number: inf).  The caller owns all memory: pages are
+ * value is exact in fp32 and in bf16, but for the two ends of the range: e4m3
+ * pages of b = 1 or 2 hold values below bf16's smallest step, 2^-133 (rounded
+ * to nearest there), and rounding up to a code may pass the largest finite
+ * number (inf).  The caller owns all memory: pages are
  * handed out by page tables d_pages [n_seqs][max_pages] (int32): position p
  * of sequence i lies in page d_pages[i][p / 16], token p % 16.  Sequences may
  * share pages that no call writes.  A page id outside [0, n_pages), -1 for
@@ -404,8 +406,7 @@ int sara_kv8_write(const sara_kv8_cache* cache, const void* d_k, int64_t k_row_s
                    int32_t n_seqs, void* stream);
 
 /* Read positions d_start[i] + t of the cache back into rows t of sequence i
- * (0 where there is no page, positions below 0 among them).  Values are exact
- * in both dtypes. */
+ * (0 where there is no page, positions below 0 among them). */
 int sara_kv8_read(const sara_kv8_cache* cache, void* d_k, int64_t k_row_stride, int64_t k_head_stride, void* d_v,
                   int64_t v_row_stride, int64_t v_head_stride, int32_t dtype, int32_t n_rows, const int32_t* d_pages,
                   int32_t max_pages, const int32_t* d_start, const int32_t* d_off, int32_t n_seqs, void* stream);

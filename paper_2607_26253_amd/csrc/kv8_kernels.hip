@@ -3,7 +3,7 @@
 // A page holds 16 tokens of one sequence: codes k, v [page][KV head][16][HD], one byte each (int8, or
 // fp8 e4m3), and for each page and KV head two exponent bytes: value = code 2^(b - 127), b = 255 is NaN.
 // A power of two as scale makes x / scale exact, so a code is the one rounding between a value and its
-// cached form, a value is exact in bf16, and a page whose scale grows (a token larger than its others
+// cached form, a value is exact in bf16 (but for e4m3 at b = 1 or 2, below bf16's 2^-133), and a page whose scale grows (a token larger than its others
 // is appended) re-rounds its codes by a shift: it ends as if written at once, but for codes that the
 // shift leaves halfway.  Against amax / 127 it costs int8 up to one bit and e4m3 nothing.
 #include <math.h>
@@ -66,7 +66,7 @@ template <int FMT> __device__ __forceinline__ u32x2 codes_bf16(uint32_t w) {
                __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
 }
 
-// four codes times a power of two as bf16, exactly
+// four codes times a power of two as bf16, exactly but for what bf16 does not hold (values below 2^-133, inf)
 template <int FMT> __device__ __forceinline__ u32x2 values_bf16(uint32_t w, float scale) {
   if (FMT == SARA_KV8_INT8) {
     float f[4];

@@ -583,3 +583,24 @@ def test_the_stride_of_a_single_row_or_head_does_not_matter(env):
     dev.write(k, k, tables, [44], [0, 6])
     sara.sara_kv8_read(*dev.args, dev.i32(tables), dev.i32([44]), dev.i32([0, 6]), back[0], back[1])
     np.testing.assert_array_equal(back[1].double().cpu().numpy(), dev.ref[1].read(tables[0], 44, 6))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_the_smallest_values_read_as_bf16(env, fmt):
+    """Pages of the three smallest scales: exact in fp32, to the nearest bf16 (steps of 2^-133, ties to even) in bf16."""
+    torch = env[0]
+    dev = Dev(env, 6, 1, 128, fmt)
+    x = np.arange(48 * 128).reshape(48, 1, 128) % 901 * 2.0 ** -135
+    x[::2] *= -1
+    x[::16, 0, 5] = R.TOP[fmt] * 2.0 ** (np.arange(3) - 126)                # b = 1, 2, 3
+    k = dev.tensor(x, torch.float32)
+    dev.write(k, -k, np.array([[0, 1, 2]]), [0], [0, 48])
+    assert dev.exp[0][:3, 0].tolist() == [1, 2, 3]
+    dev.check(np.array([[0, 1, 2]]), [0], [0, 48], torch.float32)
+    got = dev.read(np.array([[0, 1, 2]]), [0], [0, 48], torch.bfloat16)
+    for c, y in zip(dev.ref, got):
+        want = c.read([0, 1, 2], 0, 48)
+        exact = torch.from_numpy(want.astype(np.float32))
+        assert np.array_equal(exact.double().numpy(), want)
+        np.testing.assert_array_equal(y, exact.to(torch.bfloat16).double().numpy())
+        assert np.array_equal(y[32:], want[32:]) and (fmt == "int8" or not np.array_equal(y[:16], want[:16]))
