@@ -604,3 +604,134 @@ def test_the_smallest_values_read_as_bf16(env, fmt):
         assert np.array_equal(exact.double().numpy(), want)
         np.testing.assert_array_equal(y, exact.to(torch.bfloat16).double().numpy())
         assert np.array_equal(y[32:], want[32:]) and (fmt == "int8" or not np.array_equal(y[:16], want[:16]))
+
+
+# -- long splits, both kernels ------------------------------------------------------
+def check_rows(dev, q, got, tables, ctx, off, scale=None):
+    """check_attention's bound with the reference in fp64 on the device, a head at a time; tables may share pages."""
+    torch, hd, bf16 = dev.torch, dev.hd, q.dtype == dev.torch.bfloat16
+    scale, group = hd ** -0.5 if scale is None else scale, q.shape[1] // dev.hkv
+    off = list(range(len(tables) + 1)) if off is None else off
+    values = [torch.from_numpy(np.where((c.exp == 255)[:, :, None, None], np.nan, c.val)).cuda() for c in dev.ref]
+    for i, table in enumerate(np.asarray(tables)):
+        n, end = off[i + 1] - off[i], max(ctx[i], 0)
+        if n == 0:
+            continue
+        have = torch.from_numpy(np.repeat((table >= 0) & (table < dev.n_pages), 16)[:end]).cuda()
+        page = torch.from_numpy(np.where((table >= 0) & (table < dev.n_pages), table, 0)).cuda()
+        at = torch.arange(end, device="cuda")
+        seen = have[None] & (at[None] <= end - n + torch.arange(n, device="cuda")[:, None])
+        for h in range(q.shape[1]):
+            k, v = (x[page, h // group].reshape(-1, hd)[:end] for x in values)
+            bad = (k.isnan() | v.isnan()).any(1)                         # a key of a NaN page: who sees it is NaN
+            k, v = k.nan_to_num(), v.nan_to_num()
+            qh, out = q[off[i]:off[i + 1], h].double(), got[off[i]:off[i + 1], h].double()
+            s = (qh @ k.T.contiguous() * scale).masked_fill(~seen, -np.inf)
+            p = torch.exp(s - s.amax(1, keepdim=True).nan_to_num(neginf=0.0))
+            want = p @ v / p.sum(1, keepdim=True).clamp(min=1e-300)
+            nan = (seen & bad[None]).any(1)
+            assert torch.equal(out.isnan().all(1), nan) and torch.equal(out.isnan().any(1), nan), (i, h)
+            used = k[have]
+            smax = float((used.abs() @ qh.abs().T.contiguous()).amax()) * abs(scale) * 1.4427 if len(used) else 0.0
+            d = smax * 2.0 ** -22 + 2.0 ** -20 + (2.0 ** -17 if bf16 else 2.0 ** -24)
+            vmax = float(v[have].abs().amax()) if len(used) else 0.0
+            bound = 2 * d * vmax + (2.0 ** -8 if bf16 else 2.0 ** -23) * want.abs()
+            err = (out - want).abs()[~nan]
+            assert bool((err <= bound[~nan]).all()), (i, h, float((err / bound[~nan].clamp(min=1e-300)).amax()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,hd,fmt", [(16, 2, 128, "int8"), (12, 4, 64, "fp8")])
+def test_prompts_longer_than_the_page_ids_in_hand(env, hq, hkv, hd, fmt, dtype):
+    """Tiles of columns in one split each of up to 160 pages: page ids, exponents and the masks of missing pages are taken
+    64 at a time.  Pages are missing on both sides of pages 64 and 128, and at the last one."""
+    torch = env[0]
+    rng = np.random.default_rng([27, hd])
+    nq, ctx = [1300, 1100, 900], [1300, 2550, 1040]
+    dev, tables = filled(env, rng, hkv, hd, fmt, ctx)
+    tables[0, [62, 64]] = -1
+    tables[1, [63, 64, 65, 127, 128, 159]] = -1
+    tables[2, 60:65] = dev.n_pages
+    q = dev.tensor(rng.standard_normal((sum(nq), hq, hd)) * 2, torch.bfloat16 if dtype == "bf16" else torch.float32)
+    got = attend(dev, q, tables, ctx, offsets(nq))
+    check_rows(dev, q, got, tables, ctx, offsets(nq))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_many_long_contexts_read_their_page_ids_again(env, ragged, dtype):
+    """600 (sequence, KV head) pairs leave a row in one split, whose waves take their page ids 32 pairs at a time: contexts
+    on both sides of 256 pages, some missing around it.  The sequences share their pages."""
+    torch = env[0]
+    rng = np.random.default_rng(28)
+    dev, one = filled(env, rng, 2, 64, "int8", [4620])
+    ctx = [int(c) for c in rng.integers(4000, 4620, 300)]
+    ctx[:6] = [4096, 4097, 4112, 4113, 4224, 4619]
+    tables = np.repeat(one, 300, 0)
+    for i in range(0, 300, 3):
+        tables[i, rng.integers(250, 289, 5)] = -1
+    nq = [1 + i % 2 for i in range(300)] if ragged else [1] * 300
+    off = offsets(nq)
+    q = dev.tensor(rng.standard_normal((off[-1], 4, 64)) * 2, torch.bfloat16 if dtype == "bf16" else torch.float32)
+    got = attend(dev, q, tables, ctx, off if ragged else None)
+    check_rows(dev, q, got, tables, ctx, off)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_nan_pages_and_scales_in_both_kernels(env, hd, fmt):
+    """NaN pages of K and of V, page scales 2^40 apart and a scale below 0: single queries, and as many as there are tokens."""
+    torch = env[0]
+    rng = np.random.default_rng([29, hd])
+    ctx = [160, 160, 150]
+    for dtype in (torch.bfloat16, torch.float32):
+        dev, tables = filled(env, rng, 2, hd, fmt, ctx)
+        bad, good = np.ones((1, 2, hd)), np.ones((1, 2, hd))
+        bad[0, 1, 3] = np.inf
+        for i, kv in ((0, (bad, good)), (1, (good, bad))):
+            dev.write(*(dev.tensor(x, torch.float32) for x in kv), tables[i:i + 1], [100], [0, 1])
+        size = np.exp2(rng.integers(-20, 20, 10)).repeat(16)[:150, None, None]
+        dev.write(dev.tensor(rng.standard_normal((150, 2, hd)), torch.float32),
+                  dev.tensor(rng.standard_normal((150, 2, hd)) * size, torch.float32), tables[2:], [0], [0, 150])
+        for scale in (None, -0.2):
+            for end in (99, 112, 150):                                   # before the pages' NaN tokens, at them, past them
+                q = dev.tensor(rng.standard_normal((3, 4, hd)), dtype)
+                check_rows(dev, q, attend(dev, q, tables, [end] * 3, None, scale=scale), tables, [end] * 3, None, scale)
+            q = dev.tensor(rng.standard_normal((sum(ctx), 4, hd)), dtype)
+            got = attend(dev, q, tables, ctx, offsets(ctx), scale=scale)
+            check_rows(dev, q, got, tables, ctx, offsets(ctx), scale)
+            assert bool(got[150, 2:].isnan().all()) and not bool(got[:, :2].isnan().any()) and not bool(got[320:].isnan().any())
+
+
+@pytest.mark.parametrize("size", [2.0 ** -80, 2.0 ** 100])
+def test_small_and_large_values(env, size):
+    """All of V at 1e-24 and at 1e30: weights and page scales meet in bf16 parts, whose range holds them."""
+    torch = env[0]
+    rng = np.random.default_rng(30)
+    for fmt in ("int8", "fp8"):
+        dev = Dev(env, 24, 1, 64, fmt)
+        tables = make_tables(rng, [300], 19, 24)
+        dev.write(dev.tensor(rng.standard_normal((300, 1, 64)), torch.float32),
+                  dev.tensor(rng.standard_normal((300, 1, 64)) * size, torch.float32), tables, [0], [0, 300])
+        for nq in (1, 100):
+            q = dev.tensor(rng.standard_normal((nq, 4, 64)) * 2, torch.float32)
+            check_rows(dev, q, attend(dev, q, tables, [300], [0, nq]), tables, [300], [0, nq])
+
+
+def test_a_sequence_alone_and_among_others(env):
+    """The same bits where the batch cuts its context alike (pages a split follow the number of sequences and max_ctx: here
+    24 either way), and right in a batch that cuts it otherwise."""
+    torch = env[0]
+    rng = np.random.default_rng(31)
+    ctx = [900, 40, 333] + [700] * 120
+    dev, tables = filled(env, rng, 2, 128, "fp8", ctx[:4])
+    tables = np.concatenate([tables[:3], np.repeat(tables[3:], 120, 0)])
+    q = dev.tensor(rng.standard_normal((len(ctx), 12, 128)), torch.bfloat16)
+    few = attend(dev, q[:3], tables[:3], ctx[:3], None, max_ctx=900)
+    check_rows(dev, q[:3], few, tables[:3], ctx[:3], None)
+    for i in range(3):
+        alone = attend(dev, q[i:i + 1], tables[i:i + 1], ctx[i:i + 1], None, max_ctx=900)
+        assert torch.equal(alone[0], few[i]), i
+    many = attend(dev, q.repeat(6, 1, 1), np.tile(tables, (6, 1)), ctx * 6, None, max_ctx=900)   # 738 sequences: one split
+    check_rows(dev, q, many[:len(ctx)], tables, ctx, None)
+    assert torch.equal(many[:len(ctx)], many[-len(ctx):])

@@ -478,3 +478,58 @@ def test_strides_of_single_rows_and_ids_do_not_matter(env):
     ids, out = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.empty(4, device="cuda")
     sara.sara_token_logprobs(torch.randn(4, device="cuda").as_strided((4, 1), (1, 7)), ids, out)          # a vocabulary of one
     assert out.tolist() == [0.0] * 4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_a_grid_is_high(env, dtype):
+    """Rows go to the launches in chunks of 65,535."""
+    torch, sara = env
+    rng = np.random.default_rng(34)
+    n, V, k = 65535 + 700, 23, 3
+    x = rows_of(rng, n, V, dtype, torch)
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    dx = place(torch, x, td, 1, 2)
+    tok = rng.integers(-1, V + 1, n).astype(np.int32)
+    t, out, top = forward(env, dx, tok, 0.8, k)
+    check_forward(x, tok, 0.8, k, out, top)
+    g, h = rng.standard_normal(n).astype(np.float32), (rng.standard_normal(n) * 0.3).astype(np.float32)
+    for shift in (1, 0):
+        dst = place(torch, np.full((n, V), 5.0), td, shift, 2)
+        backward(env, dx, t, out, 0.8, g, h, dst)
+        check_grad(x, tok, 0.8, g.astype(np.float64), h.astype(np.float64), dst, dtype == "bf16")
+
+
+@pytest.mark.parametrize("n,V,k", [(2, 60000, 5), (600, 3000, 4)])
+def test_graph_replay(env, n, V, k):
+    """Log probabilities and gradient captured in a HIP graph (rows in splits with a join, and whole), replayed on other
+    logits with eager calls between the replays."""
+    torch, sara = env
+    x, tok = torch.empty((n, V), dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    f = dict(device="cuda", dtype=torch.float32)
+    outs = [torch.empty(n, **f), torch.empty(n, **f), torch.empty((n, 2), **f), torch.empty((n, k), dtype=torch.int32, device="cuda"),
+            torch.empty((n, k), **f), torch.empty_like(x)]
+    g, h, ws = torch.randn(n, **f), torch.randn(n, **f), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+
+    def step():
+        sara.sara_token_logprobs(x, tok, *outs[:5], temperature=0.7, workspace=ws)
+        sara.sara_token_logprobs_grad(x, tok, outs[2], outs[1], g, h, outs[5], temperature=0.7)
+
+    x.normal_()
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        x.copy_(torch.randn((n, V), device="cuda") * 3)
+        tok.copy_(torch.randint(0, V, (n,), device="cuda"))
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, outs)), i
+        lp = torch.log_softmax(x.double() / 0.7, -1)[torch.arange(n), tok.long()]
+        torch.testing.assert_close(got[0].double(), lp, rtol=2.0 ** -20, atol=2.0 ** -19)
