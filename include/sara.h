@@ -417,6 +417,7 @@ int sara_kv8_read(const sara_kv8_cache* cache, void* d_k, int64_t k_row_stride, 
  * n_heads is a multiple of the cache's KV heads; head h reads KV head
  * h / (n_heads / n_kv_heads).
  *     out = sum_j softmax_j(scale * q . k_j) v_j    over the visible positions
+ * (|scale| at most 2e38)
  * accumulated in fp32, rounded once to dtype; a row that sees nothing is 0.
  * A value whose code rounded past the largest finite number may count as the
  * largest multiple of its page's scale that is finite.

@@ -958,7 +958,8 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
   if (n_heads < 1 || n_heads % c->n_kv_heads) return einval("n_heads must be a multiple of n_kv_heads");
   if (max_ctx < 0 || max_ctx > kMaxCtx || max_ctx > (int64_t)max_pages * kBlockTok)
     return einval("max_ctx must be in [0, 16 * max_pages], at most 2^30");
-  if (!(fabsf(scale) <= 3.4e38f)) return einval("scale must be finite");
+  // scale log2(e) is a fp32 factor of the kernels
+  if (!(fabsf(scale) <= 2e38f)) return einval("scale must be finite, at most 2e38 in magnitude");
   if (n_rows == 0 || n_seqs == 0) return SARA_OK;
   if (!d_q || !d_out) return einval("null array");
   if (rows_unaligned(d_q, q_row, q_head, dtype) || rows_unaligned(d_out, o_row, o_head, dtype))

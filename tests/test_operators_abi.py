@@ -227,3 +227,10 @@ def test_the_library_builds_without_torch(tmp_path, monkeypatch, capsys, torch_t
     assert (tmp_path / "libsara.so").exists()
     assert (tmp_path / "_operators.so").exists() == torch_there
     assert ("_operators.so" in capsys.readouterr().err) != torch_there
+
+
+def test_scales_whose_base_2_form_overflows_are_refused():
+    """scale log2(e) was infinite for these: a score of 0 became NaN."""
+    for s in (2.4e38, -3e38, 3.4e38):
+        assert attend(scale=s) == BAD
+        assert b"scale" in L.sara_last_error()
