@@ -396,7 +396,8 @@ typedef struct {
  *     b = the smallest byte >= 1 with a <= M * 2^(b - 127), M = 127 or 448,
  * or, where the page keeps tokens from before d_start[i], the larger of that
  * and the page's old byte; kept codes are rounded to the new scale if it grew.
- * Codes are rounded to nearest, ties to even.  A NaN or infinite element makes
+ * What a page held past its new rows is not kept.  Codes are rounded to
+ * nearest, ties to even.  A NaN or infinite element makes
  * the page's byte 255 until a write covers the page's first token again.
  * Positions past the page table are dropped, and so are the rows of a sequence
  * with d_start[i] < 0.  No two sequences of a call may write the same page. */
@@ -420,7 +421,8 @@ int sara_kv8_read(const sara_kv8_cache* cache, void* d_k, int64_t k_row_stride, 
  * (|scale| at most 2e38)
  * accumulated in fp32, rounded once to dtype; a row that sees nothing is 0.
  * A value whose code rounded past the largest finite number may count as the
- * largest multiple of its page's scale that is finite.
+ * largest multiple of its page's scale that is finite; a weight times V's scale
+ * below 2^-126 may count as 0.
  * max_ctx <= 16 * max_pages and 2^30: no d_ctx[i] is larger (the rows of one
  * that is are NaN); it sizes the launch, so keep it near the longest.
  * d_ws: workspace of at least the bytes that sara_kv8_attention_workspace
@@ -455,7 +457,8 @@ int sara_kv8_attention(const sara_kv8_cache* cache, const void* d_q, int64_t q_r
  * Any of d_logp, d_entropy, d_stats may be NULL, d_top_* if n_top is 0.  -inf
  * logits are masked ids; a row of nothing else gives log p -inf, entropy 0,
  * stats {-inf, 0}.  A NaN or +inf logit makes the row's outputs NaN (NaN is
- * never among the top ids).  Sums are fp32; one pass over the logits.
+ * never among the top ids).  Sums are fp32, exponentials below 2^-126 count as
+ * 0; one pass over the logits.
  * d_ws: workspace of the bytes that sara_token_logprobs_workspace gives.
  * Enqueued on stream, allocates nothing. */
 int sara_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, int64_t* bytes);

@@ -436,7 +436,7 @@ def sara_kv8_write(k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d
 
 
 def sara_kv8_read(k_cache, v_cache, k_exp, v_exp, d_pages, d_start, d_off, d_k, d_v, stream=None):
-    """Read positions d_start[i] + t back into rows of d_k and d_v."""
+    """Read positions d_start[i] + t back into rows of d_k and d_v (0 where there is no page)."""
     _operator("sara_kv8_read", _ops.kv8_read, stream, (k_cache, v_cache, k_exp, v_exp, d_k, d_v, d_pages, d_start, d_off))
 
 

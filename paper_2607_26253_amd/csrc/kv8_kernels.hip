@@ -404,8 +404,10 @@ template <int HD> struct FewLds {
 //                 (2: 2^-17 of a weight; 3 for fp32 queries), so the product adds no rounding of its own
 // Queries of fp32 enter as 3 bf16 parts.  A column without a visible key gives 0.
 // What bounds it is the pages' memory traffic from some 100 rows on (512 rows at 256-1,700 tokens: 51 us, 5.1 TB/s; 32
-// rows at 3,000-4,600 in splits: 15.5 us, 4.0 TB/s), below that its load round trips (one row at 333: 7.0 us).  Blocks of
-// 8 waves take 6.7 us there, but 22 for the 32 rows' 18.3 with the join.
+// rows at 3,000-4,600 in splits: 15.7 us, 4.0 TB/s), below that its load round trips (one row at 333: 7.1 us).  Blocks of
+// 8 waves take 6.7 us there, but 22 for the 32 rows' 18.2 with the join.
+// A weight times its page's scale is held to bf16's range: below 2^-126 it may count as 0, which matters where all of V is
+// below about 1e-30 (at 1e-24 fp32 queries lose nothing).
 template <int HD, int FMT, typename T>
 __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs& a, FewLds<HD>& lds, int bx, int split) {
   constexpr int NK = HD / 64, NT = HD / 16, DV = HD / 16;   // 16-byte K loads, dim tiles, V dims a lane
@@ -635,12 +637,16 @@ template <int HD> struct TileLds {
 // slots are xor-ed with the dim step so that the 8 threads of a token row write to different banks.  V: 4 dims of 8
 // tokens are transposed in registers; row r of a 32-dim tile is dim 4 (r % 8) + r / 8, which spreads the writes and
 // leaves a lane 16 consecutive dims of the output.
-// What bounds it is VALU issue (about 400 instructions and 32 exponentials a wave and key block beside 48 MFMAs of 32
-// cycles), so both run side by side: the codes of block kb + 1 wait in registers and become bf16 in LDS between the score
+// What bounds it is VALU issue: a wave and key block has 473 vector instructions (e4m3: 349), 32 exponentials among them,
+// which take 60% of the kernel's cycles (51%), beside 48 MFMAs of 32 cycles in 40% (44%).  So both run side by side: the codes of block kb + 1 wait in registers and become bf16 in LDS between the score
 // MFMAs of block kb, their successors load behind them, and the weights of 16 keys are made between the MFMAs of the
-// 16 before.  16 sequences of 256 queries over 4,000 tokens, 16 heads: 226 us (612 TFLOP/s); one prompt of 4,590: 164
-// (525), against 182 with conversion, softmax and MFMAs one after the other.  Blocks of 8 waves convert half as much
-// each and gain nothing (16 x 256: 360 us).
+// 16 before.  16 sequences of 256 queries, the last of 4,000 tokens, 16 heads: 215 us (605 TFLOP/s; e4m3 197); one prompt
+// of 4,590: 166 (520), against 182 with conversion, softmax and MFMAs one after the other.  Blocks of 8 waves over 256
+// columns convert half as much each; they are level on other sizes and lose there (360 us, against 233 of blocks of 4 in
+// that version of the loop).
+// Queries of fp32 have 96 MFMAs (three parts of q, three of a weight) beside 718 vector instructions, and 256 registers: one
+// block a CU, whose one wave a SIMD overlaps little: vector issue 43%, MFMAs 40%.  Three prompts of 1,100-4,590: 408 us,
+// against 218 in bf16.
 template <int HD, int FMT, typename T>
 __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArgs& a, TileLds<HD>& lds, int bx, int n_bx, int split) {
   constexpr int NW = kTileWaves, NKS = HD / 16, NDT = HD / 32;
@@ -1082,8 +1088,10 @@ Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx,
   const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16);
   // Pages a split so that about `blocks` blocks share the work, at least `least`, in steps of `step`, and at most
   // 128 splits a row.  A split costs its block about 4 us before the first pages are there and the join launch 4 us
-  // more: one row at context 333 takes 7.4 us in one split, 5.4 + 2.9 and a launch in three; 32 rows at 3,000-4,600
-  // take 16.9 us in splits of 24 pages, 18.6 of 32, 18.8 of 16.
+  // more: one row at context 333 takes 7.2 us in one split, 8.6 in three.  With the join, by pages a split: 32 rows at
+  // 3,000-4,600 take 19.7 us (16), 18.7 (24, this rule's), 20.0 (32), 18.2 (40); one at 65,537 17.7 (24), 15.9 (32), 16.1
+  // (40, this rule's), 18.6 (64); one at 40,000 13.6 (24, this rule's), 14.1 (32).  Where the rule's 24 pages make more
+  // blocks than fit at once, coarser splits would gain: 4 rows at 40,000 24.5 (24), 20.7 (40); 8 at 16,000 18.6 (24), 16.7 (32).
   auto share = [&](int64_t items, int64_t blocks, int least, int step) {
     const int64_t want = std::min<int64_t>(128, std::max<int64_t>(1, blocks / std::max<int64_t>(1, items * hkv)));
     return (int)std::max<int64_t>(least, ((np + want - 1) / want + step - 1) / step * step);

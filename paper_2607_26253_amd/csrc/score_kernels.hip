@@ -216,8 +216,8 @@ __device__ __forceinline__ void write_row(const ScoreOut& out, int r, RowSum a, 
 // once.  Logits equal to the floor can be too many for that; then waves offer theirs one by one to sorted lists.
 // Offering logits as they come took 30-60 us more for 2,048 bf16 rows x 151,936 ids (k = 8-20), which sum in 105.
 // STREAM: non-temporal loads (see launch_score).
-// Bound by memory from some 100 rows on: 2,048 bf16 rows x 151,936 ids 97 us (6.4 TB/s), 512 fp32 rows with 8 top ids 61
-// (5.1); one row with 5 top ids is two launches of 6.0 and 4.4 us.
+// Bound by memory from some 100 rows on: 2,048 bf16 rows x 151,936 ids 98 us (6.3 TB/s), 512 fp32 rows with 8 top ids 61
+// (5.1); one row with 5 top ids is two launches of 6.4 and 4.5 us.
 template <typename T, int W, bool TOP, bool STREAM>
 __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__ logits, int64_t row_stride, int V,
     const int32_t* __restrict__ tok, float c, float inv_t, int n_top, int splits, float* __restrict__ part, ScoreOut out) {
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(64 * W) void k_token_logprobs(const T* __restrict__
 }
 
 // A wave per row joins its splits (at most 64): sums by lane, top ids as above from the splits' sorted lists.  38 splits
-// with 5 top ids: 4.4 us; 64 rows of 16 with 20: 7.2.
+// with 5 top ids: 4.5 us; 64 rows of 16 with 20: 7.2.
 template <typename T>
 __global__ __launch_bounds__(64) void k_token_logprobs_join(const T* __restrict__ logits, int64_t row_stride, int V,
     const int32_t* __restrict__ tok, float c, float inv_t, int k, int splits, const float* __restrict__ part,

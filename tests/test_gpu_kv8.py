@@ -615,7 +615,8 @@ def check_rows(dev, q, got, tables, ctx, off, scale=None):
     values = [torch.from_numpy(np.where((c.exp == 255)[:, :, None, None], np.nan, c.val)).cuda() for c in dev.ref]
     for i, table in enumerate(np.asarray(tables)):
         n, end = off[i + 1] - off[i], max(ctx[i], 0)
-        if n == 0:
+        if n == 0 or end == 0:
+            assert bool((got[off[i]:off[i + 1]] == 0).all())
             continue
         have = torch.from_numpy(np.repeat((table >= 0) & (table < dev.n_pages), 16)[:end]).cuda()
         page = torch.from_numpy(np.where((table >= 0) & (table < dev.n_pages), table, 0)).cuda()
