@@ -479,6 +479,51 @@ int sara_token_logprobs_grad(const void* d_logits, int32_t dtype, int64_t row_st
                              const float* d_g_logp, const float* d_g_entropy, void* d_grad, int64_t grad_row_stride,
                              void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Token log probabilities from hidden states
+ *
+ * The same of rows whose logits are products with the LM head,
+ *     logit[r][id] = sum_k hidden[r][k] weight[id][k],
+ * summed in fp32 and never stored, so that a policy update keeps neither
+ * [n_rows][vocab] logits nor their gradient.  d_hidden[r * hidden_stride + k]
+ * and d_weight[id * weight_stride + k], k < d_model, are of one dtype (SARA_BF16
+ * or SARA_F32: products at fp32 accuracy either way); 16-byte aligned, rows,
+ * strides (at least d_model) and d_model multiples of 16 bytes.  d_logp,
+ * d_entropy, d_stats, d_tok and temperature are those of sara_token_logprobs;
+ * each of the three outputs may be NULL.  A logit that is not finite (an element
+ * that is not, or a sum past fp32) makes its row's outputs NaN.
+ * d_ws: workspace of at least the bytes that sara_head_logprobs_workspace gives
+ * for the same sizes (grad 0 or 1 for the call below; 16-byte aligned), free for
+ * reuse once the stream has passed the call.  Enqueued on stream, allocates
+ * nothing; results do not depend on what else runs. */
+int sara_head_logprobs_workspace(int32_t dtype, int32_t n_rows, int32_t d_model, int32_t vocab, int32_t grad,
+                                 int32_t weight_grad_dtype, int64_t* bytes);
+int sara_head_logprobs(const void* d_hidden, int64_t hidden_stride, const void* d_weight, int64_t weight_stride,
+                       int32_t dtype, int32_t n_rows, int32_t d_model, int32_t vocab, const int32_t* d_tok, float temperature,
+                       float* d_logp, float* d_entropy, float* d_stats, void* d_ws, int64_t ws_bytes, void* stream);
+
+/* Gradients of sum_r (d_g_logp[r] * logp[r] + d_g_entropy[r] * entropy[r]): with
+ *   D[r][j] = g ([j = tok] - p_j) - h p_j (log p_j + entropy)
+ * formed by pieces of the vocabulary,
+ *   d_grad_hidden = D weight / temperature     [n_rows][d_model], in dtype
+ *   d_grad_weight = D^T hidden / temperature   [vocab][d_model], in
+ *                   weight_grad_dtype: dtype or SARA_F32 (for sums over
+ *                   micro-batches); accumulate != 0 adds to what it holds
+ * summed in fp32 and rounded once.  D enters the products of a bf16 call rounded
+ * to bf16, those of an fp32 weight gradient in two bf16 parts (2^-17 of it), and of
+ * an fp32 call in three.  Either gradient may be NULL, not both; they must not
+ * overlap the inputs.  d_stats and d_entropy are those of sara_head_logprobs on
+ * the same inputs.  d_g_logp or d_g_entropy may be NULL (0); d_entropy may be
+ * NULL if d_g_entropy is.  g counts as 0 where d_tok[r] is outside [0, vocab);
+ * rows whose g and h are 0 take no part and get 0, whatever they hold.  Without
+ * rows d_grad_weight is 0 (or stays as it is). */
+int sara_head_logprobs_grad(const void* d_hidden, int64_t hidden_stride, const void* d_weight, int64_t weight_stride,
+                            int32_t dtype, int32_t n_rows, int32_t d_model, int32_t vocab, const int32_t* d_tok,
+                            float temperature, const float* d_stats, const float* d_entropy, const float* d_g_logp,
+                            const float* d_g_entropy, void* d_grad_hidden, int64_t grad_hidden_stride, void* d_grad_weight,
+                            int64_t grad_weight_stride, int32_t weight_grad_dtype, int32_t accumulate, void* d_ws,
+                            int64_t ws_bytes, void* stream);
+
 /* Per-kernel timing of eager decode steps.  While enabled, every
  * sara_decode_step call (not the graph replays of sara_run) records a HIP
  * event pair around each kernel it launches on the context's stream, waits

@@ -33,6 +33,7 @@ EXPORTED = ["sara_init", "sara_begin_step", "sara_decode_step", "sara_posterior_
             "sara_read_profile", "sara_set_warm_start", "sara_warm_start_update", "sara_poll",
             "sara_kv8_write", "sara_kv8_read", "sara_kv8_attention_workspace", "sara_kv8_attention",
             "sara_token_logprobs_workspace", "sara_token_logprobs", "sara_token_logprobs_grad",
+            "sara_head_logprobs_workspace", "sara_head_logprobs", "sara_head_logprobs_grad",
             "sara_destroy",
             "sara_last_error"]
 
@@ -121,6 +122,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "sara_token_logprobs_workspace": [I32, I32, I32, ctypes.POINTER(I64)],
         "sara_token_logprobs": [P, I32, I64, I32, I32, P, F32, I32, P, P, P, P, P, P, I64, P],
         "sara_token_logprobs_grad": [P, I32, I64, I32, I32, P, F32, P, P, P, P, P, I64, P],
+        "sara_head_logprobs_workspace": [I32, I32, I32, I32, I32, I32, ctypes.POINTER(I64)],
+        "sara_head_logprobs": [P, I64, P, I64, I32, I32, I32, I32, P, F32, P, P, P, P, I64, P],
+        "sara_head_logprobs_grad": [P, I64, P, I64, I32, I32, I32, I32, P, F32, P, P, P, P, P, I64, P, I64, I32, I32, P, I64, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -401,7 +405,7 @@ class _Operators:
             from . import _operators
         except ImportError as e:
             raise ImportError(f"_operators.so is not built or does not load; run `python -m paper_2607_26253_amd.build` ({e})")
-        for f in ("kv8_write", "kv8_read", "kv8_attention", "token_logprobs", "token_logprobs_grad"):
+        for f in ("kv8_write", "kv8_read", "kv8_attention", "token_logprobs", "token_logprobs_grad", "head_logprobs", "head_logprobs_grad"):
             setattr(self, f, getattr(_operators, f))
         self.on = torch.cuda.stream
         return object.__getattribute__(self, name)
@@ -469,3 +473,25 @@ def sara_token_logprobs_grad(d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_
     sara_token_logprobs gave.  d_g_logp or d_g_entropy may be None."""
     _operator("sara_token_logprobs_grad", _ops.token_logprobs_grad, stream,
               (d_logits, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad, temperature))
+
+
+# -- token log probabilities from hidden states ------------------------------------------
+def sara_head_logprobs(d_hidden, d_weight, d_tok, d_logp=None, d_entropy=None, d_stats=None, temperature=1.0, workspace=None,
+                       stream=None):
+    """sara_token_logprobs of the logits d_hidden @ d_weight.T, which are not
+    stored: d_hidden [rows, d_model] and the LM head's weight d_weight [vocab,
+    d_model], both bf16 or both fp32.  Outputs that are None are not written."""
+    _operator("sara_head_logprobs", _ops.head_logprobs, stream,
+              (d_hidden, d_weight, d_tok, d_logp, d_entropy, d_stats, temperature, workspace))
+
+
+def sara_head_logprobs_grad(d_hidden, d_weight, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad_hidden, d_grad_weight,
+                            temperature=1.0, accumulate=False, workspace=None, stream=None):
+    """Gradients of sum(g_logp * logp + g_entropy * entropy) with respect to the
+    hidden states and the weight.  d_stats and d_entropy are what
+    sara_head_logprobs gave; d_g_logp or d_g_entropy may be None, and one of the
+    gradients.  d_grad_weight is of the weight's dtype or fp32; with `accumulate`
+    the gradient is added to what it holds."""
+    _operator("sara_head_logprobs_grad", _ops.head_logprobs_grad, stream,
+              (d_hidden, d_weight, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad_hidden, d_grad_weight, temperature,
+               accumulate, workspace))

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libsara.so")
 OPERATORS = os.path.join(HERE, "_operators.so")
 SOURCES = ["model_kernels.hip", "prefill_kernels.hip", "controller_kernels.hip", "kv8_kernels.hip",
-           "score_kernels.hip", "sara_api.hip"]
+           "score_kernels.hip", "head_kernels.hip", "sara_api.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          # packed fp32 arithmetic is left to no code path (all HIP sources)
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,799 @@
+// Token log probabilities from hidden states and the LM head (gfx950), without logits in memory, and both gradients.
+//
+// x_nv = h_n . W_v is formed tile by tile in fp32 and used where it is:
+//   forward    with z = x / T: per row the running maximum m, s = sum 2^u and t = sum 2^u u, u = (x - m) log2(e) / T;
+//              logp = (x_tok - m) / T - log s, H = log s - log(2) t / s
+//   gradient   D_nv = g ([v = tok] - p) - h p (log p + H) by pieces of the vocabulary, from x formed again;
+//              dH = D W / T and dW = D^T H / T, half of the power of two in 1 / T with D and half with the results: an
+//              accepted temperature takes neither out of the range of fp32
+// 8 N d V operations a training step where 6 would do with the logits kept: 2 against [rows][vocab] written and read.
+#include <float.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "sara_internal.h"
+
+namespace sara {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------------------
+// products of 256 x 256 tiles
+// ---------------------------------------------------------------------------
+// An operand: element (r, c) of part i at p[i part + r stride + c].  fp32 numbers enter as sums of bf16 parts.
+struct Mat { const uint16_t* p; int64_t stride, part; };
+
+// What a row needs for its D: 2^u (A + B u) + [v = tok] g
+struct HeadRow { float m, A, B, g; int32_t tok, on; };
+
+struct HeadTile {
+  Mat a, b;                 // M side and N side of C[m][n] = sum_k a(m, k) b(n, k)
+  int M, N, K;
+  int n_pairs;              // the part pairs whose products are summed, 4 bits each (part of a, part of b << 2), smallest first
+  uint32_t pairs;
+  int steps;                // 32-wide k steps of a split (blockIdx.y)
+  int row0, m_parts;        // stats: row of the call's first, rows of a slice of `parts`
+  int v0;                   // first vocabulary id of the N side
+  float c, inv_t;
+  const int32_t* tok;
+  float* x_tok;
+  float4* parts;            // [tile column][m_parts]: (m, s, t)
+  const HeadRow* rows;
+  uint16_t* d;              // D [part][M, up to a tile][d_stride]
+  int64_t d_stride, d_part;
+  int d_parts;
+  float* slab;              // [split][M][N]
+  void* out;                // weight gradient
+  int64_t out_stride;
+  int out_f32, add;         // add: to what is there
+};
+
+__device__ __attribute__((aligned(16))) const uint32_t kZeroUnit[4] = {0, 0, 0, 0};
+
+enum { kStats, kGradRows, kSlab, kWeight };
+
+constexpr int kTileRing = 4;           // 32-wide k stages of 32 KiB
+struct TileShared {
+  u32x4 ring[kTileRing * 32 * 64];
+  float red[3][4][256];
+  HeadRow rows[256];
+};
+
+// The softmax statistics of a block's tile: per row over its columns below `n_cols`.
+typedef f32x4 TileAcc[4][8];
+
+// One wave's half of the rows (wm) and quarter of the columns (wn): acc[n][m] of lane (row, grp) is row 16 m + row, columns
+// 16 n + 4 grp ..+3.
+__device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, TileShared& lds, int tm0, int tn0, int bn) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
+  const int wm = wave >> 2, wn = wave & 3;
+  const int left = a.N - (tn0 + 64 * wn) - 4 * grp;        // columns of this lane's first quarter and on
+  const bool full = a.N - (tn0 + 64 * wn) >= 64;
+#pragma unroll
+  for (int m = 0; m < 8; ++m) {
+    const int r = 128 * wm + 16 * m + row;
+    const int at = lds.rows[r].tok - tn0 - 64 * wn;        // the row's id, if it is here
+    if (at >= 0 && at < 64 && (at >> 2 & 3) == grp && tm0 + r < a.M) {
+      float x = 0.f;
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x = at >> 4 == n && (at & 3) == q ? acc[n][m][q] : x;
+      a.x_tok[a.row0 + tm0 + r] = x;
+    }
+    float mx = -FLT_MAX, mn = FLT_MAX;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float x = acc[n][m][q];
+        if (!full) x = 16 * n + q < left ? x : NAN;        // neither largest nor smallest
+        mx = fmaxf(mx, x);
+        mn = fminf(mn, x);
+      }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    float s = mn == -INFINITY ? NAN : 0.f, t = 0.f;        // a logit that is not finite makes the row NaN
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float u = (acc[n][m][q] - mx) * a.c;
+        if (!full) u = 16 * n + q < left ? u : -INFINITY;
+        const float e = __builtin_amdgcn_exp2f(u);
+        s += e;
+        t = fmaf(e, fmaxf(u, -FLT_MAX), t);
+      }
+    s += __shfl_xor(s, 16, 64);
+    t += __shfl_xor(t, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    t += __shfl_xor(t, 32, 64);
+    if (grp == 0) { lds.red[0][wn][r] = mx; lds.red[1][wn][r] = s; lds.red[2][wn][r] = t; }
+  }
+  __syncthreads();
+  const int r = threadIdx.x;
+  if (r >= 256 || tm0 + r >= a.M) return;
+  float m = lds.red[0][0][r], s = 0.f, t = 0.f;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) m = fmaxf(m, lds.red[0][w][r]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float u = (lds.red[0][w][r] - m) * a.c, e = __builtin_amdgcn_exp2f(u);
+    s = fmaf(e, lds.red[1][w][r], s);
+    t += fmaf(e * fmaxf(u, -FLT_MAX), lds.red[1][w][r], e * lds.red[2][w][r]);
+  }
+  a.parts[(size_t)bn * a.m_parts + tm0 + r] = make_float4(m, s, t, 0.f);
+}
+
+__device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileShared& lds, int tm0, int tn0) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
+  const int wm = wave >> 2, wn = wave & 3;
+  const int col = tn0 + 64 * wn + 4 * grp;
+#pragma unroll
+  for (int m = 0; m < 8; ++m) {
+    const int r = 128 * wm + 16 * m + row;
+    const HeadRow hr = lds.rows[r];
+    const int at = hr.tok - a.v0 - col;                      // 16 n + q where it is this lane's
+    uint16_t* y = a.d + (int64_t)(tm0 + r) * a.d_stride + col;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      float f[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
+        const float u = __builtin_amdgcn_fmed3f((acc[n][m][q] - hr.m) * a.c, -150.f, 0.f);
+        float e = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A);   // a row that met a NaN has it in A
+        e += at == 16 * n + q ? hr.g : 0.f;
+        f[q] = hr.on && col + 16 * n + q < a.N ? e : 0.f;
+      }
+      for (int p = 0; p < a.d_parts; ++p) {
+        uint32_t w0 = pack_bf16(f[0], f[1]), w1 = pack_bf16(f[2], f[3]);
+        asm("" : "+v"(w0), "+v"(w1));                        // what was rounded is what is subtracted
+        *(uint2*)(y + p * a.d_part + 16 * n) = make_uint2(w0, w1);
+        f[0] -= __uint_as_float(w0 << 16);
+        f[1] -= __uint_as_float(w0 & 0xFFFF0000u);
+        f[2] -= __uint_as_float(w1 << 16);
+        f[3] -= __uint_as_float(w1 & 0xFFFF0000u);
+      }
+    }
+  }
+}
+
+// C[m][n] = sum over part pairs and k of a(m, k) b(n, k), 256 x 256 a block of 8 waves (v_mfma_f32_16x16x32_bf16, 128 x 64 a
+// wave), by the ring and the two groups of waves half a step apart of the tile GEMM of the models.  Operands go to LDS as they
+// lie in memory, 16 bytes a lane:
+//   COL false: a(m, k) is element (m, k).  A stage holds 32 elements of a row; the 16-byte units of a row are
+//              exchanged so that the fragments' reads meet different banks.
+//   COL true:  a(m, k) is element (k, m).  A stage holds 32 rows of 256 elements, and fragments are read transposed
+//              (ds_read_b64_tr_b16); units of 32 bytes are exchanged likewise.
+// Rows past the end repeat the last one and are dropped; k past the end is zero on both sides.
+template <bool ACOL, bool BCOL, int EPI>
+__global__ __launch_bounds__(512, 2) void k_head_tile(HeadTile a) {
+  constexpr int ST = kTileRing, FPW = 4;
+  __shared__ TileShared lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int row = lane & 15, grp = lane >> 4;
+  const int wm = wave >> 2, wn = wave & 3;
+  // each XCD takes a contiguous stretch of an order that walks 4 row tiles by every column tile
+  int bn, bm;
+  {
+    const int nb = (a.N + 255) >> 8, mb = (a.M + 255) >> 8, total = nb * mb;
+    const int x = blockIdx.x & 7, per = total >> 3, rem = total & 7;
+    const int lin = x * per + min(x, rem) + (blockIdx.x >> 3);
+    const int gs = 4 * nb, g = lin / gs, gm = min(4, mb - 4 * g), r = lin - g * gs;
+    bm = 4 * g + r % gm;
+    bn = r / gm;
+  }
+  const int tm0 = 256 * bm, tn0 = 256 * bn;
+  const int k_steps = (a.K + 31) >> 5, s0 = blockIdx.y * a.steps, ns = min(a.steps, k_steps - s0), total = ns * a.n_pairs;
+  if (EPI == kStats && threadIdx.x < 256) {
+    const int tok = tm0 + (int)threadIdx.x < a.M ? a.tok[a.row0 + tm0 + threadIdx.x] : -1;
+    lds.rows[threadIdx.x].tok = tok >= a.v0 && tok < a.v0 + a.N ? tok - a.v0 : -1;
+  }
+  if (EPI == kGradRows && threadIdx.x < 256) lds.rows[threadIdx.x] = a.rows[tm0 + threadIdx.x];
+  // this wave's 4 KiB of a stage, of one operand: where a lane's 16 bytes come from at k = 0
+  const bool is_b = wave >= 4;
+  const Mat mat = is_b ? a.b : a.a;
+  const int64_t k_stride = (is_b ? BCOL : ACOL) ? 32 * mat.stride : 32;
+  const uint16_t* from[FPW];
+  int k_of[FPW];
+#pragma unroll
+  for (int j = 0; j < FPW; ++j) {
+    const int f = (wave & 3) * FPW + j;
+    if (is_b ? BCOL : ACOL) {
+      const int kr = 2 * f + (lane >> 5), u = lane & 31;
+      const int sw = (kr & 3) | (kr >> 3 & 3) << 2;
+      const int at = (is_b ? tn0 : tm0) + 16 * ((u >> 1) ^ sw) + 8 * (u & 1);
+      from[j] = mat.p + kr * mat.stride + min(at, (((is_b ? a.N : a.M) + 7) & ~7) - 8);
+      k_of[j] = kr;
+    } else {
+      const int r = lane >> 2, u = (lane & 3) ^ (r >> 1 & 3) ^ (r >> 3);
+      from[j] = mat.p + (int64_t)min((is_b ? tn0 : tm0) + 16 * f + r, (is_b ? a.N : a.M) - 1) * mat.stride + 8 * u;
+      k_of[j] = 8 * u;
+    }
+  }
+  int i_pair = 0, i_step = 0;                              // the next stage to load
+  auto issue = [&](int slot) {
+    const int pair = a.pairs >> (4 * i_pair) & 15, ks = s0 + i_step;
+    const int64_t off = (is_b ? pair >> 2 : pair & 3) * mat.part + ks * k_stride;
+    const bool tail = 32 * (ks + 1) > a.K;
+#pragma unroll
+    for (int j = 0; j < FPW; ++j) {
+      const uint16_t* p = from[j] + off;
+      if (tail) p = 32 * ks + k_of[j] < a.K ? p : (const uint16_t*)kZeroUnit;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                       (__attribute__((address_space(3))) void*)&lds.ring[(slot * 32 + wave * FPW + j) * 64], 16, 0, 0);
+    }
+    // past the last stage it is loaded again, to a slot that nobody reads, so the count of loads in flight stays exact
+    if (i_pair * ns + i_step + 1 < total && ++i_step == ns) { i_step = 0; ++i_pair; }
+  };
+  auto phase = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // fragment i of 16 rows of an operand: byte addresses in a slot
+  const int sw_row = (row * 4 + (grp ^ (row >> 1 & 3) ^ (row >> 3))) * 16;
+  const int sw_col = (8 * grp + (row >> 2)) * 512 + (row & 3) * 8, sw_xor = ((row >> 2) | grp << 2) * 32;
+  auto fragment = [&](int slot, bool b, bool col, int i) {
+    const char* base = (const char*)lds.ring + (slot * 32 + (b ? 16 : 0)) * 1024;
+    if (!col) return __builtin_bit_cast(bf16x8, *(const u32x4*)(base + sw_row + i * 1024));
+    typedef __attribute__((address_space(3))) s16x4* Lds;
+    const char* p = base + sw_col + ((32 * i) ^ sw_xor);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(const s16x4*)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(const s16x4*)(p + 4 * 512));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  TileAcc acc;
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int m = 0; m < 8; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  __syncthreads();                                         // the rows; no load of the ring is in flight yet
+#pragma unroll
+  for (int s = 0; s < ST - 1; ++s) issue(s);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * FPW) : "memory");   // stage 0 has landed
+  phase();
+  if (wave >= 4) phase();                                  // the second group runs one phase behind
+  for (int s = 0; s < total; ++s) {
+    bf16x8 wf[4], xf[8];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) wf[n] = fragment(s % ST, true, BCOL, 4 * wn + n);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) xf[m] = fragment(s % ST, false, ACOL, 8 * wm + m);
+    issue((s + ST - 1) % ST);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((ST - 2) * FPW) : "memory");   // stage s + 1 has landed
+    phase();
+#pragma unroll
+    for (int m = 0; m < 8; ++m)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[n], xf[m], acc[n][m], 0, 0, 0);
+    phase();
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the repeated loads, before the block gives its LDS back
+  if (wave < 4) phase();
+  if constexpr (EPI == kStats) {
+    tile_stats(acc, a, lds, tm0, tn0, bn + (a.v0 >> 8));
+  } else if constexpr (EPI == kGradRows) {
+    tile_grad(acc, a, lds, tm0, tn0);
+  } else {
+    const int col = tn0 + 64 * wn + 4 * grp;
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {
+      const int r = tm0 + 128 * wm + 16 * m + row;
+      if (r >= a.M) continue;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        if (col + 16 * n >= a.N) continue;                 // N is a multiple of 8
+        f32x4 v = acc[n][m];
+        if (EPI == kWeight) v *= a.inv_t;
+        if (EPI == kSlab || a.out_f32) {
+          f32x4* y = (f32x4*)(EPI == kSlab ? a.slab + ((int64_t)blockIdx.y * a.M + r) * a.N + col + 16 * n
+                                           : (float*)a.out + r * a.out_stride + col + 16 * n);
+          if (a.add) v += *y;
+          *y = v;
+        } else {
+          uint2* y = (uint2*)((uint16_t*)a.out + r * a.out_stride + col + 16 * n);
+          if (a.add) {
+            const uint2 w = *y;
+            v += f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xFFFF0000u)};
+          }
+          *y = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// few rows
+// ---------------------------------------------------------------------------
+struct HeadSum { float m, s, t; };
+__device__ __forceinline__ void head_merge(HeadSum& a, HeadSum b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  const float ua = (a.m - m) * c, ub = (b.m - m) * c;
+  const float ea = __builtin_amdgcn_exp2f(ua), eb = __builtin_amdgcn_exp2f(ub);
+  a.t = fmaf(ea * fmaxf(ua, -FLT_MAX), a.s, ea * a.t) + fmaf(eb * fmaxf(ub, -FLT_MAX), b.s, eb * b.t);
+  a.s = fmaf(ea, a.s, eb * b.s);
+  a.m = m;
+}
+
+// Up to 16 NT rows: W streams past them.  A block of 8 waves takes 128 ids at a time, a wave 16 of them, in 128-byte blocks of
+// k: a lane loads 32 consecutive bytes of an id's row, the hidden states lie in LDS (`chunk` blocks of k at a time).
+// fp32 runs on v_mfma_f32_16x16x4_f32.
+struct HeadFew {
+  const char *h, *w;
+  int64_t h_stride, w_stride;   // bytes
+  int n_rows, units, V;         // units: 16-byte units of a row
+  const int32_t* tok;
+  float c;
+  float* x_tok;
+  float4* parts;                // [block][16 NT]
+};
+constexpr int kFewLds = 65536;
+template <typename T, int NT>
+__global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
+  constexpr int CB = kFewLds / (16 * NT * 128);            // 128-byte blocks of k of a chunk
+  constexpr int DEPTH = 4;
+  __shared__ u32x4 hs[kFewLds / 16];
+  __shared__ HeadSum red[8][16 * NT];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
+  const int blocks = (a.units + 7) >> 3, chunks = (blocks + CB - 1) / CB;
+  int tok[NT];
+  HeadSum sum[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    tok[t] = 16 * t + row < a.n_rows ? a.tok[16 * t + row] : -1;
+    sum[t] = HeadSum{-FLT_MAX, 0.f, 0.f};
+  }
+  auto stage = [&](int chunk) {
+    const int nb = min(CB, blocks - chunk * CB);
+    for (int i = threadIdx.x; i < nb * 16 * NT * 8; i += 512) {
+      const int u = i & 7, r = (i >> 3) % (16 * NT), b = i / (128 * NT);
+      const int unit = 8 * (chunk * CB + b) + u;
+      u32x4 v = {0, 0, 0, 0};
+      if (r < a.n_rows && unit < a.units) v = *(const u32x4*)(a.h + r * a.h_stride + 16 * (int64_t)unit);
+      hs[(b * 16 * NT + r) * 8 + (u ^ (r & 7))] = v;
+    }
+  };
+  if (chunks == 1) {
+    stage(0);
+    __syncthreads();
+  }
+  for (int64_t v0 = 128 * (int64_t)blockIdx.x; v0 < a.V; v0 += 128 * (int64_t)gridDim.x) {
+    const int id = (int)v0 + 16 * wave;
+    const char* w = a.w + min((int64_t)id + row, (int64_t)a.V - 1) * a.w_stride + 32 * grp;
+    f32x4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    u32x4 r[DEPTH][2];
+    auto load = [&](int b, int slot) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const bool in = 8 * b + 2 * grp + s < a.units;
+        r[slot][s] = __builtin_nontemporal_load((const u32x4*)(in ? w + 128 * (int64_t)b + 16 * s : (const char*)kZeroUnit));
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) load(i, i);            // blocks past the end are zeros
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+      if (chunks > 1) {
+        __syncthreads();
+        stage(chunk);
+        __syncthreads();
+      }
+      const int b0 = chunk * CB, nb = min(CB, blocks - b0);
+      for (int b = 0; b < nb; b += DEPTH) {
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+          if (b + i < nb) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                const u32x4 h = hs[((b + i) * 16 * NT + 16 * t + row) * 8 + ((2 * grp + s) ^ (row & 7))];
+                if constexpr (sizeof(T) == 2) {
+                  acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r[i][s]), __builtin_bit_cast(bf16x8, h),
+                                                                   acc[t], 0, 0, 0);
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(r[i][s][e]), __uint_as_float(h[e]), acc[t], 0, 0, 0);
+                }
+              }
+            load(b0 + b + i + DEPTH, i);
+          }
+        }
+      }
+    }
+    // lane (row, grp): ids id + 4 grp ..+3 of rows 16 t + row
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int at = tok[t] - id - 4 * grp, left = a.V - id - 4 * grp;
+      if (at >= 0 && at < 4 && left > at) {
+        float x = acc[t][0];
+#pragma unroll
+        for (int q = 1; q < 4; ++q) x = at == q ? acc[t][q] : x;
+        a.x_tok[16 * t + row] = x;
+      }
+      HeadSum one = {-FLT_MAX, 0.f, 0.f};                  // a logit that is not finite makes the row NaN
+#pragma unroll
+      for (int q = 0; q < 4; ++q) one.m = fmaxf(one.m, q < left ? acc[t][q] : NAN);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float x = acc[t][q], u = q < left ? (x - one.m) * a.c : -INFINITY;
+        const float e = q < left && x == -INFINITY ? NAN : __builtin_amdgcn_exp2f(u);
+        one.s += e;
+        one.t = fmaf(e, fmaxf(u, -FLT_MAX), one.t);
+      }
+      head_merge(sum[t], one, a.c);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+#pragma unroll
+    for (int x = 16; x < 64; x <<= 1)
+      head_merge(sum[t], HeadSum{__shfl_xor(sum[t].m, x, 64), __shfl_xor(sum[t].s, x, 64), __shfl_xor(sum[t].t, x, 64)}, a.c);
+    if (grp == 0) red[wave][16 * t + row] = sum[t];
+  }
+  __syncthreads();
+  if (threadIdx.x < 16 * NT) {
+    HeadSum all = red[0][threadIdx.x];
+    for (int w = 1; w < 8; ++w) head_merge(all, red[w][threadIdx.x], a.c);
+    a.parts[(size_t)blockIdx.x * 16 * NT + threadIdx.x] = make_float4(all.m, all.s, all.t, 0.f);
+  }
+}
+
+// A block joins the slices of RB rows: 256 / RB threads a row.
+template <int RB>
+__global__ __launch_bounds__(256) void k_head_join(const float4* __restrict__ parts, int slices, int m_parts, int row0, int n_rows,
+    int V, const int32_t* __restrict__ tok, const float* __restrict__ x_tok, float c, float inv_t, float* logp, float* entropy,
+    float* stats) {
+  constexpr int TR = 256 / RB;
+  __shared__ HeadSum red[TR][RB];
+  const int ri = threadIdx.x % RB, sl = threadIdx.x / RB, r = blockIdx.x * RB + ri;
+  HeadSum sum = {-FLT_MAX, 0.f, 0.f};
+  if (r < n_rows)
+    for (int i = sl; i < slices; i += TR) {
+      const float4 p = parts[(size_t)i * m_parts + r];
+      head_merge(sum, HeadSum{p.x, p.y, p.z}, c);
+    }
+  red[sl][ri] = sum;
+  for (int half = TR / 2; half > 0; half >>= 1) {
+    __syncthreads();
+    if (sl < half) {
+      HeadSum x = red[sl][ri];
+      head_merge(x, red[sl + half][ri], c);
+      red[sl][ri] = x;
+    }
+  }
+  if (sl != 0 || r >= n_rows) return;
+  const HeadSum x = red[0][ri];
+  const int tk = tok[row0 + r];
+  const float ls = logf(x.s);
+  if (logp) logp[row0 + r] = tk >= 0 && tk < V ? (x_tok[row0 + r] - x.m) * inv_t - ls : 0.f;
+  if (entropy) entropy[row0 + r] = ls - 0.69314718f * (x.t / x.s);
+  if (stats) *(float2*)(stats + 2 * (size_t)(row0 + r)) = make_float2(x.s == x.s ? x.m : NAN, x.s);
+}
+
+// ---------------------------------------------------------------------------
+// operands
+// ---------------------------------------------------------------------------
+// Rows of a matrix as P bf16 parts [part][rows_out][width]: rows past the end, and those of `rows` that are off, are 0.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void k_head_parts(const T* __restrict__ x, int64_t stride, int n_rows, int d,
+    const HeadRow* __restrict__ rows, uint16_t* __restrict__ y, int rows_out, int width) {
+  const int r = blockIdx.x;
+  const bool have = r < n_rows && (!rows || rows[r].on);
+  for (int i = 4 * threadIdx.x; i < width; i += 1024) {
+    float f[4] = {0.f, 0.f, 0.f, 0.f};
+    if (have && i < d) {
+      if constexpr (sizeof(T) == 2) {
+        const uint2 w = *(const uint2*)(x + r * stride + i);
+        f[0] = __uint_as_float(w.x << 16);
+        f[1] = __uint_as_float(w.x & 0xFFFF0000u);
+        f[2] = __uint_as_float(w.y << 16);
+        f[3] = __uint_as_float(w.y & 0xFFFF0000u);
+      } else {
+        const f32x4 w = *(const f32x4*)(x + r * stride + i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) f[q] = w[q];
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      uint32_t w0 = pack_bf16(f[0], f[1]), w1 = pack_bf16(f[2], f[3]);
+      asm("" : "+v"(w0), "+v"(w1));
+      *(uint2*)(y + ((int64_t)p * rows_out + r) * width + i) = make_uint2(w0, w1);
+      f[0] -= __uint_as_float(w0 << 16);
+      f[1] -= __uint_as_float(w0 & 0xFFFF0000u);
+      f[2] -= __uint_as_float(w1 << 16);
+      f[3] -= __uint_as_float(w1 & 0xFFFF0000u);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void k_head_rows(int n_rows, int rows_out, int V, const int32_t* __restrict__ tok,
+    const float* __restrict__ stats, const float* __restrict__ entropy, const float* __restrict__ g_logp,
+    const float* __restrict__ g_ent, float scale, HeadRow* __restrict__ out) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r >= rows_out) return;
+  HeadRow o = {0.f, 0.f, 0.f, 0.f, -1, 0};
+  if (r < n_rows) {
+    const int tk = tok[r];
+    const bool has = tk >= 0 && tk < V;
+    const float m = stats[2 * (size_t)r], s = stats[2 * (size_t)r + 1];
+    const float g = has && g_logp ? g_logp[r] : 0.f, h = g_ent ? g_ent[r] : 0.f;
+    if (!(g == 0.f && h == 0.f))
+      o = HeadRow{m, -scale * (g + (h == 0.f ? 0.f : h * (entropy[r] - logf(s)))) / s, -scale * 0.69314718f * h / s, scale * g,
+                  has ? tk : -1, 1};
+  }
+  out[r] = o;
+}
+
+// dH from the splits' sums
+template <typename T>
+__global__ __launch_bounds__(256) void k_head_sum(const float* __restrict__ slab, int splits, int64_t n, int d,
+    const HeadRow* __restrict__ rows, float inv_t, T* __restrict__ out, int64_t stride) {
+  const int64_t i = 4 * (blockIdx.x * (int64_t)256 + threadIdx.x);
+  if (i >= n) return;
+  const int64_t r = i / d;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (rows[r].on)
+    for (int s = 0; s < splits; ++s) v += *(const f32x4*)(slab + s * n + i);
+  v *= inv_t;
+  T* y = out + r * stride + (i - r * d);
+  if constexpr (sizeof(T) == 2) *(uint2*)y = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+  else *(f32x4*)y = v;
+}
+
+// The weight's gradient of no rows
+__global__ __launch_bounds__(256) void k_head_zero(uint32_t* __restrict__ out, int64_t stride, int words) {
+  for (int i = threadIdx.x; i < words; i += 256) out[blockIdx.x * stride + i] = 0u;
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+constexpr uint32_t kPairs1 = 0;                            // (0, 0)
+constexpr uint32_t kPairs2 = 0x01;                         // a in two parts: (1, 0), (0, 0)
+constexpr uint32_t kPairs3 = 0x041852;                     // (2, 0), (1, 1), (0, 2), (1, 0), (0, 1), (0, 0)
+constexpr int64_t kPieceBytes = 256 << 20;                 // of D, and of the parts of a piece of an fp32 weight
+constexpr int kStatRows = 8192;                            // rows of a launch of the forward tiles
+constexpr int kFewRows = 64;
+constexpr int kCus = 256;
+
+static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool grad) {
+  HeadPlan p = {};
+  const bool f32 = dtype == SARA_F32;
+  const int cols = (V + 255) / 256;
+  auto take = [&](int64_t bytes) { const int64_t at = p.bytes; p.bytes += up(bytes, 256); return at; };
+  p.width = (int)up(d, 8);
+  if (!grad) {
+    p.few = n_rows <= kFewRows;
+    p.x_tok = take(4 * (int64_t)n_rows);
+    if (p.few) {
+      p.nt = n_rows <= 16 ? 1 : n_rows <= 32 ? 2 : 4;
+      p.few_blocks = (int)std::min<int64_t>((V + 127) / 128, 2 * kCus);
+      p.parts = take(16 * (int64_t)16 * p.nt * p.few_blocks);
+      return p;
+    }
+    p.rows_out = (int)up(n_rows, 256);
+    p.parts = take(16 * (int64_t)std::min(p.rows_out, kStatRows) * cols);
+    if (f32) {
+      p.piece = (int)std::min<int64_t>(cols, std::max<int64_t>(1, kPieceBytes / (6 * 256 * (int64_t)p.width)));
+      p.h_parts = take(6 * (int64_t)p.rows_out * p.width);
+      p.w_parts = take(6 * 256 * (int64_t)p.piece * p.width);
+    } else {
+      p.piece = cols;
+    }
+    return p;
+  }
+  p.rows_out = (int)up(n_rows, 256);
+  p.d_parts = f32 ? 3 : weight_f32 ? 2 : 1;
+  const int mb = p.rows_out / 256;
+  int64_t most = kPieceBytes / (512 * (int64_t)p.d_parts * p.rows_out);
+  if (f32) most = std::min(most, kPieceBytes / (6 * 256 * (int64_t)p.width));
+  most = std::min<int64_t>(cols, std::max<int64_t>(1, most));
+  // pieces of about the same size; whole rounds of the chip's compute units where that fits
+  const int64_t even = (cols + (cols + most - 1) / most - 1) / ((cols + most - 1) / most);
+  const int64_t round = up(even * mb, kCus) / mb;
+  p.piece = (int)(round <= most ? round : even);
+  // splits of dH's contraction: a block each a compute unit
+  const int tiles = mb * ((d + 255) / 256);
+  const int k_steps = (std::min(V, 256 * p.piece) + 31) / 32;
+  double best = 0;
+  p.splits = 1;
+  for (int s = 1; s <= 64 && s * 8 <= k_steps; ++s) {
+    const double use = (double)tiles * s / (double)up((int64_t)tiles * s, kCus);
+    if (use > best + 0.02) { best = use; p.splits = s; }
+  }
+  const int steps = (k_steps + p.splits - 1) / p.splits;   // the first piece writes every split
+  p.splits = (k_steps + steps - 1) / steps;
+  p.rows = take(sizeof(HeadRow) * (int64_t)p.rows_out);
+  p.d = take(512 * (int64_t)p.d_parts * p.rows_out * p.piece);
+  p.slab = take(4 * (int64_t)p.splits * n_rows * d);
+  p.h_parts = take(2 * (int64_t)(f32 ? 3 : 1) * p.rows_out * p.width);
+  if (f32) p.w_parts = take(6 * 256 * (int64_t)p.piece * p.width);
+  return p;
+}
+
+static int head_done(const char* what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SARA_OK : hip_fail(e, what);
+}
+
+static dim3 tile_grid(const HeadTile& t) { return dim3(((t.M + 255) / 256) * ((t.N + 255) / 256), (((t.K + 31) / 32) + t.steps - 1) / t.steps); }
+
+int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype, int n_rows, int d, int V,
+                         const int32_t* tok, float temp, float* logp, float* entropy, float* stats, void* ws, hipStream_t st) {
+  const HeadPlan p = head_plan(dtype, n_rows, d, V, 0, false);
+  const float c = (float)(1.4426950408889634 / (double)temp), inv_t = 1.f / temp;
+  float* x_tok = (float*)((char*)ws + p.x_tok);
+  float4* parts = (float4*)((char*)ws + p.parts);
+  if (p.few) {
+    const int E = dtype == SARA_BF16 ? 2 : 4;
+    const HeadFew f = {(const char*)h, (const char*)w, h_stride * E, w_stride * E, n_rows, d * E / 16, V, tok, c, x_tok, parts};
+    auto go = [&](auto k) { hipLaunchKernelGGL(k, dim3(p.few_blocks), dim3(512), 0, st, f); };
+    if (dtype == SARA_BF16) {
+      if (p.nt == 1) go(k_head_few<uint16_t, 1>);
+      else if (p.nt == 2) go(k_head_few<uint16_t, 2>);
+      else go(k_head_few<uint16_t, 4>);
+    } else {
+      if (p.nt == 1) go(k_head_few<float, 1>);
+      else if (p.nt == 2) go(k_head_few<float, 2>);
+      else go(k_head_few<float, 4>);
+    }
+    hipLaunchKernelGGL((k_head_join<1>), dim3(n_rows), dim3(256), 0, st, parts, p.few_blocks, 16 * p.nt, 0, n_rows, V, tok, x_tok, c,
+                       inv_t, logp, entropy, stats);
+    return head_done("head log probabilities launch");
+  }
+  const bool f32 = dtype == SARA_F32;
+  uint16_t *hp = (uint16_t*)((char*)ws + p.h_parts), *wp = (uint16_t*)((char*)ws + p.w_parts);
+  if (f32)
+    hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(p.rows_out), dim3(256), 0, st, (const float*)h, h_stride, n_rows, d, nullptr, hp,
+                       p.rows_out, p.width);
+  const int cols = (V + 255) / 256;
+  for (int row0 = 0; row0 < n_rows; row0 += kStatRows) {
+    const int M = std::min(kStatRows, n_rows - row0);
+    for (int c0 = 0; c0 < cols; c0 += p.piece) {
+      HeadTile t = {};
+      t.v0 = 256 * c0;
+      t.M = M;
+      t.N = std::min(V - t.v0, 256 * p.piece);
+      if (f32) {
+        if (row0 == 0 || p.piece < cols)
+          hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(t.N), dim3(256), 0, st, (const float*)w + t.v0 * w_stride, w_stride, t.N, d,
+                             nullptr, wp, 256 * p.piece, p.width);
+        t.a = Mat{hp + (int64_t)row0 * p.width, p.width, (int64_t)p.rows_out * p.width};
+        t.b = Mat{wp, p.width, 256 * (int64_t)p.piece * p.width};
+        t.K = p.width;
+        t.n_pairs = 6;
+        t.pairs = kPairs3;
+      } else {
+        t.a = Mat{(const uint16_t*)h + row0 * h_stride, h_stride, 0};
+        t.b = Mat{(const uint16_t*)w + t.v0 * w_stride, w_stride, 0};
+        t.K = d;
+        t.n_pairs = 1;
+        t.pairs = kPairs1;
+      }
+      t.steps = (t.K + 31) / 32;
+      t.row0 = row0;
+      t.m_parts = std::min(p.rows_out, kStatRows);
+      t.c = c;
+      t.tok = tok;
+      t.x_tok = x_tok;
+      t.parts = parts;
+      hipLaunchKernelGGL((k_head_tile<false, false, kStats>), tile_grid(t), dim3(512), 0, st, t);
+    }
+    hipLaunchKernelGGL((k_head_join<16>), dim3((M + 15) / 16), dim3(256), 0, st, parts, cols, std::min(p.rows_out, kStatRows), row0, M, V,
+                       tok, x_tok, c, inv_t, logp, entropy, stats);
+  }
+  return head_done("head log probabilities launch");
+}
+
+int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype, int n_rows, int d, int V,
+                              const int32_t* tok, float temp, const float* stats, const float* entropy, const float* g_logp,
+                              const float* g_ent, void* gh, int64_t gh_stride, void* gw, int64_t gw_stride, int gw_f32, int accumulate,
+                              void* ws, hipStream_t st) {
+  const int EW = gw_f32 ? 4 : 2;
+  if (n_rows == 0) {
+    if (gw && !accumulate)
+      hipLaunchKernelGGL(k_head_zero, dim3(V), dim3(256), 0, st, (uint32_t*)gw, gw_stride * EW / 4, d * EW / 4);
+    return head_done("head log probabilities gradient launch");
+  }
+  const HeadPlan p = head_plan(dtype, n_rows, d, V, gw_f32, true);
+  const bool f32 = dtype == SARA_F32;
+  const float c = (float)(1.4426950408889634 / (double)temp);
+  const int half = ilogbf(1.f / temp) / 2;
+  const float scale = ldexpf(1.f, half), inv_t = ldexpf(1.f / temp, -half);   // of D, of the results
+  auto at = [&](int64_t off) { return (char*)ws + off; };
+  HeadRow* rows = (HeadRow*)at(p.rows);
+  uint16_t *D = (uint16_t*)at(p.d), *hp = (uint16_t*)at(p.h_parts), *wp = (uint16_t*)at(p.w_parts);
+  float* slab = (float*)at(p.slab);
+  const int64_t h_part = (int64_t)p.rows_out * p.width, w_part = 256 * (int64_t)p.piece * p.width;
+  hipLaunchKernelGGL(k_head_rows, dim3(p.rows_out / 256), dim3(256), 0, st, n_rows, p.rows_out, V, tok, stats, entropy, g_logp, g_ent,
+                     scale, rows);
+  if (f32)
+    hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(p.rows_out), dim3(256), 0, st, (const float*)h, h_stride, n_rows, d, rows, hp,
+                       p.rows_out, p.width);
+  else if (gw)
+    hipLaunchKernelGGL((k_head_parts<uint16_t, 1>), dim3(p.rows_out), dim3(256), 0, st, (const uint16_t*)h, h_stride, n_rows, d, rows, hp,
+                       p.rows_out, p.width);
+  const int cols = (V + 255) / 256;
+  for (int c0 = 0; c0 < cols; c0 += p.piece) {
+    const int v0 = 256 * c0, N = std::min(V - v0, 256 * p.piece);
+    Mat wm = {(const uint16_t*)w + v0 * w_stride, w_stride, 0};
+    if (f32) {
+      hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(N), dim3(256), 0, st, (const float*)w + v0 * w_stride, w_stride, N, d, nullptr, wp,
+                         256 * p.piece, p.width);
+      wm = Mat{wp, p.width, w_part};
+    }
+    const Mat hm = {hp, p.width, h_part};
+    const Mat dm = {D, 256 * (int64_t)p.piece, 256 * (int64_t)p.piece * p.rows_out};
+    HeadTile t = {};
+    t.v0 = v0;
+    t.M = n_rows;
+    t.N = N;
+    t.a = f32 ? hm : Mat{(const uint16_t*)h, h_stride, 0};
+    t.b = wm;
+    t.K = f32 ? p.width : d;
+    t.n_pairs = f32 ? 6 : 1;
+    t.pairs = f32 ? kPairs3 : kPairs1;
+    t.steps = (t.K + 31) / 32;
+    t.c = c;
+    t.rows = rows;
+    t.d = D;
+    t.d_stride = dm.stride;
+    t.d_part = dm.part;
+    t.d_parts = p.d_parts;
+    hipLaunchKernelGGL((k_head_tile<false, false, kGradRows>), tile_grid(t), dim3(512), 0, st, t);
+    if (gh) {
+      HeadTile x = {};
+      x.a = dm;
+      x.b = wm;
+      x.M = n_rows;
+      x.N = d;
+      x.K = N;
+      x.n_pairs = f32 ? 6 : 1;
+      x.pairs = f32 ? kPairs3 : kPairs1;
+      x.steps = ((N + 31) / 32 + p.splits - 1) / p.splits;
+      x.slab = slab;
+      x.add = c0 > 0;
+      hipLaunchKernelGGL((k_head_tile<false, true, kSlab>), tile_grid(x), dim3(512), 0, st, x);
+    }
+    if (gw) {
+      HeadTile x = {};
+      x.a = dm;
+      x.b = hm;
+      x.M = N;
+      x.N = d;
+      x.K = (int)up(n_rows, 32);
+      x.n_pairs = f32 ? 6 : p.d_parts;
+      x.pairs = f32 ? kPairs3 : p.d_parts == 2 ? kPairs2 : kPairs1;
+      x.steps = x.K / 32;
+      x.inv_t = inv_t;
+      x.out = (char*)gw + v0 * gw_stride * EW;
+      x.out_stride = gw_stride;
+      x.out_f32 = gw_f32;
+      x.add = accumulate;
+      hipLaunchKernelGGL((k_head_tile<true, true, kWeight>), tile_grid(x), dim3(512), 0, st, x);
+    }
+  }
+  if (gh) {
+    const int64_t n = (int64_t)n_rows * d;
+    const dim3 grid((uint32_t)((n / 4 + 255) / 256));
+    if (f32) hipLaunchKernelGGL((k_head_sum<float>), grid, dim3(256), 0, st, slab, p.splits, n, d, rows, inv_t, (float*)gh, gh_stride);
+    else hipLaunchKernelGGL((k_head_sum<uint16_t>), grid, dim3(256), 0, st, slab, p.splits, n, d, rows, inv_t, (uint16_t*)gh, gh_stride);
+  }
+  return head_done("head log probabilities gradient launch");
+}
+
+}  // namespace sara

@@ -314,6 +314,98 @@ PyObject* token_logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// [rows, d] with contiguous rows
+struct Matrix { void* p; int64_t stride; };
+Matrix matrix(const at::Tensor& t, int64_t rows, int64_t d, const Place& at, const char* what) {
+  if (t.dim() != 2 || t.size(0) != rows || t.size(1) != d || (stride_of(t, 1, 1) != 1 && t.numel())) {
+    std::ostringstream s;
+    s << what << " must be [" << rows << ", " << d << "] with contiguous rows, not " << t.sizes();
+    value_error(s.str());
+  }
+  at.check(t, what);
+  return Matrix{t.data_ptr(), stride_of(t, 0, d)};
+}
+
+// hidden states and weight of one dtype
+struct Head { Matrix h, w; int32_t type, rows, d, V; };
+Head head(const at::Tensor& h, const at::Tensor& w, const Place& at) {
+  if (h.dim() != 2 || w.dim() != 2) value_error("hidden states must be [rows, d_model], the weight [vocab, d_model]");
+  if (h.scalar_type() != w.scalar_type()) value_error("hidden states and weight must have the same dtype");
+  Head x;
+  x.type = float_type(h, "hidden states");
+  x.rows = size32(h.size(0), "rows");
+  x.d = size32(h.size(1), "d_model");
+  x.V = size32(w.size(0), "vocab");
+  x.h = matrix(h, x.rows, x.d, at, "hidden states");
+  x.w = matrix(w, x.V, x.d, at, "weight");
+  return x;
+}
+
+// (d_hidden, d_weight, d_tok, d_logp, d_entropy, d_stats, temperature, workspace)
+PyObject* head_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 8, [&] {
+    const at::Tensor &h = tensor(a[0], "hidden states"), &w = tensor(a[1], "weight");
+    float_type(h, "hidden states");
+    const Place at(h);
+    const Head x = head(h, w, at);
+    const int32_t* tok = per_row<int32_t>(a[2], x.rows, at::kInt, at, "tokens");
+    float* logp = per_row<float>(a[3], x.rows, at::kFloat, at, "logp");
+    float* ent = per_row<float>(a[4], x.rows, at::kFloat, at, "entropy");
+    float* stats = per_row<float>(a[5], 2 * (int64_t)x.rows, at::kFloat, at, "stats");
+    const float temp = number(a[6]);
+    int64_t need = 0;
+    int rc = sara_head_logprobs_workspace(x.type, x.rows, x.d, x.V, 0, x.type, &need);
+    if (rc) return rc;
+    const Workspace ws = workspace(a[7], need, h, at);
+    void* st = at.stream();
+    rc = without_gil([&] {
+      return sara_head_logprobs(x.h.p, x.h.stride, x.w.p, x.w.stride, x.type, x.rows, x.d, x.V, tok, temp, logp, ent, stats, ws.p,
+                                ws.bytes, st);
+    });
+    return written(rc, {a[3], a[4], a[5]});
+  });
+}
+
+// (d_hidden, d_weight, d_tok, d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad_hidden, d_grad_weight, temperature, accumulate, workspace)
+PyObject* head_logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 12, [&] {
+    const at::Tensor &h = tensor(a[0], "hidden states"), &w = tensor(a[1], "weight");
+    float_type(h, "hidden states");
+    const Place at(h);
+    const Head x = head(h, w, at);
+    const int32_t* tok = per_row<int32_t>(a[2], x.rows, at::kInt, at, "tokens");
+    const float* stats = per_row<float>(a[3], 2 * (int64_t)x.rows, at::kFloat, at, "stats");
+    const float* ent = per_row<float>(a[4], x.rows, at::kFloat, at, "entropy");
+    const float* g = per_row<float>(a[5], x.rows, at::kFloat, at, "g_logp");
+    const float* ge = per_row<float>(a[6], x.rows, at::kFloat, at, "g_entropy");
+    Matrix gh = {}, gw = {};
+    int32_t gw_type = x.type;
+    if (a[7] != Py_None) {
+      const at::Tensor& t = tensor(a[7], "gradient of the hidden states");
+      if (t.scalar_type() != h.scalar_type()) value_error("the gradient of the hidden states must have their dtype");
+      gh = matrix(t, x.rows, x.d, at, "gradient of the hidden states");
+    }
+    if (a[8] != Py_None) {
+      const at::Tensor& t = tensor(a[8], "gradient of the weight");
+      gw_type = float_type(t, "gradient of the weight");
+      gw = matrix(t, x.V, x.d, at, "gradient of the weight");
+    }
+    const float temp = number(a[9]);
+    const int add = PyObject_IsTrue(a[10]);
+    if (add < 0) throw PythonError{};
+    int64_t need = 0;
+    int rc = sara_head_logprobs_workspace(x.type, x.rows, x.d, x.V, 1, gw_type, &need);
+    if (rc) return rc;
+    const Workspace ws = workspace(a[11], need, h, at);
+    void* st = at.stream();
+    rc = without_gil([&] {
+      return sara_head_logprobs_grad(x.h.p, x.h.stride, x.w.p, x.w.stride, x.type, x.rows, x.d, x.V, tok, temp, stats, ent, g, ge, gh.p,
+                                     gh.stride, gw.p, gw.stride, gw_type, add, ws.p, ws.bytes, st);
+    });
+    return written(rc, {a[7], a[8]});
+  });
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyCFunction fast() { return (PyCFunction)(void (*)())F; }
 
 PyMethodDef methods[] = {{"kv8_write", fast<kv8_rows<true>>(), METH_FASTCALL, nullptr},
@@ -321,6 +413,8 @@ PyMethodDef methods[] = {{"kv8_write", fast<kv8_rows<true>>(), METH_FASTCALL, nu
                          {"kv8_attention", fast<kv8_attention>(), METH_FASTCALL, nullptr},
                          {"token_logprobs", fast<token_logprobs>(), METH_FASTCALL, nullptr},
                          {"token_logprobs_grad", fast<token_logprobs_grad>(), METH_FASTCALL, nullptr},
+                         {"head_logprobs", fast<head_logprobs>(), METH_FASTCALL, nullptr},
+                         {"head_logprobs_grad", fast<head_logprobs_grad>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_operators", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

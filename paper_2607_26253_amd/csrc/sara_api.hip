@@ -1034,6 +1034,94 @@ extern "C" int sara_token_logprobs_grad(const void* d_logits, int32_t dtype, int
                                     d_g_entropy, temperature, d_grad, grad_row_stride, (hipStream_t)stream);
 }
 
+// Widest hidden state: the tiles' k steps and strides in bytes stay far inside 32 bits.
+static constexpr int32_t kMaxWidth = 1 << 20;
+
+static std::string head_bad(int32_t dtype, int32_t n_rows, int32_t d, int32_t vocab) {
+  if (dtype != SARA_BF16 && dtype != SARA_F32) return "dtype must be SARA_BF16 or SARA_F32";
+  if (n_rows < 0 || d < 1 || d > kMaxWidth || vocab < 1 || vocab > kMaxVocab)
+    return "n_rows must be >= 0, d_model in [1, 2^20] and vocab in [1, 2^30]";
+  if (d % (dtype == SARA_BF16 ? 8 : 4)) return "d_model must be a multiple of 16 bytes";
+  // tiles of 256 rows and 256 ids, or of 256 ids and 256 of the width, are blocks of one launch
+  const int64_t rows = ((int64_t)n_rows + 255) / 256, cols = ((int64_t)vocab + 255) / 256, wide = (d + 255) / 256;
+  if (std::max(std::max(rows * cols, cols * wide), 64 * rows * wide) > (1 << 22) || vocab > kMaxBlocks) return "too many rows or ids";
+  return "";
+}
+// a matrix whose rows are read 16 bytes at a time
+static bool matrix_bad(const void* p, int64_t stride, int64_t n, int32_t d, int64_t E) {
+  return ((uintptr_t)p & 15) || (n > 1 && (stride < d || (stride * E) % 16));
+}
+static std::string head_inputs_bad(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int32_t dtype, int32_t n_rows,
+                                   int32_t d, int32_t vocab, const int32_t* tok, float temperature) {
+  if (!(temperature >= 1e-37f) || !(temperature <= 1e37f)) return "temperature must be in [1e-37, 1e37]";
+  if (!h || !w || !tok) return "null array";
+  const int64_t E = dtype == SARA_BF16 ? 2 : 4;
+  if (matrix_bad(h, h_stride, n_rows, d, E) || matrix_bad(w, w_stride, vocab, d, E))
+    return "hidden states and weight must be 16-byte aligned, with row strides of at least d_model that are multiples of 16 bytes";
+  return "";
+}
+
+extern "C" int sara_head_logprobs_workspace(int32_t dtype, int32_t n_rows, int32_t d_model, int32_t vocab, int32_t grad,
+                                            int32_t weight_grad_dtype, int64_t* bytes) {
+  if (!bytes) return einval("null argument");
+  const std::string bad = head_bad(dtype, n_rows, d_model, vocab);
+  if (!bad.empty()) return einval(bad);
+  if (grad && weight_grad_dtype != SARA_F32 && weight_grad_dtype != dtype)
+    return einval("the weight's gradient must be of its dtype or SARA_F32");
+  *bytes = n_rows == 0 ? 0 : head_plan(dtype, n_rows, d_model, vocab, weight_grad_dtype == SARA_F32, grad != 0).bytes;
+  return SARA_OK;
+}
+
+extern "C" int sara_head_logprobs(const void* d_hidden, int64_t hidden_stride, const void* d_weight, int64_t weight_stride,
+                                  int32_t dtype, int32_t n_rows, int32_t d_model, int32_t vocab, const int32_t* d_tok,
+                                  float temperature, float* d_logp, float* d_entropy, float* d_stats, void* d_ws, int64_t ws_bytes,
+                                  void* stream) {
+  int64_t need = 0;
+  const int rc = sara_head_logprobs_workspace(dtype, n_rows, d_model, vocab, 0, dtype, &need);
+  if (rc) return rc;
+  if (n_rows == 0) return SARA_OK;
+  const std::string bad = head_inputs_bad(d_hidden, hidden_stride, d_weight, weight_stride, dtype, n_rows, d_model, vocab, d_tok, temperature);
+  if (!bad.empty()) return einval(bad);
+  if ((uintptr_t)d_stats & 7) return einval("d_stats must be 8-byte aligned");
+  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need)
+    return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
+  return launch_head_logprobs(d_hidden, hidden_stride, d_weight, weight_stride, dtype, n_rows, d_model, vocab, d_tok, temperature, d_logp,
+                              d_entropy, d_stats, d_ws, (hipStream_t)stream);
+}
+
+extern "C" int sara_head_logprobs_grad(const void* d_hidden, int64_t hidden_stride, const void* d_weight, int64_t weight_stride,
+                                       int32_t dtype, int32_t n_rows, int32_t d_model, int32_t vocab, const int32_t* d_tok,
+                                       float temperature, const float* d_stats, const float* d_entropy, const float* d_g_logp,
+                                       const float* d_g_entropy, void* d_grad_hidden, int64_t grad_hidden_stride, void* d_grad_weight,
+                                       int64_t grad_weight_stride, int32_t weight_grad_dtype, int32_t accumulate, void* d_ws,
+                                       int64_t ws_bytes, void* stream) {
+  int64_t need = 0;
+  const int rc = sara_head_logprobs_workspace(dtype, n_rows, d_model, vocab, 1, weight_grad_dtype, &need);
+  if (rc) return rc;
+  const int64_t E = dtype == SARA_BF16 ? 2 : 4, EW = weight_grad_dtype == SARA_BF16 ? 2 : 4;
+  if (d_grad_weight && matrix_bad(d_grad_weight, grad_weight_stride, vocab, d_model, EW))
+    return einval("gradients must be 16-byte aligned, with row strides of at least d_model that are multiples of 16 bytes");
+  if (!d_grad_hidden && !d_grad_weight) return einval("give d_grad_hidden, d_grad_weight or both");
+  if (n_rows == 0)
+    return launch_head_logprobs_grad(nullptr, 0, nullptr, 0, dtype, 0, d_model, vocab, nullptr, 1.f, nullptr, nullptr, nullptr, nullptr,
+                                     nullptr, 0, d_grad_weight, grad_weight_stride, weight_grad_dtype == SARA_F32, accumulate != 0,
+                                     nullptr, (hipStream_t)stream);
+  std::string bad = head_inputs_bad(d_hidden, hidden_stride, d_weight, weight_stride, dtype, n_rows, d_model, vocab, d_tok, temperature);
+  if (!bad.empty()) return einval(bad);
+  if (!d_stats) return einval("null array");
+  if (d_g_entropy && !d_entropy) return einval("a gradient of the entropy needs d_entropy");
+  if (d_grad_hidden && matrix_bad(d_grad_hidden, grad_hidden_stride, n_rows, d_model, E))
+    return einval("gradients must be 16-byte aligned, with row strides of at least d_model that are multiples of 16 bytes");
+  if (d_grad_hidden == d_hidden || d_grad_hidden == d_weight || d_grad_weight == d_weight || d_grad_weight == d_hidden ||
+      (d_grad_hidden && d_grad_hidden == d_grad_weight))
+    return einval("gradients must not be written over the inputs or each other");
+  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need)
+    return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
+  return launch_head_logprobs_grad(d_hidden, hidden_stride, d_weight, weight_stride, dtype, n_rows, d_model, vocab, d_tok, temperature,
+                                   d_stats, d_entropy, d_g_logp, d_g_entropy, d_grad_hidden, grad_hidden_stride, d_grad_weight,
+                                   grad_weight_stride, weight_grad_dtype == SARA_F32, accumulate != 0, d_ws, (hipStream_t)stream);
+}
+
 extern "C" int sara_gumbel_fast_max_error(double* h_out, void* stream) {
   if (!h_out) return einval("h_out is null");
   return launch_gumbel_check(h_out, (hipStream_t)stream);

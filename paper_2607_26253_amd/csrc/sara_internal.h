@@ -334,6 +334,21 @@ int launch_token_logprobs(const void* logits, int dtype, int64_t row_stride, int
 int launch_token_logprobs_grad(const void* logits, int dtype, int64_t row_stride, int n_rows, int V, const int32_t* tok,
                                const float* stats, const float* entropy, const float* g_logp, const float* g_ent,
                                float temp, void* grad, int64_t grad_stride, hipStream_t st);
+// launchers (log probabilities from hidden states)
+// How a call is cut and where its workspace's parts begin: few rows or tiles; vocabulary tiles (256 ids) of a piece,
+// padded rows, padded width of bf16 parts, parts of D, splits of dH's contraction.
+struct HeadPlan {
+  bool few;
+  int nt, few_blocks, piece, rows_out, width, d_parts, splits;
+  int64_t x_tok, parts, rows, d, slab, h_parts, w_parts, bytes;
+};
+HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool grad);
+int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype, int n_rows, int d, int V,
+                         const int32_t* tok, float temp, float* logp, float* entropy, float* stats, void* ws, hipStream_t st);
+int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype, int n_rows, int d, int V,
+                              const int32_t* tok, float temp, const float* stats, const float* entropy, const float* g_logp,
+                              const float* g_ent, void* gh, int64_t gh_stride, void* gw, int64_t gw_stride, int gw_f32, int accumulate,
+                              void* ws, hipStream_t st);
 int launch_convert_norms(sara_ctx* c, const void* const* w);
 int launch_gumbel_check(double* h_out, hipStream_t st);
 int launch_tile_weights(sara_ctx* c, const void* src, void* dst, int rows, int K, int tile_mul, int tile_add,
