@@ -32,6 +32,7 @@ EXPORTED = ["sara_init", "sara_begin_step", "sara_decode_step", "sara_posterior_
             "sara_sample_logits", "sara_sample_logits_noalloc", "sara_gumbel_fast_max_error", "sara_set_profiling", "sara_reset_profile",
             "sara_read_profile", "sara_set_warm_start", "sara_warm_start_update", "sara_poll",
             "sara_kv8_write", "sara_kv8_read", "sara_kv8_attention_workspace", "sara_kv8_attention",
+            "sara_kv8_group_attention_workspace", "sara_kv8_group_attention",
             "sara_token_logprobs_workspace", "sara_token_logprobs", "sara_token_logprobs_grad",
             "sara_head_logprobs_workspace", "sara_head_logprobs", "sara_head_logprobs_grad",
             "sara_destroy",
@@ -119,6 +120,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "sara_kv8_read": [P, P, I64, I64, P, I64, I64, I32, I32, P, I32, P, P, I32, P],
         "sara_kv8_attention_workspace": [I32, I32, I32, I32, I32, I32, I32, ctypes.POINTER(I64)],
         "sara_kv8_attention": [P, P, I64, I64, P, I64, I64, I32, I32, I32, P, I32, P, P, I32, I32, F32, P, I64, P],
+        "sara_kv8_group_attention_workspace": [I32, I32, I32, I32, I32, I32, I32, I32, I32, ctypes.POINTER(I64)],
+        "sara_kv8_group_attention": [P, P, I64, I64, P, I64, I64, I32, I32, I32, P, I32, P, P, I32, P, P, I32, I32, I32, F32, P, I64, P],
         "sara_token_logprobs_workspace": [I32, I32, I32, ctypes.POINTER(I64)],
         "sara_token_logprobs": [P, I32, I64, I32, I32, P, F32, I32, P, P, P, P, P, P, I64, P],
         "sara_token_logprobs_grad": [P, I32, I64, I32, I32, P, F32, P, P, P, P, P, I64, P],
@@ -405,7 +408,8 @@ class _Operators:
             from . import _operators
         except ImportError as e:
             raise ImportError(f"_operators.so is not built or does not load; run `python -m paper_2607_26253_amd.build` ({e})")
-        for f in ("kv8_write", "kv8_read", "kv8_attention", "token_logprobs", "token_logprobs_grad", "head_logprobs", "head_logprobs_grad"):
+        for f in ("kv8_write", "kv8_read", "kv8_attention", "kv8_group_attention", "token_logprobs", "token_logprobs_grad",
+                  "head_logprobs", "head_logprobs_grad"):
             setattr(self, f, getattr(_operators, f))
         self.on = torch.cuda.stream
         return object.__getattribute__(self, name)
@@ -453,6 +457,17 @@ def sara_kv8_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_of
     taken from torch's allocator."""
     _operator("sara_kv8_attention", _ops.kv8_attention, stream,
               (k_cache, v_cache, k_exp, v_exp, d_q, d_out, d_pages, d_ctx, d_off, scale, max_ctx, workspace))
+
+
+def sara_kv8_group_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx, d_off, d_groups, d_shared, d_out, scale=None,
+                             max_ctx=None, max_shared=None, workspace=None, stream=None):
+    """sara_kv8_attention where the sequences d_groups[j]..d_groups[j + 1] share
+    the whole pages of their first d_shared[j] tokens (int32 [n_groups + 1] and
+    [n_groups]): those are read once a group, through the page table of its first
+    sequence.  max_shared bounds d_shared (default: max_ctx)."""
+    _operator("sara_kv8_group_attention", _ops.kv8_group_attention, stream,
+              (k_cache, v_cache, k_exp, v_exp, d_q, d_out, d_pages, d_ctx, d_off, d_groups, d_shared, scale, max_ctx, max_shared,
+               workspace))
 
 
 # -- token log probabilities --------------------------------------------------------

@@ -356,7 +356,46 @@ struct AttnArgs {
   // partial results (HD numerators, maximum, sum): k_kv8_attn's [sequence][KV head][column][split], k_kv8_attn_tile's
   // [row][head][split]
   float *part, *part_tile;
+  // sequences in groups that share pages (k_kv8_group_*), and the partial results over those, [row][head][split]
+  const int32_t *groups, *shared;
+  int n_groups, max_shared, splits_shared, pps_shared, n_kv;
+  float* part_shared;
 };
+
+// What a block of attention works on: a sequence's whole context; the pages that a group shares, for all of its rows;
+// or what a sequence has behind those.
+enum { kWhole, kShared, kOwn };
+
+// whole pages among the tokens that a group shares
+__device__ __forceinline__ int shared_pages(const AttnArgs& a, int tokens) { return max(min(tokens, a.max_shared), 0) >> 4; }
+// of the group that sequence `seq` is in, which begins with sequence `first`
+__device__ __forceinline__ int shared_pages_of(const AttnArgs& a, int seq, int& first) {
+  const SeqRows g = find_seq<1>(a.groups, a.shared, a.n_groups, a.n_seqs, seq, 1, 0);
+  first = g.r0;
+  return g.seq >= 0 && seq < g.r1 ? shared_pages(a, g.value) : 0;
+}
+// first row of sequence i (n_seqs: one past the last row)
+__device__ __forceinline__ int first_row_of(const AttnArgs& a, int i) {
+  i = min(max(i, 0), a.n_seqs);
+  return min(max(a.off ? a.off[i] : i, 0), a.n_rows);
+}
+// The group of item b, as find_seq numbers them, by the rows of groups: seq is the group, value the tokens it shares.
+template <int DIV> __device__ __forceinline__ SeqRows find_group(const AttnArgs& a, int b, int mul) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = a.n_groups;
+  while (true) {
+    const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
+    int at = 0x7FFFFFFF;
+    if (i < hi) at = (int)((int64_t)first_row_of(a, a.groups[i]) * mul / DIV) + i;
+    const int n = __popcll(__ballot(at <= b));
+    if (n == 0) return SeqRows{-1, 0, 0, 0, 0};
+    lo += (n - 1) * step;
+    hi = min(hi, lo + step);
+    if (step > 1) continue;
+    const int r0 = first_row_of(a, a.groups[lo]);
+    return SeqRows{lo, __builtin_amdgcn_readlane(at, n - 1), r0, max(r0, first_row_of(a, a.groups[lo + 1])), a.shared[lo]};
+  }
+}
 
 // fp32 as a sum of P bf16 numbers: 8 bits (bf16 inputs are one exactly), 16, or 24
 template <int P> __device__ __forceinline__ void split_bf16(float a, float b, uint32_t* w) {
@@ -408,7 +447,7 @@ template <int HD> struct FewLds {
 // 8 waves take 6.7 us there, but 22 for the 32 rows' 18.2 with the join.
 // A weight times its page's scale is held to bf16's range: below 2^-126 it may count as 0, which matters where all of V is
 // below about 1e-30 (at 1e-24 fp32 queries lose nothing).
-template <int HD, int FMT, typename T>
+template <int HD, int FMT, typename T, int WHAT = kWhole>
 __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs& a, FewLds<HD>& lds, int bx, int split) {
   constexpr int NK = HD / 64, NT = HD / 16, DV = HD / 16;   // 16-byte K loads, dim tiles, V dims a lane
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
@@ -425,18 +464,22 @@ __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs
   const int n_cols = (r1 - r0) * G;
   if (c0 >= n_cols || (a.off && n_cols > kFewColumns)) return;
   const int p0 = split * a.pps;
+  int begin = 0, group;                                  // pages before the block's first
+  if constexpr (WHAT == kOwn) begin = shared_pages_of(a, seq, group);
   // ids of 32 of the wave's page pairs, one a lane; the first are loaded beside the context's length
   const int32_t* table = a.pages + (size_t)seq * a.max_pages;
-  auto load_ids = [&](int it) { return table[min(p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1), a.max_pages - 1)]; };
+  auto load_ids = [&](int it) { return table[min(begin + p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1), a.max_pages - 1)]; };
   int ids = load_ids(0);
-  const int ctx = max(a.ctx[seq], 0);
+  int ctx = max(a.ctx[seq], 0);
   const bool too_long = ctx > a.max_ctx;                 // more than the launch was sized for: the rows are NaN
+  if constexpr (WHAT == kOwn) ctx = max(ctx - 16 * begin, 0);   // from here on, positions count from the block's first page
   const int np = too_long ? 0 : (ctx + 15) >> 4;
   const int p1 = min(np, p0 + a.pps);
-  if (p0 >= p1 && split > 0) return;
+  if (p0 >= p1 && (WHAT == kOwn || split > 0)) return;
   // this lane's column: query row and head, and how many keys it sees
   const int cc = min(c0 + col, n_cols - 1), qt = cc / G, head = g * G + cc - qt * G;
-  const int before = ctx - (r1 - r0);                    // keys before the first query (below 0: its row sees none)
+  int before = ctx - (r1 - r0);                          // keys before the first query (below 0: its row sees none)
+  if constexpr (WHAT == kOwn) before = max(a.ctx[seq], 0) - (r1 - r0) - 16 * begin;
   const int seen = before + qt + 1;
   const int seen_all = before + c0 / G + 1;              // keys that every column sees
   u32x4 qf[QP][2 * NK];
@@ -605,7 +648,7 @@ __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs
       den += wt * l_w[w][x];
     }
     const int t = (c0 + x) / G, h = g * G + (c0 + x) - t * G;
-    if (np <= a.pps) {
+    if (WHAT == kWhole && np <= a.pps) {
       T* dst = (T*)a.out + (size_t)(r0 + t) * a.o_row + (size_t)h * a.o_head + d4;
       float f[4];
 #pragma unroll
@@ -647,7 +690,7 @@ template <int HD> struct TileLds {
 // Queries of fp32 have 96 MFMAs (three parts of q, three of a weight) beside 718 vector instructions, and 256 registers: one
 // block a CU, whose one wave a SIMD overlaps little: vector issue 43%, MFMAs 40%.  Three prompts of 1,100-4,590: 408 us,
 // against 218 in bf16.
-template <int HD, int FMT, typename T>
+template <int HD, int FMT, typename T, int WHAT = kWhole>
 __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArgs& a, TileLds<HD>& lds, int bx, int n_bx, int split) {
   constexpr int NW = kTileWaves, NKS = HD / 16, NDT = HD / 32;
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
@@ -658,27 +701,60 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
   const int item = n_bx / hkv - 1 - bx / hkv, g = bx % hkv;          // long tiles first
-  const SeqRows sr = find_seq<32 * NW>(a.off, a.ctx, a.n_seqs, a.n_rows, item, G, 1);
-  const int seq = sr.seq, r0 = sr.r0, r1 = sr.r1;
+  const SeqRows sr = WHAT == kShared ? find_group<32 * NW>(a, item, G) : find_seq<32 * NW>(a.off, a.ctx, a.n_seqs, a.n_rows, item, G, 1);
+  int seq = sr.seq;
+  const int r0 = sr.r0, r1 = sr.r1;
   if (seq < 0 || item < sr.first) return;
   const int n_cols = (r1 - r0) * G, c0 = 32 * NW * (item - sr.first);
-  if (c0 >= n_cols || n_cols <= kFewColumns) return;
-  const int ctx = max(sr.value, 0);
-  const bool too_long = ctx > a.max_ctx;
+  if (c0 >= n_cols || (WHAT != kShared && n_cols <= kFewColumns)) return;
+  int ctx = max(sr.value, 0), begin = 0, group;
+  const bool too_long = WHAT != kShared && ctx > a.max_ctx;
+  if constexpr (WHAT == kShared) {
+    ctx = 16 * shared_pages(a, sr.value);
+    seq = min(max(a.groups[sr.seq], 0), a.n_seqs - 1);              // whose table it is
+  }
+  if constexpr (WHAT == kOwn) {
+    begin = shared_pages_of(a, seq, group);
+    ctx = max(ctx - 16 * begin, 0);                                 // from here on, positions count from the block's first page
+  }
   const int np = too_long ? 0 : (ctx + 15) >> 4;
-  const int p0 = split * a.pps_tile;
-  if (p0 >= np && split > 0) return;
-  const int before = ctx - (r1 - r0);
+  const int pps = WHAT == kShared ? a.pps_shared : a.pps_tile, p0 = split * pps;
+  if (p0 >= np && (WHAT != kWhole || split > 0)) return;
+  const int before = WHAT == kOwn ? max(sr.value, 0) - (r1 - r0) - 16 * begin : ctx - (r1 - r0);
   const int c_last = min(c0 + 32 * NW, n_cols) - 1;
-  const int keys = min(max(before + c_last / G + 1, 0), ctx);       // keys that some column of the block sees
-  const int p1 = min(min(np, p0 + a.pps_tile), (keys + 15) >> 4);
+  const int keys = WHAT == kShared ? ctx : min(max(before + c_last / G + 1, 0), ctx);   // keys that some column of the block sees
+  const int p1 = min(min(np, p0 + pps), (keys + 15) >> 4);
   const int nkb = p1 > p0 ? (p1 - p0 + 3) >> 2 : 0;
   const int wc0 = c0 + 32 * wave;
   const bool live = wc0 < n_cols;
   const int cc = min(wc0 + col, n_cols - 1), qt = cc / G, head = g * G + cc - qt * G;
-  const int seen = live ? before + qt + 1 : 0;                      // keys this lane's column sees
-  const int w_seen = live ? before + min(wc0 + 31, n_cols - 1) / G + 1 : 0;   // that some column of the wave sees
-  const int w_all = before + wc0 / G + 1;                           // that every column of the wave sees
+  int seen = live ? before + qt + 1 : 0;                            // keys this lane's column sees
+  int w_seen = live ? before + min(wc0 + 31, n_cols - 1) / G + 1 : 0;   // that some column of the wave sees
+  int w_all = before + wc0 / G + 1;                                 // that every column of the wave sees
+  if constexpr (WHAT == kShared) {
+    // the rows of a group are several sequences', each with its own context
+    const int at = r0 + qt;
+    int lo = min(max(a.groups[sr.seq], 0), a.n_seqs), hi = min(max(a.groups[sr.seq + 1], 0), a.n_seqs);
+    if (a.off) {
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.off[mid] <= at) lo = mid;
+        else hi = mid;
+      }
+    } else {
+      lo = at;
+    }
+    const int all = max(a.ctx[lo], 0);
+    seen = live && all <= a.max_ctx ? min(all - (first_row_of(a, lo + 1) - at) + 1, ctx) : 0;
+    w_seen = w_all = seen;
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) {
+      w_seen = max(w_seen, __shfl_xor(w_seen, x, 64));
+      w_all = min(w_all, __shfl_xor(w_all, x, 64));
+    }
+    w_seen = __builtin_amdgcn_readfirstlane(w_seen);
+    w_all = __builtin_amdgcn_readfirstlane(w_all);
+  }
   // a negative scale becomes the sign of q; the floor keeps a masked -inf from meeting a scale of 0
   const float sl2 = fmaxf(fabsf(a.scale_log2), 1e-37f);
   u32x4 qf[QP][NKS];
@@ -702,7 +778,7 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
       }
     }
   }
-  const int32_t* table = a.pages + (size_t)seq * a.max_pages;
+  const int32_t* table = a.pages + (size_t)seq * a.max_pages + begin;
   // lane i: page i of a stretch of 64 (16 key blocks), its exponent bytes (0x10000: no page, 0x20000: NaN, 0x40000: values may be inf)
   int ids = 0, meta = 0;
   // A wave stages KR token rows of K at a time, all of one page, and the V of one page: pages, exponents and addresses
@@ -923,9 +999,10 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
   l += __shfl_xor(l, 32, 64);
   if (!live || wc0 + col >= n_cols) return;
   const float inv = too_long ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : 1.f / l;
-  const bool whole = np <= a.pps_tile;
+  const bool whole = WHAT == kWhole && np <= a.pps_tile;
   T* out = (T*)a.out + (size_t)(r0 + qt) * a.o_row + (size_t)head * a.o_head + 16 * h;
-  float* part = a.part_tile + (((size_t)(r0 + qt) * a.hq + head) * a.splits_tile + split) * (HD + 2);
+  float* part = (WHAT == kShared ? a.part_shared : a.part_tile) +
+                (((size_t)(r0 + qt) * a.hq + head) * (WHAT == kShared ? a.splits_shared : a.splits_tile) + split) * (HD + 2);
 #pragma unroll
   for (int t = 0; t < NDT; ++t) {
     float f[16];
@@ -1046,6 +1123,113 @@ __global__ __launch_bounds__(256) void k_kv8_attn_join(AttnArgs a, int hkv, int 
 }
 
 // ---------------------------------------------------------------------------
+// attention of sequences that share pages
+// ---------------------------------------------------------------------------
+// The softmax over a row's keys is joined from two sets of partial results: over the pages that its group shares, by
+// blocks of 128 columns that take the rows of the whole group (k_kv8_group_shared), and over what its sequence has behind
+// them, by the kernels above (k_kv8_group_own_*).  So a group's pages are read and converted once for all its rows.
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_group_shared(sara_kv8_cache c, AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) TileLds<HD> lds;
+  attn_tile<HD, FMT, T, kShared>(c, a, lds, blockIdx.x, gridDim.x, blockIdx.y);
+}
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_group_own_few(sara_kv8_cache c, AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) FewLds<HD> lds;
+  attn_few<HD, FMT, T, kOwn>(c, a, lds, blockIdx.x, blockIdx.y);
+}
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_group_own_tile(sara_kv8_cache c, AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) TileLds<HD> lds;
+  attn_tile<HD, FMT, T, kOwn>(c, a, lds, blockIdx.x, gridDim.x, blockIdx.y);
+}
+
+// W waves join the partial results of a (row, head), 4 / W of those a block.
+template <int HD, typename T, int W>
+__global__ __launch_bounds__(256) void k_kv8_group_join(AttnArgs a) {
+  constexpr int DL = HD / 64;                            // dims a lane
+  __shared__ float m_w[4], l_w[4], o_w[4][HD];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, G_item = blockIdx.x * (4 / W) + wave / W;
+  const bool have = G_item < a.n_rows * a.hq;
+  const int item = have ? G_item : 0, row = item / a.hq, h = item - row * a.hq;
+  SeqRows sr = {row, row, row, row + 1, 0};
+  if (a.off) sr = find_seq<1>(a.off, a.ctx, a.n_seqs, a.n_rows, row, 1, 0);
+  else sr.value = a.ctx[row];
+  const bool mine = have && sr.seq >= 0 && row >= sr.r0 && row < sr.r1;   // else a row of no sequence, left as it is
+  int first;
+  const int begin = mine ? shared_pages_of(a, sr.seq, first) : 0;
+  const int ctx = max(sr.value, 0), own = mine ? (max(ctx - 16 * begin, 0) + 15) >> 4 : 0;
+  const bool few = !a.off || (sr.r1 - sr.r0) * (a.hq / a.n_kv) <= kFewColumns, too_long = ctx > a.max_ctx;
+  const int pps = few ? a.pps : a.pps_tile, splits = few ? a.splits : a.splits_tile;
+  const int ns_shared = (begin + a.pps_shared - 1) / a.pps_shared, ns = too_long ? 0 : ns_shared + (own + pps - 1) / pps;
+  const float* p_shared = a.part_shared + (size_t)item * a.splits_shared * (HD + 2);
+  const int G = a.hq / a.n_kv;
+  const size_t own_item = few ? ((size_t)sr.seq * a.n_kv + h / G) * (a.off ? kFewColumns : G) + (row - sr.r0) * G + h % G : item;
+  const float* p_own = (few ? a.part : a.part_tile) + own_item * splits * (HD + 2) - (size_t)ns_shared * (HD + 2);
+  float m = -INFINITY, l = 0.f, o[DL] = {};
+  for (int s0 = wave % W; s0 < ns; s0 += W * kJoin) {
+    float pm[kJoin], pl[kJoin], po[kJoin][DL];
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i) {
+      const int s = min(s0 + W * i, ns - 1);
+      const float* q = (s < ns_shared ? p_shared : p_own) + (size_t)s * (HD + 2);
+      const f32x2 ml = *(const f32x2*)(q + HD);
+      pm[i] = s0 + W * i < ns ? ml[0] : -INFINITY;
+      pl[i] = ml[1];
+      if (DL == 2) {
+        const f32x2 v = *(const f32x2*)(q + 2 * lane);
+        po[i][0] = v[0];
+        po[i][DL - 1] = v[1];
+      } else {
+        po[i][0] = q[lane];
+      }
+    }
+    float mx = m;
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i) mx = fmaxf(mx, pm[i]);
+    const float sub = mx == -INFINITY ? 0.f : mx;
+    const float al = __builtin_amdgcn_exp2f(m - sub);
+    l *= al;
+#pragma unroll
+    for (int d = 0; d < DL; ++d) o[d] *= al;
+#pragma unroll
+    for (int i = 0; i < kJoin; ++i) {
+      const float w = __builtin_amdgcn_exp2f(pm[i] - sub);
+      l = fmaf(w, pl[i], l);
+#pragma unroll
+      for (int d = 0; d < DL; ++d) o[d] = fmaf(w, po[i][d], o[d]);
+    }
+    m = mx;
+  }
+  T* out = (T*)a.out + (size_t)row * a.o_row + (size_t)h * a.o_head;
+  const float nan = __uint_as_float(0x7FC00000u);
+  if constexpr (W == 1) {
+    if (!mine) return;
+    const float inv = too_long ? nan : l == 0.f ? 0.f : 1.f / l;
+    if constexpr (DL == 2 && sizeof(T) == 2) *(uint32_t*)(out + 2 * lane) = pack_bf16(o[0] * inv, o[1] * inv);
+    else
+#pragma unroll
+      for (int d = 0; d < DL; ++d) st_f32<T>(out, DL * lane + d, o[d] * inv);
+  } else {
+    if (lane == 0) { m_w[wave] = m; l_w[wave] = l; }
+#pragma unroll
+    for (int d = 0; d < DL; ++d) o_w[wave][DL * lane + d] = o[d];
+    __syncthreads();
+    if (!mine || threadIdx.x >= HD) return;
+    const float mx = fmaxf(fmaxf(m_w[0], m_w[1]), fmaxf(m_w[2], m_w[3]));
+    const float sub = mx == -INFINITY ? 0.f : mx;
+    float num = 0.f, den = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float wt = __builtin_amdgcn_exp2f(m_w[w] - sub);
+      num = fmaf(wt, o_w[w][threadIdx.x], num);
+      den = fmaf(wt, l_w[w], den);
+    }
+    st_f32<T>(out, threadIdx.x, too_long ? nan : den == 0.f ? 0.f : num / den);
+  }
+}
+
+// ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
 template <typename F> static int kv8_dispatch(const sara_kv8_cache& c, int dtype, F&& go) {
@@ -1084,6 +1268,12 @@ int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int d
   });
 }
 
+// pages a split so that about `blocks` blocks share `items`, at least `least`, in steps of `step`, at most 128 splits
+static int split_pages(int pages, int64_t items, int64_t blocks, int least, int step) {
+  const int64_t want = std::min<int64_t>(128, std::max<int64_t>(1, blocks / std::max<int64_t>(1, items)));
+  return (int)std::max<int64_t>(least, ((pages + want - 1) / want + step - 1) / step * step);
+}
+
 Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx, bool ragged) {
   const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16);
   // Pages a split so that about `blocks` blocks share the work, at least `least`, in steps of `step`, and at most
@@ -1092,10 +1282,7 @@ Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx,
   // 3,000-4,600 take 19.7 us (16), 18.7 (24, this rule's), 20.0 (32), 18.2 (40); one at 65,537 17.7 (24), 15.9 (32), 16.1
   // (40, this rule's), 18.6 (64); one at 40,000 13.6 (24, this rule's), 14.1 (32).  Where the rule's 24 pages make more
   // blocks than fit at once, coarser splits would gain: 4 rows at 40,000 24.5 (24), 20.7 (40); 8 at 16,000 18.6 (24), 16.7 (32).
-  auto share = [&](int64_t items, int64_t blocks, int least, int step) {
-    const int64_t want = std::min<int64_t>(128, std::max<int64_t>(1, blocks / std::max<int64_t>(1, items * hkv)));
-    return (int)std::max<int64_t>(least, ((np + want - 1) / want + step - 1) / step * step);
-  };
+  auto share = [&](int64_t items, int64_t blocks, int least, int step) { return split_pages(np, items * hkv, blocks, least, step); };
   Kv8Split s = {};
   s.items = (int64_t)n_seqs * (ragged ? kFewColumns / 16 : (G + 15) / 16);
   s.tile_items = ragged && (int64_t)n_rows * G > kFewColumns ? (int64_t)n_rows * G / (32 * kTileWaves) + n_seqs : 0;
@@ -1139,6 +1326,56 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
     if (s.splits_tile > 1)
       hipLaunchKernelGGL((k_kv8_attn_join<hd.value, decltype(t), true>), dim3((uint32_t)((int64_t)n_rows * hq)), dim3(256), 0,
                          st, a, c.n_kv_heads, 0);
+  });
+}
+
+Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged) {
+  const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16), np_shared = max_shared / 16;
+  auto share = [&](int pages, int64_t items, int64_t blocks, int least, int step) {
+    return split_pages(pages, items * hkv, blocks, least, step);
+  };
+  Kv8GroupSplit s = {};
+  s.few_items = (int64_t)n_seqs * (ragged ? kFewColumns / 16 : (G + 15) / 16);
+  s.tile_items = ragged && (int64_t)n_rows * G > kFewColumns ? (int64_t)n_rows * G / (32 * kTileWaves) + n_seqs : 0;
+  s.shared_items = np_shared > 0 ? (int64_t)n_rows * G / (32 * kTileWaves) + n_groups : 0;
+  s.pps = share(np, ragged ? n_seqs : s.few_items, 1024, 24, 8);
+  s.pps_tile = share(np, std::max<int64_t>(1, s.tile_items), 512, 32, 16);
+  s.pps_shared = share(std::max(1, np_shared), std::max<int64_t>(1, s.shared_items), 512, 8, 4);
+  s.splits = (np + s.pps - 1) / s.pps;
+  s.splits_tile = s.tile_items ? (np + s.pps_tile - 1) / s.pps_tile : 0;
+  s.splits_shared = s.shared_items ? (np_shared + s.pps_shared - 1) / s.pps_shared : 0;
+  const int64_t one = (int64_t)sizeof(float) * (hd + 2);
+  s.part_bytes = one * n_seqs * hkv * (ragged ? kFewColumns : G) * s.splits;
+  s.part_tile_bytes = one * n_rows * hq * s.splits_tile;
+  s.part_shared_bytes = one * n_rows * hq * s.splits_shared;
+  return s;
+}
+
+int launch_kv8_group_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows, int hq,
+                               const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
+                               const int32_t* groups, const int32_t* shared, int n_groups, int max_ctx, int max_shared, float scale,
+                               void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st) {
+  const int hkv = c.n_kv_heads;
+  const Kv8GroupSplit s = kv8_group_split(n_rows, hq, hkv, c.head_dim, n_seqs, n_groups, max_ctx, max_shared, off != nullptr);
+  char* part = (char*)ws;
+  const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
+                      s.splits, s.pps, s.splits_tile, s.pps_tile, scale * 1.4426950408889634f, (float*)part,
+                      (float*)(part + s.part_bytes), groups, shared, n_groups, max_shared, s.splits_shared, s.pps_shared, hkv,
+                      (float*)(part + s.part_bytes + s.part_tile_bytes)};
+  return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
+    if (s.shared_items)
+      hipLaunchKernelGGL((k_kv8_group_shared<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.shared_items * hkv), s.splits_shared),
+                         dim3(256), 0, st, c, a);
+    hipLaunchKernelGGL((k_kv8_group_own_few<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.few_items * hkv), s.splits), dim3(256), 0,
+                       st, c, a);
+    if (s.tile_items)
+      hipLaunchKernelGGL((k_kv8_group_own_tile<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.tile_items * hkv), s.splits_tile),
+                         dim3(256), 0, st, c, a);
+    const int64_t items = (int64_t)n_rows * hq;
+    if (s.splits + s.splits_tile + s.splits_shared > 16)
+      hipLaunchKernelGGL((k_kv8_group_join<hd.value, decltype(t), 4>), dim3((uint32_t)items), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_kv8_group_join<hd.value, decltype(t), 1>), dim3((uint32_t)((items + 3) / 4)), dim3(256), 0, st, a);
   });
 }
 

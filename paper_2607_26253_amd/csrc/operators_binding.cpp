@@ -247,6 +247,53 @@ PyObject* kv8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+int32_t bound(PyObject* o, int64_t none, const char* what) {
+  int64_t n = none;
+  if (o != Py_None) {
+    n = PyLong_AsLongLong(o);
+    if (n == -1 && PyErr_Occurred()) throw PythonError{};
+  }
+  if (n != (int32_t)n) value_error(std::string(what) + " must be below 2^31");
+  return (int32_t)n;
+}
+
+// (k_cache, v_cache, k_exp, v_exp, d_q, d_out, d_pages, d_ctx, d_off, d_groups, d_shared, scale, max_ctx, max_shared, workspace)
+PyObject* kv8_group_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 15, [&] {
+    const at::Tensor &q = tensor(a[4], "q"), &out = tensor(a[5], "out");
+    const int32_t type = float_type(q, "q");
+    if (out.scalar_type() != q.scalar_type()) value_error("out must have q's dtype");
+    const Place at(q);
+    const sara_kv8_cache c = kv8_cache(a, at);
+    if (q.dim() != 3) value_error("q must be [rows, n_heads, head_dim]");
+    const int32_t n_rows = size32(q.size(0), "rows"), heads = size32(q.size(1), "heads");
+    const Rows rq = rows3(q, n_rows, heads, c.head_dim, at, "q"), ro = rows3(out, n_rows, heads, c.head_dim, at, "out");
+    const Seqs s = sequences(a[6], a[7], a[8], n_rows, at);
+    const at::Tensor &groups = tensor(a[9], "groups"), &shared = tensor(a[10], "shared");
+    for (const at::Tensor* t : {&groups, &shared}) {
+      if (t->dim() != 1 || t->scalar_type() != at::kInt || !t->is_contiguous())
+        value_error("groups [n_groups + 1] and shared [n_groups] must be contiguous int32");
+      at.check(*t, "groups and shared");
+    }
+    if (groups.numel() != shared.numel() + 1) value_error("groups must hold one element more than shared");
+    const int32_t n_groups = size32(shared.numel(), "groups");
+    const float scale = a[11] == Py_None ? (c.head_dim == 64 ? 0.125f : 0.08838834764831845f) : number(a[11]);
+    const int32_t max_ctx = bound(a[12], 16 * (int64_t)s.width, "max_ctx"), max_shared = bound(a[13], max_ctx, "max_shared");
+    int64_t need = 0;
+    int rc = sara_kv8_group_attention_workspace(c.n_kv_heads, c.head_dim, n_rows, heads, s.n, n_groups, s.off != nullptr, max_ctx,
+                                                max_shared, &need);
+    if (rc) return rc;
+    const Workspace ws = workspace(a[14], need, q, at);
+    void* st = at.stream();
+    rc = without_gil([&] {
+      return sara_kv8_group_attention(&c, rq.p, rq.row, rq.head, ro.p, ro.row, ro.head, type, n_rows, heads, s.pages, s.width, s.seq,
+                                      s.off, s.n, groups.data_ptr<int32_t>(), shared.data_ptr<int32_t>(), n_groups, max_ctx, max_shared,
+                                      scale, ws.p, ws.bytes, st);
+    });
+    return written(rc, {a[5]});
+  });
+}
+
 // [rows, vocab] with contiguous rows
 void check_logits(const at::Tensor& t, const Place& at, const char* what) {
   if (t.dim() != 2 || (stride_of(t, 1, 1) != 1 && t.numel())) value_error(std::string(what) + " must be [rows, vocab] with contiguous rows");
@@ -411,6 +458,7 @@ template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyCFunction f
 PyMethodDef methods[] = {{"kv8_write", fast<kv8_rows<true>>(), METH_FASTCALL, nullptr},
                          {"kv8_read", fast<kv8_rows<false>>(), METH_FASTCALL, nullptr},
                          {"kv8_attention", fast<kv8_attention>(), METH_FASTCALL, nullptr},
+                         {"kv8_group_attention", fast<kv8_group_attention>(), METH_FASTCALL, nullptr},
                          {"token_logprobs", fast<token_logprobs>(), METH_FASTCALL, nullptr},
                          {"token_logprobs_grad", fast<token_logprobs_grad>(), METH_FASTCALL, nullptr},
                          {"head_logprobs", fast<head_logprobs>(), METH_FASTCALL, nullptr},

@@ -976,6 +976,55 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
                               max_ctx, scale, d_out, o_row, o_head, d_ws, (hipStream_t)stream);
 }
 
+static int64_t group_bytes(const Kv8GroupSplit& s) { return s.part_bytes + s.part_tile_bytes + s.part_shared_bytes; }
+
+extern "C" int sara_kv8_group_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads, int32_t n_seqs,
+                                                  int32_t n_groups, int32_t ragged, int32_t max_ctx, int32_t max_shared,
+                                                  int64_t* bytes) {
+  if (!bytes) return einval("null argument");
+  if (n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128))
+    return einval("n_heads must be a multiple of n_kv_heads, head_dim 64 or 128");
+  if (n_rows < 0 || n_seqs < 0 || n_groups < 0 || max_ctx < 0 || max_ctx > kMaxCtx || max_shared < 0 || max_shared > kMaxCtx)
+    return einval("sizes must be >= 0, max_ctx and max_shared <= 2^30");
+  if ((int64_t)n_rows * n_heads > (int64_t)1 << 30) return einval("too many rows or sequences");
+  *bytes = n_rows == 0 || n_seqs == 0
+               ? 0 : group_bytes(kv8_group_split(n_rows, n_heads, n_kv_heads, head_dim, n_seqs, n_groups, max_ctx, max_shared, ragged != 0));
+  return SARA_OK;
+}
+
+extern "C" int sara_kv8_group_attention(const sara_kv8_cache* c, const void* d_q, int64_t q_row, int64_t q_head, void* d_out,
+                                        int64_t o_row, int64_t o_head, int32_t dtype, int32_t n_rows, int32_t n_heads,
+                                        const int32_t* d_pages, int32_t max_pages, const int32_t* d_ctx, const int32_t* d_off,
+                                        int32_t n_seqs, const int32_t* d_groups, const int32_t* d_shared, int32_t n_groups,
+                                        int32_t max_ctx, int32_t max_shared, float scale, void* d_ws, int64_t ws_bytes, void* stream) {
+  const std::string bad = kv8_bad(c, dtype, n_rows, d_pages, max_pages, d_ctx, d_off, n_seqs);
+  if (!bad.empty()) return einval(bad);
+  if (n_heads < 1 || n_heads % c->n_kv_heads) return einval("n_heads must be a multiple of n_kv_heads");
+  if (max_ctx < 0 || max_ctx > kMaxCtx || max_ctx > (int64_t)max_pages * kBlockTok)
+    return einval("max_ctx must be in [0, 16 * max_pages], at most 2^30");
+  if (max_shared < 0 || max_shared > kMaxCtx || max_shared > (int64_t)max_pages * kBlockTok)
+    return einval("max_shared must be in [0, 16 * max_pages], at most 2^30");
+  if (!(fabsf(scale) <= 2e38f)) return einval("scale must be finite, at most 2e38 in magnitude");
+  if (n_groups < 0) return einval("n_groups must be >= 0");
+  if (n_rows == 0 || n_seqs == 0) return SARA_OK;
+  if (!d_q || !d_out || (n_groups > 0 && (!d_groups || !d_shared))) return einval("null array");
+  if (rows_unaligned(d_q, q_row, q_head, dtype) || rows_unaligned(d_out, o_row, o_head, dtype))
+    return einval("q and out must be 16-byte aligned, with row and head strides that are multiples of 16 bytes");
+  if ((int64_t)n_rows * n_heads > (int64_t)1 << 30 || (int64_t)n_seqs * std::max(n_heads, 32 * c->n_kv_heads) > (int64_t)1 << 30)
+    return einval("too many rows or sequences");
+  if (rows_overlap(o_row, o_head, n_rows, n_heads, c->head_dim)) return einval("rows and heads of out must not overlap");
+  const Kv8GroupSplit split = kv8_group_split(n_rows, n_heads, c->n_kv_heads, c->head_dim, n_seqs, n_groups, max_ctx, max_shared,
+                                              d_off != nullptr);
+  if (std::max(std::max(split.few_items, split.tile_items), split.shared_items) * c->n_kv_heads > kMaxBlocks ||
+      (int64_t)n_rows * n_heads > kMaxBlocks)
+    return einval("too many rows or sequences");
+  const int64_t need = group_bytes(split);
+  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need)
+    return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
+  return launch_kv8_group_attention(*c, d_q, dtype, q_row, q_head, n_rows, n_heads, d_pages, max_pages, d_ctx, d_off, n_seqs, d_groups,
+                                    d_shared, n_groups, max_ctx, max_shared, scale, d_out, o_row, o_head, d_ws, (hipStream_t)stream);
+}
+
 // Largest vocabulary and most rows: the kernels' ids are 32-bit and run a grid's stride past the last, the launches' row
 // numbers a chunk.
 static constexpr int32_t kMaxVocab = 1 << 30, kMaxScoreRows = 1 << 30;

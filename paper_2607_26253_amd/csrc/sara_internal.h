@@ -326,6 +326,16 @@ int launch_kv8_rows(bool write, const sara_kv8_cache& c, void* k, void* v, int d
 int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows,
                          int hq, const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
                          int max_ctx, float scale, void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st);
+// The same for sequences in groups that share pages.
+struct Kv8GroupSplit {
+  int splits, pps, splits_tile, pps_tile, splits_shared, pps_shared;
+  int64_t few_items, tile_items, shared_items, part_bytes, part_tile_bytes, part_shared_bytes;
+};
+Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged);
+int launch_kv8_group_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows, int hq,
+                               const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
+                               const int32_t* groups, const int32_t* shared, int n_groups, int max_ctx, int max_shared, float scale,
+                               void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st);
 // launchers (token log probabilities)
 int64_t score_workspace(int n_rows, int V, int k);
 int launch_token_logprobs(const void* logits, int dtype, int64_t row_stride, int n_rows, int V, const int32_t* tok,
