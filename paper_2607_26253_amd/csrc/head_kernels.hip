@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sara_internal.h"
 
@@ -22,8 +23,16 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 // ---------------------------------------------------------------------------
 // products of 256 x 256 tiles
 // ---------------------------------------------------------------------------
-// An operand: element (r, c) of part i at p[i part + r stride + c].  fp32 numbers enter as sums of bf16 parts.
-struct Mat { const uint16_t* p; int64_t stride, part; };
+// An operand of a product over k, in parts (fp32 numbers enter as sums of bf16 parts):
+//   kPacked   [32 elements of k][16 rows] blocks of 1 KiB in fragment order: lane (row, grp) of the MFMA holds k 8 grp ..+7
+//   kPackedT  the same blocks, of the transpose: k runs over their rows
+//   kCols     element (k, m) at p[k stride + m]
+//   kRowPairs element (m, k) at p[m stride + k]; loaded 64 elements of k at a time, whole lines of memory
+enum { kPacked, kPackedT, kCols, kRowPairs };
+struct Mat {
+  const uint16_t* p;
+  int64_t stride, part;     // of kPacked and kPackedT: the 16-row tiles of a k block
+};
 
 // What a row needs for its D: 2^u (A + B u) + [v = tok] g
 struct HeadRow { float m, A, B, g; int32_t tok, on; };
@@ -33,7 +42,7 @@ struct HeadTile {
   int M, N, K;
   int n_pairs;              // the part pairs whose products are summed, 4 bits each (part of a, part of b << 2), smallest first
   uint32_t pairs;
-  int steps;                // 32-wide k steps of a split (blockIdx.y)
+  int steps;                // 32-wide k steps of a split
   int row0, m_parts;        // stats: row of the call's first, rows of a slice of `parts`
   int v0;                   // first vocabulary id of the N side
   float c, inv_t;
@@ -41,9 +50,9 @@ struct HeadTile {
   float* x_tok;
   float4* parts;            // [tile column][m_parts]: (m, s, t)
   const HeadRow* rows;
-  uint16_t* d;              // D [part][M, up to a tile][d_stride]
-  int64_t d_stride, d_part;
-  int d_parts;
+  uint16_t* d;              // D, packed: [part][32 ids][16 rows]
+  int64_t d_part;
+  int d_tiles, d_parts;     // 16-row tiles
   float* slab;              // [split][M][N]
   void* out;                // weight gradient
   int64_t out_stride;
@@ -54,41 +63,59 @@ __device__ __attribute__((aligned(16))) const uint32_t kZeroUnit[4] = {0, 0, 0, 
 
 enum { kStats, kGradRows, kSlab, kWeight };
 
-constexpr int kTileRing = 4;           // 32-wide k stages of 32 KiB
-struct TileShared {
-  u32x4 ring[kTileRing * 32 * 64];
-  float red[3][4][256];
+constexpr int kTileLds = 163840;       // all of a compute unit's
+constexpr int kTileThreads = 256;
+struct TileEpilogue {                  // in the ring's place once the products are done
+  float red[3][2][256];
   HeadRow rows[256];
 };
 
-// The softmax statistics of a block's tile: per row over its columns below `n_cols`.
-typedef f32x4 TileAcc[4][8];
+// One wave's quarter of a tile: acc[n][m] of lane (row, grp) is row 16 m + row, columns 16 n + 4 grp ..+3.  The 256
+// accumulators of a lane live in accumulation registers throughout; they are only touched by these.
+typedef f32x4 TileAcc[8][8];
+__device__ __forceinline__ void acc_zero(f32x4& a) {
+  asm volatile("v_accvgpr_write_b32 %0, 0\n\tv_accvgpr_write_b32 %1, 0\n\tv_accvgpr_write_b32 %2, 0\n\tv_accvgpr_write_b32 %3, 0"
+               : "=a"(a[0]), "=a"(a[1]), "=a"(a[2]), "=a"(a[3]));
+}
+__device__ __forceinline__ float acc_read(float a) {
+  float x;
+  asm("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(a));
+  return x;
+}
+__device__ __forceinline__ f32x4 acc_read4(const f32x4& a) {
+  return f32x4{acc_read(a[0]), acc_read(a[1]), acc_read(a[2]), acc_read(a[3])};
+}
+__device__ __forceinline__ void acc_mfma(f32x4& c, bf16x8 x, bf16x8 y) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(x), "v"(y));
+}
 
-// One wave's half of the rows (wm) and quarter of the columns (wn): acc[n][m] of lane (row, grp) is row 16 m + row, columns
-// 16 n + 4 grp ..+3.
-__device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, TileShared& lds, int tm0, int tn0, int bn) {
+// The softmax statistics of a block's tile: per row over its columns below N.
+__device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, TileEpilogue& lds, int tm0, int tn0, int bn) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
-  const int wm = wave >> 2, wn = wave & 3;
-  const int left = a.N - (tn0 + 64 * wn) - 4 * grp;        // columns of this lane's first quarter and on
-  const bool full = a.N - (tn0 + 64 * wn) >= 64;
+  const int wm = wave >> 1, wn = wave & 1;
+  const int left = a.N - (tn0 + 128 * wn) - 4 * grp;        // columns of this lane's first tile and on
+  const bool full = a.N - (tn0 + 128 * wn) >= 128;
 #pragma unroll
   for (int m = 0; m < 8; ++m) {
     const int r = 128 * wm + 16 * m + row;
-    const int at = lds.rows[r].tok - tn0 - 64 * wn;        // the row's id, if it is here
-    if (at >= 0 && at < 64 && (at >> 2 & 3) == grp && tm0 + r < a.M) {
+    f32x4 z[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) z[n] = acc_read4(acc[n][m]);
+    const int at = lds.rows[r].tok - tn0 - 128 * wn;        // the row's id, if it is here
+    if (at >= 0 && at < 128 && (at >> 2 & 3) == grp && tm0 + r < a.M) {
       float x = 0.f;
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
+      for (int n = 0; n < 8; ++n)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x = at >> 4 == n && (at & 3) == q ? acc[n][m][q] : x;
+        for (int q = 0; q < 4; ++q) x = at >> 4 == n && (at & 3) == q ? z[n][q] : x;
       a.x_tok[a.row0 + tm0 + r] = x;
     }
     float mx = -FLT_MAX, mn = FLT_MAX;
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+    for (int n = 0; n < 8; ++n)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        float x = acc[n][m][q];
+        float x = z[n][q];
         if (!full) x = 16 * n + q < left ? x : NAN;        // neither largest nor smallest
         mx = fmaxf(mx, x);
         mn = fminf(mn, x);
@@ -97,10 +124,10 @@ __device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, Tile
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     float s = mn == -INFINITY ? NAN : 0.f, t = 0.f;        // a logit that is not finite makes the row NaN
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+    for (int n = 0; n < 8; ++n)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        float u = (acc[n][m][q] - mx) * a.c;
+        float u = (z[n][q] - mx) * a.c;
         if (!full) u = 16 * n + q < left ? u : -INFINITY;
         const float e = __builtin_amdgcn_exp2f(u);
         s += e;
@@ -114,12 +141,11 @@ __device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, Tile
   }
   __syncthreads();
   const int r = threadIdx.x;
-  if (r >= 256 || tm0 + r >= a.M) return;
-  float m = lds.red[0][0][r], s = 0.f, t = 0.f;
+  if (tm0 + r >= a.M) return;
+  const float m = fmaxf(lds.red[0][0][r], lds.red[0][1][r]);
+  float s = 0.f, t = 0.f;
 #pragma unroll
-  for (int w = 1; w < 4; ++w) m = fmaxf(m, lds.red[0][w][r]);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < 2; ++w) {
     const float u = (lds.red[0][w][r] - m) * a.c, e = __builtin_amdgcn_exp2f(u);
     s = fmaf(e, lds.red[1][w][r], s);
     t += fmaf(e * fmaxf(u, -FLT_MAX), lds.red[1][w][r], e * lds.red[2][w][r]);
@@ -127,183 +153,279 @@ __device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, Tile
   a.parts[(size_t)bn * a.m_parts + tm0 + r] = make_float4(m, s, t, 0.f);
 }
 
-__device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileShared& lds, int tm0, int tn0) {
+// 32 ids of D lie in fragments in the order that leaves a lane's eight values together: place 8 g + 4 b + q holds id
+// 16 b + 4 g + q.  Products over ids take the other operand in that order, D^T gives its rows back.
+__device__ __forceinline__ int id_of_place(int p) { return 16 * (p >> 2 & 1) + 4 * (p >> 3) + (p & 3); }
+
+__device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileEpilogue& lds, int tm0, int tn0) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
-  const int wm = wave >> 2, wn = wave & 3;
-  const int col = tn0 + 64 * wn + 4 * grp;
+  const int wm = wave >> 1, wn = wave & 1;
+  const int col = tn0 + 128 * wn + 4 * grp;
+  const bool full = tn0 + 256 <= a.N;
 #pragma unroll
   for (int m = 0; m < 8; ++m) {
     const int r = 128 * wm + 16 * m + row;
     const HeadRow hr = lds.rows[r];
     const int at = hr.tok - a.v0 - col;                      // 16 n + q where it is this lane's
-    uint16_t* y = a.d + (int64_t)(tm0 + r) * a.d_stride + col;
+    uint16_t* y = a.d + ((int64_t)((tn0 >> 5) + 4 * wn) * a.d_tiles + ((tm0 + r) >> 4)) * 512 + lane * 8;
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      float f[4];
+    for (int j = 0; j < 4; ++j) {
+      float f[8];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
-        const float u = __builtin_amdgcn_fmed3f((acc[n][m][q] - hr.m) * a.c, -150.f, 0.f);
-        float e = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A);   // a row that met a NaN has it in A
-        e += at == 16 * n + q ? hr.g : 0.f;
-        f[q] = hr.on && col + 16 * n + q < a.N ? e : 0.f;
+      for (int b = 0; b < 2; ++b) {
+        const f32x4 z = acc_read4(acc[2 * j + b][m]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = 16 * (2 * j + b) + q;
+          // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
+          const float u = __builtin_amdgcn_fmed3f((z[q] - hr.m) * a.c, -150.f, 0.f);
+          float e = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A);   // a row that met a NaN has it in A
+          e += at == n ? hr.g : 0.f;
+          f[4 * b + q] = hr.on && (full || col + n < a.N) ? e : 0.f;
+        }
       }
       for (int p = 0; p < a.d_parts; ++p) {
-        uint32_t w0 = pack_bf16(f[0], f[1]), w1 = pack_bf16(f[2], f[3]);
-        asm("" : "+v"(w0), "+v"(w1));                        // what was rounded is what is subtracted
-        *(uint2*)(y + p * a.d_part + 16 * n) = make_uint2(w0, w1);
-        f[0] -= __uint_as_float(w0 << 16);
-        f[1] -= __uint_as_float(w0 & 0xFFFF0000u);
-        f[2] -= __uint_as_float(w1 << 16);
-        f[3] -= __uint_as_float(w1 & 0xFFFF0000u);
+        u32x4 w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t x = pack_bf16(f[2 * q], f[2 * q + 1]);
+          asm("" : "+v"(x));                                 // what was rounded is what is subtracted
+          f[2 * q] -= __uint_as_float(x << 16);
+          f[2 * q + 1] -= __uint_as_float(x & 0xFFFF0000u);
+          w[q] = x;
+        }
+        *(u32x4*)(y + p * a.d_part + (int64_t)j * a.d_tiles * 512) = w;
       }
     }
   }
 }
 
-// C[m][n] = sum over part pairs and k of a(m, k) b(n, k), 256 x 256 a block of 8 waves (v_mfma_f32_16x16x32_bf16, 128 x 64 a
-// wave), by the ring and the two groups of waves half a step apart of the tile GEMM of the models.  Operands go to LDS as they
-// lie in memory, 16 bytes a lane:
-//   COL false: a(m, k) is element (m, k).  A stage holds 32 elements of a row; the 16-byte units of a row are
-//              exchanged so that the fragments' reads meet different banks.
-//   COL true:  a(m, k) is element (k, m).  A stage holds 32 rows of 256 elements, and fragments are read transposed
-//              (ds_read_b64_tr_b16); units of 32 bytes are exchanged likewise.
-// Rows past the end repeat the last one and are dropped; k past the end is zero on both sides.
-template <bool ACOL, bool BCOL, int EPI>
-__global__ __launch_bounds__(512, 2) void k_head_tile(HeadTile a) {
-  constexpr int ST = kTileRing, FPW = 4;
-  __shared__ TileShared lds;
+// C[m][n] = sum over part pairs and k of a(m, k) b(n, k), 256 x 256 a block of 4 waves (v_mfma_f32_16x16x32_bf16, 128 x 128 a
+// wave).  Operands go straight to LDS, 16 bytes a lane, in 32-wide k stages: a ring of five for both, or (PAIRS: kRowPairs) of
+// four for a and of three 64-wide ones for b.  What limits the loads is how many lines they touch: 32-wide pieces of rows of
+// a row-major matrix took 0.67 us a stage and compute unit, whole lines 0.44, blocks 0.40 (the MFMAs of a stage: 0.43 at
+// 2.4 GHz).  In LDS the 16-byte units of a row (32-byte units of kCols) are exchanged so that the 16 lanes which a read
+// serves at a time meet different banks; fragments of operands that lie across k are read transposed
+// (ds_read_b64_tr_b16), k in the order of id_of_place.  Rows past the end repeat the last one and are dropped; k past the
+// end is zero on both sides.
+//
+// In step s the fragments of stage s are in registers; between its 64 MFMAs a wave reads those of stage s + 1 and sends for
+// later stages, into slots whose reads are over.  One barrier a step: before it a wave waits for its own loads of stage
+// s + 1, so all have landed behind it.  The loads are written in assembly: the compiler would wait for all of them
+// before each LDS read.
+template <int AK, int BK, int EPI>
+__global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
+  constexpr bool PAIRS = BK == kRowPairs;
+  constexpr int RA = PAIRS ? 4 : 5, A_SLOT = PAIRS ? 16384 : 32768;      // slots of a, their pitch
+  constexpr int RB = PAIRS ? 3 : 5, B_SLOT = 32768, B_AT = PAIRS ? 65536 : 16384;
+  constexpr int AHEAD = PAIRS ? 4 : 5;                                   // stages that a's loads run ahead
+  __shared__ __attribute__((aligned(1024))) char ring[kTileLds];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row = lane & 15, grp = lane >> 4;
-  const int wm = wave >> 2, wn = wave & 3;
-  // each XCD takes a contiguous stretch of an order that walks 4 row tiles by every column tile
-  int bn, bm;
+  const int wm = wave >> 1, wn = wave & 1;
+  // Each XCD takes a contiguous stretch of an order that walks 4 row tiles by every column tile, one split after the other
+  int bn, bm, split;
   {
-    const int nb = (a.N + 255) >> 8, mb = (a.M + 255) >> 8, total = nb * mb;
+    const int nb = (a.N + 255) >> 8, mb = (a.M + 255) >> 8, tiles = nb * mb, total = gridDim.x;
     const int x = blockIdx.x & 7, per = total >> 3, rem = total & 7;
-    const int lin = x * per + min(x, rem) + (blockIdx.x >> 3);
+    const int all = x * per + min(x, rem) + (blockIdx.x >> 3);
+    split = all / tiles;
+    const int lin = all - split * tiles;
     const int gs = 4 * nb, g = lin / gs, gm = min(4, mb - 4 * g), r = lin - g * gs;
     bm = 4 * g + r % gm;
     bn = r / gm;
   }
   const int tm0 = 256 * bm, tn0 = 256 * bn;
-  const int k_steps = (a.K + 31) >> 5, s0 = blockIdx.y * a.steps, ns = min(a.steps, k_steps - s0), total = ns * a.n_pairs;
-  if (EPI == kStats && threadIdx.x < 256) {
-    const int tok = tm0 + (int)threadIdx.x < a.M ? a.tok[a.row0 + tm0 + threadIdx.x] : -1;
-    lds.rows[threadIdx.x].tok = tok >= a.v0 && tok < a.v0 + a.N ? tok - a.v0 : -1;
-  }
-  if (EPI == kGradRows && threadIdx.x < 256) lds.rows[threadIdx.x] = a.rows[tm0 + threadIdx.x];
-  // this wave's 4 KiB of a stage, of one operand: where a lane's 16 bytes come from at k = 0
-  const bool is_b = wave >= 4;
-  const Mat mat = is_b ? a.b : a.a;
-  const int64_t k_stride = (is_b ? BCOL : ACOL) ? 32 * mat.stride : 32;
-  const uint16_t* from[FPW];
-  int k_of[FPW];
-#pragma unroll
-  for (int j = 0; j < FPW; ++j) {
-    const int f = (wave & 3) * FPW + j;
-    if (is_b ? BCOL : ACOL) {
+  const int k_steps = (a.K + 31) >> 5, s0 = split * a.steps, ns = min(a.steps, k_steps - s0), total = ns * a.n_pairs;
+  // A wave loads 4 KiB of either operand in a step: where a lane's 16 bytes come from at k = 0, and the k they hold
+  auto unit = [&](auto kind, const Mat& mat, int t0, int n, int f, int& k_of) {
+    k_of = 0;
+    if constexpr (kind.value == kPacked) return mat.p + ((t0 >> 4) + f) * 512 + lane * 8;
+    if constexpr (kind.value == kPackedT)
+      return mat.p + ((int64_t)min((t0 >> 5) + (f >> 1), ((n + 31) >> 5) - 1) * mat.stride + (f & 1)) * 512 + lane * 8;
+    if constexpr (kind.value == kCols) {
       const int kr = 2 * f + (lane >> 5), u = lane & 31;
-      const int sw = (kr & 3) | (kr >> 3 & 3) << 2;
-      const int at = (is_b ? tn0 : tm0) + 16 * ((u >> 1) ^ sw) + 8 * (u & 1);
-      from[j] = mat.p + kr * mat.stride + min(at, (((is_b ? a.N : a.M) + 7) & ~7) - 8);
-      k_of[j] = kr;
-    } else {
-      const int r = lane >> 2, u = (lane & 3) ^ (r >> 1 & 3) ^ (r >> 3);
-      from[j] = mat.p + (int64_t)min((is_b ? tn0 : tm0) + 16 * f + r, (is_b ? a.N : a.M) - 1) * mat.stride + 8 * u;
-      k_of[j] = 8 * u;
+      k_of = kr;
+      return mat.p + kr * mat.stride + min(t0 + 16 * ((u >> 1) ^ (kr & 15)) + 8 * (u & 1), n - 8);
     }
-  }
-  int i_pair = 0, i_step = 0;                              // the next stage to load
-  auto issue = [&](int slot) {
-    const int pair = a.pairs >> (4 * i_pair) & 15, ks = s0 + i_step;
-    const int64_t off = (is_b ? pair >> 2 : pair & 3) * mat.part + ks * k_stride;
-    const bool tail = 32 * (ks + 1) > a.K;
-#pragma unroll
-    for (int j = 0; j < FPW; ++j) {
-      const uint16_t* p = from[j] + off;
-      if (tail) p = 32 * ks + k_of[j] < a.K ? p : (const uint16_t*)kZeroUnit;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                       (__attribute__((address_space(3))) void*)&lds.ring[(slot * 32 + wave * FPW + j) * 64], 16, 0, 0);
-    }
-    // past the last stage it is loaded again, to a slot that nobody reads, so the count of loads in flight stays exact
-    if (i_pair * ns + i_step + 1 < total && ++i_step == ns) { i_step = 0; ++i_pair; }
+    const int r = 8 * f + (lane >> 3), u = (lane & 7) ^ (r >> 1 & 7);
+    k_of = 8 * u;
+    return mat.p + (int64_t)min(t0 + r, n - 1) * mat.stride + 8 * u;
   };
-  auto phase = [&]() {
+  constexpr std::integral_constant<int, AK> ak{};
+  constexpr std::integral_constant<int, BK> bk{};
+  const int64_t a_step = AK == kPacked ? a.a.stride * 512 : 1024;
+  const int64_t b_step = BK == kPacked ? a.b.stride * 512 : BK == kPackedT ? 1024 : BK == kCols ? 32 * a.b.stride : 64;
+  constexpr int BF = PAIRS ? 8 : 4;                        // loads of b that a wave keeps addresses of
+  const uint16_t *fa[4], *fb[BF];
+  int unused;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) fa[j] = unit(ak, a.a, tm0, a.M, 4 * wave + j, unused);
+#pragma unroll
+  for (int j = 0; j < BF; ++j) fb[j] = unit(bk, a.b, tn0, a.N, BF * wave + j, unused);
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+  auto load = [&](const uint16_t* p, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(ring_at + at), "v"(p));
+  };
+  // The next stage to load.  Past the last one it is loaded again, to slots that nobody reads, so that the count of loads
+  // in flight stays exact.
+  int i_pair = 0, i_step = 0, i_seen = 0;
+  bool tail = false;
+  int64_t a_off = 0, b_off = 0;
+  uint32_t a_slot = 0, b_slot = 0;
+  auto place = [&]() {
+    const int pair = a.pairs >> (4 * i_pair) & 15, ks = s0 + i_step;
+    a_off = (pair & 3) * a.a.part + ks * a_step;
+    b_off = (pair >> 2) * a.b.part + (PAIRS ? min(i_seen >> 1, (k_steps - 1) >> 1) : ks) * b_step;
+    // k that ends inside the stage, of the operands that are not padded with zeros
+    if constexpr (BK == kCols || BK == kRowPairs) {
+      constexpr int W = PAIRS ? 64 : 32;
+      const int k0 = (PAIRS ? min(i_seen >> 1, (k_steps - 1) >> 1) : ks) * W;
+      const bool ends = k0 + W > a.K;
+      if (ends || tail) {
+#pragma unroll
+        for (int j = 0; j < BF; ++j) {
+          int k;
+          const uint16_t* p = unit(bk, a.b, tn0, a.N, BF * wave + j, k);
+          fb[j] = k0 + k < a.K ? p : (const uint16_t*)kZeroUnit - b_off;
+        }
+      }
+      tail = ends;
+    }
+  };
+  auto next = [&]() {
+    ++i_seen;
+    if (i_pair * ns + i_step + 1 < total && ++i_step == ns) { i_step = 0; ++i_pair; }
+    a_slot = a_slot == (RA - 1) * A_SLOT ? 0 : a_slot + A_SLOT;
+    if (!PAIRS || !(i_seen & 1)) b_slot = b_slot == (RB - 1) * B_SLOT ? 0 : b_slot + B_SLOT;
+    place();
+  };
+  // With pairs, the b of stages s + 4 and s + 5 goes with steps s and s + 1 (s even): half of its rows each
+  auto send_b = [&](int j, int half) { load(fb[4 * half + j] + b_off, B_AT + b_slot + (BF * wave + 4 * half + j) * 1024); };
+  auto send_a = [&](int j) { load(fa[j] + a_off, a_slot + (4 * wave + j) * 1024); };
+  typedef __attribute__((address_space(3))) s16x4* Lds8;
+  // byte address of fragment i of this wave's half of an operand; of those read transposed, the part with k below 16.  The
+  // 16 columns of a transposed b's fragments 2 j and 2 j + 1 are fours of 32 in turn, so that a lane's results are eight in a row.
+  auto address = [&](auto kind, bool b, int i) {
+    const int t = 8 * (b ? wn : wm) + i;
+    if constexpr (kind.value == kPacked) return t * 1024 + (row + 16 * grp) * 16;
+    const int c = b ? (row & 3) * 16 + (t & 1) * 8 : (row & 3) * 8 + (t & 1) * 32;   // byte of 32 columns
+    if constexpr (kind.value == kPackedT) return (t >> 1) * 2048 + (c >> 4) * 256 + (4 * grp + (row >> 2)) * 16 + (c & 15);
+    const int k = 4 * grp + (row >> 2);
+    if constexpr (kind.value == kCols) return k * 512 + ((((t & ~1) + (c >> 5)) ^ k) * 32) + (c & 31);
+    return (16 * t + row) * 128;
+  };
+  s16x4 lo;
+  auto read = [&](auto kind, bool b, uint32_t slot, int i, int part, int half, bf16x8& f) {
+    const char* p = ring + slot + address(kind, b, i);
+    if constexpr (kind.value == kPacked) {
+      if (part == 0) f = __builtin_bit_cast(bf16x8, *(const u32x4*)p);
+    } else if constexpr (kind.value == kRowPairs) {
+      if (part == 0) f = __builtin_bit_cast(bf16x8, *(const u32x4*)(p + (((4 * half + grp) ^ (row >> 1)) * 16)));
+    } else if (part == 0) {
+      lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds8)(const s16x4*)p);
+    } else {
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds8)(const s16x4*)(p + (kind.value == kPackedT ? 1024 : 8192)));
+      f = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
+  auto barrier = [&]() {
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  // fragment i of 16 rows of an operand: byte addresses in a slot
-  const int sw_row = (row * 4 + (grp ^ (row >> 1 & 3) ^ (row >> 3))) * 16;
-  const int sw_col = (8 * grp + (row >> 2)) * 512 + (row & 3) * 8, sw_xor = ((row >> 2) | grp << 2) * 32;
-  auto fragment = [&](int slot, bool b, bool col, int i) {
-    const char* base = (const char*)lds.ring + (slot * 32 + (b ? 16 : 0)) * 1024;
-    if (!col) return __builtin_bit_cast(bf16x8, *(const u32x4*)(base + sw_row + i * 1024));
-    typedef __attribute__((address_space(3))) s16x4* Lds;
-    const char* p = base + sw_col + ((32 * i) ^ sw_xor);
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(const s16x4*)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(const s16x4*)(p + 4 * 512));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-  };
   TileAcc acc;
 #pragma unroll
-  for (int n = 0; n < 4; ++n)
+  for (int n = 0; n < 8; ++n)
 #pragma unroll
-    for (int m = 0; m < 8; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-  __syncthreads();                                         // the rows; no load of the ring is in flight yet
+    for (int m = 0; m < 8; ++m) acc_zero(acc[n][m]);
+  bf16x8 wf[2][8], xf[2][8];
+  place();
 #pragma unroll
-  for (int s = 0; s < ST - 1; ++s) issue(s);
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((ST - 2) * FPW) : "memory");   // stage 0 has landed
-  phase();
-  if (wave >= 4) phase();                                  // the second group runs one phase behind
-  for (int s = 0; s < total; ++s) {
-    bf16x8 wf[4], xf[8];
+  for (int s = 0; s < AHEAD; ++s) {
 #pragma unroll
-    for (int n = 0; n < 4; ++n) wf[n] = fragment(s % ST, true, BCOL, 4 * wn + n);
+    for (int j = 0; j < 4; ++j) send_b(j, PAIRS ? s & 1 : 0);
 #pragma unroll
-    for (int m = 0; m < 8; ++m) xf[m] = fragment(s % ST, false, ACOL, 8 * wm + m);
-    issue((s + ST - 1) % ST);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((ST - 2) * FPW) : "memory");   // stage s + 1 has landed
-    phase();
-#pragma unroll
-    for (int m = 0; m < 8; ++m)
-#pragma unroll
-      for (int n = 0; n < 4; ++n) acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[n], xf[m], acc[n][m], 0, 0, 0);
-    phase();
+    for (int j = 0; j < 4; ++j) send_a(j);
+    next();
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the repeated loads, before the block gives its LDS back
-  if (wave < 4) phase();
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PAIRS ? 20 : 32) : "memory");   // stage 0 has landed
+  barrier();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    read(bk, true, B_AT, i, 0, 0, wf[0][i]);
+    read(bk, true, B_AT, i, 1, 0, wf[0][i]);
+    read(ak, false, 0, i, 0, 0, xf[0][i]);
+    read(ak, false, 0, i, 1, 0, xf[0][i]);
+  }
+  uint32_t a_read = A_SLOT, b_read = PAIRS ? 0 : B_SLOT;   // the slots of stage s + 1
+  auto step = [&](auto par) {
+    constexpr int P = par.value;                           // s & 1
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PAIRS ? (P ? 12 : 16) : 24) : "memory");
+    barrier();
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        acc_mfma(acc[n][i], wf[P][n], xf[P][i]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (n < 2) read(bk, true, B_AT + b_read, i, n, P ^ 1, wf[P ^ 1][i]);
+        else if (n < 4) read(ak, false, a_read, i, n - 2, 0, xf[P ^ 1][i]);
+        else if (n == 5) { if (i < 4) send_b(i, PAIRS ? P : 0); else send_a(i - 4); }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    a_read = a_read == (RA - 1) * A_SLOT ? 0 : a_read + A_SLOT;
+    if (!PAIRS || P == 0) b_read = b_read == (RB - 1) * B_SLOT ? 0 : b_read + B_SLOT;
+    next();
+  };
+  for (int s = 0; s < total; s += 2) {
+    step(std::integral_constant<int, 0>{});
+    if (s + 1 < total) step(std::integral_constant<int, 1>{});
+  }
+  // the repeated loads, and the results on their way to the accumulators
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+  barrier();
+  TileEpilogue& lds = *(TileEpilogue*)ring;
   if constexpr (EPI == kStats) {
+    const int tok = tm0 + (int)threadIdx.x < a.M ? a.tok[a.row0 + tm0 + threadIdx.x] : -1;
+    lds.rows[threadIdx.x].tok = tok >= a.v0 && tok < a.v0 + a.N ? tok - a.v0 : -1;
+    __syncthreads();
     tile_stats(acc, a, lds, tm0, tn0, bn + (a.v0 >> 8));
   } else if constexpr (EPI == kGradRows) {
+    lds.rows[threadIdx.x] = a.rows[tm0 + threadIdx.x];
+    __syncthreads();
     tile_grad(acc, a, lds, tm0, tn0);
   } else {
-    const int col = tn0 + 64 * wn + 4 * grp;
+    const int c0 = tn0 + 128 * wn + 8 * grp;
 #pragma unroll
     for (int m = 0; m < 8; ++m) {
-      const int r = tm0 + 128 * wm + 16 * m + row;
+      const int p = 16 * (m & 1) + row;
+      const int r = tm0 + 128 * wm + (EPI == kWeight ? 32 * (m >> 1) + id_of_place(p) : 16 * m + row);
       if (r >= a.M) continue;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        if (col + 16 * n >= a.N) continue;                 // N is a multiple of 8
-        f32x4 v = acc[n][m];
-        if (EPI == kWeight) v *= a.inv_t;
+      for (int j = 0; j < 4; ++j) {
+        const int col = c0 + 32 * j;
+        if (col >= a.N) continue;                          // N is a multiple of 4
+        f32x4 v[2] = {acc_read4(acc[2 * j][m]), acc_read4(acc[2 * j + 1][m])};
+        if (EPI == kWeight) { v[0] *= a.inv_t; v[1] *= a.inv_t; }
         if (EPI == kSlab || a.out_f32) {
-          f32x4* y = (f32x4*)(EPI == kSlab ? a.slab + ((int64_t)blockIdx.y * a.M + r) * a.N + col + 16 * n
-                                           : (float*)a.out + r * a.out_stride + col + 16 * n);
-          if (a.add) v += *y;
-          *y = v;
-        } else {
-          uint2* y = (uint2*)((uint16_t*)a.out + r * a.out_stride + col + 16 * n);
-          if (a.add) {
-            const uint2 w = *y;
-            v += f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
-                       __uint_as_float(w.y & 0xFFFF0000u)};
+          f32x4* y = (f32x4*)(EPI == kSlab ? a.slab + ((int64_t)split * a.M + r) * a.N + col : (float*)a.out + r * a.out_stride + col);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (col + 4 * h >= a.N) continue;
+            if (a.add) v[h] += y[h];
+            y[h] = v[h];
           }
-          *y = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        } else {
+          u32x4* y = (u32x4*)((uint16_t*)a.out + r * a.out_stride + col);   // bf16: N is a multiple of 8
+          if (a.add) {
+            const u32x4 w = *y;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q >> 2][q & 3] += __uint_as_float(q & 1 ? w[q >> 1] & 0xFFFF0000u : w[q >> 1] << 16);
+          }
+          *y = u32x4{pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]), pack_bf16(v[1][2], v[1][3])};
         }
       }
     }
@@ -484,36 +606,47 @@ __global__ __launch_bounds__(256) void k_head_join(const float4* __restrict__ pa
 // ---------------------------------------------------------------------------
 // operands
 // ---------------------------------------------------------------------------
-// Rows of a matrix as P bf16 parts [part][rows_out][width]: rows past the end, and those of `rows` that are off, are 0.
+// Rows of a matrix packed, as P bf16 parts: rows past the end, those of `rows` that are off and elements past d are 0.  A block
+// takes 16 rows, a wave 32 elements of k at a time.
 template <typename T, int P>
-__global__ __launch_bounds__(256) void k_head_parts(const T* __restrict__ x, int64_t stride, int n_rows, int d,
-    const HeadRow* __restrict__ rows, uint16_t* __restrict__ y, int rows_out, int width) {
-  const int r = blockIdx.x;
+__global__ __launch_bounds__(256) void k_head_pack(const T* __restrict__ x, int64_t stride, int n_rows, int d,
+    const HeadRow* __restrict__ rows, uint16_t* __restrict__ y, int tiles, int k_blocks) {
+  const int lane = threadIdx.x & 63, r = blockIdx.x * 16 + (lane & 15);
   const bool have = r < n_rows && (!rows || rows[r].on);
-  for (int i = 4 * threadIdx.x; i < width; i += 1024) {
-    float f[4] = {0.f, 0.f, 0.f, 0.f};
-    if (have && i < d) {
+  for (int kb = blockIdx.y * 4 + (threadIdx.x >> 6); kb < k_blocks; kb += 4 * gridDim.y) {
+    const int k = 32 * kb + 8 * (lane >> 4);
+    float f[8] = {};
+    if (have) {
       if constexpr (sizeof(T) == 2) {
-        const uint2 w = *(const uint2*)(x + r * stride + i);
-        f[0] = __uint_as_float(w.x << 16);
-        f[1] = __uint_as_float(w.x & 0xFFFF0000u);
-        f[2] = __uint_as_float(w.y << 16);
-        f[3] = __uint_as_float(w.y & 0xFFFF0000u);
+        if (k < d) {
+          const u32x4 w = *(const u32x4*)(x + r * stride + k);
+          if (P == 1) {
+            *(u32x4*)(y + ((int64_t)kb * tiles + blockIdx.x) * 512 + lane * 8) = w;
+            continue;
+          }
+        }
       } else {
-        const f32x4 w = *(const f32x4*)(x + r * stride + i);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) f[q] = w[q];
+        for (int h = 0; h < 2; ++h)
+          if (k + 4 * h < d) {                             // d is a multiple of 4
+            const f32x4 w = *(const f32x4*)(x + r * stride + k + 4 * h);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) f[4 * h + q] = w[q];
+          }
       }
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      uint32_t w0 = pack_bf16(f[0], f[1]), w1 = pack_bf16(f[2], f[3]);
-      asm("" : "+v"(w0), "+v"(w1));
-      *(uint2*)(y + ((int64_t)p * rows_out + r) * width + i) = make_uint2(w0, w1);
-      f[0] -= __uint_as_float(w0 << 16);
-      f[1] -= __uint_as_float(w0 & 0xFFFF0000u);
-      f[2] -= __uint_as_float(w1 << 16);
-      f[3] -= __uint_as_float(w1 & 0xFFFF0000u);
+      u32x4 w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t v = pack_bf16(f[2 * q], f[2 * q + 1]);
+        asm("" : "+v"(v));
+        f[2 * q] -= __uint_as_float(v << 16);
+        f[2 * q + 1] -= __uint_as_float(v & 0xFFFF0000u);
+        w[q] = v;
+      }
+      *(u32x4*)(y + (((int64_t)p * k_blocks + kb) * tiles + blockIdx.x) * 512 + lane * 8) = w;
     }
   }
 }
@@ -575,7 +708,7 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
   const bool f32 = dtype == SARA_F32;
   const int cols = (V + 255) / 256;
   auto take = [&](int64_t bytes) { const int64_t at = p.bytes; p.bytes += up(bytes, 256); return at; };
-  p.width = (int)up(d, 8);
+  p.width = (int)up(d, 32);
   if (!grad) {
     p.few = n_rows <= kFewRows;
     p.x_tok = take(4 * (int64_t)n_rows);
@@ -587,13 +720,9 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
     }
     p.rows_out = (int)up(n_rows, 256);
     p.parts = take(16 * (int64_t)std::min(p.rows_out, kStatRows) * cols);
-    if (f32) {
-      p.piece = (int)std::min<int64_t>(cols, std::max<int64_t>(1, kPieceBytes / (6 * 256 * (int64_t)p.width)));
-      p.h_parts = take(6 * (int64_t)p.rows_out * p.width);
-      p.w_parts = take(6 * 256 * (int64_t)p.piece * p.width);
-    } else {
-      p.piece = cols;
-    }
+    p.h_parts = take((f32 ? 6 : 2) * (int64_t)p.rows_out * p.width);
+    p.piece = f32 ? (int)std::min<int64_t>(cols, std::max<int64_t>(1, kPieceBytes / (6 * 256 * (int64_t)p.width))) : cols;
+    if (f32) p.w_parts = take(6 * 256 * (int64_t)p.piece * p.width);
     return p;
   }
   p.rows_out = (int)up(n_rows, 256);
@@ -630,7 +759,18 @@ static int head_done(const char* what) {
   return e == hipSuccess ? SARA_OK : hip_fail(e, what);
 }
 
-static dim3 tile_grid(const HeadTile& t) { return dim3(((t.M + 255) / 256) * ((t.N + 255) / 256), (((t.K + 31) / 32) + t.steps - 1) / t.steps); }
+static dim3 tile_grid(const HeadTile& t) {
+  return dim3(((t.M + 255) / 256) * ((t.N + 255) / 256) * ((((t.K + 31) / 32) + t.steps - 1) / t.steps));
+}
+
+// packed into rows_out rows (a multiple of 16) of `width` elements (of 32)
+static void pack(bool f32, const void* x, int64_t stride, int n_rows, int d, const HeadRow* rows, uint16_t* y, int rows_out, int width,
+                 hipStream_t st) {
+  const int tiles = rows_out / 16, blocks = width / 32;
+  const dim3 grid(tiles, std::max(1, std::min((blocks + 3) / 4, 2048 / tiles)));
+  if (f32) hipLaunchKernelGGL((k_head_pack<float, 3>), grid, dim3(256), 0, st, (const float*)x, stride, n_rows, d, rows, y, tiles, blocks);
+  else hipLaunchKernelGGL((k_head_pack<uint16_t, 1>), grid, dim3(256), 0, st, (const uint16_t*)x, stride, n_rows, d, rows, y, tiles, blocks);
+}
 
 int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype, int n_rows, int d, int V,
                          const int32_t* tok, float temp, float* logp, float* entropy, float* stats, void* ws, hipStream_t st) {
@@ -657,9 +797,8 @@ int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t
   }
   const bool f32 = dtype == SARA_F32;
   uint16_t *hp = (uint16_t*)((char*)ws + p.h_parts), *wp = (uint16_t*)((char*)ws + p.w_parts);
-  if (f32)
-    hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(p.rows_out), dim3(256), 0, st, (const float*)h, h_stride, n_rows, d, nullptr, hp,
-                       p.rows_out, p.width);
+  const int h_tiles = p.rows_out / 16, w_tiles = 16 * p.piece;
+  pack(f32, h, h_stride, n_rows, d, nullptr, hp, p.rows_out, p.width, st);
   const int cols = (V + 255) / 256;
   for (int row0 = 0; row0 < n_rows; row0 += kStatRows) {
     const int M = std::min(kStatRows, n_rows - row0);
@@ -668,22 +807,10 @@ int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t
       t.v0 = 256 * c0;
       t.M = M;
       t.N = std::min(V - t.v0, 256 * p.piece);
-      if (f32) {
-        if (row0 == 0 || p.piece < cols)
-          hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(t.N), dim3(256), 0, st, (const float*)w + t.v0 * w_stride, w_stride, t.N, d,
-                             nullptr, wp, 256 * p.piece, p.width);
-        t.a = Mat{hp + (int64_t)row0 * p.width, p.width, (int64_t)p.rows_out * p.width};
-        t.b = Mat{wp, p.width, 256 * (int64_t)p.piece * p.width};
-        t.K = p.width;
-        t.n_pairs = 6;
-        t.pairs = kPairs3;
-      } else {
-        t.a = Mat{(const uint16_t*)h + row0 * h_stride, h_stride, 0};
-        t.b = Mat{(const uint16_t*)w + t.v0 * w_stride, w_stride, 0};
-        t.K = d;
-        t.n_pairs = 1;
-        t.pairs = kPairs1;
-      }
+      t.a = Mat{hp + (int64_t)row0 / 16 * 512, h_tiles, (int64_t)p.rows_out * p.width};
+      t.K = f32 ? p.width : d;
+      t.n_pairs = f32 ? 6 : 1;
+      t.pairs = f32 ? kPairs3 : kPairs1;
       t.steps = (t.K + 31) / 32;
       t.row0 = row0;
       t.m_parts = std::min(p.rows_out, kStatRows);
@@ -691,7 +818,15 @@ int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t
       t.tok = tok;
       t.x_tok = x_tok;
       t.parts = parts;
-      hipLaunchKernelGGL((k_head_tile<false, false, kStats>), tile_grid(t), dim3(512), 0, st, t);
+      if (f32) {
+        if (row0 == 0 || p.piece < cols)
+          pack(true, (const float*)w + t.v0 * w_stride, w_stride, t.N, d, nullptr, wp, 256 * p.piece, p.width, st);
+        t.b = Mat{wp, w_tiles, 256 * (int64_t)p.piece * p.width};
+        hipLaunchKernelGGL((k_head_tile<kPacked, kPacked, kStats>), tile_grid(t), dim3(kTileThreads), 0, st, t);
+      } else {
+        t.b = Mat{(const uint16_t*)w + t.v0 * w_stride, w_stride, 0};
+        hipLaunchKernelGGL((k_head_tile<kPacked, kRowPairs, kStats>), tile_grid(t), dim3(kTileThreads), 0, st, t);
+      }
     }
     hipLaunchKernelGGL((k_head_join<16>), dim3((M + 15) / 16), dim3(256), 0, st, parts, cols, std::min(p.rows_out, kStatRows), row0, M, V,
                        tok, x_tok, c, inv_t, logp, entropy, stats);
@@ -718,31 +853,24 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
   HeadRow* rows = (HeadRow*)at(p.rows);
   uint16_t *D = (uint16_t*)at(p.d), *hp = (uint16_t*)at(p.h_parts), *wp = (uint16_t*)at(p.w_parts);
   float* slab = (float*)at(p.slab);
-  const int64_t h_part = (int64_t)p.rows_out * p.width, w_part = 256 * (int64_t)p.piece * p.width;
   hipLaunchKernelGGL(k_head_rows, dim3(p.rows_out / 256), dim3(256), 0, st, n_rows, p.rows_out, V, tok, stats, entropy, g_logp, g_ent,
                      scale, rows);
-  if (f32)
-    hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(p.rows_out), dim3(256), 0, st, (const float*)h, h_stride, n_rows, d, rows, hp,
-                       p.rows_out, p.width);
-  else if (gw)
-    hipLaunchKernelGGL((k_head_parts<uint16_t, 1>), dim3(p.rows_out), dim3(256), 0, st, (const uint16_t*)h, h_stride, n_rows, d, rows, hp,
-                       p.rows_out, p.width);
-  const int cols = (V + 255) / 256;
+  pack(f32, h, h_stride, n_rows, d, rows, hp, p.rows_out, p.width, st);
+  const int cols = (V + 255) / 256, tiles = p.rows_out / 16;
+  const Mat hm = {hp, tiles, (int64_t)p.rows_out * p.width}, dm = {D, tiles, 256 * (int64_t)p.piece * p.rows_out};
+  auto go = [&](auto kernel, const HeadTile& t) { hipLaunchKernelGGL(kernel, tile_grid(t), dim3(kTileThreads), 0, st, t); };
   for (int c0 = 0; c0 < cols; c0 += p.piece) {
     const int v0 = 256 * c0, N = std::min(V - v0, 256 * p.piece);
     Mat wm = {(const uint16_t*)w + v0 * w_stride, w_stride, 0};
     if (f32) {
-      hipLaunchKernelGGL((k_head_parts<float, 3>), dim3(N), dim3(256), 0, st, (const float*)w + v0 * w_stride, w_stride, N, d, nullptr, wp,
-                         256 * p.piece, p.width);
-      wm = Mat{wp, p.width, w_part};
+      pack(true, (const float*)w + v0 * w_stride, w_stride, N, d, nullptr, wp, 256 * p.piece, p.width, st);
+      wm = Mat{wp, 16 * p.piece, 256 * (int64_t)p.piece * p.width};
     }
-    const Mat hm = {hp, p.width, h_part};
-    const Mat dm = {D, 256 * (int64_t)p.piece, 256 * (int64_t)p.piece * p.rows_out};
     HeadTile t = {};
     t.v0 = v0;
     t.M = n_rows;
     t.N = N;
-    t.a = f32 ? hm : Mat{(const uint16_t*)h, h_stride, 0};
+    t.a = hm;
     t.b = wm;
     t.K = f32 ? p.width : d;
     t.n_pairs = f32 ? 6 : 1;
@@ -751,10 +879,11 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
     t.c = c;
     t.rows = rows;
     t.d = D;
-    t.d_stride = dm.stride;
+    t.d_tiles = tiles;
     t.d_part = dm.part;
     t.d_parts = p.d_parts;
-    hipLaunchKernelGGL((k_head_tile<false, false, kGradRows>), tile_grid(t), dim3(512), 0, st, t);
+    if (f32) go(k_head_tile<kPacked, kPacked, kGradRows>, t);
+    else go(k_head_tile<kPacked, kRowPairs, kGradRows>, t);
     if (gh) {
       HeadTile x = {};
       x.a = dm;
@@ -767,7 +896,8 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
       x.steps = ((N + 31) / 32 + p.splits - 1) / p.splits;
       x.slab = slab;
       x.add = c0 > 0;
-      hipLaunchKernelGGL((k_head_tile<false, true, kSlab>), tile_grid(x), dim3(512), 0, st, x);
+      if (f32) go(k_head_tile<kPacked, kPackedT, kSlab>, x);
+      else go(k_head_tile<kPacked, kCols, kSlab>, x);
     }
     if (gw) {
       HeadTile x = {};
@@ -784,7 +914,7 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
       x.out_stride = gw_stride;
       x.out_f32 = gw_f32;
       x.add = accumulate;
-      hipLaunchKernelGGL((k_head_tile<true, true, kWeight>), tile_grid(x), dim3(512), 0, st, x);
+      go(k_head_tile<kPackedT, kPackedT, kWeight>, x);
     }
   }
   if (gh) {
