@@ -8,6 +8,7 @@
 //              accepted temperature takes neither out of the range of fp32
 // 8 N d V operations a training step where 6 would do with the logits kept: 2 against [rows][vocab] written and read.
 #include <float.h>
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -264,45 +265,62 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
 #pragma unroll
   for (int j = 0; j < BF; ++j) fb[j] = unit(bk, a.b, tn0, a.N, BF * wave + j, unused);
   const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
-  auto load = [&](const uint16_t* p, uint32_t at) {
+  auto load = [&](const char* p, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(ring_at + at), "v"(p));
   };
-  // The next stage to load.  Past the last one it is loaded again, to slots that nobody reads, so that the count of loads
-  // in flight stays exact.
-  int i_pair = 0, i_step = 0, i_seen = 0;
+  // The next stage to load.  For `run` stages the addresses only grow; then comes k that ends inside a stage or the next pair
+  // of parts.  Past the last stage it is loaded again, to slots that nobody reads, so that the count of loads in flight
+  // stays exact.
+  int i_pair = 0, i_step = 0, i_seen = 0, run = 0;
   bool tail = false;
-  int64_t a_off = 0, b_off = 0;
+  int64_t a_at = 0, b_at = 0, a_grow = 2 * a_step, b_grow = 2 * b_step;   // added to the addresses, in bytes
   uint32_t a_slot = 0, b_slot = 0;
   auto place = [&]() {
     const int pair = a.pairs >> (4 * i_pair) & 15, ks = s0 + i_step;
-    a_off = (pair & 3) * a.a.part + ks * a_step;
-    b_off = (pair >> 2) * a.b.part + (PAIRS ? min(i_seen >> 1, (k_steps - 1) >> 1) : ks) * b_step;
-    // k that ends inside the stage, of the operands that are not padded with zeros
-    if constexpr (BK == kCols || BK == kRowPairs) {
+    const int kb = PAIRS ? i_seen >> 1 : ks;
+    a_at = 2 * ((pair & 3) * a.a.part + ks * a_step);
+    b_at = 2 * ((pair >> 2) * a.b.part + kb * b_step);
+    run = ns - 1 - i_step;
+    if constexpr (BK == kCols || BK == kRowPairs) {        // not padded with zeros
       constexpr int W = PAIRS ? 64 : 32;
-      const int k0 = (PAIRS ? min(i_seen >> 1, (k_steps - 1) >> 1) : ks) * W;
-      const bool ends = k0 + W > a.K;
+      const bool ends = W * (kb + 1) > a.K;
       if (ends || tail) {
 #pragma unroll
         for (int j = 0; j < BF; ++j) {
           int k;
           const uint16_t* p = unit(bk, a.b, tn0, a.N, BF * wave + j, k);
-          fb[j] = k0 + k < a.K ? p : (const uint16_t*)kZeroUnit - b_off;
+          fb[j] = W * kb + k < a.K ? p : (const uint16_t*)((const char*)kZeroUnit - b_at);
         }
       }
       tail = ends;
+      const int full = a.K / W;                            // stages (or pairs) before the one that ends inside
+      if (!ends) run = min(run, (PAIRS ? 2 * full - i_seen : full - ks) - 1);
     }
   };
-  auto next = [&]() {
-    ++i_seen;
-    if (i_pair * ns + i_step + 1 < total && ++i_step == ns) { i_step = 0; ++i_pair; }
+  auto grow = [&](int odd) {                               // odd: of the stage just sent
     a_slot = a_slot == (RA - 1) * A_SLOT ? 0 : a_slot + A_SLOT;
-    if (!PAIRS || !(i_seen & 1)) b_slot = b_slot == (RB - 1) * B_SLOT ? 0 : b_slot + B_SLOT;
-    place();
+    if (!PAIRS || odd) b_slot = b_slot == (RB - 1) * B_SLOT ? 0 : b_slot + B_SLOT;
+    a_at += a_grow;
+    if (!PAIRS || odd) b_at += b_grow;
+  };
+  auto plain = [&](int n) { run -= n; i_step += n; i_seen += n; };   // n stages were sent so
+  auto next = [&](int odd) {
+    grow(odd);
+    if (run > 0) { plain(1); return; }
+    ++i_seen;
+    if (i_pair * ns + i_step + 1 < total) {
+      if (++i_step == ns) { i_step = 0; ++i_pair; }
+      place();
+    } else if (a_grow != 0) {                              // that was the last
+      a_at -= a_grow;
+      if (!PAIRS || odd) b_at -= b_grow;
+      a_grow = b_grow = 0;
+      run = INT_MAX;
+    }
   };
   // With pairs, the b of stages s + 4 and s + 5 goes with steps s and s + 1 (s even): half of its rows each
-  auto send_b = [&](int j, int half) { load(fb[4 * half + j] + b_off, B_AT + b_slot + (BF * wave + 4 * half + j) * 1024); };
-  auto send_a = [&](int j) { load(fa[j] + a_off, a_slot + (4 * wave + j) * 1024); };
+  auto send_b = [&](int j, int half) { load((const char*)fb[4 * half + j] + b_at, B_AT + b_slot + (BF * wave + 4 * half + j) * 1024); };
+  auto send_a = [&](int j) { load((const char*)fa[j] + a_at, a_slot + (4 * wave + j) * 1024); };
   typedef __attribute__((address_space(3))) s16x4* Lds8;
   // byte address of fragment i of this wave's half of an operand; of those read transposed, the part with k below 16.  The
   // 16 columns of a transposed b's fragments 2 j and 2 j + 1 are fours of 32 in turn, so that a lane's results are eight in a row.
@@ -349,7 +367,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
     for (int j = 0; j < 4; ++j) send_b(j, PAIRS ? s & 1 : 0);
 #pragma unroll
     for (int j = 0; j < 4; ++j) send_a(j);
-    next();
+    next(s & 1);
   }
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PAIRS ? 20 : 32) : "memory");   // stage 0 has landed
   barrier();
@@ -361,9 +379,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
     read(ak, false, 0, i, 1, 0, xf[0][i]);
   }
   uint32_t a_read = A_SLOT, b_read = PAIRS ? 0 : B_SLOT;   // the slots of stage s + 1
-  auto step = [&](auto par) {
+  auto step = [&](auto par, auto is_plain) {
     constexpr int P = par.value;                           // s & 1
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PAIRS ? (P ? 12 : 16) : 24) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PAIRS ? (P ? 9 : 16) : 24) : "memory");
     barrier();
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -373,16 +391,27 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
         __builtin_amdgcn_sched_barrier(0);
         if (n < 2) read(bk, true, B_AT + b_read, i, n, P ^ 1, wf[P ^ 1][i]);
         else if (n < 4) read(ak, false, a_read, i, n - 2, 0, xf[P ^ 1][i]);
-        else if (n == 5) { if (i < 4) send_b(i, PAIRS ? P : 0); else send_a(i - 4); }
+        else if (i < 4 && n == 5) send_b(i, PAIRS ? P : 0);
+        else if (i < 4 && n == 7) send_a(i);
+        else if (is_plain.value && i == 5 && n == 5) grow(P);   // scalar work in the MFMAs' shade
         __builtin_amdgcn_sched_barrier(0);
       }
     a_read = a_read == (RA - 1) * A_SLOT ? 0 : a_read + A_SLOT;
     if (!PAIRS || P == 0) b_read = b_read == (RB - 1) * B_SLOT ? 0 : b_read + B_SLOT;
-    next();
+    if (!is_plain.value) next(P);
   };
-  for (int s = 0; s < total; s += 2) {
-    step(std::integral_constant<int, 0>{});
-    if (s + 1 < total) step(std::integral_constant<int, 1>{});
+  constexpr std::integral_constant<int, 0> even{};
+  constexpr std::integral_constant<int, 1> odd{};
+  for (int s = 0; s < total;) {
+    const int n = min(run, total - s) & ~1;
+    for (int i = 0; i < n; i += 2) {
+      step(even, std::true_type{});
+      step(odd, std::true_type{});
+    }
+    plain(n);
+    s += n;
+    if (s < total) { step(even, std::false_type{}); ++s; }
+    if (s < total) { step(odd, std::false_type{}); ++s; }
   }
   // the repeated loads, and the results on their way to the accumulators
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
@@ -498,7 +527,8 @@ __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const bool in = 8 * b + 2 * grp + s < a.units;
-        r[slot][s] = __builtin_nontemporal_load((const u32x4*)(in ? w + 128 * (int64_t)b + 16 * s : (const char*)kZeroUnit));
+        const char* p = in ? w + 128 * (int64_t)b + 16 * s : (const char*)kZeroUnit;
+        r[slot][s] = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4*)p);
       }
     };
 #pragma unroll
