@@ -490,7 +490,7 @@ constexpr int kFewLds = 65536;
 template <typename T, int NT>
 __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
   constexpr int CB = kFewLds / (16 * NT * 128);            // 128-byte blocks of k of a chunk
-  constexpr int DEPTH = 4;
+  constexpr int DEPTH = NT == 4 ? 4 : 8;                                // blocks of k in flight; CB is a multiple
   __shared__ u32x4 hs[kFewLds / 16];
   __shared__ HeadSum red[8][16 * NT];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
@@ -503,7 +503,7 @@ __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
     sum[t] = HeadSum{-FLT_MAX, 0.f, 0.f};
   }
   auto stage = [&](int chunk) {
-    const int nb = min(CB, blocks - chunk * CB);
+    const int nb = min(CB, (blocks - chunk * CB + DEPTH - 1) / DEPTH * DEPTH);   // blocks past the end are zeros on both sides
     for (int i = threadIdx.x; i < nb * 16 * NT * 8; i += 512) {
       const int u = i & 7, r = (i >> 3) % (16 * NT), b = i / (128 * NT);
       const int unit = 8 * (chunk * CB + b) + u;
@@ -543,23 +543,23 @@ __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
       for (int b = 0; b < nb; b += DEPTH) {
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
-          if (b + i < nb) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+          for (int s = 0; s < 2; ++s)
 #pragma unroll
-              for (int t = 0; t < NT; ++t) {
-                const u32x4 h = hs[((b + i) * 16 * NT + 16 * t + row) * 8 + ((2 * grp + s) ^ (row & 7))];
-                if constexpr (sizeof(T) == 2) {
-                  acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r[i][s]), __builtin_bit_cast(bf16x8, h),
-                                                                   acc[t], 0, 0, 0);
-                } else {
+            for (int t = 0; t < NT; ++t) {
+              const u32x4 h = hs[((b + i) * 16 * NT + 16 * t + row) * 8 + ((2 * grp + s) ^ (row & 7))];
+              if constexpr (sizeof(T) == 2) {
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r[i][s]), __builtin_bit_cast(bf16x8, h),
+                                                                 acc[t], 0, 0, 0);
+              } else {
 #pragma unroll
-                  for (int e = 0; e < 4; ++e)
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(r[i][s][e]), __uint_as_float(h[e]), acc[t], 0, 0, 0);
-                }
+                for (int e = 0; e < 4; ++e)
+                  acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(r[i][s][e]), __uint_as_float(h[e]), acc[t], 0, 0, 0);
               }
-            load(b0 + b + i + DEPTH, i);
-          }
+            }
+          __builtin_amdgcn_sched_barrier(0);               // else the loads gather behind the products
+          load(b0 + b + i + DEPTH, i);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
