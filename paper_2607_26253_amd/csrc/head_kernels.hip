@@ -35,8 +35,8 @@ struct Mat {
   int64_t stride, part;     // of kPacked and kPackedT: the 16-row tiles of a k block
 };
 
-// What a row needs for its D: 2^u (A + B u) + [v = tok] g
-struct HeadRow { float m, A, B, g; int32_t tok, on; };
+// What a row needs for its D: 2^u (A + B u) + [v = tok] g; elements above `big` are taken more exactly
+struct HeadRow { float m, A, B, g, big; int32_t tok, on; };
 
 struct HeadTile {
   Mat a, b;                 // M side and N side of C[m][n] = sum_k a(m, k) b(n, k)
@@ -53,7 +53,12 @@ struct HeadTile {
   const HeadRow* rows;
   uint16_t* d;              // D, packed: [part][32 ids][16 rows]
   int64_t d_part;
-  int d_tiles, d_parts;     // 16-row tiles
+  int d_tiles, d_parts;     // 16-row tiles; parts of every element
+  // D's last part is kept where it counts.  Bytes: does a 256-row tile need it in a 32-id step (of dH), a 256-id tile in a
+  // 32-row step (of dW)?  Written by the tiles of D; read in the products, where `sparse` is that part of a (0: none).
+  uint8_t *id_flags, *row_flags;
+  const uint8_t* flags;
+  int id_flags_stride, row_flags_stride, flags_stride, sparse;
   float* slab;              // [split][M][N]
   void* out;                // weight gradient
   int64_t out_stride;
@@ -69,6 +74,7 @@ constexpr int kTileThreads = 256;
 struct TileEpilogue {                  // in the ring's place once the products are done
   float red[3][2][256];
   HeadRow rows[256];
+  uint32_t bits[4];
 };
 
 // One wave's quarter of a tile: acc[n][m] of lane (row, grp) is row 16 m + row, columns 16 n + 4 grp ..+3.  The 256
@@ -163,40 +169,76 @@ __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileE
   const int wm = wave >> 1, wn = wave & 1;
   const int col = tn0 + 128 * wn + 4 * grp;
   const bool full = tn0 + 256 <= a.N;
+  auto values = [&](const HeadRow& hr, int m, int j, float* f) {
+    const int at = hr.tok - a.v0 - col;                      // 16 n + q where it is this lane's
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const f32x4 z = acc_read4(acc[2 * j + b][m]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = 16 * (2 * j + b) + q;
+        // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
+        const float u = __builtin_amdgcn_fmed3f((z[q] - hr.m) * a.c, -150.f, 0.f);
+        float e = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A);   // a row that met a NaN has it in A
+        e += at == n ? hr.g : 0.f;
+        f[4 * b + q] = hr.on && (full || col + n < a.N) ? e : 0.f;
+      }
+    }
+  };
+  auto part = [&](float* f) {                                // rounded; f keeps the rest
+    u32x4 w;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t x = pack_bf16(f[2 * q], f[2 * q + 1]);
+      asm("" : "+v"(x));                                     // what was rounded is what is subtracted
+      f[2 * q] -= __uint_as_float(x << 16);
+      f[2 * q + 1] -= __uint_as_float(x & 0xFFFF0000u);
+      w[q] = x;
+    }
+    return w;
+  };
+  auto block = [&](int m, int j, int p) {
+    return (u32x4*)(a.d + ((int64_t)((tn0 >> 5) + 4 * wn + j) * a.d_tiles + ((tm0 + 128 * wm + 16 * m) >> 4)) * 512 + lane * 8 + p * a.d_part);
+  };
+  uint32_t ids = 0, rows = 0;                                // bits: 32-id and 32-row steps with an element above `big`
 #pragma unroll
   for (int m = 0; m < 8; ++m) {
-    const int r = 128 * wm + 16 * m + row;
-    const HeadRow hr = lds.rows[r];
-    const int at = hr.tok - a.v0 - col;                      // 16 n + q where it is this lane's
-    uint16_t* y = a.d + ((int64_t)((tn0 >> 5) + 4 * wn) * a.d_tiles + ((tm0 + r) >> 4)) * 512 + lane * 8;
+    const HeadRow hr = lds.rows[128 * wm + 16 * m + row];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float f[8];
+      values(hr, m, j, f);
+      float mx = 0.f;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const f32x4 z = acc_read4(acc[2 * j + b][m]);
+      for (int q = 0; q < 8; ++q) mx = fmaxf(mx, fabsf(f[q]));
+      if (mx > hr.big) { ids |= 1u << j; rows |= 1u << (m >> 1); }
+      for (int p = 0; p < a.d_parts; ++p) *block(m, j, p) = part(f);
+    }
+  }
+  if (!a.id_flags) return;
+  uint32_t bits = 0;                                         // of the wave: ids in bits 0..3, rows in bits 4..7
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = 16 * (2 * j + b) + q;
-          // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
-          const float u = __builtin_amdgcn_fmed3f((z[q] - hr.m) * a.c, -150.f, 0.f);
-          float e = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A);   // a row that met a NaN has it in A
-          e += at == n ? hr.g : 0.f;
-          f[4 * b + q] = hr.on && (full || col + n < a.N) ? e : 0.f;
-        }
-      }
-      for (int p = 0; p < a.d_parts; ++p) {
-        u32x4 w;
+  for (int i = 0; i < 4; ++i) bits |= (__any(ids >> i & 1) ? 1u << i : 0u) | (__any(rows >> i & 1) ? 16u << i : 0u);
+  if (lane == 0) lds.bits[wave] = bits;
+  __syncthreads();
+  const uint32_t my_ids = (lds.bits[wn] | lds.bits[2 + wn]) & 15, my_rows = (lds.bits[2 * wm] | lds.bits[2 * wm + 1]) >> 4;
+  if (threadIdx.x < 16) {
+    const int i = threadIdx.x & 3, half = threadIdx.x >> 2 & 1;
+    if (threadIdx.x < 8) a.id_flags[(int64_t)(tm0 >> 8) * a.id_flags_stride + (tn0 >> 5) + threadIdx.x] = (lds.bits[half] | lds.bits[2 + half]) >> i & 1;
+    else a.row_flags[(int64_t)(tn0 >> 8) * a.row_flags_stride + (tm0 >> 5) + threadIdx.x - 8] = (lds.bits[2 * half] | lds.bits[2 * half + 1]) >> (4 + i) & 1;
+  }
+  // the last part of the steps that some element asks for
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t x = pack_bf16(f[2 * q], f[2 * q + 1]);
-          asm("" : "+v"(x));                                 // what was rounded is what is subtracted
-          f[2 * q] -= __uint_as_float(x << 16);
-          f[2 * q + 1] -= __uint_as_float(x & 0xFFFF0000u);
-          w[q] = x;
-        }
-        *(u32x4*)(y + p * a.d_part + (int64_t)j * a.d_tiles * 512) = w;
-      }
+  for (int m = 0; m < 8; ++m) {
+    if (my_ids == 0 && !(my_rows >> (m >> 1) & 1)) continue;
+    const HeadRow hr = lds.rows[128 * wm + 16 * m + row];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (!((my_ids >> j | my_rows >> (m >> 1)) & 1)) continue;
+      float f[8];
+      values(hr, m, j, f);
+      for (int p = 0; p < a.d_parts; ++p) (void)part(f);
+      *block(m, j, a.d_parts) = part(f);
     }
   }
 }
@@ -237,7 +279,39 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
     bn = r / gm;
   }
   const int tm0 = 256 * bm, tn0 = 256 * bn;
-  const int k_steps = (a.K + 31) >> 5, s0 = split * a.steps, ns = min(a.steps, k_steps - s0), total = ns * a.n_pairs;
+  const int k_steps = (a.K + 31) >> 5, s0 = split * a.steps, ns = min(a.steps, k_steps - s0), dense = ns * a.n_pairs;
+  // Steps that want D's last part, 64 a lane; they come first.  left: how many are still to be sent.
+  constexpr bool SPARSE = EPI == kSlab || EPI == kWeight;
+  uint64_t wanted = 0, sp_bits = 0;
+  int sp_lane = -1, sp_at = 0, sp_left = 0;
+  auto sp_next = [&]() {
+    sp_bits &= sp_bits - 1;
+    if (sp_bits == 0) {
+      const uint64_t who = __ballot(wanted != 0) & (sp_lane < 0 ? ~0ull : ~((2ull << sp_lane) - 1));
+      sp_lane = __ffsll((unsigned long long)who) - 1;
+      sp_bits = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(wanted >> 32), sp_lane) << 32 |
+                (uint32_t)__builtin_amdgcn_readlane((int)wanted, sp_lane);
+    }
+    sp_at = 64 * sp_lane + __ffsll((unsigned long long)sp_bits) - 1;
+  };
+  if (SPARSE && a.sparse) {
+    const uint8_t* f = a.flags + (int64_t)bm * a.flags_stride + s0 + 64 * lane;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (64 * lane + 16 * i < ns) {
+        const u32x4 w = *(const u32x4*)(f + 16 * i);
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          if (64 * lane + 16 * i + q < ns) wanted |= (uint64_t)(w[q >> 2] >> (8 * (q & 3)) & 1) << (16 * i + q);
+      }
+    n = __popcll(wanted);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) n += __shfl_xor(n, x, 64);
+    sp_left = __builtin_amdgcn_readfirstlane(n);
+    if (sp_left > 0) sp_next();
+  }
+  const int total = dense + sp_left;
   // A wave loads 4 KiB of either operand in a step: where a lane's 16 bytes come from at k = 0, and the k they hold
   auto unit = [&](auto kind, const Mat& mat, int t0, int n, int f, int& k_of) {
     k_of = 0;
@@ -276,11 +350,12 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
   int64_t a_at = 0, b_at = 0, a_grow = 2 * a_step, b_grow = 2 * b_step;   // added to the addresses, in bytes
   uint32_t a_slot = 0, b_slot = 0;
   auto place = [&]() {
-    const int pair = a.pairs >> (4 * i_pair) & 15, ks = s0 + i_step;
+    const bool sp = SPARSE && sp_left > 0;
+    const int pair = sp ? a.sparse : a.pairs >> (4 * i_pair) & 15, ks = s0 + (sp ? sp_at : i_step);
     const int kb = PAIRS ? i_seen >> 1 : ks;
     a_at = 2 * ((pair & 3) * a.a.part + ks * a_step);
     b_at = 2 * ((pair >> 2) * a.b.part + kb * b_step);
-    run = ns - 1 - i_step;
+    run = sp ? 0 : ns - 1 - i_step;
     if constexpr (BK == kCols || BK == kRowPairs) {        // not padded with zeros
       constexpr int W = PAIRS ? 64 : 32;
       const bool ends = W * (kb + 1) > a.K;
@@ -294,7 +369,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
       }
       tail = ends;
       const int full = a.K / W;                            // stages (or pairs) before the one that ends inside
-      if (!ends) run = min(run, (PAIRS ? 2 * full - i_seen : full - ks) - 1);
+      if (!ends && !sp) run = min(run, (PAIRS ? 2 * full - i_seen : full - ks) - 1);
     }
   };
   auto grow = [&](int odd) {                               // odd: of the stage just sent
@@ -308,7 +383,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
     grow(odd);
     if (run > 0) { plain(1); return; }
     ++i_seen;
-    if (i_pair * ns + i_step + 1 < total) {
+    if (SPARSE && sp_left > 0) {
+      if (--sp_left > 0) sp_next();
+      place();
+    } else if (i_pair * ns + i_step + 1 < dense) {
       if (++i_step == ns) { i_step = 0; ++i_pair; }
       place();
     } else if (a_grow != 0) {                              // that was the last
@@ -681,20 +759,29 @@ __global__ __launch_bounds__(256) void k_head_pack(const T* __restrict__ x, int6
   }
 }
 
+// A bf16 number is off by up to 2^-8 of itself; a gradient row is made of few large elements of D and many small ones, whose
+// errors are independent.  Elements above kBig of a row's scale get one part more (32 x 256 of their neighbours with
+// them), which leaves some 2^-9 sqrt(kBig) of the row.
+constexpr float kBig = 1.f / 32;
+
 __global__ __launch_bounds__(256) void k_head_rows(int n_rows, int rows_out, int V, const int32_t* __restrict__ tok,
     const float* __restrict__ stats, const float* __restrict__ entropy, const float* __restrict__ g_logp,
     const float* __restrict__ g_ent, float scale, HeadRow* __restrict__ out) {
   const int r = blockIdx.x * 256 + threadIdx.x;
   if (r >= rows_out) return;
-  HeadRow o = {0.f, 0.f, 0.f, 0.f, -1, 0};
+  HeadRow o = {0.f, 0.f, 0.f, 0.f, 0.f, -1, 0};
   if (r < n_rows) {
     const int tk = tok[r];
     const bool has = tk >= 0 && tk < V;
     const float m = stats[2 * (size_t)r], s = stats[2 * (size_t)r + 1];
     const float g = has && g_logp ? g_logp[r] : 0.f, h = g_ent ? g_ent[r] : 0.f;
     if (!(g == 0.f && h == 0.f))
-      o = HeadRow{m, -scale * (g + (h == 0.f ? 0.f : h * (entropy[r] - logf(s)))) / s, -scale * 0.69314718f * h / s, scale * g,
-                  has ? tk : -1, 1};
+    {
+      // 1 / s is the largest p: |g| (1 - 1 / s) is at most |D| at the row's id, the other term |D| at its likeliest
+      const float hl = h == 0.f ? 0.f : h * (entropy[r] - logf(s));
+      o = HeadRow{m, -scale * (g + hl) / s, -scale * 0.69314718f * h / s, scale * g,
+                  kBig * scale * (fabsf(g) * (1.f - 1.f / s) + fabsf(hl) / s), has ? tk : -1, 1};
+    }
   }
   out[r] = o;
 }
@@ -726,7 +813,8 @@ __global__ __launch_bounds__(256) void k_head_zero(uint32_t* __restrict__ out, i
 constexpr uint32_t kPairs1 = 0;                            // (0, 0)
 constexpr uint32_t kPairs2 = 0x01;                         // a in two parts: (1, 0), (0, 0)
 constexpr uint32_t kPairs3 = 0x041852;                     // (2, 0), (1, 1), (0, 2), (1, 0), (0, 1), (0, 0)
-constexpr int64_t kPieceBytes = 256 << 20;                 // of D, and of the parts of a piece of an fp32 weight
+constexpr int64_t kPieceBytes = 448 << 20;                 // of D, and of the parts of a piece of an fp32 weight
+constexpr int kMaxSteps = 4096;                            // k steps of a block: 64 flags a lane
 constexpr int kStatRows = 8192;                            // rows of a launch of the forward tiles
 constexpr int kFewRows = 64;
 constexpr int kCus = 256;
@@ -757,8 +845,9 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
   }
   p.rows_out = (int)up(n_rows, 256);
   p.d_parts = f32 ? 3 : weight_f32 ? 2 : 1;
+  const int all_parts = p.d_parts + (f32 ? 0 : 1);
   const int mb = p.rows_out / 256;
-  int64_t most = kPieceBytes / (512 * (int64_t)p.d_parts * p.rows_out);
+  int64_t most = kPieceBytes / (512 * (int64_t)all_parts * p.rows_out);
   if (f32) most = std::min(most, kPieceBytes / (6 * 256 * (int64_t)p.width));
   most = std::min<int64_t>(cols, std::max<int64_t>(1, most));
   // pieces of about the same size; whole rounds of the chip's compute units where that fits
@@ -770,14 +859,17 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
   const int k_steps = (std::min(V, 256 * p.piece) + 31) / 32;
   double best = 0;
   p.splits = 1;
-  for (int s = 1; s <= 64 && s * 8 <= k_steps; ++s) {
+  const int fewest = (k_steps + kMaxSteps - 1) / kMaxSteps;
+  for (int s = fewest; s <= std::max(64, fewest) && (s == fewest || s * 16 <= k_steps); ++s) {
     const double use = (double)tiles * s / (double)up((int64_t)tiles * s, kCus);
     if (use > best + 0.02) { best = use; p.splits = s; }
   }
-  const int steps = (k_steps + p.splits - 1) / p.splits;   // the first piece writes every split
+  const int steps = (int)up((k_steps + p.splits - 1) / p.splits, 16);   // the first piece writes every split
   p.splits = (k_steps + steps - 1) / steps;
   p.rows = take(sizeof(HeadRow) * (int64_t)p.rows_out);
-  p.d = take(512 * (int64_t)p.d_parts * p.rows_out * p.piece);
+  p.d = take(512 * (int64_t)all_parts * p.rows_out * p.piece);
+  p.id_flags = take((int64_t)mb * up(8 * p.piece, 64));
+  p.row_flags = take((int64_t)p.piece * up(p.rows_out / 32, 64));
   p.slab = take(4 * (int64_t)p.splits * n_rows * d);
   p.h_parts = take(2 * (int64_t)(f32 ? 3 : 1) * p.rows_out * p.width);
   if (f32) p.w_parts = take(6 * 256 * (int64_t)p.piece * p.width);
@@ -887,6 +979,8 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
                      scale, rows);
   pack(f32, h, h_stride, n_rows, d, rows, hp, p.rows_out, p.width, st);
   const int cols = (V + 255) / 256, tiles = p.rows_out / 16;
+  uint8_t *id_flags = (uint8_t*)at(p.id_flags), *row_flags = (uint8_t*)at(p.row_flags);
+  const int id_stride = (int)up(8 * p.piece, 64), row_stride = (int)up(p.rows_out / 32, 64);
   const Mat hm = {hp, tiles, (int64_t)p.rows_out * p.width}, dm = {D, tiles, 256 * (int64_t)p.piece * p.rows_out};
   auto go = [&](auto kernel, const HeadTile& t) { hipLaunchKernelGGL(kernel, tile_grid(t), dim3(kTileThreads), 0, st, t); };
   for (int c0 = 0; c0 < cols; c0 += p.piece) {
@@ -912,6 +1006,12 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
     t.d_tiles = tiles;
     t.d_part = dm.part;
     t.d_parts = p.d_parts;
+    if (!f32) {
+      t.id_flags = id_flags;
+      t.row_flags = row_flags;
+      t.id_flags_stride = id_stride;
+      t.row_flags_stride = row_stride;
+    }
     if (f32) go(k_head_tile<kPacked, kPacked, kGradRows>, t);
     else go(k_head_tile<kPacked, kRowPairs, kGradRows>, t);
     if (gh) {
@@ -923,7 +1023,10 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
       x.K = N;
       x.n_pairs = f32 ? 6 : 1;
       x.pairs = f32 ? kPairs3 : kPairs1;
-      x.steps = ((N + 31) / 32 + p.splits - 1) / p.splits;
+      x.steps = (int)up(((N + 31) / 32 + p.splits - 1) / p.splits, 16);
+      x.flags = id_flags;
+      x.flags_stride = id_stride;
+      x.sparse = f32 ? 0 : 1;
       x.slab = slab;
       x.add = c0 > 0;
       if (f32) go(k_head_tile<kPacked, kPackedT, kSlab>, x);
@@ -939,6 +1042,9 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
       x.n_pairs = f32 ? 6 : p.d_parts;
       x.pairs = f32 ? kPairs3 : p.d_parts == 2 ? kPairs2 : kPairs1;
       x.steps = x.K / 32;
+      x.flags = row_flags;
+      x.flags_stride = row_stride;
+      x.sparse = f32 ? 0 : p.d_parts;
       x.inv_t = inv_t;
       x.out = (char*)gw + v0 * gw_stride * EW;
       x.out_stride = gw_stride;

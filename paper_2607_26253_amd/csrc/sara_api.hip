@@ -1086,6 +1086,9 @@ extern "C" int sara_token_logprobs_grad(const void* d_logits, int32_t dtype, int
 // Widest hidden state: the tiles' k steps and strides in bytes stay far inside 32 bits.
 static constexpr int32_t kMaxWidth = 1 << 20;
 
+// Most rows of a gradient: a block keeps a flag for each of its 4,096 steps of 32.
+static constexpr int32_t kMaxGradRows = 1 << 17;
+
 static std::string head_bad(int32_t dtype, int32_t n_rows, int32_t d, int32_t vocab) {
   if (dtype != SARA_BF16 && dtype != SARA_F32) return "dtype must be SARA_BF16 or SARA_F32";
   if (n_rows < 0 || d < 1 || d > kMaxWidth || vocab < 1 || vocab > kMaxVocab)
@@ -1117,6 +1120,7 @@ extern "C" int sara_head_logprobs_workspace(int32_t dtype, int32_t n_rows, int32
   if (!bad.empty()) return einval(bad);
   if (grad && weight_grad_dtype != SARA_F32 && weight_grad_dtype != dtype)
     return einval("the weight's gradient must be of its dtype or SARA_F32");
+  if (grad && n_rows > kMaxGradRows) return einval("too many rows: at most 131,072, the rest with accumulate");
   *bytes = n_rows == 0 ? 0 : head_plan(dtype, n_rows, d_model, vocab, weight_grad_dtype == SARA_F32, grad != 0).bytes;
   return SARA_OK;
 }

@@ -350,7 +350,7 @@ int launch_token_logprobs_grad(const void* logits, int dtype, int64_t row_stride
 struct HeadPlan {
   bool few;
   int nt, few_blocks, piece, rows_out, width, d_parts, splits;
-  int64_t x_tok, parts, rows, d, slab, h_parts, w_parts, bytes;
+  int64_t x_tok, parts, rows, d, id_flags, row_flags, slab, h_parts, w_parts, bytes;
 };
 HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool grad);
 int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype, int n_rows, int d, int V,
