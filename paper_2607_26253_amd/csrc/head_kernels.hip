@@ -35,8 +35,9 @@ struct Mat {
   int64_t stride, part;     // of kPacked and kPackedT: the 16-row tiles of a k block
 };
 
-// What a row needs for its D: 2^u (A + B u) + [v = tok] g; elements above `big` are taken more exactly
-struct HeadRow { float m, A, B, g, big; int32_t tok, on; };
+// What a row needs for its D: 2^u (A + B u) + [v = tok] g; logits above `large` make elements
+// that are taken more exactly
+struct HeadRow { float m, A, B, g, large; int32_t tok, on; };
 
 struct HeadTile {
   Mat a, b;                 // M side and N side of C[m][n] = sum_k a(m, k) b(n, k)
@@ -53,7 +54,7 @@ struct HeadTile {
   const HeadRow* rows;
   uint16_t* d;              // D, packed: [part][32 ids][16 rows]
   int64_t d_part;
-  int d_tiles, d_parts;     // 16-row tiles; parts of every element
+  int d_tiles;              // 16-row tiles
   // D's last part is kept where it counts.  Bytes: does a 256-row tile need it in a 32-id step (of dH), a 256-id tile in a
   // 32-row step (of dW)?  Written by the tiles of D; read in the products, where `sparse` is that part of a (0: none).
   uint8_t *id_flags, *row_flags;
@@ -67,7 +68,7 @@ struct HeadTile {
 
 __device__ __attribute__((aligned(16))) const uint32_t kZeroUnit[4] = {0, 0, 0, 0};
 
-enum { kStats, kGradRows, kSlab, kWeight };
+enum { kStats, kSlab, kWeight, kGradRows };   // kGradRows + p: p parts of every element of D
 
 constexpr int kTileLds = 163840;       // all of a compute unit's
 constexpr int kTileThreads = 256;
@@ -86,7 +87,7 @@ __device__ __forceinline__ void acc_zero(f32x4& a) {
 }
 __device__ __forceinline__ float acc_read(float a) {
   float x;
-  asm("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(a));
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(a));   // volatile: a value read twice is not kept in between
   return x;
 }
 __device__ __forceinline__ f32x4 acc_read4(const f32x4& a) {
@@ -98,7 +99,7 @@ __device__ __forceinline__ void acc_mfma(f32x4& c, bf16x8 x, bf16x8 y) {
 
 // The softmax statistics of a block's tile: per row over its columns below N.
 __device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, TileEpilogue& lds, int tm0, int tn0, int bn) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
   const int wm = wave >> 1, wn = wave & 1;
   const int left = a.N - (tn0 + 128 * wn) - 4 * grp;        // columns of this lane's first tile and on
   const bool full = a.N - (tn0 + 128 * wn) >= 128;
@@ -164,81 +165,82 @@ __device__ __forceinline__ void tile_stats(TileAcc& acc, const HeadTile& a, Tile
 // 16 b + 4 g + q.  Products over ids take the other operand in that order, D^T gives its rows back.
 __device__ __forceinline__ int id_of_place(int p) { return 16 * (p >> 2 & 1) + 4 * (p >> 3) + (p & 3); }
 
+// PARTS of every element of D, and the last part of the steps of 32 ids or rows that have a large one (a.id_flags).
+template <int PARTS>
 __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileEpilogue& lds, int tm0, int tn0) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
   const int wm = wave >> 1, wn = wave & 1;
   const int col = tn0 + 128 * wn + 4 * grp;
   const bool full = tn0 + 256 <= a.N;
-  auto values = [&](const HeadRow& hr, int m, int j, float* f) {
-    const int at = hr.tok - a.v0 - col;                      // 16 n + q where it is this lane's
+  uint32_t my_ids = 0, my_rows = 0;                          // steps of this wave's that want the last part
+  if (a.id_flags) {
+    uint32_t bits = 0;                                       // of the wave: ids in bits 0..3, rows in bits 4..7
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const f32x4 z = acc_read4(acc[2 * j + b][m]);
+    for (int m = 0; m < 8; ++m) {
+      const HeadRow& hr = lds.rows[128 * wm + 16 * m + row];
+      const float large = hr.large;
+      const int at = hr.tok - a.v0 - col;                    // the row's id itself is taken for large
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int n = 16 * (2 * j + b) + q;
-        // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
-        const float u = __builtin_amdgcn_fmed3f((z[q] - hr.m) * a.c, -150.f, 0.f);
-        float e = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A);   // a row that met a NaN has it in A
-        e += at == n ? hr.g : 0.f;
-        f[4 * b + q] = hr.on && (full || col + n < a.N) ? e : 0.f;
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 x = acc_read4(acc[2 * j][m]), y = acc_read4(acc[2 * j + 1][m]);
+        const float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+        if (__any(mx > large || (unsigned)(at + 4 * grp - 32 * j) < 32u)) bits |= 1u << j | 16u << (m >> 1);
       }
     }
-  };
-  auto part = [&](float* f) {                                // rounded; f keeps the rest
-    u32x4 w;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      uint32_t x = pack_bf16(f[2 * q], f[2 * q + 1]);
-      asm("" : "+v"(x));                                     // what was rounded is what is subtracted
-      f[2 * q] -= __uint_as_float(x << 16);
-      f[2 * q + 1] -= __uint_as_float(x & 0xFFFF0000u);
-      w[q] = x;
-    }
-    return w;
-  };
-  auto block = [&](int m, int j, int p) {
-    return (u32x4*)(a.d + ((int64_t)((tn0 >> 5) + 4 * wn + j) * a.d_tiles + ((tm0 + 128 * wm + 16 * m) >> 4)) * 512 + lane * 8 + p * a.d_part);
-  };
-  uint32_t ids = 0, rows = 0;                                // bits: 32-id and 32-row steps with an element above `big`
-#pragma unroll
-  for (int m = 0; m < 8; ++m) {
-    const HeadRow hr = lds.rows[128 * wm + 16 * m + row];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float f[8];
-      values(hr, m, j, f);
-      float mx = 0.f;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) mx = fmaxf(mx, fabsf(f[q]));
-      if (mx > hr.big) { ids |= 1u << j; rows |= 1u << (m >> 1); }
-      for (int p = 0; p < a.d_parts; ++p) *block(m, j, p) = part(f);
+    if (lane == 0) lds.bits[wave] = bits;
+    __syncthreads();
+    my_ids = __builtin_amdgcn_readfirstlane((lds.bits[wn] | lds.bits[2 + wn]) & 15);
+    my_rows = __builtin_amdgcn_readfirstlane((lds.bits[2 * wm] | lds.bits[2 * wm + 1]) >> 4);
+    if (threadIdx.x < 16) {
+      const int i = threadIdx.x & 3, half = threadIdx.x >> 2 & 1;
+      if (threadIdx.x < 8)
+        a.id_flags[(int64_t)(tm0 >> 8) * a.id_flags_stride + (tn0 >> 5) + threadIdx.x] = (lds.bits[half] | lds.bits[2 + half]) >> i & 1;
+      else
+        a.row_flags[(int64_t)(tn0 >> 8) * a.row_flags_stride + (tm0 >> 5) + threadIdx.x - 8] =
+            (lds.bits[2 * half] | lds.bits[2 * half + 1]) >> (4 + i) & 1;
     }
   }
-  if (!a.id_flags) return;
-  uint32_t bits = 0;                                         // of the wave: ids in bits 0..3, rows in bits 4..7
-#pragma unroll
-  for (int i = 0; i < 4; ++i) bits |= (__any(ids >> i & 1) ? 1u << i : 0u) | (__any(rows >> i & 1) ? 16u << i : 0u);
-  if (lane == 0) lds.bits[wave] = bits;
-  __syncthreads();
-  const uint32_t my_ids = (lds.bits[wn] | lds.bits[2 + wn]) & 15, my_rows = (lds.bits[2 * wm] | lds.bits[2 * wm + 1]) >> 4;
-  if (threadIdx.x < 16) {
-    const int i = threadIdx.x & 3, half = threadIdx.x >> 2 & 1;
-    if (threadIdx.x < 8) a.id_flags[(int64_t)(tm0 >> 8) * a.id_flags_stride + (tn0 >> 5) + threadIdx.x] = (lds.bits[half] | lds.bits[2 + half]) >> i & 1;
-    else a.row_flags[(int64_t)(tn0 >> 8) * a.row_flags_stride + (tm0 >> 5) + threadIdx.x - 8] = (lds.bits[2 * half] | lds.bits[2 * half + 1]) >> (4 + i) & 1;
-  }
-  // the last part of the steps that some element asks for
 #pragma unroll
   for (int m = 0; m < 8; ++m) {
-    if (my_ids == 0 && !(my_rows >> (m >> 1) & 1)) continue;
+    __builtin_amdgcn_sched_barrier(0);                       // else the rows' values gather in front
     const HeadRow hr = lds.rows[128 * wm + 16 * m + row];
+    const int at = hr.tok - a.v0 - col;                      // 32 j + 16 b + q where it is this lane's
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (!((my_ids >> j | my_rows >> (m >> 1)) & 1)) continue;
+      // A row that is off has A = B = 0 and no id here; one that met a NaN has it in A
       float f[8];
-      values(hr, m, j, f);
-      for (int p = 0; p < a.d_parts; ++p) (void)part(f);
-      *block(m, j, a.d_parts) = part(f);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const f32x4 z = acc_read4(acc[2 * j + b][m]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
+          const float u = __builtin_amdgcn_fmed3f((z[q] - hr.m) * a.c, -150.f, 0.f);
+          f[4 * b + q] = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A);
+        }
+      }
+      if (__any((unsigned)(at - 32 * j) < 32u && (at & 12) == 0))
+#pragma unroll
+        for (int n = 0; n < 8; ++n) f[n] += at == 32 * j + 16 * (n >> 2) + (n & 3) ? hr.g : 0.f;
+      if (!full)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) f[n] = col + 32 * j + 16 * (n >> 2) + (n & 3) < a.N ? f[n] : 0.f;
+      u32x4* y = (u32x4*)(a.d + ((int64_t)((tn0 >> 5) + 4 * wn + j) * a.d_tiles + ((tm0 + 128 * wm + 16 * m) >> 4)) * 512);   // scalar
+      auto store = [&](int p) {                              // rounded; f keeps the rest
+        u32x4 w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t x = pack_bf16(f[2 * q], f[2 * q + 1]);
+          asm("" : "+v"(x));                                 // what was rounded is what is subtracted
+          f[2 * q] -= __uint_as_float(x << 16);
+          f[2 * q + 1] -= __uint_as_float(x & 0xFFFF0000u);
+          w[q] = x;
+        }
+        (y + p * (a.d_part / 8))[lane] = w;
+      };
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) store(p);
+      if ((my_ids >> j | my_rows >> (m >> 1)) & 1) store(PARTS);
     }
   }
 }
@@ -500,10 +502,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
     lds.rows[threadIdx.x].tok = tok >= a.v0 && tok < a.v0 + a.N ? tok - a.v0 : -1;
     __syncthreads();
     tile_stats(acc, a, lds, tm0, tn0, bn + (a.v0 >> 8));
-  } else if constexpr (EPI == kGradRows) {
+  } else if constexpr (EPI > kGradRows) {
     lds.rows[threadIdx.x] = a.rows[tm0 + threadIdx.x];
     __syncthreads();
-    tile_grad(acc, a, lds, tm0, tn0);
+    tile_grad<EPI - kGradRows>(acc, a, lds, tm0, tn0);
   } else {
     const int c0 = tn0 + 128 * wn + 8 * grp;
 #pragma unroll
@@ -762,11 +764,11 @@ __global__ __launch_bounds__(256) void k_head_pack(const T* __restrict__ x, int6
 // A bf16 number is off by up to 2^-8 of itself; a gradient row is made of few large elements of D and many small ones, whose
 // errors are independent.  Elements above kBig of a row's scale get one part more (32 x 256 of their neighbours with
 // them), which leaves some 2^-9 sqrt(kBig) of the row.
-constexpr float kBig = 1.f / 32;
+constexpr float kBig = 1.f / 16;
 
 __global__ __launch_bounds__(256) void k_head_rows(int n_rows, int rows_out, int V, const int32_t* __restrict__ tok,
     const float* __restrict__ stats, const float* __restrict__ entropy, const float* __restrict__ g_logp,
-    const float* __restrict__ g_ent, float scale, HeadRow* __restrict__ out) {
+    const float* __restrict__ g_ent, float scale, float inv_c, HeadRow* __restrict__ out) {
   const int r = blockIdx.x * 256 + threadIdx.x;
   if (r >= rows_out) return;
   HeadRow o = {0.f, 0.f, 0.f, 0.f, 0.f, -1, 0};
@@ -777,10 +779,12 @@ __global__ __launch_bounds__(256) void k_head_rows(int n_rows, int rows_out, int
     const float g = has && g_logp ? g_logp[r] : 0.f, h = g_ent ? g_ent[r] : 0.f;
     if (!(g == 0.f && h == 0.f))
     {
-      // 1 / s is the largest p: |g| (1 - 1 / s) is at most |D| at the row's id, the other term |D| at its likeliest
-      const float hl = h == 0.f ? 0.f : h * (entropy[r] - logf(s));
-      o = HeadRow{m, -scale * (g + hl) / s, -scale * 0.69314718f * h / s, scale * g,
-                  kBig * scale * (fabsf(g) * (1.f - 1.f / s) + fabsf(hl) / s), has ? tk : -1, 1};
+      // 1 / s is the largest p: |g| (1 - 1 / s) is at most |D| at the row's id, the other term |D| at its likeliest.  Where
+      // 2^u |A| and 2^u |B u| <= 1.07 2^(u / 2) |B| are below half of kBig of that, D is below kBig of it.
+      const float hl = h == 0.f ? 0.f : h * (entropy[r] - logf(s)), A = -(g + hl) / s, B = -0.69314718f * h / s;
+      const float half = 0.5f * kBig * (fabsf(g) * (1.f - 1.f / s) + fabsf(hl) / s);
+      const float u = B == 0.f ? log2f(2.f * half / fabsf(A)) : fminf(log2f(half / fabsf(A)), 2.f * log2f(half / (1.07f * fabsf(B))));
+      o = HeadRow{m, scale * A, scale * B, scale * g, m + fminf(u, 0.f) * inv_c, has ? tk : -1, 1};
     }
   }
   out[r] = o;
@@ -976,7 +980,7 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
   uint16_t *D = (uint16_t*)at(p.d), *hp = (uint16_t*)at(p.h_parts), *wp = (uint16_t*)at(p.w_parts);
   float* slab = (float*)at(p.slab);
   hipLaunchKernelGGL(k_head_rows, dim3(p.rows_out / 256), dim3(256), 0, st, n_rows, p.rows_out, V, tok, stats, entropy, g_logp, g_ent,
-                     scale, rows);
+                     scale, 1.f / c, rows);
   pack(f32, h, h_stride, n_rows, d, rows, hp, p.rows_out, p.width, st);
   const int cols = (V + 255) / 256, tiles = p.rows_out / 16;
   uint8_t *id_flags = (uint8_t*)at(p.id_flags), *row_flags = (uint8_t*)at(p.row_flags);
@@ -1005,15 +1009,15 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
     t.d = D;
     t.d_tiles = tiles;
     t.d_part = dm.part;
-    t.d_parts = p.d_parts;
     if (!f32) {
       t.id_flags = id_flags;
       t.row_flags = row_flags;
       t.id_flags_stride = id_stride;
       t.row_flags_stride = row_stride;
     }
-    if (f32) go(k_head_tile<kPacked, kPacked, kGradRows>, t);
-    else go(k_head_tile<kPacked, kRowPairs, kGradRows>, t);
+    if (f32) go(k_head_tile<kPacked, kPacked, kGradRows + 3>, t);
+    else if (p.d_parts == 2) go(k_head_tile<kPacked, kRowPairs, kGradRows + 2>, t);
+    else go(k_head_tile<kPacked, kRowPairs, kGradRows + 1>, t);
     if (gh) {
       HeadTile x = {};
       x.a = dm;
