@@ -437,8 +437,8 @@ int sara_kv8_attention(const sara_kv8_cache* cache, const void* d_q, int64_t q_r
                        void* stream);
 
 /* The same attention where sequences come in groups that share pages, as the
- * rollouts of a prompt do: the shared pages are read once for all rows of a
- * group.  Group j holds the sequences [d_groups[j], d_groups[j + 1]) (d_groups
+ * rollouts of a prompt do: where that pays, the shared pages are read once for
+ * all rows of a group.  Group j holds the sequences [d_groups[j], d_groups[j + 1]) (d_groups
  * [n_groups + 1], not decreasing, inside [0, n_seqs]; a sequence of no group
  * shares nothing); they have d_shared[j] tokens in common, of which the whole
  * pages among the first max_shared are shared.  Positions in those
@@ -446,10 +446,10 @@ int sara_kv8_attention(const sara_kv8_cache* cache, const void* d_q, int64_t q_r
  * d_ctx and the other tables hold there, later positions through each
  * sequence's own.  Every sequence may have any d_ctx, less than d_shared among
  * them; all else is as above.  max_shared <= 16 * max_pages and 2^30: keep it near the
- * longest; sharing pays from some two sequences and some pages on.
- * d_ws is always needed. */
+ * longest. */
 int sara_kv8_group_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads, int32_t n_seqs,
-                                       int32_t n_groups, int32_t ragged, int32_t max_ctx, int32_t max_shared, int64_t* bytes);
+                                       int32_t n_groups, int32_t ragged, int32_t max_ctx, int32_t max_shared, int32_t dtype,
+                                       int64_t* bytes);
 int sara_kv8_group_attention(const sara_kv8_cache* cache, const void* d_q, int64_t q_row_stride, int64_t q_head_stride,
                              void* d_out, int64_t out_row_stride, int64_t out_head_stride, int32_t dtype, int32_t n_rows,
                              int32_t n_heads, const int32_t* d_pages, int32_t max_pages, const int32_t* d_ctx,

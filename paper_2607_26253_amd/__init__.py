@@ -120,7 +120,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "sara_kv8_read": [P, P, I64, I64, P, I64, I64, I32, I32, P, I32, P, P, I32, P],
         "sara_kv8_attention_workspace": [I32, I32, I32, I32, I32, I32, I32, ctypes.POINTER(I64)],
         "sara_kv8_attention": [P, P, I64, I64, P, I64, I64, I32, I32, I32, P, I32, P, P, I32, I32, F32, P, I64, P],
-        "sara_kv8_group_attention_workspace": [I32, I32, I32, I32, I32, I32, I32, I32, I32, ctypes.POINTER(I64)],
+        "sara_kv8_group_attention_workspace": [I32] * 10 + [ctypes.POINTER(I64)],
         "sara_kv8_group_attention": [P, P, I64, I64, P, I64, I64, I32, I32, I32, P, I32, P, P, I32, P, P, I32, I32, I32, F32, P, I64, P],
         "sara_token_logprobs_workspace": [I32, I32, I32, ctypes.POINTER(I64)],
         "sara_token_logprobs": [P, I32, I64, I32, I32, P, F32, I32, P, P, P, P, P, P, I64, P],
@@ -463,8 +463,8 @@ def sara_kv8_group_attention(d_q, k_cache, v_cache, k_exp, v_exp, d_pages, d_ctx
                              max_ctx=None, max_shared=None, workspace=None, stream=None):
     """sara_kv8_attention where the sequences d_groups[j]..d_groups[j + 1] share
     the whole pages of their first d_shared[j] tokens (int32 [n_groups + 1] and
-    [n_groups]): those are read once a group, through the page table of its first
-    sequence.  max_shared bounds d_shared (default: max_ctx)."""
+    [n_groups]): those are read through the page table of the group's first
+    sequence, once for the group where that pays.  max_shared bounds d_shared (default: max_ctx)."""
     _operator("sara_kv8_group_attention", _ops.kv8_group_attention, stream,
               (k_cache, v_cache, k_exp, v_exp, d_q, d_out, d_pages, d_ctx, d_off, d_groups, d_shared, scale, max_ctx, max_shared,
                workspace))

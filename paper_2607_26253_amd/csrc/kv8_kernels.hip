@@ -356,15 +356,17 @@ struct AttnArgs {
   // partial results (HD numerators, maximum, sum): k_kv8_attn's [sequence][KV head][column][split], k_kv8_attn_tile's
   // [row][head][split]
   float *part, *part_tile;
-  // sequences in groups that share pages (k_kv8_group_*), and the partial results over those, [row][head][split]
+  // sequences in groups that share pages (k_kv8_group_*), and the partial results over those, [row][head][split][HD + 4]
   const int32_t *groups, *shared;
   int n_groups, max_shared, splits_shared, pps_shared, n_kv;
   float* part_shared;
+  int finish;               // rows whose own keys are one split join the shared pages' results where they end
 };
 
-// What a block of attention works on: a sequence's whole context; the pages that a group shares, for all of its rows;
-// or what a sequence has behind those.
-enum { kWhole, kShared, kOwn };
+// What a block of attention works on: a sequence's whole context, through its own page table or with the pages that its
+// group shares through the first sequence's; the pages that a group shares, for all of its rows; or what a sequence has
+// behind those.
+enum { kWhole, kVia, kShared, kOwn };
 
 // whole pages among the tokens that a group shares
 __device__ __forceinline__ int shared_pages(const AttnArgs& a, int tokens) { return max(min(tokens, a.max_shared), 0) >> 4; }
@@ -379,21 +381,34 @@ __device__ __forceinline__ int first_row_of(const AttnArgs& a, int i) {
   i = min(max(i, 0), a.n_seqs);
   return min(max(a.off ? a.off[i] : i, 0), a.n_rows);
 }
-// The group of item b, as find_seq numbers them, by the rows of groups: seq is the group, value the tokens it shares.
-template <int DIV> __device__ __forceinline__ SeqRows find_group(const AttnArgs& a, int b, int mul) {
+// The group of item b, as find_seq numbers them, by the rows of groups: its rows, its first sequence and one past its last,
+// and the tokens it shares.
+struct GroupRows { int group, first, r0, r1, seq0, seq1, shared; };
+template <int DIV> __device__ __forceinline__ GroupRows find_group(const AttnArgs& a, int b, int mul) {
   const int lane = threadIdx.x & 63;
   int lo = 0, hi = a.n_groups;
   while (true) {
     const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-    int at = 0x7FFFFFFF;
-    if (i < hi) at = (int)((int64_t)first_row_of(a, a.groups[i]) * mul / DIV) + i;
+    int at = 0x7FFFFFFF, s0 = 0, s1 = 0, r0 = 0, r1 = 0, shared = 0;
+    if (i < hi) {
+      s0 = a.groups[i];
+      if (step <= 1) { s1 = a.groups[i + 1]; shared = a.shared[i]; }
+      r0 = first_row_of(a, s0);
+      if (step <= 1) r1 = first_row_of(a, s1);
+      at = (int)((int64_t)r0 * mul / DIV) + i;
+    }
     const int n = __popcll(__ballot(at <= b));
-    if (n == 0) return SeqRows{-1, 0, 0, 0, 0};
+    if (n == 0) return GroupRows{-1, 0, 0, 0, 0, 0, 0};
     lo += (n - 1) * step;
     hi = min(hi, lo + step);
     if (step > 1) continue;
-    const int r0 = first_row_of(a, a.groups[lo]);
-    return SeqRows{lo, __builtin_amdgcn_readlane(at, n - 1), r0, max(r0, first_row_of(a, a.groups[lo + 1])), a.shared[lo]};
+    GroupRows g = {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readlane(at, n - 1), __builtin_amdgcn_readlane(r0, n - 1),
+                   __builtin_amdgcn_readlane(r1, n - 1), __builtin_amdgcn_readlane(s0, n - 1), __builtin_amdgcn_readlane(s1, n - 1),
+                   __builtin_amdgcn_readlane(shared, n - 1)};
+    g.r1 = max(g.r0, g.r1);
+    g.seq0 = min(max(g.seq0, 0), a.n_seqs);
+    g.seq1 = min(max(g.seq1, 0), a.n_seqs);
+    return g;
   }
 }
 
@@ -428,6 +443,22 @@ constexpr int kTileWaves = 4;          // one for each page of a key block
 // over 4,000 tokens: 226 us, against 229 with the maximum itself).
 constexpr float kSlack = 8.f;
 
+// A row's partial results over the `begin` pages that its group shares, joined into a maximum m, a sum l and numerators:
+// take(partial numerators, factor of those so far, weight of these).
+template <int HD, typename F>
+__device__ __forceinline__ void join_shared(const AttnArgs& a, int row, int head, int begin, float& m, float& l, F&& take) {
+  const int ns = (begin + a.pps_shared - 1) / a.pps_shared;
+  const float* p = a.part_shared + ((size_t)row * a.hq + head) * a.splits_shared * (HD + 4);
+  for (int s = 0; s < ns; ++s, p += HD + 4) {
+    const f32x2 ml = *(const f32x2*)(p + HD);
+    const float to = fmaxf(m, ml[0]), sub = to == -INFINITY ? 0.f : to;
+    const float old = __builtin_amdgcn_exp2f(m - sub), w = __builtin_amdgcn_exp2f(ml[0] - sub);
+    l = fmaf(w, ml[1], old * l);
+    take(p, old, w);
+    m = to;
+  }
+}
+
 template <int HD> struct FewLds {
   float m_w[4][16], l_w[4][16], o_w[4][16][HD + 4];
 };
@@ -447,7 +478,7 @@ template <int HD> struct FewLds {
 // 8 waves take 6.7 us there, but 22 for the 32 rows' 18.2 with the join.
 // A weight times its page's scale is held to bf16's range: below 2^-126 it may count as 0, which matters where all of V is
 // below about 1e-30 (at 1e-24 fp32 queries lose nothing).
-template <int HD, int FMT, typename T, int WHAT = kWhole>
+template <int HD, int FMT, typename T, int WHAT>
 __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs& a, FewLds<HD>& lds, int bx, int split) {
   constexpr int NK = HD / 64, NT = HD / 16, DV = HD / 16;   // 16-byte K loads, dim tiles, V dims a lane
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
@@ -464,18 +495,23 @@ __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs
   const int n_cols = (r1 - r0) * G;
   if (c0 >= n_cols || (a.off && n_cols > kFewColumns)) return;
   const int p0 = split * a.pps;
-  int begin = 0, group;                                  // pages before the block's first
-  if constexpr (WHAT == kOwn) begin = shared_pages_of(a, seq, group);
+  int begin = 0, owner = 0, shared = 0;                  // pages before the block's first; pages through another's table
+  if constexpr (WHAT == kOwn) begin = shared_pages_of(a, seq, owner);
+  if constexpr (WHAT == kVia) shared = shared_pages_of(a, seq, owner);
   // ids of 32 of the wave's page pairs, one a lane; the first are loaded beside the context's length
   const int32_t* table = a.pages + (size_t)seq * a.max_pages;
-  auto load_ids = [&](int it) { return table[min(begin + p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1), a.max_pages - 1)]; };
+  auto load_ids = [&](int it) {
+    const int i = min(begin + p0 + 2 * wave + 8 * (it + (lane >> 1)) + (lane & 1), a.max_pages - 1);
+    if constexpr (WHAT == kVia) return (i < shared ? a.pages + (size_t)owner * a.max_pages : table)[i];
+    return table[i];
+  };
   int ids = load_ids(0);
   int ctx = max(a.ctx[seq], 0);
   const bool too_long = ctx > a.max_ctx;                 // more than the launch was sized for: the rows are NaN
   if constexpr (WHAT == kOwn) ctx = max(ctx - 16 * begin, 0);   // from here on, positions count from the block's first page
   const int np = too_long ? 0 : (ctx + 15) >> 4;
   const int p1 = min(np, p0 + a.pps);
-  if (p0 >= p1 && (WHAT == kOwn || split > 0)) return;
+  if (p0 >= p1 && (split > 0 || (WHAT == kOwn && !a.finish))) return;
   // this lane's column: query row and head, and how many keys it sees
   const int cc = min(c0 + col, n_cols - 1), qt = cc / G, head = g * G + cc - qt * G;
   int before = ctx - (r1 - r0);                          // keys before the first query (below 0: its row sees none)
@@ -648,7 +684,13 @@ __device__ __forceinline__ void attn_few(const sara_kv8_cache& c, const AttnArgs
       den += wt * l_w[w][x];
     }
     const int t = (c0 + x) / G, h = g * G + (c0 + x) - t * G;
-    if (WHAT == kWhole && np <= a.pps) {
+    if ((WHAT < kShared || a.finish) && np <= a.pps) {
+      if constexpr (WHAT == kOwn) {
+        float m_all = mx;
+        join_shared<HD>(a, r0 + t, h, begin, m_all, den, [&](const float* q, float old, float w) {
+          num = old * num + w * *(const f32x4*)(q + d4);
+        });
+      }
       T* dst = (T*)a.out + (size_t)(r0 + t) * a.o_row + (size_t)h * a.o_head + d4;
       float f[4];
 #pragma unroll
@@ -690,7 +732,7 @@ template <int HD> struct TileLds {
 // Queries of fp32 have 96 MFMAs (three parts of q, three of a weight) beside 718 vector instructions, and 256 registers: one
 // block a CU, whose one wave a SIMD overlaps little: vector issue 43%, MFMAs 40%.  Three prompts of 1,100-4,590: 408 us,
 // against 218 in bf16.
-template <int HD, int FMT, typename T, int WHAT = kWhole>
+template <int HD, int FMT, typename T, int WHAT>
 __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArgs& a, TileLds<HD>& lds, int bx, int n_bx, int split) {
   constexpr int NW = kTileWaves, NKS = HD / 16, NDT = HD / 32;
   constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
@@ -701,25 +743,33 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, h = lane >> 5;
   const int hkv = c.n_kv_heads, G = a.hq / hkv;
   const int item = n_bx / hkv - 1 - bx / hkv, g = bx % hkv;          // long tiles first
-  const SeqRows sr = WHAT == kShared ? find_group<32 * NW>(a, item, G) : find_seq<32 * NW>(a.off, a.ctx, a.n_seqs, a.n_rows, item, G, 1);
+  SeqRows sr = {};
+  GroupRows gr = {};
+  if constexpr (WHAT == kShared) {
+    gr = find_group<32 * NW>(a, item, G);
+    sr = SeqRows{gr.group, gr.first, gr.r0, gr.r1, gr.shared};
+  } else {
+    sr = find_seq<32 * NW>(a.off, a.ctx, a.n_seqs, a.n_rows, item, G, 1);
+  }
   int seq = sr.seq;
   const int r0 = sr.r0, r1 = sr.r1;
   if (seq < 0 || item < sr.first) return;
   const int n_cols = (r1 - r0) * G, c0 = 32 * NW * (item - sr.first);
   if (c0 >= n_cols || (WHAT != kShared && n_cols <= kFewColumns)) return;
-  int ctx = max(sr.value, 0), begin = 0, group;
+  int ctx = max(sr.value, 0), begin = 0, owner = 0, shared = 0;
   const bool too_long = WHAT != kShared && ctx > a.max_ctx;
   if constexpr (WHAT == kShared) {
     ctx = 16 * shared_pages(a, sr.value);
-    seq = min(max(a.groups[sr.seq], 0), a.n_seqs - 1);              // whose table it is
+    seq = gr.seq0;                                                  // whose table it is
   }
   if constexpr (WHAT == kOwn) {
-    begin = shared_pages_of(a, seq, group);
+    begin = shared_pages_of(a, seq, owner);
     ctx = max(ctx - 16 * begin, 0);                                 // from here on, positions count from the block's first page
   }
+  if constexpr (WHAT == kVia) shared = shared_pages_of(a, seq, owner);
   const int np = too_long ? 0 : (ctx + 15) >> 4;
   const int pps = WHAT == kShared ? a.pps_shared : a.pps_tile, p0 = split * pps;
-  if (p0 >= np && (WHAT != kWhole || split > 0)) return;
+  if (p0 >= np && (split > 0 || WHAT == kShared || (WHAT == kOwn && !a.finish))) return;
   const int before = WHAT == kOwn ? max(sr.value, 0) - (r1 - r0) - 16 * begin : ctx - (r1 - r0);
   const int c_last = min(c0 + 32 * NW, n_cols) - 1;
   const int keys = WHAT == kShared ? ctx : min(max(before + c_last / G + 1, 0), ctx);   // keys that some column of the block sees
@@ -734,7 +784,7 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
   if constexpr (WHAT == kShared) {
     // the rows of a group are several sequences', each with its own context
     const int at = r0 + qt;
-    int lo = min(max(a.groups[sr.seq], 0), a.n_seqs), hi = min(max(a.groups[sr.seq + 1], 0), a.n_seqs);
+    int lo = gr.seq0, hi = gr.seq1;
     if (a.off) {
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -791,7 +841,8 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
   auto load = [&](int kb) {
     if ((kb & 15) == 0) {
       const int pg = p0 + 4 * kb + lane;
-      const int id = pg < p1 ? table[pg] : -1;
+      const int32_t* from = WHAT == kVia && pg < shared ? a.pages + (size_t)owner * a.max_pages : table;
+      const int id = pg < p1 ? from[pg] : -1;
       const bool have = id >= 0 && id < c.n_pages;
       ids = have ? id : 0;
       const size_t block = (size_t)ids * hkv + g;
@@ -998,11 +1049,25 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
   }
   l += __shfl_xor(l, 32, 64);
   if (!live || wc0 + col >= n_cols) return;
+  const bool whole = (WHAT < kShared || (WHAT == kOwn && a.finish)) && np <= a.pps_tile;
+  if constexpr (WHAT == kOwn) {
+    if (whole)
+      join_shared<HD>(a, r0 + qt, head, begin, m, l, [&](const float* q, float old, float w) {
+#pragma unroll
+        for (int t = 0; t < NDT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const f32x4 v = *(const f32x4*)(q + 32 * t + 16 * h + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[t][4 * i + (e >> 2)] = fmaf(w, v[i], old * o[t][4 * i + (e >> 2)]);
+          }
+      });
+  }
   const float inv = too_long ? __uint_as_float(0x7FC00000u) : l == 0.f ? 0.f : 1.f / l;
-  const bool whole = WHAT == kWhole && np <= a.pps_tile;
   T* out = (T*)a.out + (size_t)(r0 + qt) * a.o_row + (size_t)head * a.o_head + 16 * h;
   float* part = (WHAT == kShared ? a.part_shared : a.part_tile) +
-                (((size_t)(r0 + qt) * a.hq + head) * (WHAT == kShared ? a.splits_shared : a.splits_tile) + split) * (HD + 2);
+                (((size_t)(r0 + qt) * a.hq + head) * (WHAT == kShared ? a.splits_shared : a.splits_tile) + split) *
+                    (WHAT == kShared ? HD + 4 : HD + 2);
 #pragma unroll
   for (int t = 0; t < NDT; ++t) {
     float f[16];
@@ -1013,6 +1078,9 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
       for (int e = 0; e < 16; ++e) f[e] *= inv;
       store8<T>(out + 32 * t, f);
       store8<T>(out + 32 * t + 8, f + 8);
+    } else if constexpr (WHAT == kShared) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) *(f32x4*)(part + 32 * t + 16 * h + e) = f32x4{f[e], f[e + 1], f[e + 2], f[e + 3]};
     } else {
 #pragma unroll
       for (int e = 0; e < 16; e += 2) *(f32x2*)(part + 32 * t + 16 * h + e) = f32x2{f[e], f[e + 1]};
@@ -1021,23 +1089,23 @@ __device__ __forceinline__ void attn_tile(const sara_kv8_cache& c, const AttnArg
   if (!whole && h == 0) *(f32x2*)(part + HD) = f32x2{m, l};
 }
 
-template <int HD, int FMT, typename T>
+template <int HD, int FMT, typename T, int WHAT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void k_kv8_attn(sara_kv8_cache c, AttnArgs a) {
   __shared__ __attribute__((aligned(16))) FewLds<HD> lds;
-  attn_few<HD, FMT, T>(c, a, lds, blockIdx.x, blockIdx.y);
+  attn_few<HD, FMT, T, WHAT>(c, a, lds, blockIdx.x, blockIdx.y);
 }
-template <int HD, int FMT, typename T>
+template <int HD, int FMT, typename T, int WHAT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_tile(sara_kv8_cache c, AttnArgs a) {
   __shared__ __attribute__((aligned(16))) TileLds<HD> lds;
-  attn_tile<HD, FMT, T>(c, a, lds, blockIdx.x, gridDim.x, blockIdx.y);
+  attn_tile<HD, FMT, T, WHAT>(c, a, lds, blockIdx.x, gridDim.x, blockIdx.y);
 }
 // Both in one launch (see launch_kv8_attention): n_tile x splits_tile blocks of tiles, then n_few x splits of few columns.
-template <int HD, int FMT, typename T>
+template <int HD, int FMT, typename T, int WHAT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_attn_both(sara_kv8_cache c, AttnArgs a, int n_tile, int n_few) {
   __shared__ __attribute__((aligned(16))) union { FewLds<HD> few; TileLds<HD> tile; } lds;
   const int b = blockIdx.x, few = b - n_tile * a.splits_tile;
-  if (few < 0) attn_tile<HD, FMT, T>(c, a, lds.tile, b % n_tile, n_tile, b / n_tile);
-  else attn_few<HD, FMT, T>(c, a, lds.few, few % n_few, few / n_few);
+  if (few < 0) attn_tile<HD, FMT, T, WHAT>(c, a, lds.tile, b % n_tile, n_tile, b / n_tile);
+  else attn_few<HD, FMT, T, WHAT>(c, a, lds.few, few % n_few, few / n_few);
 }
 
 // A block per (row, head) joins the splits of rows that have more than one: its 4 waves take every fourth split,
@@ -1144,35 +1212,64 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_group_own_t
   attn_tile<HD, FMT, T, kOwn>(c, a, lds, blockIdx.x, gridDim.x, blockIdx.y);
 }
 
-// W waves join the partial results of a (row, head), 4 / W of those a block.
-template <int HD, typename T, int W>
-__global__ __launch_bounds__(256) void k_kv8_group_join(AttnArgs a) {
+// All three in one launch, where they are few (see launch_kv8_group_attention).
+template <int HD, int FMT, typename T>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_group_all(sara_kv8_cache c, AttnArgs a, int n_shared, int n_tile,
+    int n_few) {
+  __shared__ __attribute__((aligned(16))) union { FewLds<HD> few; TileLds<HD> tile; } lds;
+  const int b = blockIdx.x, tile = b - n_shared * a.splits_shared, few = tile - n_tile * a.splits_tile;
+  if (tile < 0) attn_tile<HD, FMT, T, kShared>(c, a, lds.tile, b % n_shared, n_shared, b / n_shared);
+  else if (few < 0) attn_tile<HD, FMT, T, kOwn>(c, a, lds.tile, tile % n_tile, n_tile, tile / n_tile);
+  else attn_few<HD, FMT, T, kOwn>(c, a, lds.few, few % n_few, few / n_few);
+}
+
+// W waves join the partial results of a (row, head), 4 / W of those a block.  TILE: the rows of k_kv8_group_own_tile's
+// sequences, by their number; else those of k_kv8_group_own_few's, `cols` columns for each sequence and KV head.
+template <int HD, typename T, int W, bool TILE>
+__global__ __launch_bounds__(256) void k_kv8_group_join(AttnArgs a, int items, int cols) {
   constexpr int DL = HD / 64;                            // dims a lane
   __shared__ float m_w[4], l_w[4], o_w[4][HD];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, G_item = blockIdx.x * (4 / W) + wave / W;
-  const bool have = G_item < a.n_rows * a.hq;
-  const int item = have ? G_item : 0, row = item / a.hq, h = item - row * a.hq;
-  SeqRows sr = {row, row, row, row + 1, 0};
-  if (a.off) sr = find_seq<1>(a.off, a.ctx, a.n_seqs, a.n_rows, row, 1, 0);
-  else sr.value = a.ctx[row];
-  const bool mine = have && sr.seq >= 0 && row >= sr.r0 && row < sr.r1;   // else a row of no sequence, left as it is
-  int first;
-  const int begin = mine ? shared_pages_of(a, sr.seq, first) : 0;
-  const int ctx = max(sr.value, 0), own = mine ? (max(ctx - 16 * begin, 0) + 15) >> 4 : 0;
-  const bool few = !a.off || (sr.r1 - sr.r0) * (a.hq / a.n_kv) <= kFewColumns, too_long = ctx > a.max_ctx;
-  const int pps = few ? a.pps : a.pps_tile, splits = few ? a.splits : a.splits_tile;
-  const int ns_shared = (begin + a.pps_shared - 1) / a.pps_shared, ns = too_long ? 0 : ns_shared + (own + pps - 1) / pps;
-  const float* p_shared = a.part_shared + (size_t)item * a.splits_shared * (HD + 2);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, item = min((int)blockIdx.x * (4 / W) + wave / W, items - 1);
   const int G = a.hq / a.n_kv;
-  const size_t own_item = few ? ((size_t)sr.seq * a.n_kv + h / G) * (a.off ? kFewColumns : G) + (row - sr.r0) * G + h % G : item;
-  const float* p_own = (few ? a.part : a.part_tile) + own_item * splits * (HD + 2) - (size_t)ns_shared * (HD + 2);
+  int seq, row, h, r0, r1, ctx;
+  bool mine = (int)blockIdx.x * (4 / W) + wave / W < items;
+  if (TILE) {
+    row = item / a.hq;
+    h = item - row * a.hq;
+    const SeqRows sr = find_seq<1>(a.off, a.ctx, a.n_seqs, a.n_rows, row, 1, 0);
+    seq = sr.seq;
+    r0 = sr.r0;
+    ctx = sr.value;
+    mine = mine && seq >= 0 && row >= sr.r0 && row < sr.r1 && (sr.r1 - sr.r0) * G > kFewColumns;
+  } else {
+    const int gc = item / cols, x = item - gc * cols;
+    seq = gc / a.n_kv;
+    ctx = a.ctx[seq];
+    seq_rows(a.off, seq, a.n_rows, r0, r1);
+    const int n_cols = (r1 - r0) * G;
+    mine = mine && x < n_cols && !(a.off && n_cols > kFewColumns);
+    row = r0 + x / G;
+    h = (gc - seq * a.n_kv) * G + x % G;
+  }
+  if (W == 4 && !mine) return;                             // a block is one row
+  int first;
+  const int begin = mine ? shared_pages_of(a, seq, first) : 0;
+  ctx = max(ctx, 0);
+  const int own = mine ? (max(ctx - 16 * begin, 0) + 15) >> 4 : 0;
+  const bool too_long = ctx > a.max_ctx;
+  const int pps = TILE ? a.pps_tile : a.pps, splits = TILE ? a.splits_tile : a.splits;
+  if (a.finish && own <= pps) mine = false;                // joined already
+  if (W == 4 && !mine) return;
+  const int ns_shared = (begin + a.pps_shared - 1) / a.pps_shared, ns = too_long || !mine ? 0 : ns_shared + (own + pps - 1) / pps;
+  const float* p_shared = a.part_shared + ((size_t)row * a.hq + h) * a.splits_shared * (HD + 4);
+  const float* p_own = (TILE ? a.part_tile : a.part) + (size_t)item * splits * (HD + 2);
   float m = -INFINITY, l = 0.f, o[DL] = {};
   for (int s0 = wave % W; s0 < ns; s0 += W * kJoin) {
     float pm[kJoin], pl[kJoin], po[kJoin][DL];
 #pragma unroll
     for (int i = 0; i < kJoin; ++i) {
       const int s = min(s0 + W * i, ns - 1);
-      const float* q = (s < ns_shared ? p_shared : p_own) + (size_t)s * (HD + 2);
+      const float* q = s < ns_shared ? p_shared + (size_t)s * (HD + 4) : p_own + (size_t)(s - ns_shared) * (HD + 2);
       const f32x2 ml = *(const f32x2*)(q + HD);
       pm[i] = s0 + W * i < ns ? ml[0] : -INFINITY;
       pl[i] = ml[1];
@@ -1215,7 +1312,7 @@ __global__ __launch_bounds__(256) void k_kv8_group_join(AttnArgs a) {
 #pragma unroll
     for (int d = 0; d < DL; ++d) o_w[wave][DL * lane + d] = o[d];
     __syncthreads();
-    if (!mine || threadIdx.x >= HD) return;
+    if (threadIdx.x >= HD) return;
     const float mx = fmaxf(fmaxf(m_w[0], m_w[1]), fmaxf(m_w[2], m_w[3]));
     const float sub = mx == -INFINITY ? 0.f : mx;
     float num = 0.f, den = 0.f;
@@ -1298,25 +1395,22 @@ Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx,
   return s;
 }
 
-int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows,
-                         int hq, const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
-                         int max_ctx, float scale, void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st) {
-  const Kv8Split s = kv8_split(n_rows, hq, c.n_kv_heads, c.head_dim, n_seqs, max_ctx, off != nullptr);
-  const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
-                      s.splits, s.pps, s.splits_tile, s.pps_tile, scale * 1.4426950408889634f, (float*)ws,
-                      (float*)((char*)ws + s.part_bytes)};
+// kWhole or kVia
+template <int WHAT> static int launch_attention(const sara_kv8_cache& c, int dtype, const Kv8Split& s, const AttnArgs& a, hipStream_t st) {
+  const int n_seqs = a.n_seqs, n_rows = a.n_rows, hq = a.hq;
+  const int32_t* off = a.off;
   return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
     const int n_few = (int)(s.items * c.n_kv_heads), n_tile = (int)(s.tile_items * c.n_kv_heads);
     // One launch for both where the blocks of few columns fit beside each other at the tiles' two a CU: 64 sequences of
     // 1-33 fp32 queries over up to 63 tokens 12.4 -> 8.0 us, of 1-33 bf16 ones over up to 500 31.2 -> 22.9.  More of them
     // lose the third wave a SIMD that streaming pages wants: 512 sequences of 1-2 queries over 1,000 tokens 70 -> 80.
     if (s.tile_items && (int64_t)n_few * s.splits <= 512) {
-      hipLaunchKernelGGL((k_kv8_attn_both<hd.value, fmt.value, decltype(t)>), dim3(n_tile * s.splits_tile + n_few * s.splits), dim3(256),
+      hipLaunchKernelGGL((k_kv8_attn_both<hd.value, fmt.value, decltype(t), WHAT>), dim3(n_tile * s.splits_tile + n_few * s.splits), dim3(256),
                          0, st, c, a, n_tile, n_few);
     } else {
-      hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t)>), dim3(n_few, s.splits), dim3(256), 0, st, c, a);
+      hipLaunchKernelGGL((k_kv8_attn<hd.value, fmt.value, decltype(t), WHAT>), dim3(n_few, s.splits), dim3(256), 0, st, c, a);
       if (s.tile_items)
-        hipLaunchKernelGGL((k_kv8_attn_tile<hd.value, fmt.value, decltype(t)>), dim3(n_tile, s.splits_tile), dim3(256), 0, st, c, a);
+        hipLaunchKernelGGL((k_kv8_attn_tile<hd.value, fmt.value, decltype(t), WHAT>), dim3(n_tile, s.splits_tile), dim3(256), 0, st, c, a);
     }
     if (s.splits > 1) {
       const int cols = off ? kFewColumns : hq / c.n_kv_heads;
@@ -1329,7 +1423,19 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
   });
 }
 
-Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged) {
+int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows,
+                         int hq, const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
+                         int max_ctx, float scale, void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st) {
+  const Kv8Split s = kv8_split(n_rows, hq, c.n_kv_heads, c.head_dim, n_seqs, max_ctx, off != nullptr);
+  const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
+                      s.splits, s.pps, s.splits_tile, s.pps_tile, scale * 1.4426950408889634f, (float*)ws,
+                      (float*)((char*)ws + s.part_bytes)};
+  return launch_attention<kWhole>(c, dtype, s, a, st);
+}
+
+constexpr int kSharedBlocks = 1024;
+Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged,
+                              int dtype) {
   const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16), np_shared = max_shared / 16;
   auto share = [&](int pages, int64_t items, int64_t blocks, int least, int step) {
     return split_pages(pages, items * hkv, blocks, least, step);
@@ -1337,17 +1443,40 @@ Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, i
   Kv8GroupSplit s = {};
   s.few_items = (int64_t)n_seqs * (ragged ? kFewColumns / 16 : (G + 15) / 16);
   s.tile_items = ragged && (int64_t)n_rows * G > kFewColumns ? (int64_t)n_rows * G / (32 * kTileWaves) + n_seqs : 0;
-  s.shared_items = np_shared > 0 ? (int64_t)n_rows * G / (32 * kTileWaves) + n_groups : 0;
+  s.shared_items = np_shared > 0 && n_groups > 0 ? (int64_t)n_rows * G / (32 * kTileWaves) + n_groups : 0;
   s.pps = share(np, ragged ? n_seqs : s.few_items, 1024, 24, 8);
   s.pps_tile = share(np, std::max<int64_t>(1, s.tile_items), 512, 32, 16);
-  s.pps_shared = share(std::max(1, np_shared), std::max<int64_t>(1, s.shared_items), 512, 8, 4);
+  // the tiles that there are if groups are alike: numbering them leaves room for one more a group
+  const int64_t cols = n_groups > 0 ? ((int64_t)n_rows * G + n_groups - 1) / n_groups : 0;
+  const int64_t tiles = std::max<int64_t>(1, n_groups * ((cols + 32 * kTileWaves - 1) / (32 * kTileWaves)));
+  s.pps_shared = share(std::max(1, np_shared), tiles, kSharedBlocks, tiles * hkv < 64 ? 8 : 16, 4);
   s.splits = (np + s.pps - 1) / s.pps;
   s.splits_tile = s.tile_items ? (np + s.pps_tile - 1) / s.pps_tile : 0;
   s.splits_shared = s.shared_items ? (np_shared + s.pps_shared - 1) / s.pps_shared : 0;
+  // Few blocks run in one launch, which a join follows; more of them end with the shared pages' results in hand, unless
+  // those are many.
+  s.all = (s.few_items * s.splits + s.tile_items * s.splits_tile) * hkv <= 512;
+  s.finish = !s.all && s.splits_shared <= 8;
   const int64_t one = (int64_t)sizeof(float) * (hd + 2);
-  s.part_bytes = one * n_seqs * hkv * (ragged ? kFewColumns : G) * s.splits;
-  s.part_tile_bytes = one * n_rows * hq * s.splits_tile;
-  s.part_shared_bytes = one * n_rows * hq * s.splits_shared;
+  if (!s.finish || s.splits > 1) s.part_bytes = (one * n_seqs * hkv * (ragged ? kFewColumns : G) * s.splits + 15) / 16 * 16;
+  if (!s.finish || s.splits_tile > 1) s.part_tile_bytes = (one * n_rows * hq * s.splits_tile + 15) / 16 * 16;
+  s.part_shared_bytes = (int64_t)sizeof(float) * (hd + 4) * n_rows * hq * s.splits_shared;
+  // What a group shares is taken apart where that saves more than it costs: the partial results' way to memory and back and
+  // about 12 us of launches.  Without it every sequence reads those pages, most of them from the caches, at some 8 TB/s if its
+  // columns are few, or in tiles of 128 columns that a single sequence may not fill (1.8 us a key block and compute
+  // unit; 3.4 with fp32 queries).  Eight rollouts of one prompt of 497 tokens: 10 us together, 13 apart; 512 rows of 64
+  // prompts of 256-1,024 tokens 67 and 60; 32 rows behind 65,536 tokens 136 and 74; 3,700 rows behind four prompts of
+  // 1,100-4,590 tokens 214 and 239.
+  double saved = 0;
+  if (s.shared_items) {
+    const int64_t of_seq = (int64_t)n_rows * G / std::max(1, n_seqs), fill = 32 * kTileWaves;
+    if (of_seq <= kFewColumns)
+      saved = (double)std::max(0, n_seqs - n_groups) * max_shared * hkv * hd * 2 / 8e6;
+    else
+      saved = (double)std::max<int64_t>(0, n_seqs * ((of_seq + fill - 1) / fill) - tiles) * hkv * (max_shared / 64) *
+              (dtype == SARA_BF16 ? 1.8 : 3.4) / 256;
+  }
+  s.apart = saved > 12 + 2 * s.part_shared_bytes / 4e6;
   return s;
 }
 
@@ -1356,26 +1485,45 @@ int launch_kv8_group_attention(const sara_kv8_cache& c, const void* q, int dtype
                                const int32_t* groups, const int32_t* shared, int n_groups, int max_ctx, int max_shared, float scale,
                                void* out, int64_t o_row, int64_t o_head, void* ws, hipStream_t st) {
   const int hkv = c.n_kv_heads;
-  const Kv8GroupSplit s = kv8_group_split(n_rows, hq, hkv, c.head_dim, n_seqs, n_groups, max_ctx, max_shared, off != nullptr);
+  const Kv8GroupSplit s = kv8_group_split(n_rows, hq, hkv, c.head_dim, n_seqs, n_groups, max_ctx, max_shared, off != nullptr, dtype);
   char* part = (char*)ws;
+  if (!s.apart) {
+    const Kv8Split w = kv8_split(n_rows, hq, hkv, c.head_dim, n_seqs, max_ctx, off != nullptr);
+    const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
+                        w.splits, w.pps, w.splits_tile, w.pps_tile, scale * 1.4426950408889634f, (float*)part,
+                        (float*)(part + w.part_bytes), groups, shared, n_groups, max_shared};
+    return n_groups > 0 && max_shared >= 16 ? launch_attention<kVia>(c, dtype, w, a, st) : launch_attention<kWhole>(c, dtype, w, a, st);
+  }
   const AttnArgs a = {q, out, q_row, q_head, o_row, o_head, pages, ctx, off, max_pages, max_ctx, n_seqs, n_rows, hq,
                       s.splits, s.pps, s.splits_tile, s.pps_tile, scale * 1.4426950408889634f, (float*)part,
                       (float*)(part + s.part_bytes), groups, shared, n_groups, max_shared, s.splits_shared, s.pps_shared, hkv,
-                      (float*)(part + s.part_bytes + s.part_tile_bytes)};
+                      (float*)(part + s.part_bytes + s.part_tile_bytes), s.finish};
   return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
-    if (s.shared_items)
-      hipLaunchKernelGGL((k_kv8_group_shared<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.shared_items * hkv), s.splits_shared),
-                         dim3(256), 0, st, c, a);
-    hipLaunchKernelGGL((k_kv8_group_own_few<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.few_items * hkv), s.splits), dim3(256), 0,
-                       st, c, a);
-    if (s.tile_items)
-      hipLaunchKernelGGL((k_kv8_group_own_tile<hd.value, fmt.value, decltype(t)>), dim3((uint32_t)(s.tile_items * hkv), s.splits_tile),
-                         dim3(256), 0, st, c, a);
-    const int64_t items = (int64_t)n_rows * hq;
-    if (s.splits + s.splits_tile + s.splits_shared > 16)
-      hipLaunchKernelGGL((k_kv8_group_join<hd.value, decltype(t), 4>), dim3((uint32_t)items), dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL((k_kv8_group_join<hd.value, decltype(t), 1>), dim3((uint32_t)((items + 3) / 4)), dim3(256), 0, st, a);
+    const int n_shared = (int)(s.shared_items * hkv), n_tile = (int)(s.tile_items * hkv), n_few = (int)(s.few_items * hkv);
+    if (s.all) {
+      hipLaunchKernelGGL((k_kv8_group_all<hd.value, fmt.value, decltype(t)>),
+                         dim3(n_shared * s.splits_shared + n_tile * s.splits_tile + n_few * s.splits), dim3(256), 0, st, c, a, n_shared,
+                         n_tile, n_few);
+    } else {
+      if (n_shared)
+        hipLaunchKernelGGL((k_kv8_group_shared<hd.value, fmt.value, decltype(t)>), dim3(n_shared, s.splits_shared), dim3(256), 0, st, c, a);
+      hipLaunchKernelGGL((k_kv8_group_own_few<hd.value, fmt.value, decltype(t)>), dim3(n_few, s.splits), dim3(256), 0, st, c, a);
+      if (n_tile)
+        hipLaunchKernelGGL((k_kv8_group_own_tile<hd.value, fmt.value, decltype(t)>), dim3(n_tile, s.splits_tile), dim3(256), 0, st, c, a);
+    }
+    const int cols = off ? kFewColumns : hq / hkv, few = n_seqs * hkv * cols, rows = n_rows * hq;
+    const bool many = s.finish || s.splits + s.splits_tile + s.splits_shared > 16;   // splits to a row
+    auto join = [&](auto k, int items, int waves) {
+      hipLaunchKernelGGL(k, dim3((uint32_t)((items + 4 / waves - 1) / (4 / waves))), dim3(256), 0, st, a, items, cols);
+    };
+    if (!s.finish || s.splits > 1) {
+      if (many) join(k_kv8_group_join<hd.value, decltype(t), 4, false>, few, 4);
+      else join(k_kv8_group_join<hd.value, decltype(t), 1, false>, few, 1);
+    }
+    if (n_tile && (!s.finish || s.splits_tile > 1)) {
+      if (many) join(k_kv8_group_join<hd.value, decltype(t), 4, true>, rows, 4);
+      else join(k_kv8_group_join<hd.value, decltype(t), 1, true>, rows, 1);
+    }
   });
 }
 

@@ -281,7 +281,7 @@ PyObject* kv8_group_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t max_ctx = bound(a[12], 16 * (int64_t)s.width, "max_ctx"), max_shared = bound(a[13], max_ctx, "max_shared");
     int64_t need = 0;
     int rc = sara_kv8_group_attention_workspace(c.n_kv_heads, c.head_dim, n_rows, heads, s.n, n_groups, s.off != nullptr, max_ctx,
-                                                max_shared, &need);
+                                                max_shared, type, &need);
     if (rc) return rc;
     const Workspace ws = workspace(a[14], need, q, at);
     void* st = at.stream();

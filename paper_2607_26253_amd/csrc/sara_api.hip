@@ -976,19 +976,29 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
                               max_ctx, scale, d_out, o_row, o_head, d_ws, (hipStream_t)stream);
 }
 
-static int64_t group_bytes(const Kv8GroupSplit& s) { return s.part_bytes + s.part_tile_bytes + s.part_shared_bytes; }
+// Bytes that a grouped call needs for its partial results, and blocks of its largest launch.
+struct GroupNeed { int64_t bytes, blocks; };
+static GroupNeed group_need(int32_t hkv, int32_t hd, int32_t n_rows, int32_t hq, int32_t n_seqs, int32_t n_groups, bool ragged,
+                            int32_t max_ctx, int32_t max_shared, int32_t dtype) {
+  const Kv8GroupSplit g = kv8_group_split(n_rows, hq, hkv, hd, n_seqs, n_groups, max_ctx, max_shared, ragged, dtype);
+  if (g.apart)
+    return {g.part_bytes + g.part_tile_bytes + g.part_shared_bytes, std::max(std::max(g.few_items, g.tile_items), g.shared_items) * hkv};
+  const Kv8Split s = kv8_split(n_rows, hq, hkv, hd, n_seqs, max_ctx, ragged);
+  return {s.part_bytes + s.part_tile_bytes, std::max(s.items, s.tile_items) * hkv};
+}
 
 extern "C" int sara_kv8_group_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads, int32_t n_seqs,
                                                   int32_t n_groups, int32_t ragged, int32_t max_ctx, int32_t max_shared,
-                                                  int64_t* bytes) {
+                                                  int32_t dtype, int64_t* bytes) {
   if (!bytes) return einval("null argument");
   if (n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128))
     return einval("n_heads must be a multiple of n_kv_heads, head_dim 64 or 128");
   if (n_rows < 0 || n_seqs < 0 || n_groups < 0 || max_ctx < 0 || max_ctx > kMaxCtx || max_shared < 0 || max_shared > kMaxCtx)
     return einval("sizes must be >= 0, max_ctx and max_shared <= 2^30");
   if ((int64_t)n_rows * n_heads > (int64_t)1 << 30) return einval("too many rows or sequences");
+  if (dtype != SARA_BF16 && dtype != SARA_F32) return einval("dtype must be SARA_BF16 or SARA_F32");
   *bytes = n_rows == 0 || n_seqs == 0
-               ? 0 : group_bytes(kv8_group_split(n_rows, n_heads, n_kv_heads, head_dim, n_seqs, n_groups, max_ctx, max_shared, ragged != 0));
+               ? 0 : group_need(n_kv_heads, head_dim, n_rows, n_heads, n_seqs, n_groups, ragged != 0, max_ctx, max_shared, dtype).bytes;
   return SARA_OK;
 }
 
@@ -1013,14 +1023,10 @@ extern "C" int sara_kv8_group_attention(const sara_kv8_cache* c, const void* d_q
   if ((int64_t)n_rows * n_heads > (int64_t)1 << 30 || (int64_t)n_seqs * std::max(n_heads, 32 * c->n_kv_heads) > (int64_t)1 << 30)
     return einval("too many rows or sequences");
   if (rows_overlap(o_row, o_head, n_rows, n_heads, c->head_dim)) return einval("rows and heads of out must not overlap");
-  const Kv8GroupSplit split = kv8_group_split(n_rows, n_heads, c->n_kv_heads, c->head_dim, n_seqs, n_groups, max_ctx, max_shared,
-                                              d_off != nullptr);
-  if (std::max(std::max(split.few_items, split.tile_items), split.shared_items) * c->n_kv_heads > kMaxBlocks ||
-      (int64_t)n_rows * n_heads > kMaxBlocks)
-    return einval("too many rows or sequences");
-  const int64_t need = group_bytes(split);
-  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need)
-    return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
+  const GroupNeed g = group_need(c->n_kv_heads, c->head_dim, n_rows, n_heads, n_seqs, n_groups, d_off != nullptr, max_ctx, max_shared, dtype);
+  if (g.blocks > kMaxBlocks || (int64_t)n_rows * n_heads > kMaxBlocks) return einval("too many rows or sequences");
+  if (g.bytes > 0 && (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < g.bytes))
+    return einval("workspace of " + std::to_string(g.bytes) + " bytes, 16-byte aligned, is needed");
   return launch_kv8_group_attention(*c, d_q, dtype, q_row, q_head, n_rows, n_heads, d_pages, max_pages, d_ctx, d_off, n_seqs, d_groups,
                                     d_shared, n_groups, max_ctx, max_shared, scale, d_out, o_row, o_head, d_ws, (hipStream_t)stream);
 }

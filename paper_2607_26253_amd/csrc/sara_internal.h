@@ -330,8 +330,10 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
 struct Kv8GroupSplit {
   int splits, pps, splits_tile, pps_tile, splits_shared, pps_shared;
   int64_t few_items, tile_items, shared_items, part_bytes, part_tile_bytes, part_shared_bytes;
+  bool apart, all, finish;   // the shared pages on their own; one launch for all of it; rows of one own split need no join
 };
-Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged);
+Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged,
+                              int dtype);
 int launch_kv8_group_attention(const sara_kv8_cache& c, const void* q, int dtype, int64_t q_row, int64_t q_head, int n_rows, int hq,
                                const int32_t* pages, int max_pages, const int32_t* ctx, const int32_t* off, int n_seqs,
                                const int32_t* groups, const int32_t* shared, int n_groups, int max_ctx, int max_shared, float scale,
