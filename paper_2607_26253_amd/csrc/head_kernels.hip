@@ -766,28 +766,237 @@ __global__ __launch_bounds__(256) void k_head_pack(const T* __restrict__ x, int6
 // them), which leaves some 2^-9 sqrt(kBig) of the row.
 constexpr float kBig = 1.f / 16;
 
-__global__ __launch_bounds__(256) void k_head_rows(int n_rows, int rows_out, int V, const int32_t* __restrict__ tok,
-    const float* __restrict__ stats, const float* __restrict__ entropy, const float* __restrict__ g_logp,
-    const float* __restrict__ g_ent, float scale, float inv_c, HeadRow* __restrict__ out) {
-  const int r = blockIdx.x * 256 + threadIdx.x;
-  if (r >= rows_out) return;
+struct HeadGrads {
+  int n_rows, V;
+  const int32_t* tok;
+  const float *stats, *entropy, *g_logp, *g_ent;
+  float scale, inv_c;
+};
+__device__ __forceinline__ HeadRow head_row(const HeadGrads& a, int r) {
   HeadRow o = {0.f, 0.f, 0.f, 0.f, 0.f, -1, 0};
-  if (r < n_rows) {
-    const int tk = tok[r];
-    const bool has = tk >= 0 && tk < V;
-    const float m = stats[2 * (size_t)r], s = stats[2 * (size_t)r + 1];
-    const float g = has && g_logp ? g_logp[r] : 0.f, h = g_ent ? g_ent[r] : 0.f;
-    if (!(g == 0.f && h == 0.f))
-    {
-      // 1 / s is the largest p: |g| (1 - 1 / s) is at most |D| at the row's id, the other term |D| at its likeliest.  Where
-      // 2^u |A| and 2^u |B u| <= 1.07 2^(u / 2) |B| are below half of kBig of that, D is below kBig of it.
-      const float hl = h == 0.f ? 0.f : h * (entropy[r] - logf(s)), A = -(g + hl) / s, B = -0.69314718f * h / s;
-      const float half = 0.5f * kBig * (fabsf(g) * (1.f - 1.f / s) + fabsf(hl) / s);
-      const float u = B == 0.f ? log2f(2.f * half / fabsf(A)) : fminf(log2f(half / fabsf(A)), 2.f * log2f(half / (1.07f * fabsf(B))));
-      o = HeadRow{m, scale * A, scale * B, scale * g, m + fminf(u, 0.f) * inv_c, has ? tk : -1, 1};
+  if (r >= a.n_rows) return o;
+  const int tk = a.tok[r];
+  const bool has = tk >= 0 && tk < a.V;
+  const float m = a.stats[2 * (size_t)r], s = a.stats[2 * (size_t)r + 1];
+  const float g = has && a.g_logp ? a.g_logp[r] : 0.f, h = a.g_ent ? a.g_ent[r] : 0.f;
+  if (g == 0.f && h == 0.f) return o;
+  // 1 / s is the largest p: |g| (1 - 1 / s) is at most |D| at the row's id, the other term |D| at its likeliest.  Where
+  // 2^u |A| and 2^u |B u| <= 1.07 2^(u / 2) |B| are below half of kBig of that, D is below kBig of it.
+  const float hl = h == 0.f ? 0.f : h * (a.entropy[r] - logf(s)), A = -(g + hl) / s, B = -0.69314718f * h / s;
+  const float half = 0.5f * kBig * (fabsf(g) * (1.f - 1.f / s) + fabsf(hl) / s);
+  const float u = B == 0.f ? log2f(2.f * half / fabsf(A)) : fminf(log2f(half / fabsf(A)), 2.f * log2f(half / (1.07f * fabsf(B))));
+  return HeadRow{m, a.scale * A, a.scale * B, a.scale * g, m + fminf(u, 0.f) * a.inv_c, has ? tk : -1, 1};
+}
+
+__global__ __launch_bounds__(256) void k_head_rows(HeadGrads a, int rows_out, HeadRow* __restrict__ out) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r < rows_out) out[r] = head_row(a, r);
+}
+
+// ---------------------------------------------------------------------------
+// small problems
+// ---------------------------------------------------------------------------
+// Tiles of 32 x 32 on v_mfma_f32_16x16x4_f32, whose products of bf16 or fp32 numbers are exact before their sum in fp32: no
+// operand is packed or taken in parts, and D stays in fp32.  The four waves of a block take every fourth 16 elements of k,
+// straight from memory to registers four steps ahead, and join their sums in LDS.
+struct Rows { const void* p; int64_t stride; };
+
+struct HeadSmall {
+  HeadGrads g;              // of the forward: n_rows, V and tok
+  Rows h, w;
+  int d, m_parts;
+  float c, inv_t;
+  float* x_tok;
+  float4* parts;            // [32 ids][m_parts]
+  float* D;                 // [rows, a multiple of 32][ld], zero past the last row and id
+  int ld, h_blocks;         // blocks of dH, those of dW follow
+  HeadRow* rows;
+  void *gh, *gw;
+  int64_t gh_stride, gw_stride;
+  int gw_f32, add;
+};
+
+// 16 columns (or rows) of an operand by 16 of k: element (m, k) at p[m stride + k], or ACROSS at p[k stride + m].  Lane
+// (m, grp) takes k = 16 step + 4 grp ..+3; those at K and past it are 0, as are (ON) rows k that are off.
+template <typename T, bool ACROSS, bool ON>
+struct SmallOperand {
+  static constexpr int W = sizeof(T) == 2 && !ACROSS ? 2 : 4;
+  struct Raw { uint32_t w[W]; int on[ON ? 4 : 1]; };
+  const T* p;
+  const HeadRow* rows;
+  int64_t stride;
+  int K, k0;
+  __device__ SmallOperand(Rows m, const HeadRow* r, int t0, int n, int K_) : rows(r), stride(m.stride), K(K_) {
+    const int lane = threadIdx.x & 63, at = min(t0 + (lane & 15), n - 1);
+    k0 = 4 * (lane >> 4);
+    p = (const T*)m.p + (ACROSS ? at : at * m.stride);
+  }
+  __device__ __forceinline__ void load(Raw& x, int step) const {
+    const int k = k0 + 16 * step;
+    if constexpr (ACROSS) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int kk = min(k + j, K - 1);
+        if constexpr (sizeof(T) == 2) x.w[j] = p[kk * stride];
+        else x.w[j] = __float_as_uint(p[kk * stride]);
+        if (ON) x.on[j] = rows[kk].on;
+      }
+    } else {                                               // K is a multiple of 4
+      const T* q = p + min(k, K - 4);
+      if constexpr (sizeof(T) == 2) { const u32x2 v = *(const u32x2*)q; x.w[0] = v[0]; x.w[1] = v[1]; }
+      else { const u32x4 v = *(const u32x4*)q; x.w[0] = v[0]; x.w[1] = v[1]; x.w[2] = v[2]; x.w[3] = v[3]; }
     }
   }
-  out[r] = o;
+  __device__ __forceinline__ f32x4 value(const Raw& x, int step) const {
+    const int k = k0 + 16 * step;
+    f32x4 f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (W == 2) f[j] = __uint_as_float(j & 1 ? x.w[j >> 1] & 0xFFFF0000u : x.w[j >> 1] << 16);
+      else f[j] = __uint_as_float(sizeof(T) == 2 ? x.w[j] << 16 : x.w[j]);
+      f[j] = k + j < K && (!ON || x.on[ON ? j : 0]) ? f[j] : 0.f;
+    }
+    return f;
+  }
+};
+
+struct SmallLds {
+  float part[4][32][36];
+  HeadRow rows[32];
+};
+
+// Of the tile's sum: columns 4 (t % 8) ..+3 of row t / 8 for thread t
+template <typename A, typename B>
+__device__ __forceinline__ f32x4 small_tile(const A& a0, const A& a1, const B& b0, const B& b1, int K, SmallLds& lds) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
+  const int steps = (K + 15) >> 4;
+  constexpr int DEPTH = 4;
+  struct { typename A::Raw a[2]; typename B::Raw b[2]; } at[DEPTH];
+  auto load = [&](int s, int u) {
+    const int st = min(s, steps - 1);
+    a0.load(at[u].a[0], st);
+    a1.load(at[u].a[1], st);
+    b0.load(at[u].b[0], st);
+    b1.load(at[u].b[1], st);
+  };
+  f32x4 acc[2][2] = {};
+#pragma unroll
+  for (int u = 0; u < DEPTH; ++u) load(wave + 4 * u, u);
+  for (int s = wave; s < steps; s += 4 * DEPTH) {
+#pragma unroll
+    for (int u = 0; u < DEPTH; ++u) {
+      const int st = s + 4 * u;
+      if (st < steps) {
+        const f32x4 x[2] = {a0.value(at[u].a[0], st), a1.value(at[u].a[1], st)};
+        const f32x4 y[2] = {b0.value(at[u].b[0], st), b1.value(at[u].b[1], st)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[m][j], y[n][j], acc[m][n], 0, 0, 0);
+      }
+      load(st + 4 * DEPTH, u);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) lds.part[wave][16 * m + 4 * grp + q][16 * n + row] = acc[m][n][q];
+  __syncthreads();
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v += *(const f32x4*)&lds.part[w][threadIdx.x >> 3][4 * (threadIdx.x & 7)];
+  return v;
+}
+
+// The statistics of a tile of logits, or its D
+template <typename T, bool GRAD>
+__global__ __launch_bounds__(256, 2) void k_head_small(HeadSmall a) {
+  __shared__ __attribute__((aligned(16))) SmallLds lds;
+  const int M = a.g.n_rows, V = a.g.V, mb = (M + 31) >> 5, bn = blockIdx.x / mb, m0 = 32 * (blockIdx.x - bn * mb), n0 = 32 * bn;
+  if (GRAD && threadIdx.x < 32) {
+    const HeadRow r = head_row(a.g, m0 + threadIdx.x);
+    lds.rows[threadIdx.x] = r;
+    if (bn == 0) a.rows[m0 + threadIdx.x] = r;
+  }
+  typedef SmallOperand<T, false, false> Op;
+  const f32x4 z = small_tile(Op(a.h, nullptr, m0, M, a.d), Op(a.h, nullptr, m0 + 16, M, a.d), Op(a.w, nullptr, n0, V, a.d),
+                             Op(a.w, nullptr, n0 + 16, V, a.d), a.d, lds);
+  const int ri = threadIdx.x >> 3, r = m0 + ri, id = n0 + 4 * (threadIdx.x & 7), left = V - id;
+  if constexpr (GRAD) {
+    const HeadRow hr = lds.rows[ri];
+    f32x4 y;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      // x formed again may lie above the forward's maximum by its rounding, which a low temperature would blow up
+      const float u = __builtin_amdgcn_fmed3f((z[q] - hr.m) * a.c, -150.f, 0.f);
+      y[q] = __builtin_amdgcn_exp2f(u) * fmaf(hr.B, u, hr.A) + (id + q == hr.tok ? hr.g : 0.f);
+      if (!hr.on || q >= left) y[q] = 0.f;
+    }
+    *(f32x4*)(a.D + (int64_t)r * a.ld + id) = y;
+  } else {
+    const int tok = r < M ? a.g.tok[r] - id : -1;
+    HeadSum sum = {-FLT_MAX, 0.f, 0.f};                    // a logit that is not finite makes the row NaN
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      sum.m = fmaxf(sum.m, q < left ? z[q] : NAN);
+      if (q == tok && q < left) a.x_tok[r] = z[q];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float u = q < left ? (z[q] - sum.m) * a.c : -INFINITY;
+      const float e = q < left && z[q] == -INFINITY ? NAN : __builtin_amdgcn_exp2f(u);
+      sum.s += e;
+      sum.t = fmaf(e, fmaxf(u, -FLT_MAX), sum.t);
+    }
+#pragma unroll
+    for (int x = 1; x < 8; x <<= 1)
+      head_merge(sum, HeadSum{__shfl_xor(sum.m, x, 64), __shfl_xor(sum.s, x, 64), __shfl_xor(sum.t, x, 64)}, a.c);
+    if ((threadIdx.x & 7) == 0 && r < M) a.parts[(size_t)bn * a.m_parts + r] = make_float4(sum.m, sum.s, sum.t, 0.f);
+  }
+}
+
+// dH = D W and dW = D^T H
+template <typename T>
+__global__ __launch_bounds__(256, 2) void k_head_small_grads(HeadSmall a) {
+  __shared__ __attribute__((aligned(16))) SmallLds lds;
+  const int R = a.g.n_rows, V = a.g.V, nb = (a.d + 31) >> 5;
+  const bool of_h = (int)blockIdx.x < a.h_blocks;
+  const int b = of_h ? blockIdx.x : blockIdx.x - a.h_blocks, bm = b / nb, m0 = 32 * bm, n0 = 32 * (b - bm * nb);
+  const int ri = m0 + (threadIdx.x >> 3), col = n0 + 4 * (threadIdx.x & 7);
+  const Rows D = {a.D, a.ld};
+  f32x4 v;
+  if (of_h) {
+    typedef SmallOperand<float, false, false> A;
+    typedef SmallOperand<T, true, false> B;
+    v = small_tile(A(D, nullptr, m0, R, a.ld), A(D, nullptr, m0 + 16, R, a.ld), B(a.w, nullptr, n0, a.d, V), B(a.w, nullptr, n0 + 16, a.d, V),
+                   V, lds);
+    if (ri >= R || col >= a.d) return;                     // d is a multiple of 4
+    v = a.rows[ri].on ? v * a.inv_t : f32x4{0.f, 0.f, 0.f, 0.f};   // whatever the weight holds
+    T* y = (T*)a.gh + ri * a.gh_stride + col;
+    if constexpr (sizeof(T) == 2) *(uint2*)y = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    else *(f32x4*)y = v;
+    return;
+  }
+  typedef SmallOperand<float, true, false> A;
+  typedef SmallOperand<T, true, true> B;
+  v = small_tile(A(D, nullptr, m0, V, R), A(D, nullptr, m0 + 16, V, R), B(a.h, a.rows, n0, a.d, R), B(a.h, a.rows, n0 + 16, a.d, R), R, lds);
+  if (ri >= V || col >= a.d) return;
+  v *= a.inv_t;
+  if (a.gw_f32) {
+    f32x4* y = (f32x4*)((float*)a.gw + ri * a.gw_stride + col);
+    if (a.add) v += *y;
+    *y = v;
+  } else {
+    u32x2* y = (u32x2*)((uint16_t*)a.gw + ri * a.gw_stride + col);
+    if (a.add)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] += __uint_as_float(q & 1 ? (*y)[q >> 1] & 0xFFFF0000u : (*y)[q >> 1] << 16);
+    *y = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  }
 }
 
 // dH from the splits' sums
@@ -825,6 +1034,22 @@ constexpr int kCus = 256;
 
 static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
+// us of a product of small tiles and of large ones in `pairs` pairs of parts, by rounds of the compute units: 2.4 and 4 us for
+// each 256 of k and pair, half of that where a small tile has a compute unit to itself.  In all (small, large):
+//   fp32  509 rows, width 256, 512 ids     forward 12, 53   gradients 18, 186
+//         777      1024       4096                132, 133            306, 311
+//         1024     1024       8192                302, 143            735, 374
+//   bf16  512      512        2048                 31, 31              66, 105
+//         1024     512        2048                 54, 31             120, 131
+//         1024     1024       8192                297, 41             749, 155
+static double small_us(int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles = ((M + 31) / 32) * ((N + 31) / 32);
+  return 5 + (tiles <= kCus ? 0.5 : (double)(up(tiles, kCus) / kCus)) * K * 2.4 / 256;
+}
+static double large_us(int64_t M, int64_t N, int64_t K, int pairs) {
+  return 14 + (double)(up(((M + 255) / 256) * ((N + 255) / 256), kCus) / kCus) * K * pairs * 4 / 256;
+}
+
 HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool grad) {
   HeadPlan p = {};
   const bool f32 = dtype == SARA_F32;
@@ -840,11 +1065,25 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
       p.parts = take(16 * (int64_t)16 * p.nt * p.few_blocks);
       return p;
     }
+    p.small = small_us(n_rows, V, d) < large_us(n_rows, V, d, f32 ? 6 : 1) + (f32 ? 10 : 5);   // and what packing takes
+    if (p.small) {
+      p.parts = take(16 * (int64_t)n_rows * ((V + 31) / 32));
+      return p;
+    }
     p.rows_out = (int)up(n_rows, 256);
     p.parts = take(16 * (int64_t)std::min(p.rows_out, kStatRows) * cols);
     p.h_parts = take((f32 ? 6 : 2) * (int64_t)p.rows_out * p.width);
     p.piece = f32 ? (int)std::min<int64_t>(cols, std::max<int64_t>(1, kPieceBytes / (6 * 256 * (int64_t)p.width))) : cols;
     if (f32) p.w_parts = take(6 * 256 * (int64_t)p.piece * p.width);
+    return p;
+  }
+  const int pairs = f32 ? 6 : 1;
+  p.small = small_us(n_rows, V, d) + small_us(n_rows, d, V) + small_us(V, d, n_rows) <
+            large_us(n_rows, V, d, pairs) + large_us(n_rows, d, (V + 63) / 64, pairs) + large_us(V, d, n_rows, pairs) + (f32 ? 75 : 40);
+  if (p.small) {
+    p.width = (int)up(V, 32);
+    p.rows = take(sizeof(HeadRow) * up(n_rows, 32));
+    p.d = take(4 * up(n_rows, 32) * p.width);
     return p;
   }
   p.rows_out = (int)up(n_rows, 256);
@@ -921,6 +1160,25 @@ int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t
                        inv_t, logp, entropy, stats);
     return head_done("head log probabilities launch");
   }
+  if (p.small) {
+    HeadSmall a = {};
+    a.g.n_rows = n_rows;
+    a.g.V = V;
+    a.g.tok = tok;
+    a.h = Rows{h, h_stride};
+    a.w = Rows{w, w_stride};
+    a.d = d;
+    a.m_parts = n_rows;
+    a.c = c;
+    a.x_tok = x_tok;
+    a.parts = parts;
+    const dim3 grid((n_rows + 31) / 32 * ((V + 31) / 32));
+    if (dtype == SARA_F32) hipLaunchKernelGGL((k_head_small<float, false>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_head_small<uint16_t, false>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_head_join<16>), dim3((n_rows + 15) / 16), dim3(256), 0, st, parts, (V + 31) / 32, n_rows, 0, n_rows, V, tok, x_tok, c,
+                       inv_t, logp, entropy, stats);
+    return head_done("head log probabilities launch");
+  }
   const bool f32 = dtype == SARA_F32;
   uint16_t *hp = (uint16_t*)((char*)ws + p.h_parts), *wp = (uint16_t*)((char*)ws + p.w_parts);
   const int h_tiles = p.rows_out / 16, w_tiles = 16 * p.piece;
@@ -979,8 +1237,32 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
   HeadRow* rows = (HeadRow*)at(p.rows);
   uint16_t *D = (uint16_t*)at(p.d), *hp = (uint16_t*)at(p.h_parts), *wp = (uint16_t*)at(p.w_parts);
   float* slab = (float*)at(p.slab);
-  hipLaunchKernelGGL(k_head_rows, dim3(p.rows_out / 256), dim3(256), 0, st, n_rows, p.rows_out, V, tok, stats, entropy, g_logp, g_ent,
-                     scale, 1.f / c, rows);
+  const HeadGrads g = {n_rows, V, tok, stats, entropy, g_logp, g_ent, scale, 1.f / c};
+  if (p.small) {
+    HeadSmall a = {};
+    a.g = g;
+    a.h = Rows{h, h_stride};
+    a.w = Rows{w, w_stride};
+    a.d = d;
+    a.c = c;
+    a.inv_t = inv_t;
+    a.D = (float*)D;
+    a.ld = p.width;
+    a.rows = rows;
+    a.gh = gh;
+    a.gw = gw;
+    a.gh_stride = gh_stride;
+    a.gw_stride = gw_stride;
+    a.gw_f32 = gw_f32;
+    a.add = accumulate;
+    a.h_blocks = gh ? (n_rows + 31) / 32 * ((d + 31) / 32) : 0;
+    const dim3 of_d((n_rows + 31) / 32 * ((V + 31) / 32)), of_grads(a.h_blocks + (gw ? (V + 31) / 32 * ((d + 31) / 32) : 0));
+    auto go = [&](auto k, dim3 grid) { hipLaunchKernelGGL(k, grid, dim3(256), 0, st, a); };
+    if (dtype == SARA_F32) { go(k_head_small<float, true>, of_d); go(k_head_small_grads<float>, of_grads); }
+    else { go(k_head_small<uint16_t, true>, of_d); go(k_head_small_grads<uint16_t>, of_grads); }
+    return head_done("head log probabilities gradient launch");
+  }
+  hipLaunchKernelGGL(k_head_rows, dim3(p.rows_out / 256), dim3(256), 0, st, g, p.rows_out, rows);
   pack(f32, h, h_stride, n_rows, d, rows, hp, p.rows_out, p.width, st);
   const int cols = (V + 255) / 256, tiles = p.rows_out / 16;
   uint8_t *id_flags = (uint8_t*)at(p.id_flags), *row_flags = (uint8_t*)at(p.row_flags);

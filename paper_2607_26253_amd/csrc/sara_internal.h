@@ -347,10 +347,10 @@ int launch_token_logprobs_grad(const void* logits, int dtype, int64_t row_stride
                                const float* stats, const float* entropy, const float* g_logp, const float* g_ent,
                                float temp, void* grad, int64_t grad_stride, hipStream_t st);
 // launchers (log probabilities from hidden states)
-// How a call is cut and where its workspace's parts begin: few rows or tiles; vocabulary tiles (256 ids) of a piece,
+// How a call is cut and where its workspace's parts begin: few rows, small tiles or large ones; vocabulary tiles (256 ids) of a piece,
 // padded rows, padded width of bf16 parts, parts of D, splits of dH's contraction.
 struct HeadPlan {
-  bool few;
+  bool few, small;
   int nt, few_blocks, piece, rows_out, width, d_parts, splits;
   int64_t x_tok, parts, rows, d, id_flags, row_flags, slab, h_parts, w_parts, bytes;
 };

@@ -126,10 +126,13 @@ def check_gradients(env, gh, gw, x, e, start=None):
 
 SIZES = [(1, 8, 1), (1, 64, 257), (2, 72, 16), (3, 40, 500), (15, 136, 129), (16, 512, 1000), (17, 256, 4097), (33, 1032, 300),
          (64, 200, 2000), (65, 72, 511), (255, 64, 256), (256, 32, 257), (257, 128, 768), (300, 1000, 1031), (513, 264, 520)]
+# past what small tiles take, with ends inside the large ones: for fp32 too
+BIG = (1100, 1032, 5001)
+LARGE = [BIG, (2500, 1000, 2065), (70, 1544, 33001)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows,d,V", SIZES)
+@pytest.mark.parametrize("rows,d,V", SIZES + LARGE)
 def test_log_probabilities_and_gradients(env, rows, d, V, dtype):
     torch, _ = env
     T = (1.0, 0.7, 1.3)[rows % 3]
@@ -145,22 +148,22 @@ def test_log_probabilities_and_gradients(env, rows, d, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [5, 70])
-def test_width_of_four(env, rows, dtype):
+@pytest.mark.parametrize("rows,V", [(5, 300), (70, 300), (70, 130001)])
+def test_width_of_four(env, rows, V, dtype):
     """fp32 rows of 16 bytes end inside a unit of eight bf16 parts; the narrowest bf16 row is eight wide."""
     d = 8 if dtype == "bf16" else 4
     for width in (d, 5 * d):
-        x = make(env, rows, width, 300, dtype)
+        x = make(env, rows, width, V, dtype)
         e = exact(env, x, 1.0)
         out = forward(env, x)
         check_forward(out, e)
         check_gradients(env, *gradients(env, x, out), x, e)
 
 
-@pytest.mark.parametrize("rows", [9, 80])
-def test_one_gradient_at_a_time_and_either_cotangent(env, rows):
+@pytest.mark.parametrize("rows,d,V", [(9, 96, 700), (80, 96, 700), BIG])
+def test_one_gradient_at_a_time_and_either_cotangent(env, rows, d, V):
     torch, _ = env
-    x = make(env, rows, 96, 700, "bf16")
+    x = make(env, rows, d, V, "bf16")
     out = forward(env, x)
     both = gradients(env, x, out)
     gh, none = gradients(env, x, out, weight=False)
@@ -175,23 +178,24 @@ def test_one_gradient_at_a_time_and_either_cotangent(env, rows):
     assert bool((gh == 0).all()) and bool((gw == 0).all())
 
 
+@pytest.mark.parametrize("rows,d,V", [(70, 128, 900), BIG])
 @pytest.mark.parametrize("sums", ["bf16", "f32"])
-def test_accumulates(env, sums):
+def test_accumulates(env, sums, rows, d, V):
     torch, _ = env
     sums = torch.bfloat16 if sums == "bf16" else torch.float32
-    x = make(env, 70, 128, 900, "bf16")
+    x = make(env, rows, d, V, "bf16")
     out = forward(env, x)
-    start = torch.randn((900, 128), device="cuda").to(sums)
+    start = torch.randn((V, d), device="cuda").to(sums)
     gh, gw = gradients(env, x, out, accumulate=True, start=start)
     check_gradients(env, gh, gw, x, exact(env, x, 1.0), start=start)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [20, 300])
-def test_rows_that_ask_for_nothing_may_hold_anything(env, rows, dtype):
+@pytest.mark.parametrize("rows,d,V", [(20, 128, 600), (300, 128, 600), BIG])
+def test_rows_that_ask_for_nothing_may_hold_anything(env, rows, d, V, dtype):
     """Padding rows of NaN and infinities change no gradient; their own is 0 and their statistics are NaN."""
     torch, _ = env
-    x = make(env, rows, 128, 600, dtype)
+    x = make(env, rows, d, V, dtype)
     pad = torch.arange(rows, device="cuda") % 7 == 3
     x["gl"][pad], x["ge"][pad] = 0.0, 0.0
     clean = x["h"].clone()
@@ -201,7 +205,7 @@ def test_rows_that_ask_for_nothing_may_hold_anything(env, rows, dtype):
     x["h"][pad] = torch.tensor([math.nan, math.inf, -math.inf], device="cuda").repeat(rows)[:int(pad.sum())][:, None].to(x["h"].dtype)
     x["clean"] = clean
     out = forward(env, x)
-    assert bool(out["logp"][pad & (x["tok"] >= 0) & (x["tok"] < 600)].isnan().all()) and bool(out["ent"][pad].isnan().all())
+    assert bool(out["logp"][pad & (x["tok"] >= 0) & (x["tok"] < V)].isnan().all()) and bool(out["ent"][pad].isnan().all())
     assert bool(out["stats"][pad].isnan().all())
     check_forward({k: v[~pad] for k, v in out.items()}, {k: v[~pad] for k, v in e.items() if k not in ("h", "w")})
     gh, gw = gradients(env, x, out)
@@ -209,12 +213,12 @@ def test_rows_that_ask_for_nothing_may_hold_anything(env, rows, dtype):
     check_gradients(env, gh, gw, x, e)
 
 
-@pytest.mark.parametrize("rows", [3, 90])
+@pytest.mark.parametrize("rows,d,V", [(3, 64, 400), (90, 64, 400), BIG])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_logits_that_are_not_finite(env, rows, bad):
+def test_logits_that_are_not_finite(env, rows, d, V, bad):
     """One bad element of one row reaches that row's outputs and its gradient only, one of the weight every row."""
     torch, _ = env
-    x = make(env, rows, 64, 400, "bf16")
+    x = make(env, rows, d, V, "bf16")
     x["tok"][:] = 5
     x["gl"][:] = 1.0
     good = forward(env, x)
@@ -228,24 +232,24 @@ def test_logits_that_are_not_finite(env, rows, bad):
     gh, _ = gradients(env, x, out, weight=False)
     assert bool(gh[1].isnan().all()) and torch.equal(gh[keep], ok[0][keep])
     x["h"][1, 9] = 1.0
-    x["w"][399, 9] = bad
+    x["w"][V - 1, 9] = bad
     out = forward(env, x)
     assert bool(out["logp"].isnan().all()) and bool(out["stats"].isnan().all())
 
 
-@pytest.mark.parametrize("rows", [4, 100])
+@pytest.mark.parametrize("rows,d,V", [(4, 64, 700), (100, 64, 700), BIG])
 @pytest.mark.parametrize("T", [1e-37, 1e-3, 30.0, 1e37])
-def test_temperatures(env, rows, T):
+def test_temperatures(env, rows, d, V, T):
     """Cold rows put everything on their largest logit, hot ones are uniform; logits far apart and equal."""
     torch, _ = env
-    x = make(env, rows, 64, 700, "f32", spread=1.0)
+    x = make(env, rows, d, V, "f32", spread=1.0)
     x["h"], x["w"] = (x["h"] * 2).round(), (x["w"] * 8).round()       # products and sums are exact
     x["w"][::3] = x["w"][0]
     logits = x["h"].double() @ x["w"].double().T.contiguous()
     out = forward(env, x, T)
     lp = torch.log_softmax((logits - logits.amax(-1, keepdim=True)) / T, -1)
-    tok = x["tok"].clamp(0, 699).long()
-    has = (x["tok"] >= 0) & (x["tok"] < 700)
+    tok = x["tok"].clamp(0, V - 1).long()
+    has = (x["tok"] >= 0) & (x["tok"] < V)
     want = torch.where(has, lp.gather(1, tok[:, None])[:, 0], torch.zeros_like(lp[:, 0]))
     # at 1e-37 logits 53 apart make log probabilities of -5.3e38, which is past fp32's 3.4e38: -inf, as fp32 rounds them
     near = (out["logp"].double() - want).abs() <= 2.0 ** -18 * (1 + want.abs())
@@ -276,8 +280,8 @@ def test_pieces_of_the_vocabulary(env):
 
 def test_many_rows(env):
     """Forward tiles run 8,192 rows at a time."""
-    for dtype in ("bf16", "f32"):
-        x = make(env, 8300, 16, 300, dtype)
+    for d, V, dtype in ((16, 300, "bf16"), (16, 300, "f32"), (1032, 520, "bf16"), (1032, 520, "f32")):
+        x = make(env, 8300, d, V, dtype)
         check_forward(forward(env, x), exact(env, x, 1.0))
 
 
@@ -316,12 +320,12 @@ def test_gradient_against_differences(env):
         assert abs((ends[0] - ends[1]) / (2 * step) - float((grad.double() * way).sum())) <= 10 * step ** 2 + 1e-4
 
 
-@pytest.mark.parametrize("rows", [7, 130])
-def test_streams_graphs_and_workspaces(env, rows):
+@pytest.mark.parametrize("rows,d,V", [(7, 128, 1500), (130, 128, 1500), BIG])
+def test_streams_graphs_and_workspaces(env, rows, d, V):
     """Replays on inputs that change, on a side stream, with the caller's workspace, give the eager results bit for bit."""
     torch, sara = env
     import ctypes
-    sizes = dict(rows=rows, d=128, V=1500, dtype="bf16")
+    sizes = dict(rows=rows, d=d, V=V, dtype="bf16")
     xs = [make(env, seed=s, **sizes) for s in range(3)]
     eager = []
     for x in xs:
@@ -330,7 +334,7 @@ def test_streams_graphs_and_workspaces(env, rows):
     need = ctypes.c_int64(0)
     space = []
     for grad in (0, 1):
-        assert sara._lib.sara_head_logprobs_workspace(1, rows, 128, 1500, grad, 1, ctypes.byref(need)) == 0
+        assert sara._lib.sara_head_logprobs_workspace(1, rows, d, V, grad, 1, ctypes.byref(need)) == 0
         space.append(torch.full((need.value,), 255, device="cuda", dtype=torch.uint8))
     live = {k: v.clone() for k, v in xs[0].items()}
     out = {k: torch.empty_like(v) for k, v in eager[0][0].items()}
@@ -408,8 +412,9 @@ def test_refusals(env):
             bwd(**kw)
 
 
-def test_reruns_are_bit_identical(env):
-    x = make(env, 300, 256, 5000, "bf16")
+@pytest.mark.parametrize("rows,d,V", [(300, 256, 5000), BIG])
+def test_reruns_are_bit_identical(env, rows, d, V):
+    x = make(env, rows, d, V, "bf16")
     out = [forward(env, x) for _ in range(2)]
     assert all(env[0].equal(out[0][k], out[1][k]) for k in out[0])
     a, b = (gradients(env, x, out[0]) for _ in range(2))
