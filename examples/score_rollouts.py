@@ -14,6 +14,11 @@ the policy gradient of their tokens.
    most likely alternatives; sara_token_logprobs_grad the gradient of
    -sum(advantage * log p + beta * entropy) / tokens with respect to the logits,
    from which the LM head's gradient is accumulated.
+4. The same loss as an update takes it: each answer is one ragged piece, whose
+   attention takes the prompt's pages as its group's (sara_kv8_group_attention),
+   and all tokens together go through the LM head without logits in memory
+   (sara_head_logprobs, sara_head_logprobs_grad), which give the gradients of the
+   LM head and of the hidden states.
 """
 import argparse
 import math
@@ -57,9 +62,10 @@ class CachedDecoder:
         x1, x2 = x.float().chunk(2, -1)
         return torch.cat([x1 * c - x2 * s, x2 * c + x1 * s], -1).bfloat16()
 
-    def forward(self, tokens, pos, table, start, off, ctx, max_ctx):
+    def forward(self, tokens, pos, table, start, off, ctx, max_ctx, groups=None):
         """Hidden states of new tokens: rows off[i]..off[i + 1] (one a sequence without `off`) follow the start[i] tokens
-        that the cache holds of sequence i; ctx[i] counts both."""
+        that the cache holds of sequence i; ctx[i] counts both.  groups: (first sequences, tokens in common, most of them)
+        of sequences that share a prompt's pages."""
         m, w = self.m, self.w
         hq, hkv, hd, T = m["n_heads"], m["n_kv_heads"], m["head_dim"], len(tokens)
         h = w["embed"][tokens.long()].float()
@@ -70,7 +76,10 @@ class CachedDecoder:
             v = (x @ w[f"l{l}.wv"].T).view(T, hkv, hd)
             sara.sara_kv8_write(*cache, k, v, table, start, off)
             o = torch.empty_like(q)
-            sara.sara_kv8_attention(q, *cache, table, ctx, off, o, max_ctx=max_ctx)
+            if groups is None:
+                sara.sara_kv8_attention(q, *cache, table, ctx, off, o, max_ctx=max_ctx)
+            else:
+                sara.sara_kv8_group_attention(q, *cache, table, ctx, off, groups[0], groups[1], o, max_ctx=max_ctx, max_shared=groups[2])
             h = h + (o.view(T, hq * hd) @ w[f"l{l}.wo"].T).float()
             x = self.norm(h, w[f"l{l}.ffn_norm"])
             g = torch.nn.functional.silu((x @ w[f"l{l}.wg"].T).float()) * (x @ w[f"l{l}.wu"].T).float()
@@ -102,17 +111,18 @@ def generate(cfg, pool, weights):
     return out
 
 
-def score(cfg, rollouts, weights, fmt="int8", beta=0.01, n_top=3):
-    """Log probabilities, entropies and alternatives of the rollouts' tokens, and the gradient of the LM head."""
-    w = {n: torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).cuda().view(torch.bfloat16) for n, a in weights.items()}
-    n = len(rollouts)
+def upload(weights):
+    return {n: torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).cuda().view(torch.bfloat16) for n, a in weights.items()}
+
+
+def lay_out(rollouts):
+    """Lengths of prompts and answers, tokens in whole pages of a prompt (its last token apart), page tables in which a
+    prompt's rollouts have those in common, the first rollout of each prompt, and the pages of them all."""
     plen = np.array([len(p) for _, p, _, _ in rollouts])
     glen = np.array([len(g) for _, _, g, _ in rollouts])
-    shared = (plen - 1) // PAGE * PAGE                    # whole pages of the prompt, its last token apart
+    shared = (plen - 1) // PAGE * PAGE
     width = int(-(-(plen + glen).max() // PAGE))
-    max_ctx = width * PAGE
-    # page tables: a prompt's rollouts have its whole pages in common
-    table, at, of_prompt = np.full((n, width), -1, np.int64), 0, {}
+    table, at, of_prompt = np.full((len(rollouts), width), -1, np.int64), 0, {}
     for i, (u, _, _, _) in enumerate(rollouts):
         common = shared[i] // PAGE
         if u not in of_prompt:
@@ -121,6 +131,15 @@ def score(cfg, rollouts, weights, fmt="int8", beta=0.01, n_top=3):
         own = -(-(plen[i] + glen[i]) // PAGE) - common
         table[i, :common], table[i, common:common + own] = of_prompt[u][1], np.arange(at, at + own)
         at += own
+    return plen, glen, shared, table, [i for i, _ in of_prompt.values()], at
+
+
+def score(cfg, rollouts, weights, fmt="int8", beta=0.01, n_top=3):
+    """Log probabilities, entropies and alternatives of the rollouts' tokens, and the gradient of the LM head."""
+    w = upload(weights)
+    n = len(rollouts)
+    plen, glen, shared, table, of_prompt, at = lay_out(rollouts)
+    max_ctx = table.shape[1] * PAGE
     dec = CachedDecoder(cfg["model"], w, max(at, 1), fmt)
     tab = i32(table)
     weight = 1.0 / int(glen.sum())
@@ -152,7 +171,7 @@ def score(cfg, rollouts, weights, fmt="int8", beta=0.01, n_top=3):
         out["top"][seqs, i] = ids.cpu().numpy()
 
     # the prompts' whole pages, once a prompt
-    first = [i for i, _ in of_prompt.values() if shared[i]]
+    first = [i for i in of_prompt if shared[i]]
     if first:
         piece(first, [0] * len(first), [rollouts[i][1][:shared[i]] for i in first])
     # the rest of each rollout's prompt, in pages of its own
@@ -165,6 +184,38 @@ def score(cfg, rollouts, weights, fmt="int8", beta=0.01, n_top=3):
         hidden, _ = piece(seqs, plen[seqs] + i - 1, [rollouts[s][2][i - 1:i] for s in seqs])
         take(seqs, hidden, i)
     return out
+
+
+def update(cfg, rollouts, weights, fmt="int8", beta=0.01, grouped=True):
+    """The loss's log probabilities and entropies of all tokens, one rollout's after the other's, the hidden states before
+    them, and the gradients of both sides of the LM head.  A prompt's rollouts follow each other."""
+    w = upload(weights)
+    plen, glen, shared, table, of_prompt, at = lay_out(rollouts)
+    max_ctx, tab = table.shape[1] * PAGE, i32(table)
+    dec = CachedDecoder(cfg["model"], w, max(at, 1), fmt)
+    first = [i for i in of_prompt if shared[i]]
+    if first:
+        tokens = [rollouts[i][1][:shared[i]] for i in first]
+        off = np.concatenate([[0], np.cumsum([len(t) for t in tokens])])
+        dec.forward(i32(np.concatenate(tokens)), i32(np.concatenate([np.arange(len(t)) for t in tokens])), tab[i32(first).long()].contiguous(),
+                    i32(np.zeros(len(first))), i32(off), i32(shared[first]), max_ctx)
+    # what is left of a prompt and its answer but for the last token
+    tokens = [np.concatenate([p[s:], g[:-1]]) for (_, p, g, _), s in zip(rollouts, shared)]
+    off = np.concatenate([[0], np.cumsum([len(t) for t in tokens])])
+    pos = np.concatenate([s + np.arange(len(t)) for t, s in zip(tokens, shared)])
+    groups = (i32(of_prompt + [len(rollouts)]), i32(shared[of_prompt]), int(shared.max())) if grouped else None
+    hidden = dec.forward(i32(np.concatenate(tokens)), i32(pos), tab, i32(shared), i32(off), i32(shared + np.diff(off)), max_ctx, groups)
+    before = np.concatenate([np.arange(off[i + 1] - g, off[i + 1]) for i, g in enumerate(glen)])
+    hidden = hidden[i32(before).long()].contiguous()
+    tok = i32(np.concatenate([g for _, _, g, _ in rollouts]))
+    adv = np.repeat([a for _, _, _, a in rollouts], glen)
+    T = len(tok)
+    logp, ent, stats = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty((T, 2), device="cuda")
+    sara.sara_head_logprobs(hidden, w["lm_head"], tok, logp, ent, stats)
+    g = torch.tensor(-adv / T, device="cuda", dtype=torch.float32)
+    grad_hidden, grad = torch.empty_like(hidden), torch.empty(w["lm_head"].shape, device="cuda")
+    sara.sara_head_logprobs_grad(hidden, w["lm_head"], tok, stats, ent, g, torch.full_like(g, -beta / T), grad_hidden, grad)
+    return dict(logp=logp, entropy=ent, hidden=hidden, tok=tok, g=g, grad_hidden=grad_hidden, grad=grad)
 
 
 def small_config(layers=2, vocab=None):
@@ -192,6 +243,9 @@ def main():
     print(f"{len(rollouts)} rollouts, {n_tok} tokens: mean log p {out['logp'].sum() / n_tok:.4f} "
           f"(uniform {-math.log(cfg['model']['vocab']):.4f}), mean entropy {out['entropy'].sum() / n_tok:.4f}, "
           f"most likely id sampled {100 * hit:.1f}%, LM head gradient norm {float(out['grad'].norm()):.4e}")
+    out = update(cfg, rollouts, weights, a.format)
+    print(f"the update: mean log p {float(out['logp'].mean()):.4f}, mean entropy {float(out['entropy'].mean()):.4f}, "
+          f"LM head gradient norm {float(out['grad'].norm()):.4e}, hidden states' {float(out['grad_hidden'].float().norm()):.4e}")
 
 
 if __name__ == "__main__":
