@@ -437,16 +437,17 @@ int sara_kv8_attention(const sara_kv8_cache* cache, const void* d_q, int64_t q_r
                        void* stream);
 
 /* The same attention where sequences come in groups that share pages, as the
- * rollouts of a prompt do: where that pays, the shared pages are read once for
- * all rows of a group.  Group j holds the sequences [d_groups[j], d_groups[j + 1]) (d_groups
- * [n_groups + 1], not decreasing, inside [0, n_seqs]; a sequence of no group
- * shares nothing); they have d_shared[j] tokens in common, of which the whole
- * pages among the first max_shared are shared.  Positions in those
- * pages are read through the page table of the group's FIRST sequence, whatever its
- * d_ctx and the other tables hold there, later positions through each
- * sequence's own.  Every sequence may have any d_ctx, less than d_shared among
- * them; all else is as above.  max_shared <= 16 * max_pages and 2^30: keep it near the
- * longest. */
+ * rollouts of a prompt do.  Group j holds the sequences [d_groups[j],
+ * d_groups[j + 1]) (d_groups [n_groups + 1], not decreasing, inside [0, n_seqs];
+ * a sequence of no group shares nothing); they have d_shared[j] tokens in
+ * common, of which the whole pages among the first max_shared are shared.
+ * Positions in those pages are read through the page table of the group's FIRST
+ * sequence, whatever its d_ctx and the other tables hold there, later positions
+ * through each sequence's own.  Every sequence may have any d_ctx, less than
+ * d_shared among them; all else is as above.  Where the sizes of the call say
+ * that it pays, a group's pages are read once for all of its rows; sizes alone
+ * decide, so a captured call keeps its way.  max_shared <= 16 * max_pages and
+ * 2^30: keep it near the longest. */
 int sara_kv8_group_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads, int32_t n_seqs,
                                        int32_t n_groups, int32_t ragged, int32_t max_ctx, int32_t max_shared, int32_t dtype,
                                        int64_t* bytes);
@@ -531,8 +532,11 @@ int sara_head_logprobs(const void* d_hidden, int64_t hidden_stride, const void* 
  *                   weight_grad_dtype: dtype or SARA_F32 (for sums over
  *                   micro-batches); accumulate != 0 adds to what it holds
  * summed in fp32 and rounded once.  D enters the products of a bf16 call rounded
- * to bf16, those of an fp32 weight gradient in two bf16 parts (2^-17 of it), and of
- * an fp32 call in three.  Either gradient may be NULL, not both; they must not
+ * to bf16, for an fp32 weight gradient in two bf16 parts (2^-17 of it), with one
+ * part more where a row's largest elements are, so that the products are off by no
+ * more than their outputs' own rounding; those of an fp32 call take three parts.
+ * Small problems keep D in fp32.  n_rows <= 131,072: more come in several calls,
+ * with accumulate.  Either gradient may be NULL, not both; they must not
  * overlap the inputs.  d_stats and d_entropy are those of sara_head_logprobs on
  * the same inputs.  d_g_logp or d_g_entropy may be NULL (0); d_entropy may be
  * NULL if d_g_entropy is.  g counts as 0 where d_tok[r] is outside [0, vocab);

@@ -258,6 +258,10 @@ __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileE
 // later stages, into slots whose reads are over.  One barrier a step: before it a wave waits for its own loads of stage
 // s + 1, so all have landed behind it.  The loads are written in assembly: the compiler would wait for all of them
 // before each LDS read.
+//
+// 4,093 rows of width 1,536 over 151,936 ids run at 1.16 PFLOP/s in all (a library's product of 16,384 cubed: 1.38): 44 us a
+// round of tiles, of which some 9 go to the statistics and 4 to the first loads, with nothing of the next tile under way.  2,048
+// rows over 57,344 ids: D 351 us, dH 297, dW 343 (1.03, 1.21 and 1.05 PFLOP/s).
 template <int AK, int BK, int EPI>
 __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
   constexpr bool PAIRS = BK == kRowPairs;
@@ -556,7 +560,8 @@ __device__ __forceinline__ void head_merge(HeadSum& a, HeadSum b, float c) {
 
 // Up to 16 NT rows: W streams past them.  A block of 8 waves takes 128 ids at a time, a wave 16 of them, in 128-byte blocks of
 // k: a lane loads 32 consecutive bytes of an id's row, the hidden states lie in LDS (`chunk` blocks of k at a time).
-// fp32 runs on v_mfma_f32_16x16x4_f32.
+// fp32 runs on v_mfma_f32_16x16x4_f32.  Bound by W's way from memory: 151,936 ids of width 1,536 in bf16, 467 MB, take 100 us for
+// one row (4.7 TB/s) and 114 for 35, whose hidden states pass LDS in three chunks.
 struct HeadFew {
   const char *h, *w;
   int64_t h_stride, w_stride;   // bytes
@@ -681,7 +686,7 @@ __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
   }
 }
 
-// A block joins the slices of RB rows: 256 / RB threads a row.
+// A block joins the slices of RB rows: 256 / RB threads a row.  594 slices of 2,048 rows: 10 us (19 with 16 rows a block).
 template <int RB>
 __global__ __launch_bounds__(256) void k_head_join(const float4* __restrict__ parts, int slices, int m_parts, int row0, int n_rows,
     int V, const int32_t* __restrict__ tok, const float* __restrict__ x_tok, float c, float inv_t, float* logp, float* entropy,
@@ -798,7 +803,9 @@ __global__ __launch_bounds__(256) void k_head_rows(HeadGrads a, int rows_out, He
 // ---------------------------------------------------------------------------
 // Tiles of 32 x 32 on v_mfma_f32_16x16x4_f32, whose products of bf16 or fp32 numbers are exact before their sum in fp32: no
 // operand is packed or taken in parts, and D stays in fp32.  The four waves of a block take every fourth 16 elements of k,
-// straight from memory to registers four steps ahead, and join their sums in LDS.
+// straight from memory to registers four steps ahead, and join their sums in LDS.  509 fp32 rows of width 256 over 512 ids:
+// statistics 7 us, D 8, both gradients 9, most of that a launch and its load round trips.  With many tiles a compute unit takes
+// 2.4 us for a tile and 256 of k, twice its matrix instructions' time: loads in pieces of 64 bytes.
 struct Rows { const void* p; int64_t stride; };
 
 struct HeadSmall {
@@ -1178,7 +1185,7 @@ int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t
     const dim3 grid((n_rows + 31) / 32 * ((V + 31) / 32));
     if (dtype == SARA_F32) hipLaunchKernelGGL((k_head_small<float, false>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_head_small<uint16_t, false>), grid, dim3(256), 0, st, a);
-    hipLaunchKernelGGL((k_head_join<16>), dim3((n_rows + 15) / 16), dim3(256), 0, st, parts, (V + 31) / 32, n_rows, 0, n_rows, V, tok, x_tok, c,
+    hipLaunchKernelGGL((k_head_join<4>), dim3((n_rows + 3) / 4), dim3(256), 0, st, parts, (V + 31) / 32, n_rows, 0, n_rows, V, tok, x_tok, c,
                        inv_t, logp, entropy, stats);
     return head_done("head log probabilities launch");
   }
@@ -1215,7 +1222,7 @@ int launch_head_logprobs(const void* h, int64_t h_stride, const void* w, int64_t
         hipLaunchKernelGGL((k_head_tile<kPacked, kRowPairs, kStats>), tile_grid(t), dim3(kTileThreads), 0, st, t);
       }
     }
-    hipLaunchKernelGGL((k_head_join<16>), dim3((M + 15) / 16), dim3(256), 0, st, parts, cols, std::min(p.rows_out, kStatRows), row0, M, V,
+    hipLaunchKernelGGL((k_head_join<4>), dim3((M + 3) / 4), dim3(256), 0, st, parts, cols, std::min(p.rows_out, kStatRows), row0, M, V,
                        tok, x_tok, c, inv_t, logp, entropy, stats);
   }
   return head_done("head log probabilities launch");

@@ -1196,6 +1196,10 @@ __global__ __launch_bounds__(256) void k_kv8_attn_join(AttnArgs a, int hkv, int 
 // The softmax over a row's keys is joined from two sets of partial results: over the pages that its group shares, by
 // blocks of 128 columns that take the rows of the whole group (k_kv8_group_shared), and over what its sequence has behind
 // them, by the kernels above (k_kv8_group_own_*).  So a group's pages are read and converted once for all its rows.
+// Partial results stay in fp32 (o, maximum, sum).  512 rows of 64 prompts of 256-1,024 tokens, 16 heads over two, e4m3:
+// shared pages 21 us, own pages with the join 49 (198 MB, 4.0 TB/s).  32 rows behind 65,536 int8 tokens: 59, 9 and 9 us,
+// where the loop over key blocks takes half of the first (its vector instructions) and the blocks' start and 35 MB of partial
+// results the rest.
 template <int HD, int FMT, typename T>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_group_shared(sara_kv8_cache c, AttnArgs a) {
   __shared__ __attribute__((aligned(16))) TileLds<HD> lds;
