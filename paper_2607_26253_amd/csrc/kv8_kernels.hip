@@ -1197,9 +1197,9 @@ __global__ __launch_bounds__(256) void k_kv8_attn_join(AttnArgs a, int hkv, int 
 // blocks of 128 columns that take the rows of the whole group (k_kv8_group_shared), and over what its sequence has behind
 // them, by the kernels above (k_kv8_group_own_*).  So a group's pages are read and converted once for all its rows.
 // Partial results stay in fp32 (o, maximum, sum).  512 rows of 64 prompts of 256-1,024 tokens, 16 heads over two, e4m3:
-// shared pages 21 us, own pages with the join 49 (198 MB, 4.0 TB/s).  32 rows behind 65,536 int8 tokens: 59, 9 and 9 us,
-// where the loop over key blocks takes half of the first (its vector instructions) and the blocks' start and 35 MB of partial
-// results the rest.
+// shared pages 21 us, own pages with the join 49 (198 MB, 4.0 TB/s).  32 rows behind 65,536 int8 tokens: the
+// loop over key blocks takes 35 of 61 us (2.2 us a key block and compute unit, its vector instructions), the blocks' start,
+// 35 MB of partial results and their join the rest.
 template <int HD, int FMT, typename T>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_kv8_group_shared(sara_kv8_cache c, AttnArgs a) {
   __shared__ __attribute__((aligned(16))) TileLds<HD> lds;
@@ -1458,8 +1458,12 @@ Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, i
   s.splits_tile = s.tile_items ? (np + s.pps_tile - 1) / s.pps_tile : 0;
   s.splits_shared = s.shared_items ? (np_shared + s.pps_shared - 1) / s.pps_shared : 0;
   // Few blocks run in one launch, which a join follows; more of them end with the shared pages' results in hand, unless
-  // those are many.
-  s.all = (s.few_items * s.splits + s.tile_items * s.splits_tile) * hkv <= 512;
+  // those are many.  Few: of those that have keys to work on if every sequence has a group.  32 rows behind 65,536
+  // tokens 61 us, 70 in two launches and the join.
+  const int np_own = std::max(1, np - np_shared);
+  auto has_keys = [&](int pages) { return (np_own + pages - 1) / pages; };
+  s.all = (s.few_items * has_keys(s.pps) + s.tile_items * has_keys(s.pps_tile)) * hkv <= 512 &&
+          (s.few_items * s.splits + s.tile_items * s.splits_tile) * hkv <= 8192;
   s.finish = !s.all && s.splits_shared <= 8;
   const int64_t one = (int64_t)sizeof(float) * (hd + 2);
   if (!s.finish || s.splits > 1) s.part_bytes = (one * n_seqs * hkv * (ragged ? kFewColumns : G) * s.splits + 15) / 16 * 16;

@@ -144,6 +144,35 @@ def test_many_groups_and_many_sequences(env):
     b.check(qq, b.run(qq, offsets(nq)), offsets(nq))
 
 
+@pytest.mark.parametrize("n,ragged", [(300, False), (140, True), (300, True)])
+def test_many_sequences_and_long_answers(env, n, ragged):
+    """Launches too large to run as one: rows that take the shared pages' results where they end, beside some whose own
+    pages are several splits."""
+    rng = np.random.default_rng([20, n])
+    members = [5] * (n // 5)
+    shared = [int(x) for x in rng.integers(30, 400, len(members))]
+    ctx = [int(shared[i // 5] + x) for i, x in enumerate(rng.integers(0, 60, n))]
+    for i in (3, 77, n - 1):
+        ctx[i] = 8000 - i
+    b = Batch(env, rng, 2, 64, "int8", members, shared, ctx)
+    nq = [int(x) for x in rng.choice([0, 1, 2, 9], n)] if ragged else [1] * n
+    if ragged:
+        nq[3], nq[77], nq[78] = 3, 40, 30
+    off = offsets(nq) if ragged else None
+    q = b.q(rng, sum(nq), 8, "bf16")
+    b.check(q, b.run(q, off), off)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_of_one_long_prompt(env, dtype):
+    """More splits of the shared pages than a row takes at its end."""
+    rng = np.random.default_rng(21)
+    ctx = [int(1500 + x) for x in rng.integers(-100, 100, 270)]
+    b = Batch(env, rng, 2, 64, "fp8", [270], [1500], ctx)
+    q = b.q(rng, 270, 8, dtype)
+    b.check(q, b.run(q))
+
+
 def test_bounds_of_the_launch(env):
     """max_shared below a prompt: the rest is each sequence's own.  max_ctx below a context: its rows are NaN, no other's."""
     rng = np.random.default_rng(7)
