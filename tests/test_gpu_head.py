@@ -270,7 +270,7 @@ def test_temperatures(env, rows, d, V, T):
 
 
 def test_pieces_of_the_vocabulary(env):
-    """D of 1,100 rows over 130,000 ids passes a piece's 256 MiB; the last piece is short."""
+    """D of 1,100 rows over 130,000 ids, in two parts, passes a piece's 448 MiB; the last piece is short."""
     x = make(env, 1100, 64, 130001, "bf16")
     e = exact(env, x, 1.0)
     out = forward(env, x)
