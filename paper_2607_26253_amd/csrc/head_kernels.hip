@@ -817,6 +817,8 @@ struct HeadSmall {
   float4* parts;            // [32 ids][m_parts]
   float* D;                 // [rows, a multiple of 32][ld], zero past the last row and id
   int ld, h_blocks;         // blocks of dH, those of dW follow
+  int h_tiles, h_steps;     // of a split of dH's contraction; with several their sums go to slab [split][rows][d]
+  float* slab;
   HeadRow* rows;
   void *gh, *gw;
   int64_t gh_stride, gw_stride;
@@ -872,11 +874,10 @@ struct SmallLds {
   HeadRow rows[32];
 };
 
-// Of the tile's sum: columns 4 (t % 8) ..+3 of row t / 8 for thread t
+// Of the tile's sum over the 16-wide steps [first, steps) of k: columns 4 (t % 8) ..+3 of row t / 8 for thread t
 template <typename A, typename B>
-__device__ __forceinline__ f32x4 small_tile(const A& a0, const A& a1, const B& b0, const B& b1, int K, SmallLds& lds) {
+__device__ __forceinline__ f32x4 small_tile(const A& a0, const A& a1, const B& b0, const B& b1, int first, int steps, SmallLds& lds) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
-  const int steps = (K + 15) >> 4;
   constexpr int DEPTH = 4;
   struct { typename A::Raw a[2]; typename B::Raw b[2]; } at[DEPTH];
   auto load = [&](int s, int u) {
@@ -888,8 +889,8 @@ __device__ __forceinline__ f32x4 small_tile(const A& a0, const A& a1, const B& b
   };
   f32x4 acc[2][2] = {};
 #pragma unroll
-  for (int u = 0; u < DEPTH; ++u) load(wave + 4 * u, u);
-  for (int s = wave; s < steps; s += 4 * DEPTH) {
+  for (int u = 0; u < DEPTH; ++u) load(first + wave + 4 * u, u);
+  for (int s = first + wave; s < steps; s += 4 * DEPTH) {
 #pragma unroll
     for (int u = 0; u < DEPTH; ++u) {
       const int st = s + 4 * u;
@@ -931,7 +932,7 @@ __global__ __launch_bounds__(256, 2) void k_head_small(HeadSmall a) {
   }
   typedef SmallOperand<T, false, false> Op;
   const f32x4 z = small_tile(Op(a.h, nullptr, m0, M, a.d), Op(a.h, nullptr, m0 + 16, M, a.d), Op(a.w, nullptr, n0, V, a.d),
-                             Op(a.w, nullptr, n0 + 16, V, a.d), a.d, lds);
+                             Op(a.w, nullptr, n0 + 16, V, a.d), 0, (a.d + 15) >> 4, lds);
   const int ri = threadIdx.x >> 3, r = m0 + ri, id = n0 + 4 * (threadIdx.x & 7), left = V - id;
   if constexpr (GRAD) {
     const HeadRow hr = lds.rows[ri];
@@ -972,7 +973,8 @@ __global__ __launch_bounds__(256, 2) void k_head_small_grads(HeadSmall a) {
   __shared__ __attribute__((aligned(16))) SmallLds lds;
   const int R = a.g.n_rows, V = a.g.V, nb = (a.d + 31) >> 5;
   const bool of_h = (int)blockIdx.x < a.h_blocks;
-  const int b = of_h ? blockIdx.x : blockIdx.x - a.h_blocks, bm = b / nb, m0 = 32 * bm, n0 = 32 * (b - bm * nb);
+  const int split = of_h ? blockIdx.x / a.h_tiles : 0;
+  const int b = of_h ? blockIdx.x - split * a.h_tiles : blockIdx.x - a.h_blocks, bm = b / nb, m0 = 32 * bm, n0 = 32 * (b - bm * nb);
   const int ri = m0 + (threadIdx.x >> 3), col = n0 + 4 * (threadIdx.x & 7);
   const Rows D = {a.D, a.ld};
   f32x4 v;
@@ -980,8 +982,12 @@ __global__ __launch_bounds__(256, 2) void k_head_small_grads(HeadSmall a) {
     typedef SmallOperand<float, false, false> A;
     typedef SmallOperand<T, true, false> B;
     v = small_tile(A(D, nullptr, m0, R, a.ld), A(D, nullptr, m0 + 16, R, a.ld), B(a.w, nullptr, n0, a.d, V), B(a.w, nullptr, n0 + 16, a.d, V),
-                   V, lds);
+                   split * a.h_steps, min((split + 1) * a.h_steps, (V + 15) >> 4), lds);
     if (ri >= R || col >= a.d) return;                     // d is a multiple of 4
+    if (a.h_blocks > a.h_tiles) {
+      *(f32x4*)(a.slab + ((int64_t)split * R + ri) * a.d + col) = v;
+      return;
+    }
     v = a.rows[ri].on ? v * a.inv_t : f32x4{0.f, 0.f, 0.f, 0.f};   // whatever the weight holds
     T* y = (T*)a.gh + ri * a.gh_stride + col;
     if constexpr (sizeof(T) == 2) *(uint2*)y = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
@@ -990,7 +996,8 @@ __global__ __launch_bounds__(256, 2) void k_head_small_grads(HeadSmall a) {
   }
   typedef SmallOperand<float, true, false> A;
   typedef SmallOperand<T, true, true> B;
-  v = small_tile(A(D, nullptr, m0, V, R), A(D, nullptr, m0 + 16, V, R), B(a.h, a.rows, n0, a.d, R), B(a.h, a.rows, n0 + 16, a.d, R), R, lds);
+  v = small_tile(A(D, nullptr, m0, V, R), A(D, nullptr, m0 + 16, V, R), B(a.h, a.rows, n0, a.d, R), B(a.h, a.rows, n0 + 16, a.d, R), 0,
+                 (R + 15) >> 4, lds);
   if (ri >= V || col >= a.d) return;
   v *= a.inv_t;
   if (a.gw_f32) {
@@ -1042,16 +1049,19 @@ constexpr int kCus = 256;
 static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // us of a product of small tiles and of large ones in `pairs` pairs of parts, by rounds of the compute units: 2.4 and 4 us for
-// each 256 of k and pair, half of that where a small tile has a compute unit to itself.  In all (small, large):
+// each 256 of k and pair, half of that where a small tile has a compute unit to itself, but 0.75 for a start and its stores
+// where many follow each other.  In all (small, large):
 //   fp32  509 rows, width 256, 512 ids     forward 12, 53   gradients 18, 186
 //         777      1024       4096                132, 133            306, 311
 //         1024     1024       8192                302, 143            735, 374
 //   bf16  512      512        2048                 31, 31              66, 105
 //         1024     512        2048                 54, 31             120, 131
 //         1024     1024       8192                297, 41             749, 155
-static double small_us(int64_t M, int64_t N, int64_t K) {
-  const int64_t tiles = ((M + 31) / 32) * ((N + 31) / 32);
-  return 5 + (tiles <= kCus ? 0.5 : (double)(up(tiles, kCus) / kCus)) * K * 2.4 / 256;
+static double small_us(int64_t M, int64_t N, int64_t K, int splits = 1) {
+  const int64_t tiles = ((M + 31) / 32) * ((N + 31) / 32) * splits;
+  K = (K + splits - 1) / splits;
+  const double tile = 2.4 * K / 256;
+  return (splits > 1 ? 10 : 5) + (tiles <= kCus ? 0.5 * tile : (double)(up(tiles, kCus) / kCus) * std::max(tile, 0.75));
 }
 static double large_us(int64_t M, int64_t N, int64_t K, int pairs) {
   return 14 + (double)(up(((M + 255) / 256) * ((N + 255) / 256), kCus) / kCus) * K * pairs * 4 / 256;
@@ -1085,12 +1095,22 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
     return p;
   }
   const int pairs = f32 ? 6 : 1;
-  p.small = small_us(n_rows, V, d) + small_us(n_rows, d, V) + small_us(V, d, n_rows) <
-            large_us(n_rows, V, d, pairs) + large_us(n_rows, d, (V + 63) / 64, pairs) + large_us(V, d, n_rows, pairs) + (f32 ? 75 : 40);
+  // Splits of a small dH's contraction, of 1,024 ids or more.  Two fp32 rows of width 256 over 151,936 ids: 238 us
+  // for the gradients, 640 in large tiles.
+  const int ids16 = (V + 15) / 16;
+  const int64_t h_tiles = (int64_t)((n_rows + 31) / 32) * ((d + 31) / 32);
+  const int h_splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / h_tiles, ids16 / 64));
+  const double large = large_us(n_rows, V, d, pairs) + large_us(n_rows, d, (V + 63) / 64, pairs) + large_us(V, d, n_rows, pairs);
+  // The parts of an fp32 weight are written once and read for each pair, twice over: 34 bytes an element
+  const double parts = f32 ? (double)V * d * 34 / 5e6 : 0;
+  p.small = small_us(n_rows, V, d) + small_us(n_rows, d, V, h_splits) + small_us(V, d, n_rows) < std::max(large, parts) + (f32 ? 75 : 40);
   if (p.small) {
     p.width = (int)up(V, 32);
     p.rows = take(sizeof(HeadRow) * up(n_rows, 32));
     p.d = take(4 * up(n_rows, 32) * p.width);
+    p.h_steps = (ids16 + h_splits - 1) / h_splits;
+    p.splits = (ids16 + p.h_steps - 1) / p.h_steps;
+    if (p.splits > 1) p.slab = take(4 * (int64_t)p.splits * n_rows * d);
     return p;
   }
   p.rows_out = (int)up(n_rows, 256);
@@ -1247,6 +1267,12 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
   HeadRow* rows = (HeadRow*)at(p.rows);
   uint16_t *D = (uint16_t*)at(p.d), *hp = (uint16_t*)at(p.h_parts), *wp = (uint16_t*)at(p.w_parts);
   float* slab = (float*)at(p.slab);
+  auto sum = [&]() {
+    const int64_t n = (int64_t)n_rows * d;
+    const dim3 grid((uint32_t)((n / 4 + 255) / 256));
+    if (f32) hipLaunchKernelGGL((k_head_sum<float>), grid, dim3(256), 0, st, slab, p.splits, n, d, rows, inv_t, (float*)gh, gh_stride);
+    else hipLaunchKernelGGL((k_head_sum<uint16_t>), grid, dim3(256), 0, st, slab, p.splits, n, d, rows, inv_t, (uint16_t*)gh, gh_stride);
+  };
   const HeadGrads g = {n_rows, V, tok, stats, entropy, g_logp, g_ent, scale, 1.f / c};
   if (p.small) {
     HeadSmall a = {};
@@ -1265,11 +1291,15 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
     a.gw_stride = gw_stride;
     a.gw_f32 = gw_f32;
     a.add = accumulate;
-    a.h_blocks = gh ? (n_rows + 31) / 32 * ((d + 31) / 32) : 0;
+    a.h_tiles = (n_rows + 31) / 32 * ((d + 31) / 32);
+    a.h_steps = p.h_steps;
+    a.h_blocks = gh ? p.splits * a.h_tiles : 0;
+    a.slab = slab;
     const dim3 of_d((n_rows + 31) / 32 * ((V + 31) / 32)), of_grads(a.h_blocks + (gw ? (V + 31) / 32 * ((d + 31) / 32) : 0));
     auto go = [&](auto k, dim3 grid) { hipLaunchKernelGGL(k, grid, dim3(256), 0, st, a); };
     if (dtype == SARA_F32) { go(k_head_small<float, true>, of_d); go(k_head_small_grads<float>, of_grads); }
     else { go(k_head_small<uint16_t, true>, of_d); go(k_head_small_grads<uint16_t>, of_grads); }
+    if (gh && p.splits > 1) sum();
     return head_done("head log probabilities gradient launch");
   }
   hipLaunchKernelGGL(k_head_rows, dim3(p.rows_out / 256), dim3(256), 0, st, g, p.rows_out, rows);
@@ -1349,12 +1379,7 @@ int launch_head_logprobs_grad(const void* h, int64_t h_stride, const void* w, in
       go(k_head_tile<kPackedT, kPackedT, kWeight>, x);
     }
   }
-  if (gh) {
-    const int64_t n = (int64_t)n_rows * d;
-    const dim3 grid((uint32_t)((n / 4 + 255) / 256));
-    if (f32) hipLaunchKernelGGL((k_head_sum<float>), grid, dim3(256), 0, st, slab, p.splits, n, d, rows, inv_t, (float*)gh, gh_stride);
-    else hipLaunchKernelGGL((k_head_sum<uint16_t>), grid, dim3(256), 0, st, slab, p.splits, n, d, rows, inv_t, (uint16_t*)gh, gh_stride);
-  }
+  if (gh) sum();
   return head_done("head log probabilities gradient launch");
 }
 

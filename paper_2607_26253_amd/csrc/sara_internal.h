@@ -348,10 +348,11 @@ int launch_token_logprobs_grad(const void* logits, int dtype, int64_t row_stride
                                float temp, void* grad, int64_t grad_stride, hipStream_t st);
 // launchers (log probabilities from hidden states)
 // How a call is cut and where its workspace's parts begin: few rows, small tiles or large ones; vocabulary tiles (256 ids) of a piece,
-// padded rows, padded width of bf16 parts, parts of D, splits of dH's contraction.
+// padded rows, padded width of bf16 parts, parts of D, splits of dH's contraction (small: of h_steps
+// of 16 ids).
 struct HeadPlan {
   bool few, small;
-  int nt, few_blocks, piece, rows_out, width, d_parts, splits;
+  int nt, few_blocks, piece, rows_out, width, d_parts, splits, h_steps;
   int64_t x_tok, parts, rows, d, id_flags, row_flags, slab, h_parts, w_parts, bytes;
 };
 HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool grad);

@@ -129,10 +129,12 @@ SIZES = [(1, 8, 1), (1, 64, 257), (2, 72, 16), (3, 40, 500), (15, 136, 129), (16
 # past what small tiles take, with ends inside the large ones: for fp32 too
 BIG = (1100, 1032, 5001)
 LARGE = [BIG, (2500, 1000, 2065), (70, 1544, 33001)]
+# few rows and many ids: dH's contraction in splits
+LONG = [(2, 72, 40000), (33, 200, 9001), (1, 8, 2049)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows,d,V", SIZES + LARGE)
+@pytest.mark.parametrize("rows,d,V", SIZES + LARGE + LONG)
 def test_log_probabilities_and_gradients(env, rows, d, V, dtype):
     torch, _ = env
     T = (1.0, 0.7, 1.3)[rows % 3]
