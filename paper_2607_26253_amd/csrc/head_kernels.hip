@@ -604,9 +604,14 @@ __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
   for (int64_t v0 = 128 * (int64_t)blockIdx.x; v0 < a.V; v0 += 128 * (int64_t)gridDim.x) {
     const int id = (int)v0 + 16 * wave;
     const char* w = a.w + min((int64_t)id + row, (int64_t)a.V - 1) * a.w_stride + 32 * grp;
-    f32x4 acc[NT];
+    // Several sums of a logit, of smaller numbers and fewer roundings in a row: with one the largest logit of a row was
+    // off by some 2e-6, and so was the sum of exponentials
+    constexpr int SUMS = NT == 4 ? 2 : 4;
+    f32x4 part[NT][SUMS], acc[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < SUMS; ++i) part[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     u32x4 r[DEPTH][2];
     auto load = [&](int b, int slot) {
 #pragma unroll
@@ -633,13 +638,14 @@ __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
               const u32x4 h = hs[((b + i) * 16 * NT + 16 * t + row) * 8 + ((2 * grp + s) ^ (row & 7))];
+              f32x4& z = part[t][(2 * i + s) % SUMS];
               if constexpr (sizeof(T) == 2) {
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r[i][s]), __builtin_bit_cast(bf16x8, h),
-                                                                 acc[t], 0, 0, 0);
+                z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r[i][s]), __builtin_bit_cast(bf16x8, h),
+                                                            z, 0, 0, 0);
               } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(r[i][s][e]), __uint_as_float(h[e]), acc[t], 0, 0, 0);
+                  z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(r[i][s][e]), __uint_as_float(h[e]), z, 0, 0, 0);
               }
             }
           __builtin_amdgcn_sched_barrier(0);               // else the loads gather behind the products
@@ -651,6 +657,11 @@ __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
     // lane (row, grp): ids id + 4 grp ..+3 of rows 16 t + row
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int n = SUMS / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) part[t][i] += part[t][i + n];
+      acc[t] = part[t][0];
       const int at = tok[t] - id - 4 * grp, left = a.V - id - 4 * grp;
       if (at >= 0 && at < 4 && left > at) {
         float x = acc[t][0];
