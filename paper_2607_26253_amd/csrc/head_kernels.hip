@@ -36,8 +36,15 @@ struct Mat {
 };
 
 // What a row needs for its D: 2^u (A + B u) + [v = tok] g; logits above `large` make elements
-// that are taken more exactly
+// that are taken more exactly.  on: 0 where nothing is asked of the row, 2 where elements may pass bf16's range, else 1.
 struct HeadRow { float m, A, B, g, large; int32_t tok, on; };
+
+// The first of a number's bf16 parts is bf16's largest finite number where rounding would pass it: the parts that follow
+// hold what is left, as ever.  An infinity stays one.
+constexpr float kBf16Max = 0x1.FEp127f;
+__device__ __forceinline__ float first_part(float f) {
+  return fabsf(f) < INFINITY ? __builtin_amdgcn_fmed3f(f, -kBf16Max, kBf16Max) : f;
+}
 
 struct HeadTile {
   Mat a, b;                 // M side and N side of C[m][n] = sum_k a(m, k) b(n, k)
@@ -205,6 +212,7 @@ __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileE
     __builtin_amdgcn_sched_barrier(0);                       // else the rows' values gather in front
     const HeadRow hr = lds.rows[128 * wm + 16 * m + row];
     const int at = hr.tok - a.v0 - col;                      // 32 j + 16 b + q where it is this lane's
+    const bool huge = __any(hr.on == 2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       // A row that is off has A = B = 0 and no id here; one that met a NaN has it in A
@@ -231,6 +239,7 @@ __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileE
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t x = pack_bf16(f[2 * q], f[2 * q + 1]);
+          if (p == 0 && huge) x = pack_bf16(first_part(f[2 * q]), first_part(f[2 * q + 1]));
           asm("" : "+v"(x));                                 // what was rounded is what is subtracted
           f[2 * q] -= __uint_as_float(x << 16);
           f[2 * q + 1] -= __uint_as_float(x & 0xFFFF0000u);
@@ -766,7 +775,7 @@ __global__ __launch_bounds__(256) void k_head_pack(const T* __restrict__ x, int6
       u32x4 w;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        uint32_t v = pack_bf16(f[2 * q], f[2 * q + 1]);
+        uint32_t v = p == 0 ? pack_bf16(first_part(f[2 * q]), first_part(f[2 * q + 1])) : pack_bf16(f[2 * q], f[2 * q + 1]);
         asm("" : "+v"(v));
         f[2 * q] -= __uint_as_float(v << 16);
         f[2 * q + 1] -= __uint_as_float(v & 0xFFFF0000u);
@@ -801,7 +810,8 @@ __device__ __forceinline__ HeadRow head_row(const HeadGrads& a, int r) {
   const float hl = h == 0.f ? 0.f : h * (a.entropy[r] - logf(s)), A = -(g + hl) / s, B = -0.69314718f * h / s;
   const float half = 0.5f * kBig * (fabsf(g) * (1.f - 1.f / s) + fabsf(hl) / s);
   const float u = B == 0.f ? log2f(2.f * half / fabsf(A)) : fminf(log2f(half / fabsf(A)), 2.f * log2f(half / (1.07f * fabsf(B))));
-  return HeadRow{m, a.scale * A, a.scale * B, a.scale * g, m + fminf(u, 0.f) * a.inv_c, has ? tk : -1, 1};
+  const float most = a.scale * (fabsf(A) + 0.54f * fabsf(B) + fabsf(g));   // 2^u |u| <= 0.531
+  return HeadRow{m, a.scale * A, a.scale * B, a.scale * g, m + fminf(u, 0.f) * a.inv_c, has ? tk : -1, most > 0.5f * kBf16Max ? 2 : 1};
 }
 
 __global__ __launch_bounds__(256) void k_head_rows(HeadGrads a, int rows_out, HeadRow* __restrict__ out) {

@@ -421,3 +421,68 @@ def test_reruns_are_bit_identical(env, rows, d, V):
     assert all(env[0].equal(out[0][k], out[1][k]) for k in out[0])
     a, b = (gradients(env, x, out[0]) for _ in range(2))
     assert env[0].equal(a[0], b[0]) and env[0].equal(a[1], b[1])
+
+
+LOWEST = -3.4028234663852886e38                           # finfo(float32).min
+
+
+def masked_heads(env, rows, d, V, T):
+    """fp32 weights whose element 0 is fp32's lowest number for the ids 1, 8, 15, ...: every row has 0.25 to 0.75 there,
+    so those ids' logits are finite and count for nothing.  One hidden element is the lowest number too, where every id has 0.
+    -> inputs, which ids count, the definition's results."""
+    torch, _ = env
+    x = make(env, rows, d, V, "f32")
+    keep = torch.arange(V, device="cuda") % 7 != 1
+    x["h"][:, 0] = 0.25 + 0.5 * torch.rand(rows, device="cuda", generator=torch.Generator(device="cuda").manual_seed(rows))
+    x["w"][~keep, 0] = LOWEST
+    x["h"][1, 3] = LOWEST
+    x["w"][:, 3] = 0.0
+    x["gl"][1], x["ge"][1] = 0.1, 0.01                    # dW[:, 3] = D[1] * lowest stays finite
+    here = (x["tok"] >= 0) & (x["tok"] < V)
+    x["tok"][here] -= (x["tok"][here] % 7 == 1).int()     # tokens that count
+    number = torch.cumsum(keep, 0) - 1
+    few = dict(x, w=x["w"][keep])
+    few["tok"] = torch.where(here, number[x["tok"].clamp(0, V - 1).long()], torch.full_like(number[:1], -1)).int()
+    e = exact(env, few, T)
+    for k in ("D", "Derr"):                               # the ids that count for nothing have no D
+        e[k] = torch.zeros((rows, V), device="cuda", dtype=torch.float64).index_copy_(1, keep.nonzero()[:, 0], e[k])
+    e["w"] = x["w"].double()
+    return x, keep, e
+
+
+@pytest.mark.parametrize("rows,d,V", [(5, 64, 300), (90, 64, 300), BIG])
+def test_lowest_finite_numbers(env, rows, d, V):
+    """Elements past bf16's largest finite number leave everything finite, whatever the size of the call."""
+    torch, _ = env
+    T = 0.9
+    x, keep, e = masked_heads(env, rows, d, V, T)
+    out = forward(env, x, T)
+    check_forward(out, e)
+    gh, gw = gradients(env, x, out, T)
+    check_gradients(env, gh, gw, x, e)
+    assert bool((gw[~keep] == 0).all())
+    # their own log probabilities, near -1e38: x is one product of 24 bits, the rest of it and log s are below its rounding
+    y = dict(x, tok=torch.full_like(x["tok"], 8))
+    logp = forward(env, y, T)["logp"].double()
+    want = (x["h"][:, 0].double() * LOWEST - e["top"]) / T
+    assert bool(((logp / want - 1).abs() <= 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,d,V", [(90, 64, 300), BIG])
+def test_largest_finite_cotangents(env, rows, d, V, dtype):
+    """D past bf16's largest finite number: an fp32 call is as exact as ever; in a bf16 call D counts as that number at
+    least, which is within its 2^-8.  p is below 2^-9 where it matters, so that D at the row's id keeps its size."""
+    torch, _ = env
+    x = make(env, rows, d, V, dtype, spread=0.25)
+    x["gl"][:], x["ge"][:] = 0.0, 0.0
+    x["tok"][:] = torch.arange(rows, device="cuda") % V   # one large row an id in the small call, a few in the large one
+    x["gl"][7], x["gl"][rows - 1] = -LOWEST, LOWEST
+    x["h"], x["w"] = x["h"] * 0.125, x["w"] * 0.125       # products below fp32's largest
+    e = exact(env, x, 1.0)
+    assert float(e["D"].abs().max()) > 0.995 * -LOWEST
+    out = forward(env, x)
+    gh, gw = gradients(env, x, out)
+    check_gradients(env, gh, gw, x, e)
+    if dtype == "bf16":
+        check_gradients(env, *gradients(env, x, out, sums=torch.float32), x, e)
