@@ -1068,6 +1068,7 @@ constexpr int kFewRows = 64;
 constexpr int kCus = 256;
 
 static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+static int64_t tiles32(int64_t M, int64_t N) { return (M + 31) / 32 * ((N + 31) / 32); }   // blocks of small tiles
 
 // us of a product of small tiles and of large ones in `pairs` pairs of parts, by rounds of the compute units: 2.4 and 4 us for
 // each 256 of k and pair, half of that where a small tile has a compute unit to itself, but 0.75 for a start and its stores
@@ -1079,7 +1080,7 @@ static int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 //         1024     512        2048                 54, 31             120, 131
 //         1024     1024       8192                297, 41             749, 155
 static double small_us(int64_t M, int64_t N, int64_t K, int splits = 1) {
-  const int64_t tiles = ((M + 31) / 32) * ((N + 31) / 32) * splits;
+  const int64_t tiles = tiles32(M, N) * splits;
   K = (K + splits - 1) / splits;
   const double tile = 2.4 * K / 256;
   return (splits > 1 ? 10 : 5) + (tiles <= kCus ? 0.5 * tile : (double)(up(tiles, kCus) / kCus) * std::max(tile, 0.75));
@@ -1103,7 +1104,8 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
       p.parts = take(16 * (int64_t)16 * p.nt * p.few_blocks);
       return p;
     }
-    p.small = small_us(n_rows, V, d) < large_us(n_rows, V, d, f32 ? 6 : 1) + (f32 ? 10 : 5);   // and what packing takes
+    p.small = small_us(n_rows, V, d) < large_us(n_rows, V, d, f32 ? 6 : 1) + (f32 ? 10 : 5) &&   // and what packing takes
+              tiles32(n_rows, V) <= kMaxBlocks;
     if (p.small) {
       p.parts = take(16 * (int64_t)n_rows * ((V + 31) / 32));
       return p;
@@ -1119,12 +1121,13 @@ HeadPlan head_plan(int dtype, int n_rows, int d, int V, int weight_f32, bool gra
   // Splits of a small dH's contraction, of 1,024 ids or more.  Two fp32 rows of width 256 over 151,936 ids: 238 us
   // for the gradients, 640 in large tiles.
   const int ids16 = (V + 15) / 16;
-  const int64_t h_tiles = (int64_t)((n_rows + 31) / 32) * ((d + 31) / 32);
+  const int64_t h_tiles = tiles32(n_rows, d);
   const int h_splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / h_tiles, ids16 / 64));
   const double large = large_us(n_rows, V, d, pairs) + large_us(n_rows, d, (V + 63) / 64, pairs) + large_us(V, d, n_rows, pairs);
   // The parts of an fp32 weight are written once and read for each pair, twice over: 34 bytes an element
   const double parts = f32 ? (double)V * d * 34 / 5e6 : 0;
-  p.small = small_us(n_rows, V, d) + small_us(n_rows, d, V, h_splits) + small_us(V, d, n_rows) < std::max(large, parts) + (f32 ? 75 : 40);
+  p.small = small_us(n_rows, V, d) + small_us(n_rows, d, V, h_splits) + small_us(V, d, n_rows) < std::max(large, parts) + (f32 ? 75 : 40) &&
+            tiles32(n_rows, V) <= kMaxBlocks && h_splits * h_tiles + tiles32(V, d) <= kMaxBlocks;
   if (p.small) {
     p.width = (int)up(V, 32);
     p.rows = take(sizeof(HeadRow) * up(n_rows, 32));

@@ -872,9 +872,6 @@ extern "C" int sara_sample_logits_noalloc(const float* d_logits, int32_t n_rows,
                                     eos_id, forced_eos_u32, d_tok, (hipStream_t)stream);
 }
 
-// A launch's grid holds fewer than 2^32 threads along x: blocks of 256 that the calls on an 8-bit cache may have.
-static constexpr int64_t kMaxBlocks = (1 << 24) - 1;
-
 // Arguments that the calls on an 8-bit cache share; "" when they are in order.
 static std::string kv8_bad(const sara_kv8_cache* c, int32_t dtype, int32_t n_rows, const int32_t* d_pages,
                            int32_t max_pages, const int32_t* d_seq, const int32_t* d_off, int32_t n_seqs) {

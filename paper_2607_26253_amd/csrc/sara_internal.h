@@ -312,6 +312,9 @@ int launch_sample_rows_noalloc(const float* logits, int n_rows, int V, const int
                                uint64_t seed, int step, float temp, float top_p, int eos, uint32_t feos,
                                int32_t* tok, hipStream_t st);
 // launchers (8-bit KV cache)
+// A launch's grid holds fewer than 2^32 threads along x: blocks of 256 that a call on the caller's tensors may have.
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;
+
 // How an attention call is cut, for the kernel of few columns and for the one of column tiles: most context splits of a
 // row, pages a split, work items, and the partial results' bytes in the workspace.
 struct Kv8Split {

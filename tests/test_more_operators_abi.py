@@ -123,3 +123,13 @@ def test_head_of_no_rows_and_workspaces():
                     for backward in (0, 1):
                         rc, need = head_need(dtype, rows, d, V, backward, dtype)
                         assert rc == OK and 0 < need < (3 << 30) + 64 * rows * (d + 512), (rows, dtype, d, V, backward, need)
+
+
+def test_wide_heads_fit_their_launches():
+    """Small tiles of a weight's gradient are vocab d / 1024 blocks, of which a launch holds 2^24 - 1: 16,383 x 1,024 and the
+    1,024 of dH are one too many and go in large tiles, whose workspace holds a piece of the weight in bf16 parts (453 MB)."""
+    rc, need = head_need(F32, 1, 32768, 32 * 16382, 1, F32)
+    assert rc == OK and need < 1 << 27
+    for V in (32 * 16382 + 1, 524289, 600000):
+        rc, need = head_need(F32, 1, 32768, V, 1, F32)
+        assert rc == OK and need > 1 << 28
