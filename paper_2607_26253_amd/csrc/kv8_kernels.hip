@@ -1375,6 +1375,11 @@ static int split_pages(int pages, int64_t items, int64_t blocks, int least, int 
   return (int)std::max<int64_t>(least, ((pages + want - 1) / want + step - 1) / step * step);
 }
 
+// One launch for both where the blocks of few columns fit beside each other at the tiles' two a CU: 64 sequences of
+// 1-33 fp32 queries over up to 63 tokens 12.4 -> 8.0 us, of 1-33 bf16 ones over up to 500 31.2 -> 22.9.  More of them
+// lose the third wave a SIMD that streaming pages wants: 512 sequences of 1-2 queries over 1,000 tokens 70 -> 80.
+static bool both_in_one(const Kv8Split& s, int hkv) { return s.tile_items && s.items * hkv * s.splits <= 512; }
+
 Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx, bool ragged) {
   const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16);
   // Pages a split so that about `blocks` blocks share the work, at least `least`, in steps of `step`, and at most
@@ -1396,6 +1401,10 @@ Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx,
   const int64_t one = (int64_t)sizeof(float) * (hd + 2);
   if (s.splits > 1) s.part_bytes = (one * n_seqs * hkv * (ragged ? kFewColumns : G) * s.splits + 15) / 16 * 16;
   if (s.splits_tile > 1) s.part_tile_bytes = one * n_rows * hq * s.splits_tile;
+  const int64_t few = s.items * hkv, tiles = s.tile_items * hkv;
+  s.blocks = both_in_one(s, hkv) ? tiles * s.splits_tile + few * s.splits : std::max(few, tiles);
+  if (s.splits > 1) s.blocks = std::max(s.blocks, (int64_t)n_seqs * hkv * (ragged ? kFewColumns : G));
+  if (s.splits_tile > 1) s.blocks = std::max(s.blocks, (int64_t)n_rows * hq);
   return s;
 }
 
@@ -1405,10 +1414,7 @@ template <int WHAT> static int launch_attention(const sara_kv8_cache& c, int dty
   const int32_t* off = a.off;
   return kv8_dispatch(c, dtype, [&](auto hd, auto fmt, auto t) {
     const int n_few = (int)(s.items * c.n_kv_heads), n_tile = (int)(s.tile_items * c.n_kv_heads);
-    // One launch for both where the blocks of few columns fit beside each other at the tiles' two a CU: 64 sequences of
-    // 1-33 fp32 queries over up to 63 tokens 12.4 -> 8.0 us, of 1-33 bf16 ones over up to 500 31.2 -> 22.9.  More of them
-    // lose the third wave a SIMD that streaming pages wants: 512 sequences of 1-2 queries over 1,000 tokens 70 -> 80.
-    if (s.tile_items && (int64_t)n_few * s.splits <= 512) {
+    if (both_in_one(s, c.n_kv_heads)) {
       hipLaunchKernelGGL((k_kv8_attn_both<hd.value, fmt.value, decltype(t), WHAT>), dim3(n_tile * s.splits_tile + n_few * s.splits), dim3(256),
                          0, st, c, a, n_tile, n_few);
     } else {
@@ -1438,6 +1444,8 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
 }
 
 constexpr int kSharedBlocks = 1024;
+// blocks of the join of so many (row, head)s
+static int64_t join_blocks(const Kv8GroupSplit& s, int64_t items) { return (items * s.join_waves() + 3) / 4; }
 Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged,
                               int dtype) {
   const int G = hq / hkv, np = std::max(1, (max_ctx + 15) / 16), np_shared = max_shared / 16;
@@ -1469,6 +1477,10 @@ Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, i
   if (!s.finish || s.splits > 1) s.part_bytes = (one * n_seqs * hkv * (ragged ? kFewColumns : G) * s.splits + 15) / 16 * 16;
   if (!s.finish || s.splits_tile > 1) s.part_tile_bytes = (one * n_rows * hq * s.splits_tile + 15) / 16 * 16;
   s.part_shared_bytes = (int64_t)sizeof(float) * (hd + 4) * n_rows * hq * s.splits_shared;
+  const int64_t few = s.few_items * hkv, own = s.tile_items * hkv, common = s.shared_items * hkv;
+  s.blocks = s.all ? common * s.splits_shared + own * s.splits_tile + few * s.splits : std::max(std::max(few, own), common);
+  if (s.joins_few()) s.blocks = std::max(s.blocks, join_blocks(s, (int64_t)n_seqs * hkv * (ragged ? kFewColumns : G)));
+  if (s.joins_tile()) s.blocks = std::max(s.blocks, join_blocks(s, (int64_t)n_rows * hq));
   // What a group shares is taken apart where that saves more than it costs: the partial results' way to memory and back and
   // about 12 us of launches.  Without it every sequence reads those pages, most of them from the caches, at some 8 TB/s if its
   // columns are few, or in tiles of 128 columns that a single sequence may not fill (1.8 us a key block and compute
@@ -1520,17 +1532,14 @@ int launch_kv8_group_attention(const sara_kv8_cache& c, const void* q, int dtype
         hipLaunchKernelGGL((k_kv8_group_own_tile<hd.value, fmt.value, decltype(t)>), dim3(n_tile, s.splits_tile), dim3(256), 0, st, c, a);
     }
     const int cols = off ? kFewColumns : hq / hkv, few = n_seqs * hkv * cols, rows = n_rows * hq;
-    const bool many = s.finish || s.splits + s.splits_tile + s.splits_shared > 16;   // splits to a row
-    auto join = [&](auto k, int items, int waves) {
-      hipLaunchKernelGGL(k, dim3((uint32_t)((items + 4 / waves - 1) / (4 / waves))), dim3(256), 0, st, a, items, cols);
-    };
-    if (!s.finish || s.splits > 1) {
-      if (many) join(k_kv8_group_join<hd.value, decltype(t), 4, false>, few, 4);
-      else join(k_kv8_group_join<hd.value, decltype(t), 1, false>, few, 1);
+    auto join = [&](auto k, int items) { hipLaunchKernelGGL(k, dim3((uint32_t)join_blocks(s, items)), dim3(256), 0, st, a, items, cols); };
+    if (s.joins_few()) {
+      if (s.join_waves() == 4) join(k_kv8_group_join<hd.value, decltype(t), 4, false>, few);
+      else join(k_kv8_group_join<hd.value, decltype(t), 1, false>, few);
     }
-    if (n_tile && (!s.finish || s.splits_tile > 1)) {
-      if (many) join(k_kv8_group_join<hd.value, decltype(t), 4, true>, rows, 4);
-      else join(k_kv8_group_join<hd.value, decltype(t), 1, true>, rows, 1);
+    if (s.joins_tile()) {
+      if (s.join_waves() == 4) join(k_kv8_group_join<hd.value, decltype(t), 4, true>, rows);
+      else join(k_kv8_group_join<hd.value, decltype(t), 1, true>, rows);
     }
   });
 }

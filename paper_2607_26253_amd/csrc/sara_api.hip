@@ -965,7 +965,7 @@ extern "C" int sara_kv8_attention(const sara_kv8_cache* c, const void* d_q, int6
     return einval("too many rows or sequences");
   if (rows_overlap(o_row, o_head, n_rows, n_heads, c->head_dim)) return einval("rows and heads of out must not overlap");
   const Kv8Split split = kv8_split(n_rows, n_heads, c->n_kv_heads, c->head_dim, n_seqs, max_ctx, d_off != nullptr);
-  if (std::max(split.items, split.tile_items) * c->n_kv_heads > kMaxBlocks) return einval("too many rows or sequences");
+  if (split.blocks > kMaxBlocks) return einval("too many rows or sequences");
   const int64_t need = split.part_bytes + split.part_tile_bytes;
   if (need > 0 && (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need))
     return einval("workspace of " + std::to_string(need) + " bytes, 16-byte aligned, is needed");
@@ -978,10 +978,9 @@ struct GroupNeed { int64_t bytes, blocks; };
 static GroupNeed group_need(int32_t hkv, int32_t hd, int32_t n_rows, int32_t hq, int32_t n_seqs, int32_t n_groups, bool ragged,
                             int32_t max_ctx, int32_t max_shared, int32_t dtype) {
   const Kv8GroupSplit g = kv8_group_split(n_rows, hq, hkv, hd, n_seqs, n_groups, max_ctx, max_shared, ragged, dtype);
-  if (g.apart)
-    return {g.part_bytes + g.part_tile_bytes + g.part_shared_bytes, std::max(std::max(g.few_items, g.tile_items), g.shared_items) * hkv};
+  if (g.apart) return {g.part_bytes + g.part_tile_bytes + g.part_shared_bytes, g.blocks};
   const Kv8Split s = kv8_split(n_rows, hq, hkv, hd, n_seqs, max_ctx, ragged);
-  return {s.part_bytes + s.part_tile_bytes, std::max(s.items, s.tile_items) * hkv};
+  return {s.part_bytes + s.part_tile_bytes, s.blocks};
 }
 
 extern "C" int sara_kv8_group_attention_workspace(int32_t n_kv_heads, int32_t head_dim, int32_t n_rows, int32_t n_heads, int32_t n_seqs,

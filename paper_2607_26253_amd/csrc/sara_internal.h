@@ -316,10 +316,11 @@ int launch_sample_rows_noalloc(const float* logits, int n_rows, int V, const int
 constexpr int64_t kMaxBlocks = (1 << 24) - 1;
 
 // How an attention call is cut, for the kernel of few columns and for the one of column tiles: most context splits of a
-// row, pages a split, work items, and the partial results' bytes in the workspace.
+// row, pages a split, work items, the partial results' bytes in the workspace, and the blocks of its largest launch, the
+// joins among them.
 struct Kv8Split {
   int splits, pps, splits_tile, pps_tile;
-  int64_t items, tile_items, part_bytes, part_tile_bytes;
+  int64_t items, tile_items, part_bytes, part_tile_bytes, blocks;
 };
 Kv8Split kv8_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int max_ctx, bool ragged);
 int64_t kv8_rows_blocks(int n_seqs, int n_rows, bool ragged, int hkv);
@@ -332,8 +333,11 @@ int launch_kv8_attention(const sara_kv8_cache& c, const void* q, int dtype, int6
 // The same for sequences in groups that share pages.
 struct Kv8GroupSplit {
   int splits, pps, splits_tile, pps_tile, splits_shared, pps_shared;
-  int64_t few_items, tile_items, shared_items, part_bytes, part_tile_bytes, part_shared_bytes;
+  int64_t few_items, tile_items, shared_items, part_bytes, part_tile_bytes, part_shared_bytes, blocks;
   bool apart, all, finish;   // the shared pages on their own; one launch for all of it; rows of one own split need no join
+  bool joins_few() const { return !finish || splits > 1; }
+  bool joins_tile() const { return tile_items && (!finish || splits_tile > 1); }
+  int join_waves() const { return finish || splits + splits_tile + splits_shared > 16 ? 4 : 1; }   // of a row and head
 };
 Kv8GroupSplit kv8_group_split(int n_rows, int hq, int hkv, int hd, int n_seqs, int n_groups, int max_ctx, int max_shared, bool ragged,
                               int dtype);

@@ -133,3 +133,14 @@ def test_wide_heads_fit_their_launches():
     for V in (32 * 16382 + 1, 524289, 600000):
         rc, need = head_need(F32, 1, 32768, V, 1, F32)
         assert rc == OK and need > 1 << 28
+
+
+@pytest.mark.parametrize("n_seqs", [65536, 70000, 300000])
+def test_group_joins_past_a_launch_are_refused(n_seqs):
+    """Few rows of many mostly empty sequences behind a long prompt: the join is 32 blocks for each sequence and KV head, of
+    which a launch holds 2^24 - 1; the launches before it would have been enqueued."""
+    rc, need = group_need(hkv=8, n_rows=100, heads=8, n_seqs=n_seqs, ragged=1, max_ctx=66000, max_shared=65536)
+    assert rc == OK and need > 32 * 8 * n_seqs * 128 * 4
+    assert group(cache(n_kv_heads=8), row=1024, o_row=1024, n_rows=100, heads=8, max_pages=4125, n_seqs=n_seqs, max_ctx=66000,
+                 max_shared=65536, ws=P, ws_bytes=need) == BAD
+    assert b"too many" in L.sara_last_error()
