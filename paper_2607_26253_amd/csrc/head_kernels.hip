@@ -234,12 +234,11 @@ __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileE
 #pragma unroll
         for (int n = 0; n < 8; ++n) f[n] = col + 32 * j + 16 * (n >> 2) + (n & 3) < a.N ? f[n] : 0.f;
       u32x4* y = (u32x4*)(a.d + ((int64_t)((tn0 >> 5) + 4 * wn + j) * a.d_tiles + ((tm0 + 128 * wm + 16 * m) >> 4)) * 512);   // scalar
-      auto store = [&](int p) {                              // rounded; f keeps the rest
+      auto store = [&](int p, auto may_pass) {               // rounded; f keeps the rest
         u32x4 w;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          uint32_t x = pack_bf16(f[2 * q], f[2 * q + 1]);
-          if (p == 0 && huge) x = pack_bf16(first_part(f[2 * q]), first_part(f[2 * q + 1]));
+          uint32_t x = may_pass.value ? pack_bf16(first_part(f[2 * q]), first_part(f[2 * q + 1])) : pack_bf16(f[2 * q], f[2 * q + 1]);
           asm("" : "+v"(x));                                 // what was rounded is what is subtracted
           f[2 * q] -= __uint_as_float(x << 16);
           f[2 * q + 1] -= __uint_as_float(x & 0xFFFF0000u);
@@ -247,9 +246,11 @@ __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileE
         }
         (y + p * (a.d_part / 8))[lane] = w;
       };
+      if (huge) store(0, std::true_type{});
+      else store(0, std::false_type{});
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) store(p);
-      if ((my_ids >> j | my_rows >> (m >> 1)) & 1) store(PARTS);
+      for (int p = 1; p < PARTS; ++p) store(p, std::false_type{});
+      if ((my_ids >> j | my_rows >> (m >> 1)) & 1) store(PARTS, std::false_type{});
     }
   }
 }
