@@ -572,7 +572,9 @@ __device__ __forceinline__ void head_merge(HeadSum& a, HeadSum b, float c) {
 // Up to 16 NT rows: W streams past them.  A block of 8 waves takes 128 ids at a time, a wave 16 of them, in 128-byte blocks of
 // k: a lane loads 32 consecutive bytes of an id's row, the hidden states lie in LDS (`chunk` blocks of k at a time).
 // fp32 runs on v_mfma_f32_16x16x4_f32.  Bound by W's way from memory: 151,936 ids of width 1,536 in bf16, 467 MB, take 100 us for
-// one row (4.7 TB/s) and 114 for 35, whose hidden states pass LDS in three chunks.
+// one row (4.7 TB/s), 105 for 17 to 32 and 116 for 35 to 64, whose hidden states pass LDS in two and three chunks; in fp32, 933 MB, 198, 215
+// and 300, of which the matrix instructions of 64 rows are some 190.  Eight blocks of k in flight leave 17 to 32 rows no
+// registers for their sums: the call took 136 us in bf16 and 264 in fp32, for 110 and 217.
 struct HeadFew {
   const char *h, *w;
   int64_t h_stride, w_stride;   // bytes
@@ -586,7 +588,7 @@ constexpr int kFewLds = 65536;
 template <typename T, int NT>
 __global__ __launch_bounds__(512, 4) void k_head_few(HeadFew a) {
   constexpr int CB = kFewLds / (16 * NT * 128);            // 128-byte blocks of k of a chunk
-  constexpr int DEPTH = NT == 4 ? 4 : 8;                                // blocks of k in flight; CB is a multiple
+  constexpr int DEPTH = NT == 1 ? 8 : 4;                   // blocks of k in flight; CB is a multiple
   __shared__ u32x4 hs[kFewLds / 16];
   __shared__ HeadSum red[8][16 * NT];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
