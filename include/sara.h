@@ -509,7 +509,8 @@ int sara_token_logprobs_grad(const void* d_logits, int32_t dtype, int64_t row_st
  * summed in fp32 and never stored, so that a policy update keeps neither
  * [n_rows][vocab] logits nor their gradient.  d_hidden[r * hidden_stride + k]
  * and d_weight[id * weight_stride + k], k < d_model, are of one dtype (SARA_BF16
- * or SARA_F32: products at fp32 accuracy either way); 16-byte aligned, rows,
+ * or SARA_F32: products at fp32 accuracy either way, but for low bits of numbers
+ * below 2^-110, which bf16 parts may not hold); 16-byte aligned, rows,
  * strides (at least d_model) and d_model multiples of 16 bytes.  d_logp,
  * d_entropy, d_stats, d_tok and temperature are those of sara_token_logprobs;
  * each of the three outputs may be NULL.  A logit that is not finite (an element
@@ -532,9 +533,11 @@ int sara_head_logprobs(const void* d_hidden, int64_t hidden_stride, const void* 
  *                   weight_grad_dtype: dtype or SARA_F32 (for sums over
  *                   micro-batches); accumulate != 0 adds to what it holds
  * summed in fp32 and rounded once.  D enters the products of a bf16 call rounded
- * to bf16, for an fp32 weight gradient in two bf16 parts (2^-17 of it), with one
- * part more where a row's largest elements are, so that the products are off by no
- * more than their outputs' own rounding; those of an fp32 call take three parts.
+ * to bf16 (2^-8 of an element), for an fp32 weight gradient in two bf16 parts
+ * (2^-17), with one part more where a row's largest elements are: a gradient that
+ * a few elements make is off by its own rounding, in norm.  That is no bound for
+ * each output: one whose terms are all small, or cancel, is off by up to 2^-8
+ * (2^-17) of those terms more.  The products of an fp32 call take three parts.
  * Small problems keep D in fp32.  n_rows <= 131,072: more come in several calls,
  * with accumulate.  Either gradient may be NULL, not both; they must not
  * overlap the inputs.  d_stats and d_entropy are those of sara_head_logprobs on

@@ -486,3 +486,72 @@ def test_largest_finite_cotangents(env, rows, d, V, dtype):
     check_gradients(env, gh, gw, x, e)
     if dtype == "bf16":
         check_gradients(env, *gradients(env, x, out, sums=torch.float32), x, e)
+
+
+def rows_of_few_large(env, rows, d, V):
+    """Rows whose D is a large element or two, each of an id that no other row has, beside 32 of a thirtieth of it and
+    thousands of next to nothing: ids at 6 (the 32), at -6 and, in two rows of three, one at 9.5.
+    -> inputs, rows that ask for something, ids of large elements, those among them whose p is next to nothing."""
+    torch, _ = env
+    g = torch.Generator(device="cuda").manual_seed(rows + V)
+    dev = dict(generator=g, device="cuda")
+    h, w = torch.randn((rows, d), **dev) * 0.25, torch.randn((V, d), **dev) / 16
+    sinks = 37 + 151 * torch.arange(32, device="cuda")
+    order = torch.randperm(V, **dev)
+    order = order[~torch.isin(order, sinks)]
+    tok, likely = order[:rows], order[rows:2 * rows]
+    kind = torch.arange(rows, device="cuda") % 3          # log probability; entropy; both
+    w[:, 0] = -6.0
+    w[sinks, 0] = 6.0
+    leans = kind > 0
+    h[leans] = w[likely[leans]] * (15.5 * 256 / d)
+    h[:, 0] = 1.0
+    gl, ge = 0.5 + torch.rand(rows, **dev), 0.5 + torch.rand(rows, **dev)
+    gl[kind == 1], ge[kind == 0] = 0.0, 0.0
+    on = torch.arange(rows, device="cuda") % 29 != 5
+    on[96:128] = False                                    # a step of 32 rows without any
+    gl[~on], ge[~on] = 0.0, 0.0
+    few = tok[on & (kind != 1)]
+    x = dict(h=h.bfloat16(), w=w.bfloat16(), tok=tok.int(), gl=gl, ge=ge)
+    return x, on, torch.cat([few, likely[on & leans]]), few
+
+
+@pytest.mark.parametrize("rows,d,V", [BIG, (2500, 1000, 20001), (1100, 264, 130001)])
+def test_large_elements_of_D_count_exactly(env, rows, d, V):
+    """The large elements' further part, in norm: a gradient in bf16 is off by its own rounding (and a tenth of it), where one
+    bf16 part of D would leave 1.2 to 1.4 times that (sqrt(2) where both roundings are independent; dH's largest column is 12
+    times a row's D, whose rounding the output's partly repeats); the weight's gradient in fp32 by less than half of what two parts would.
+    Both of those come from the definition with D rounded so.  Predicted: what the small elements leave adds (32 / 30^2)
+    of the variance, 2%; the fp32 sums' roundings of some 160 steps in a walk are 13 x 2^-24, an eighth of two parts'
+    2^-16 / sqrt(3) / 1.5.  What the products read has to be written: the workspace is full of NaN before."""
+    torch, sara = env
+    import ctypes
+    x, on, ids, few = rows_of_few_large(env, rows, d, V)
+    out = forward(env, x)
+    e = exact(env, x, 1.0)
+    results = {}
+    for sums in (torch.bfloat16, torch.float32):
+        need = ctypes.c_int64(0)
+        assert sara._lib.sara_head_logprobs_workspace(1, rows, d, V, 1, int(sums == torch.bfloat16), ctypes.byref(need)) == 0
+        ws = torch.full((need.value,), 255, device="cuda", dtype=torch.uint8)
+        gh, results[sums] = gradients(env, x, out, sums=sums, workspace=ws)
+        check_gradients(env, gh, results[sums], x, e)
+    D = e["D"]
+    one = D.bfloat16().double()
+    two = one + (D - one).bfloat16().double()
+    h, w = e["h"], e["w"]
+
+    def off(got, want):
+        return float((got.double() - want).norm())
+
+    want, coarse = (D[on] @ w), (one[on] @ w)
+    own = off(want.bfloat16(), want)
+    assert off(coarse.bfloat16(), want) >= 1.2 * own
+    assert off(gh[on], want) <= 1.1 * own, (off(gh[on], want) / own)
+    Dt = D[:, ids].T.contiguous()
+    want, coarse = Dt @ h, one[:, ids].T.contiguous() @ h
+    own = off(want.bfloat16(), want)
+    assert off(coarse.bfloat16(), want) >= 1.3 * own
+    assert off(results[torch.bfloat16][ids], want) <= 1.1 * own, (off(results[torch.bfloat16][ids], want) / own)
+    want, coarse = D[:, few].T.contiguous() @ h, two[:, few].T.contiguous() @ h
+    assert off(results[torch.float32][few], want) <= 0.5 * off(coarse, want), off(results[torch.float32][few], want) / off(coarse, want)
