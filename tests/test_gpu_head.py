@@ -555,3 +555,86 @@ def test_large_elements_of_D_count_exactly(env, rows, d, V):
     assert off(results[torch.bfloat16][ids], want) <= 1.1 * own, (off(results[torch.bfloat16][ids], want) / own)
     want, coarse = D[:, few].T.contiguous() @ h, two[:, few].T.contiguous() @ h
     assert off(results[torch.float32][few], want) <= 0.5 * off(coarse, want), off(results[torch.float32][few], want) / off(coarse, want)
+
+
+def whole_numbers(env, rows, d, V, seed=0):
+    """fp32 inputs whose products and sums are exact, so that nothing but exponentials and the gradients' sums rounds."""
+    torch, _ = env
+    x = make(env, rows, d, V, "f32", seed)
+    x["h"], x["w"] = x["h"].round(), (x["w"] * (math.sqrt(d) / 2)).round() * 2.0 ** -round(math.log2(d) / 2)
+    return x
+
+
+def without_moves(x, e, T=1.0):
+    """The bounds of exact logits."""
+    lp, p = x["lp"], x["lp"].exp()
+    gl, ge = x["gl"].double().abs(), x["ge"].double().abs()
+    e["Derr"] = 2.0 ** -17 * (p * (gl[:, None] + ge[:, None] * (lp.abs() + e["ent"][:, None] + 2))) / T + 2.0 ** -22 * e["D"].abs()
+    e["dx"], e["moved"] = 0 * e["dx"], 0 * e["moved"]
+    return e
+
+
+@pytest.mark.parametrize("exact_logits", [False, True])
+def test_fp32_pieces_of_the_vocabulary(env, exact_logits):
+    """The weight of 19,237 ids of width 8,192 passes in three pieces in either direction, the last of them short (37, 37 and
+    2 tiles forward; 26, 26 and 24 backward), each packed in the others' place and added to dH."""
+    torch, _ = env
+    rows, d, V = 300, 8192, 19237
+    x = whole_numbers(env, rows, d, V) if exact_logits else make(env, rows, d, V, "f32")
+    e = exact(env, x, 1.0)
+    if exact_logits:
+        x["lp"] = torch.log_softmax(e["h"] @ e["w"].T.contiguous(), -1)
+        e = without_moves(x, e)
+    out = forward(env, x)
+    check_forward(out, e)
+    check_gradients(env, *gradients(env, x, out), x, e)
+
+
+def test_fp32_pieces_and_many_rows(env):
+    """Each 8,192 rows go through all pieces of the weight, packed again."""
+    x = whole_numbers(env, 8300, 8192, 19237)
+    e = exact(env, x, 1.0)
+    e["dx"], e["moved"] = 0 * e["dx"], 0 * e["moved"]
+    check_forward(forward(env, x), e)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_offsets_in_large_tiles(env, dtype):
+    """A weight and its gradient whose last rows lie past 2^32 bytes, by their strides, in sizes that large tiles take."""
+    torch, sara = env
+    rows, d, V = 300, 1032, 70000
+    x = make(env, rows, d, V, dtype)
+    dt = x["w"].dtype
+    big = torch.zeros((V, 32768), device="cuda", dtype=dt)
+    big[:, 800:800 + d] = x["w"]
+    x["w"] = big[:, 800:800 + d]
+    e = exact(env, x, 1.0)
+    out = forward(env, x)
+    check_forward(out, e)
+    far = torch.full((V, 32768), 7.0, device="cuda", dtype=dt)
+    gh, gw = torch.empty_like(x["h"]), far[:, 1600:1600 + d]
+    sara.sara_head_logprobs_grad(x["h"], x["w"], x["tok"], out["stats"], out["ent"], x["gl"], x["ge"], gh, gw)
+    check_gradients(env, gh, gw, x, e)
+    assert bool((far[:, :1600] == 7).all()) and bool((far[:, 1600 + d:] == 7).all())
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("dtype,sums", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("rows,d,V", [(90, 72, 1000), (2, 72, 9000), BIG])
+def test_rows_apart(env, rows, d, V, dtype, sums, accumulate):
+    """Hidden states, weight and both gradients as parts of wider tensors, whose other elements stay as they are."""
+    torch, sara = env
+    x = make(env, rows, d, V, dtype, pad=24, wpad=40)
+    e = exact(env, x, 1.0)
+    out = forward(env, x)
+    check_forward(out, e)
+    td = torch.bfloat16 if sums == "bf16" else torch.float32
+    wide_h = torch.full((rows, d + 56), 7.0, device="cuda", dtype=x["h"].dtype)
+    wide_w = torch.full((V, d + 72), 7.0, device="cuda", dtype=td)
+    gh, gw = wide_h[:, 16:16 + d], wide_w[:, 24:24 + d]
+    gw.copy_(torch.randn((V, d), device="cuda"))
+    start = gw.clone()
+    sara.sara_head_logprobs_grad(x["h"], x["w"], x["tok"], out["stats"], out["ent"], x["gl"], x["ge"], gh, gw, accumulate=accumulate)
+    check_gradients(env, gh, gw, x, e, start if accumulate else None)
+    for wide, first in ((wide_h, 16), (wide_w, 24)):
+        assert bool((wide[:, :first] == 7).all()) and bool((wide[:, first + d:] == 7).all())
