@@ -373,3 +373,42 @@ def test_no_rows(env):
     b = Batch(env, rng, 2, 64, "int8", [2], [32], [40, 33])
     q = b.q(rng, 0, 4, "bf16")
     assert b.run(q, [0, 0, 0]).shape == (0, 4, 64)
+
+
+@pytest.fixture(scope="module")
+def device():
+    import torch
+
+    import paper_2607_26253_amd as sara
+    return torch, sara
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("groups,max_shared,max_ctx", [(120, 128, 384), (600, 512, 576)])
+def test_the_first_groups_in_a_call_of_their_own(device, groups, max_shared, max_ctx, ragged):
+    """Half of the groups, called alone, give the same results bit for bit: by each sequence through its group's table (the
+    first size) and with the shared pages apart (the second); contexts of one split in either call."""
+    torch, sara = device
+    rng = np.random.default_rng([groups, ragged])
+    hkv, hd, hq, members, pages = 2, 128, 12, 5, 4000
+    n = groups * members
+    g = torch.Generator(device="cuda").manual_seed(groups)
+    codes = [torch.randint(-90, 91, (pages, hkv, 16, hd), generator=g, device="cuda", dtype=torch.int8) for _ in range(2)]
+    exps = [torch.randint(119, 123, (pages, hkv), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    i32 = lambda x: torch.tensor(np.asarray(x, np.int32), device="cuda")
+    table = rng.integers(0, pages, (n, max_ctx // 16))
+    shared = rng.integers(0, max_shared + 1, groups)
+    ctx = np.clip(np.repeat(shared, members) + rng.integers(-20, 60, n), 0, max_ctx)
+    off = offsets([int(x) for x in rng.choice([0, 1, 2, 9], n)]) if ragged else list(range(n + 1))
+    q = torch.randn((off[-1], hq, hd), generator=g, device="cuda").bfloat16()
+
+    def call(k):
+        m = k * members
+        out = torch.full((off[m], hq, hd), 7.0, device="cuda", dtype=q.dtype)
+        sara.sara_kv8_group_attention(q[:off[m]], *codes, *exps, i32(table[:m]), i32(ctx[:m]), i32(off[:m + 1]) if ragged else None,
+                                      i32(range(0, m + 1, members)), i32(shared[:k]), out, max_ctx=max_ctx, max_shared=max_shared)
+        return out
+
+    whole, half = call(groups), call(groups // 2)
+    assert torch.equal(whole[:half.shape[0]], half)
+    assert not bool(whole.isnan().any()) and float(whole.float().abs().amax()) > 0.1
