@@ -269,9 +269,9 @@ __device__ __forceinline__ void tile_grad(TileAcc& acc, const HeadTile& a, TileE
 // s + 1, so all have landed behind it.  The loads are written in assembly: the compiler would wait for all of them
 // before each LDS read.
 //
-// 4,093 rows of width 1,536 over 151,936 ids run at 1.16 PFLOP/s in all (a library's product of 16,384 cubed: 1.38): 44 us a
+// 4,093 rows of width 1,536 over 151,936 ids run at 1.17 PFLOP/s in all (a library's product of 16,384 cubed: 1.38): 44 us a
 // round of tiles, of which some 9 go to the statistics and 4 to the first loads, with nothing of the next tile under way.  2,048
-// rows over 57,344 ids: D 351 us, dH 297, dW 343 (1.03, 1.21 and 1.05 PFLOP/s).
+// rows over 57,344 ids: D 346 us, dH 285, dW 337 (1.04, 1.27 and 1.07 PFLOP/s).
 template <int AK, int BK, int EPI>
 __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
   constexpr bool PAIRS = BK == kRowPairs;
