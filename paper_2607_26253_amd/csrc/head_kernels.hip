@@ -356,7 +356,8 @@ __global__ __launch_bounds__(kTileThreads, 1) void k_head_tile(HeadTile a) {
   for (int j = 0; j < BF; ++j) fb[j] = unit(bk, a.b, tn0, a.N, BF * wave + j, unused);
   const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
   auto load = [&](const char* p, uint32_t at) {
-    uint32_t m0;                                           // where the load goes: written here, which the compiler has to know
+    // m0, where in LDS the load goes, is read as the load is issued; as an output the compiler knows that it is overwritten
+    uint32_t m0;
     asm volatile("s_mov_b32 %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off" : "={m0}"(m0) : "s"(ring_at + at), "v"(p));
   };
   // The next stage to load.  For `run` stages the addresses only grow; then comes k that ends inside a stage or the next pair
